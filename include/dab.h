@@ -441,6 +441,125 @@ int dab_binarized_weights(const float* W, int32_t F, int32_t n, const float* alp
 int dab_weight_gradient(const float* W, int32_t F, int32_t n, const float* thr_val, const int32_t* thr_idx,
                         const uint8_t* alpha_is_upper, const float* upstream, float* G_out, void* stream);
 
+/*
+ * The real-valued ends of a binarized network: what a training step keeps for its backward pass, the
+ * loss, and the layers that are not binarized when they serve.  Section 5.1 leaves a network's first
+ * and last layers real; with a large vocabulary behind the last one these are a language model's
+ * largest matrices.
+ *
+ * Element types of these calls, and the strides of their inputs: a matrix [rows][cols] is given with
+ * the distance ld of its rows in elements (ld >= cols, any alignment of the rows), so that a slice of
+ * columns needs no copy.  Outputs are contiguous.  Offsets are 64-bit.  Base pointers are 16-byte aligned
+ * (DAB_ERR_ALIGN), fp32 vectors, scale bytes and targets as their type wants.
+ */
+typedef enum dab_dtype {
+    DAB_F32 = 0,
+    DAB_BF16 = 1,
+    DAB_F16 = 2
+} dab_dtype;
+
+/*
+ * dab_ckpt8_save / dab_ckpt8_restore - a layer's real input held in 8 bits until its backward pass.
+ * A group is 32 neighbouring channels of a row (the last one may be short).  With a the largest
+ * magnitude of a group and f = floor(log2 a), its exponent is e = f - 6, or f - 5 where a 2^-e would
+ * lie at or above 127.5; a value is q = x 2^-e rounded to the nearest integer, ties to even, so |q| <= 127 and
+ * |x - q 2^e| <= 2^(e-1) < a/127.  f - 6 is kept within -110 .. 120, and |q| at 127.  The scale is a
+ * power of two because undoing it is then exact in every type that has 8 significant bits: a
+ * restored value is a bf16 number.
+ *
+ *   X    [rows][cols] of dtype, rows ldx apart
+ *   Q    int8 [rows][32*ceil(cols/32)] out, zeros behind the last channel
+ *   S    uint8 [rows][ceil(cols/32)] out: e + 127; a group of zeros has 17; a group with an
+ *        infinity or a NaN has 255, and is restored as NaN throughout
+ * restore writes [rows][cols] of dtype, rows ldx apart (f16: rounded to nearest, infinite where too large).
+ */
+int dab_ckpt8_save(const void* X, int32_t dtype, int32_t rows, int32_t cols, int64_t ldx, int8_t* Q, uint8_t* S, void* stream);
+int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows, int32_t cols, void* X, int32_t dtype, int64_t ldx,
+                      void* stream);
+
+/*
+ * dab_ckpt8_weight_gradient - the upstream gradient of a fully-connected layer's weights from its saved
+ * input: dW[f][c] = sum over rows of dY[row][f] * (q 2^e)[row][c], which is what dab_weight_gradient takes as
+ * `upstream` for a binarized layer.  On the matrix cores in bf16: the saved values are bf16 numbers, a
+ * bf16 gradient is used as it is, an f16 one as the sum of two bf16 numbers and an fp32 one as the sum of
+ * three, so that every product is exact and only the fp32 accumulation rounds.
+ *
+ *   dY   [rows][F] of dtype, rows lddy apart;   dW  fp32 [F][cols] out
+ *   ws   dab_ckpt8_weight_gradient_workspace_bytes(...) bytes, 256-byte aligned
+ */
+size_t dab_ckpt8_weight_gradient_workspace_bytes(int32_t rows, int32_t cols, int32_t F, int32_t dtype, int64_t lddy);
+int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t lddy, const int8_t* Q, const uint8_t* S, int32_t rows,
+                              int32_t cols, int32_t F, float* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dab_head_loss - softmax cross entropy of L = H W^T over a vocabulary, without the logits: for every token t
+ *     lse_t = log sum_v exp(L_tv),   loss_t = lse_t - L_t,target(t).
+ * The products run on the matrix cores a block of the vocabulary at a time; of a block only its rows'
+ * maxima and sums and the targets' logits leave the compute unit.  Sums and logits are fp32.  fp32
+ * inputs are multiplied as sums of three bf16 numbers (six products of pieces, what is left out is
+ * below 2^-24 of a term).
+ *
+ *   H        [T][D] of dtype (DAB_BF16 or DAB_F32; DAB_F16 -> DAB_ERR_UNSUPPORTED: softmax gradients leave its
+ *            range), rows ldh apart
+ *   W        [V][D] of the same dtype, rows ldw apart
+ *   targets  [T] int64; ignore_index marks a token without a loss (its row of H may hold anything, infinities and NaN
+ *            among it: loss 0, no part in any gradient).  A target that is neither that nor one of 0 .. V-1 gives a loss of
+ *            NaN, and its token no part in any gradient.
+ *   loss     [T] fp32 out, lse [T] fp32 out (0 for an ignored token)
+ *   ws       dab_head_loss_workspace_bytes(...) bytes, 256-byte aligned
+ */
+size_t dab_head_loss_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw);
+int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,
+                  int64_t ignore_index, int32_t T, int32_t D, int32_t V, float* loss, float* lse, void* ws, size_t ws_bytes,
+                  void* stream);
+
+/*
+ * dab_head_loss_gradient - its gradient.  With g_t the gradient with respect to loss_t,
+ *     P_tv = g_t (exp(L_tv - lse_t) - [v = target(t)]),   dH = P W,   dW = P^T H,
+ * the logits recomputed a piece of the vocabulary at a time.  P is rounded to bf16 where H and W are bf16 (as those
+ * are: the products stay on the matrix cores, and dH and dW are rounded to bf16 themselves); for fp32 it is
+ * held as three bf16 numbers like them.  Sums are fp32; no atomics: the same inputs give the same bits.
+ *
+ *   lse      [T] fp32 of dab_head_loss for the same H, W, targets
+ *   g        [T] fp32, or NULL for 1
+ *   dH       [T][D] of dtype out (zero rows for ignored tokens), dW [V][D] of dtype out
+ */
+size_t dab_head_loss_gradient_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw);
+int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,
+                           int64_t ignore_index, const float* lse, const float* g, int32_t T, int32_t D, int32_t V, void* dH,
+                           void* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dab_w4_pack / dab_w4_unpack - weights of a real layer in 4 bits: groups of 32 neighbouring weights of a row
+ * share a power of two, a weight is a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (codes 0 .. 7, the sign 8).
+ * With a the largest magnitude of a group and f = floor(log2 a), the exponent is e = f - 2, or f - 1 where
+ * a 2^-e would exceed 7 (further from 6 than half the step before it); values go to the nearest level, ties to the even
+ * code, what lies above 6 to 6.  f - 2 is kept within -110 .. 120.
+ *
+ *   W   [F][K] of dtype, rows ldw apart
+ *   Q   uint8 [ceil(F/16)][ceil(K/128)][64][16] out: piece l of a block of 16 rows and 128 weights holds
+ *       row l % 16, weights 32 (l / 16) .. + 31 of the block, two to a byte, the lower weight in the lower four bits.
+ *       (What one lane of a wavefront takes; a block is one contiguous kilobyte.)  Zeros past F and K.
+ *   S   uint8 [ceil(F/16)][ceil(K/512)][64][4] out: e + 127 of piece l of block 4 i + j at [.][i][l][j]; 17 for
+ *       groups of zeros and past F and K.  A group with an infinity or a NaN has 255 and codes 7: it is restored as NaN.
+ * unpack writes fp32 [F][K].
+ */
+int dab_w4_pack(const void* W, int32_t dtype, int32_t F, int32_t K, int64_t ldw, uint8_t* Q, uint8_t* S, void* stream);
+int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, float* W, void* stream);
+
+/*
+ * dab_w4_matvec - Y[b][f] = sum_k X[b][k] W[f][k] with packed weights, for one token or a few (any B is right; the
+ * weights are read once for every 64 bf16, 32 f16 or 21 fp32 tokens).  On the matrix cores in bf16, which hold a 4-bit weight times its
+ * scale exactly; f16 inputs are sums of two bf16 numbers, fp32 ones of three: only the fp32 accumulation
+ * rounds, and a 16-bit Y once more.
+ *
+ *   X   [B][K] of dtype, rows ldx apart;  Y  [B][F] of dtype out
+ *   ws  dab_w4_matvec_workspace_bytes(...) bytes, 256-byte aligned (0 for aligned bf16 inputs)
+ */
+size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx);
+int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F,
+                  void* Y, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

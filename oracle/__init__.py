@@ -14,6 +14,7 @@ layers     Sign binarization of activations, the two-valued filter of Corollary 
            the direct float64 convolution / fully-connected product, the integer
            side channel (s1, sA) and the popcount form of the same dot product.
 packing    Reference bit packers that pin the bit order of the packed operands.
+real_ends  Inputs saved in 8 bits, 4-bit weights and their layout, softmax cross entropy with its gradient.
 
 Parity status: every function here is pinned by the CPU tests (exact rational
 brute force over all masks, closed forms, library cross-checks); none is

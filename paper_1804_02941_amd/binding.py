@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_float, c_int, c_int32, c_size_t, c_void_p
+from ctypes import c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -25,6 +25,7 @@ DAB_OK = 0
 DAB_ERR_NULL, DAB_ERR_SHAPE, DAB_ERR_ALIGN, DAB_ERR_WORKSPACE, DAB_ERR_UNSUPPORTED, DAB_ERR_HIP = 1, 2, 3, 4, 5, 6
 DAB_LAYOUT_NHWC = 0
 DAB_LAYOUT_NCHW = 1
+DAB_F32, DAB_BF16, DAB_F16 = 0, 1, 2
 
 
 class DabError(RuntimeError):
@@ -96,6 +97,22 @@ _SIGNATURES = {
                                       c_void_p, c_void_p]),
     "dab_weight_gradient": (c_int, [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                     c_void_p]),
+    "dab_ckpt8_save": (c_int, [c_void_p, c_int32, c_int32, c_int32, c_int64, c_void_p, c_void_p, c_void_p]),
+    "dab_ckpt8_restore": (c_int, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_int64, c_void_p]),
+    "dab_ckpt8_weight_gradient_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int64]),
+    "dab_ckpt8_weight_gradient": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                          c_void_p, c_void_p, c_size_t, c_void_p]),
+    "dab_head_loss_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int64, c_int64]),
+    "dab_head_loss": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int32, c_int32, c_int32,
+                              c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "dab_head_loss_gradient_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int64, c_int64]),
+    "dab_head_loss_gradient": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p, c_void_p,
+                                       c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "dab_w4_pack": (c_int, [c_void_p, c_int32, c_int32, c_int32, c_int64, c_void_p, c_void_p, c_void_p]),
+    "dab_w4_unpack": (c_int, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
+    "dab_w4_matvec_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int64]),
+    "dab_w4_matvec": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                              c_size_t, c_void_p]),
 }
 
 _lib = None
@@ -511,4 +528,162 @@ def dab_wbin_fc(X, E_packed, alpha, beta, out=None, ws=None):
     nbytes = call.dab_wbin_fc_workspace_bytes(B, Kin, F)
     ws = _workspace(nbytes, dev, ws)
     call.dab_wbin_fc(B, Kin, F, X, E_packed, alpha, beta, Y, ws, nbytes)
+    return Y
+
+
+# ------------------------------------------------------------------ the real-valued ends of a network
+_REAL = {torch.float32: DAB_F32, torch.bfloat16: DAB_BF16, torch.float16: DAB_F16}
+
+
+def _matrix(t, name):
+    """(address, element type, distance of the rows) of a matrix on the GPU whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a tensor on the GPU")
+    if t.dtype not in _REAL:
+        raise TypeError(f"{name}: expected torch.float32, torch.bfloat16 or torch.float16, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected two dimensions, got {t.dim()}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
+        raise ValueError(f"{name}: the elements of a row must be contiguous and rows apart")
+    return t.data_ptr(), _REAL[t.dtype], t.stride(0) if rows > 1 else cols
+
+
+def _shaped(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _result(out, shape, dtype, dev, name):
+    """The caller's output tensor, checked, or a new one."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _ptr(out, dtype, name)
+    return _shaped(out, shape, name)
+
+
+def _scratch(nbytes, dev, ws):
+    """(tensor, address, bytes) of a caller's workspace that is large enough, else of a new one."""
+    ws = _workspace(nbytes, dev, ws)
+    return ws, ws.data_ptr() if ws is not None else None, nbytes
+
+
+def ckpt8_outputs(rows, cols, dev):
+    """Empty (Q, S) of dab_ckpt8_save."""
+    groups = (cols + 31) // 32
+    return (torch.empty((rows, 32 * groups), dtype=torch.int8, device=dev), torch.empty((rows, groups), dtype=torch.uint8, device=dev))
+
+
+def _saved(Q, S, cols):
+    rows, groups = Q.shape[0], (cols + 31) // 32
+    _shaped(Q, (rows, 32 * groups), "Q"), _shaped(S, (rows, groups), "S")
+    return _ptr(Q, torch.int8, "Q"), _ptr(S, torch.uint8, "S"), rows
+
+
+def dab_ckpt8_save(X, out=None):
+    """X [rows, cols] fp32, bf16 or f16 -> (Q int8 [rows, 32 ceil(cols/32)], S uint8 [rows, ceil(cols/32)])."""
+    ptr, dtype, ld = _matrix(X, "X")
+    rows, cols = X.shape
+    Q, S = out if out is not None else ckpt8_outputs(rows, cols, X.device)
+    q, s, n = _saved(Q, S, cols)
+    if n != rows:
+        raise ValueError(f"Q: expected {rows} rows, got {n}")
+    _check("dab_ckpt8_save", lib().dab_ckpt8_save(ptr, dtype, rows, cols, ld, q, s, _stream()))
+    return Q, S
+
+
+def dab_ckpt8_restore(Q, S, cols, dtype=torch.float32, out=None):
+    """What dab_ckpt8_save() kept of `cols` channels, as a tensor [rows, cols] of dtype (or into `out`)."""
+    q, s, rows = _saved(Q, S, cols)
+    X = out if out is not None else torch.empty((rows, cols), dtype=dtype, device=Q.device)
+    ptr, code, ld = _matrix(_shaped(X, (rows, cols), "out"), "out")
+    _check("dab_ckpt8_restore", lib().dab_ckpt8_restore(q, s, rows, cols, ptr, code, ld, _stream()))
+    return X
+
+
+def dab_ckpt8_weight_gradient(dY, Q, S, cols, out=None, ws=None):
+    """dW = dY^T X fp32 [F, cols] from dY [rows, F] (fp32, bf16 or f16) and what dab_ckpt8_save() kept of X [rows, cols]."""
+    ptr, dtype, ld = _matrix(dY, "dY")
+    q, s, rows = _saved(Q, S, cols)
+    F = _shaped(dY, (rows, dY.shape[1]), "dY").shape[1]
+    dW = _result(out, (F, cols), torch.float32, dY.device, "out")
+    nbytes = lib().dab_ckpt8_weight_gradient_workspace_bytes(rows, cols, F, dtype, ld)
+    ws, at, nbytes = _scratch(nbytes, dY.device, ws)
+    _check("dab_ckpt8_weight_gradient", lib().dab_ckpt8_weight_gradient(ptr, dtype, ld, q, s, rows, cols, F, dW.data_ptr(), at, nbytes,
+                                                                        _stream()))
+    return dW
+
+
+def _head(H, W, targets):
+    h, dtype, ldh = _matrix(H, "H")
+    w, dtype_w, ldw = _matrix(W, "W")
+    if dtype != dtype_w:
+        raise TypeError(f"W: expected {H.dtype}, got {W.dtype}")
+    T, D = H.shape
+    _shaped(W, (W.shape[0], D), "W")
+    return h, ldh, w, ldw, dtype, _ptr(_shaped(targets, (T,), "targets"), torch.int64, "targets"), T, D, W.shape[0]
+
+
+def dab_head_loss(H, W, targets, ignore_index=-100, out=None, ws=None):
+    """Softmax cross entropy of H [T, D] W [V, D]^T (bf16 or fp32) with targets int64 [T] -> (loss fp32 [T], lse fp32 [T])."""
+    h, ldh, w, ldw, dtype, t, T, D, V = _head(H, W, targets)
+    loss, lse = out if out is not None else (None, None)
+    loss, lse = _result(loss, (T,), torch.float32, H.device, "loss"), _result(lse, (T,), torch.float32, H.device, "lse")
+    ws, at, nbytes = _scratch(lib().dab_head_loss_workspace_bytes(T, D, V, dtype, ldh, ldw), H.device, ws)
+    _check("dab_head_loss", lib().dab_head_loss(h, ldh, w, ldw, dtype, t, ignore_index, T, D, V, loss.data_ptr(), lse.data_ptr(), at, nbytes,
+                                                _stream()))
+    return loss, lse
+
+
+def dab_head_loss_gradient(H, W, targets, lse, g=None, ignore_index=-100, out=None, ws=None):
+    """(dH, dW) of sum_t g_t loss_t (g fp32 [T], or None for ones), with lse from dab_head_loss() for the same H, W and targets."""
+    h, ldh, w, ldw, dtype, t, T, D, V = _head(H, W, targets)
+    dH, dW = out if out is not None else (None, None)
+    dH, dW = _result(dH, (T, D), H.dtype, H.device, "dH"), _result(dW, (V, D), H.dtype, H.device, "dW")
+    l = _ptr(_shaped(lse, (T,), "lse"), torch.float32, "lse")
+    gp = None if g is None else _ptr(_shaped(g, (T,), "g"), torch.float32, "g")
+    ws, at, nbytes = _scratch(lib().dab_head_loss_gradient_workspace_bytes(T, D, V, dtype, ldh, ldw), H.device, ws)
+    _check("dab_head_loss_gradient", lib().dab_head_loss_gradient(h, ldh, w, ldw, dtype, t, ignore_index, l, gp, T, D, V, dH.data_ptr(),
+                                                                  dW.data_ptr(), at, nbytes, _stream()))
+    return dH, dW
+
+
+def w4_outputs(F, K, dev):
+    """Empty (Q, S) of dab_w4_pack."""
+    return (torch.empty(((F + 15) // 16, (K + 127) // 128, 64, 16), dtype=torch.uint8, device=dev),
+            torch.empty(((F + 15) // 16, (K + 511) // 512, 64, 4), dtype=torch.uint8, device=dev))
+
+
+def _packed(Q, S, F, K):
+    _shaped(Q, ((F + 15) // 16, (K + 127) // 128, 64, 16), "Q"), _shaped(S, ((F + 15) // 16, (K + 511) // 512, 64, 4), "S")
+    return _ptr(Q, torch.uint8, "Q"), _ptr(S, torch.uint8, "S")
+
+
+def dab_w4_pack(W, out=None):
+    """W [F, K] fp32, bf16 or f16 -> (Q, S): 4-bit codes and scale bytes in the layout of include/dab.h."""
+    ptr, dtype, ld = _matrix(W, "W")
+    F, K = W.shape
+    Q, S = out if out is not None else w4_outputs(F, K, W.device)
+    q, s = _packed(Q, S, F, K)
+    _check("dab_w4_pack", lib().dab_w4_pack(ptr, dtype, F, K, ld, q, s, _stream()))
+    return Q, S
+
+
+def dab_w4_unpack(Q, S, F, K, out=None):
+    """The weights that dab_w4_pack()'s (Q, S) stand for, fp32 [F, K]."""
+    q, s = _packed(Q, S, F, K)
+    W = _result(out, (F, K), torch.float32, Q.device, "out")
+    _check("dab_w4_unpack", lib().dab_w4_unpack(q, s, F, K, W.data_ptr(), _stream()))
+    return W
+
+
+def dab_w4_matvec(X, Q, S, F, out=None, ws=None):
+    """X [B, K] (fp32, bf16 or f16) times the F packed rows -> Y [B, F] of X's type."""
+    ptr, dtype, ld = _matrix(X, "X")
+    B, K = X.shape
+    q, s = _packed(Q, S, F, K)
+    Y = _result(out, (B, F), X.dtype, X.device, "out")
+    ws, at, nbytes = _scratch(lib().dab_w4_matvec_workspace_bytes(B, K, F, dtype, ld), X.device, ws)
+    _check("dab_w4_matvec", lib().dab_w4_matvec(ptr, dtype, ld, q, s, B, K, F, Y.data_ptr(), at, nbytes, _stream()))
     return Y

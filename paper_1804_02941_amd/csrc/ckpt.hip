@@ -1,0 +1,127 @@
+// A layer's input in 8 bits: save, restore (the weight gradient from it: head.hip's neighbour product16.h).
+//
+// Both are one pass over memory: save reads size bytes a value and writes 1 + 1/32, restore the other way round.  Four lanes
+// hold a group of 32, eight values each, so that a lane's load is 16 or 32 bytes and its store 8, and the group's largest magnitude is two
+// exchanges between neighbouring lanes.  A wavefront takes as many whole rows, or as much of a row, as 512 values are.
+#include "real16.h"
+
+namespace dab {
+
+constexpr int kSaveWaves = 4;        // wavefronts per workgroup
+
+struct Rows8 {
+    int rows, cols, groups;          // groups of a row
+    int lanes_log2;                  // lanes that share a row within a wavefront
+    int row_parts;                   // pieces of 64 lanes that a row takes
+    int64_t ld;
+    int vec;
+};
+
+// Row and first column of this lane's eight values; false past the end.
+__device__ __forceinline__ bool my_eight(const Rows8& g, int* row, int* c) {
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kSaveWaves + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int64_t block = unit / g.row_parts;
+    const int part = static_cast<int>(unit - block * g.row_parts);
+    const int64_t r = (block << (6 - g.lanes_log2)) + (lane >> g.lanes_log2);
+    *c = (part * 64 + (lane & ((1 << g.lanes_log2) - 1))) * 8;
+    *row = static_cast<int>(r);
+    return r < g.rows && *c < g.groups * 32;
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kSaveWaves) void ckpt8_save_kernel(const T* __restrict__ X, Rows8 g, int8_t* __restrict__ Q,
+                                                                     uint8_t* __restrict__ S) {
+    int row, c;
+    const bool in = my_eight(g, &row, &c);                   // whole groups are in or out, and the exchange stays in a group
+    float v[8] = {};
+    if (in) load8(X + row * g.ld, c, g.cols, g.vec, v);
+    const uint32_t m = group_max(v);
+    if (!in) return;
+    uint64_t word = 0;
+    int code = 255;
+    if (m < 0x7f800000u) {
+        const int e = group_exponent<6>(m);
+        const float inv = pow2f(-e);
+        code = e + 127;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int q = static_cast<int>(fminf(fmaxf(rintf(v[i] * inv), -127.f), 127.f));
+            word |= static_cast<uint64_t>(static_cast<uint8_t>(q)) << (8 * i);
+        }
+    }
+    const int64_t at = static_cast<int64_t>(row) * g.groups;
+    *reinterpret_cast<uint64_t*>(Q + at * 32 + c) = word;
+    if ((c & 31) == 0) S[at + (c >> 5)] = static_cast<uint8_t>(code);
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kSaveWaves) void ckpt8_restore_kernel(const int8_t* __restrict__ Q, const uint8_t* __restrict__ S,
+                                                                        Rows8 g, T* __restrict__ X) {
+    int row, c;
+    if (!my_eight(g, &row, &c)) return;
+    const int64_t at = static_cast<int64_t>(row) * g.groups;
+    const uint64_t word = *reinterpret_cast<const uint64_t*>(Q + at * 32 + c);
+    const int code = S[at + (c >> 5)];
+    const float scale = code == 255 ? __builtin_nanf("") : pow2f(code - 127);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(static_cast<int8_t>(word >> (8 * i))) * scale;
+    store8(X + row * g.ld, c, g.cols, g.vec, v);
+}
+
+static Rows8 rows8_of(int rows, int cols, int64_t ld, int64_t size) {
+    Rows8 g{};
+    g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ld = ld;
+    g.vec = ld * size % 16 == 0;
+    const int lanes = g.groups * 4;
+    g.lanes_log2 = 2;
+    while (g.lanes_log2 < 6 && (1 << g.lanes_log2) < lanes) ++g.lanes_log2;
+    g.row_parts = ceil_div(lanes, 64);
+    return g;
+}
+
+static int check_rows(const void* X, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, const void* Q, const void* S) {
+    if (!X || !Q || !S) return DAB_ERR_NULL;
+    if (rows < 1 || cols < 1 || ld < cols) return DAB_ERR_SHAPE;
+    if (!real_dtype(dtype) || cols > INT32_MAX - 64) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(X, 16) || misaligned(Q, 16)) return DAB_ERR_ALIGN;
+    return DAB_OK;
+}
+
+// Workgroups of a pass; 0 if they are more than a launch takes.
+static unsigned save_grid(const Rows8& g) {
+    const int64_t units = ceil_div64(g.rows, int64_t{1} << (6 - g.lanes_log2)) * g.row_parts;
+    const int64_t n = ceil_div64(units, kSaveWaves);
+    return n <= INT32_MAX ? static_cast<unsigned>(n) : 0;
+}
+
+}  // namespace dab
+
+extern "C" int dab_ckpt8_save(const void* X, int32_t dtype, int32_t rows, int32_t cols, int64_t ldx, int8_t* Q, uint8_t* S,
+                              void* stream) {
+    using namespace dab;
+    if (int rc = check_rows(X, dtype, rows, cols, ldx, Q, S)) return rc;
+    const Rows8 g = rows8_of(rows, cols, ldx, dtype_bytes(dtype));
+    const unsigned grid = save_grid(g);
+    if (grid == 0) return DAB_ERR_UNSUPPORTED;
+    const auto st = static_cast<hipStream_t>(stream);
+    const dim3 block(64 * kSaveWaves);
+    if (dtype == DAB_F32) return launch(ckpt8_save_kernel<float>, dim3(grid), block, 0, st, static_cast<const float*>(X), g, Q, S);
+    if (dtype == DAB_BF16) return launch(ckpt8_save_kernel<bf16>, dim3(grid), block, 0, st, static_cast<const bf16*>(X), g, Q, S);
+    return launch(ckpt8_save_kernel<f16>, dim3(grid), block, 0, st, static_cast<const f16*>(X), g, Q, S);
+}
+
+extern "C" int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows, int32_t cols, void* X, int32_t dtype, int64_t ldx,
+                                 void* stream) {
+    using namespace dab;
+    if (int rc = check_rows(X, dtype, rows, cols, ldx, Q, S)) return rc;
+    const Rows8 g = rows8_of(rows, cols, ldx, dtype_bytes(dtype));
+    const unsigned grid = save_grid(g);
+    if (grid == 0) return DAB_ERR_UNSUPPORTED;
+    const auto st = static_cast<hipStream_t>(stream);
+    const dim3 block(64 * kSaveWaves);
+    if (dtype == DAB_F32) return launch(ckpt8_restore_kernel<float>, dim3(grid), block, 0, st, Q, S, g, static_cast<float*>(X));
+    if (dtype == DAB_BF16) return launch(ckpt8_restore_kernel<bf16>, dim3(grid), block, 0, st, Q, S, g, static_cast<bf16*>(X));
+    return launch(ckpt8_restore_kernel<f16>, dim3(grid), block, 0, st, Q, S, g, static_cast<f16*>(X));
+}

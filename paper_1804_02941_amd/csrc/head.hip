@@ -1,0 +1,224 @@
+// Softmax cross entropy over a large vocabulary and its gradient, without the logits.
+//
+// loss: one product H W^T whose tiles leave only each token's maximum and sum of exponentials over a block of words, and the
+// target's logit; a second, small kernel joins the blocks.  gradient: a piece of the vocabulary at a time, the
+// product again, now written out as P = g (softmax - onehot) in bf16, and the two products dW = P^T H (the piece's
+// rows of dW, finished) and dH += P W (fp32 until the last piece).  8 T D V flops, two of them for taking the logits twice.
+#include "product16.h"
+
+namespace dab {
+
+// One workgroup: 32 tokens, eight threads each.
+__global__ __launch_bounds__(256) void head_join_kernel(const float2* __restrict__ stats, const float* __restrict__ target_logit,
+                                                        const int64_t* __restrict__ targets, int64_t ignore, int T, int V, int blocks,
+                                                        float* __restrict__ loss, float* __restrict__ lse) {
+    __shared__ float2 part[8][32];
+    const int t = blockIdx.x * 32 + (threadIdx.x & 31), u = threadIdx.x >> 5;
+    float big = -__builtin_inff(), sum = 0.f;
+    if (t < T)
+        for (int i = u; i < blocks; i += 8) {
+            const float2 s = stats[static_cast<int64_t>(i) * T + t];
+            const float top = fmaxf(big, s.x);
+            // (a block of minus infinities alone adds nothing, and exp of its difference would be undefined)
+            if (s.x != -__builtin_inff()) sum = (big == -__builtin_inff() ? 0.f : sum * expf(big - top)) + s.y * expf(s.x - top);
+            big = top;
+        }
+    part[u][threadIdx.x & 31] = float2{big, sum};
+    __syncthreads();
+    if (u != 0 || t >= T) return;
+    for (int i = 1; i < 8; ++i) {
+        const float2 s = part[i][threadIdx.x];
+        const float top = fmaxf(big, s.x);
+        if (s.x != -__builtin_inff()) sum = (big == -__builtin_inff() ? 0.f : sum * expf(big - top)) + s.y * expf(s.x - top);
+        big = top;
+    }
+    const int64_t target = targets[t];
+    const bool dead = no_loss(target, ignore, V);
+    const float l = big + logf(sum);
+    lse[t] = dead ? 0.f : l;
+    loss[t] = target == ignore ? 0.f : dead ? __builtin_nanf("") : l - target_logit[t];
+}
+
+struct HeadPlan {
+    int P;                           // planes
+    int n_seg;
+    bool h_direct, w_direct;
+    int64_t ldh, ldw;
+    int piece, n_pieces;             // words of a piece
+    int64_t ldp;
+    Plan16 logits, dh, dw;           // of a piece (the last one may be smaller)
+    size_t h_at, w_at, stats_at, target_at, p_at, acc_at, part_at, bytes;
+};
+
+static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
+    return (dtype == DAB_BF16 || dtype == DAB_F32) && ldh < (1 << 23) && ldw < (1 << 23) && T < (1 << 30) && V < (1 << 30) &&
+           ceil_div64(T, 128) * ceil_div64(V, 128) < INT32_MAX / 64 && ceil_div64(T, 128) * ceil_div64(D, 128) < INT32_MAX / 1024;
+}
+
+static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw, bool gradient) {
+    HeadPlan p{};
+    p.P = dtype_pieces(dtype);
+    p.n_seg = p.P == 1 ? 1 : 6;
+    p.w_direct = dtype == DAB_BF16 && D % 8 == 0 && ldw % 8 == 0;
+    // (a gradient reads H with the rows of ignored tokens cleared, whatever they hold)
+    p.h_direct = !gradient && dtype == DAB_BF16 && D % 8 == 0 && ldh % 8 == 0;
+    p.ldh = p.h_direct ? ldh : round_up(D, 8);
+    p.ldw = p.w_direct ? ldw : round_up(D, 8);
+    size_t at = 0;
+    auto room = [&at](int64_t bytes) {
+        const size_t here = at;
+        at += static_cast<size_t>(round_up(bytes, 256));
+        return here;
+    };
+    p.h_at = p.h_direct ? 0 : room(static_cast<int64_t>(p.P) * T * p.ldh * 2);
+    p.w_at = p.w_direct ? 0 : room(static_cast<int64_t>(p.P) * V * p.ldw * 2);
+    if (!gradient) {
+        p.logits = plan16(T, V, D, p.n_seg, false);
+        const int words = stats_words16(p.logits);
+        p.stats_at = room((ceil_div64(V, words) + 8) * T * 8);
+        p.target_at = room(static_cast<int64_t>(T) * 4);
+    } else {
+        // pieces of up to 256 MB of P, which is about what the memory-side cache holds, of equal size
+        int64_t words = (int64_t{256} << 20) / (int64_t{2} * p.P * T) / 1024 * 1024;
+        if (words < 1024) words = 1024;
+        if (words > V) words = V;
+        p.n_pieces = static_cast<int>(ceil_div64(V, words));
+        p.piece = static_cast<int>(round_up(ceil_div64(V, p.n_pieces), 256));
+        p.n_pieces = ceil_div(V, p.piece);
+        p.ldp = p.piece;
+        p.logits = plan16(T, p.piece, D, p.n_seg, false);
+        p.dh = plan16(T, D, p.piece, p.n_seg, true);
+        p.dw = plan16(p.piece, D, T, p.n_seg, true);
+        p.p_at = room(static_cast<int64_t>(p.P) * T * p.ldp * 2);
+        p.acc_at = room(p.n_pieces > 1 ? static_cast<int64_t>(T) * D * 4 : 0);
+        p.part_at = room(static_cast<int64_t>(p.dh.part_bytes > p.dw.part_bytes ? p.dh.part_bytes : p.dw.part_bytes));
+    }
+    p.bytes = at;
+    return p;
+}
+
+static int head_check(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const void* targets, int32_t T, int32_t D,
+                      int32_t V) {
+    if (!H || !W || !targets) return DAB_ERR_NULL;
+    if (T < 1 || D < 1 || V < 1 || ldh < D || ldw < D) return DAB_ERR_SHAPE;
+    if (!head_sizes(T, D, V, dtype, ldh, ldw)) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(H, 16) || misaligned(W, 16) || misaligned(targets, 8)) return DAB_ERR_ALIGN;
+    return DAB_OK;
+}
+
+static void head_segments(Product16& g, int n_seg) {
+    // pairs of pieces in order of size; what is left out is below 2^-24 of a term
+    static const uint8_t a[6] = {0, 0, 1, 1, 0, 2}, b[6] = {0, 1, 0, 1, 2, 0};
+    g.n_seg = n_seg;
+    for (int i = 0; i < n_seg; ++i) g.seg_a[i] = a[i], g.seg_b[i] = b[i];
+}
+
+// The operands as bf16 planes, in the workspace where they are not already.
+static int head_operands(const HeadPlan& p, const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype,
+                         const int64_t* targets, int64_t ignore, int T, int D, int V, char* ws, hipStream_t st, Operand16* h, Operand16* w) {
+    *h = {static_cast<const bf16*>(H), p.ldh, static_cast<int64_t>(T) * p.ldh};
+    *w = {static_cast<const bf16*>(W), p.ldw, static_cast<int64_t>(V) * p.ldw};
+    if (!p.h_direct) {
+        bf16* out = reinterpret_cast<bf16*>(ws + p.h_at);
+        if (int rc = launch_planes16(H, dtype, T, D, ldh, targets, ignore, V, out, p.ldh, st)) return rc;
+        h->p = out;
+    }
+    if (!p.w_direct) {
+        bf16* out = reinterpret_cast<bf16*>(ws + p.w_at);
+        if (int rc = launch_planes16(W, dtype, V, D, ldw, nullptr, 0, 0, out, p.ldw, st)) return rc;
+        w->p = out;
+    }
+    return DAB_OK;
+}
+
+}  // namespace dab
+
+extern "C" size_t dab_head_loss_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
+    using namespace dab;
+    if (T < 1 || D < 1 || V < 1 || ldh < D || ldw < D || !head_sizes(T, D, V, dtype, ldh, ldw)) return 0;
+    return head_plan(T, D, V, dtype, ldh, ldw, false).bytes;
+}
+
+extern "C" size_t dab_head_loss_gradient_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
+    using namespace dab;
+    if (T < 1 || D < 1 || V < 1 || ldh < D || ldw < D || !head_sizes(T, D, V, dtype, ldh, ldw)) return 0;
+    return head_plan(T, D, V, dtype, ldh, ldw, true).bytes;
+}
+
+extern "C" int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,
+                             int64_t ignore_index, int32_t T, int32_t D, int32_t V, float* loss, float* lse, void* ws, size_t ws_bytes,
+                             void* stream) {
+    using namespace dab;
+    if (!loss || !lse) return DAB_ERR_NULL;
+    if (int rc = head_check(H, ldh, W, ldw, dtype, targets, T, D, V)) return rc;
+    if (misaligned(loss, 4) || misaligned(lse, 4)) return DAB_ERR_ALIGN;
+    const HeadPlan p = head_plan(T, D, V, dtype, ldh, ldw, false);
+    if (!ws || ws_bytes < p.bytes || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    if (int rc = ensure_device_ready()) return rc;
+    const auto st = static_cast<hipStream_t>(stream);
+    char* base = static_cast<char*>(ws);
+    Product16 g{};
+    if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &g.A, &g.B)) return rc;
+    g.M = T, g.N = V, g.K = D, g.V = V;
+    head_segments(g, p.n_seg);
+    g.targets = targets, g.ignore_index = ignore_index;
+    g.stats = reinterpret_cast<float2*>(base + p.stats_at);
+    g.target_logit = reinterpret_cast<float*>(base + p.target_at);
+    if (int rc = launch16(kEpiStats, false, false, g, p.logits, st)) return rc;
+    const int blocks = ceil_div(V, stats_words16(p.logits));
+    return launch(head_join_kernel, dim3(ceil_div(T, 32)), dim3(256), 0, st, g.stats, g.target_logit, targets, ignore_index, T, V, blocks,
+                  loss, lse);
+}
+
+extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,
+                                      int64_t ignore_index, const float* lse, const float* grad, int32_t T, int32_t D, int32_t V,
+                                      void* dH, void* dW, void* ws, size_t ws_bytes, void* stream) {
+    using namespace dab;
+    if (!lse || !dH || !dW) return DAB_ERR_NULL;
+    if (int rc = head_check(H, ldh, W, ldw, dtype, targets, T, D, V)) return rc;
+    if (misaligned(lse, 4) || misaligned(grad, 4) || misaligned(dH, 16) || misaligned(dW, 16)) return DAB_ERR_ALIGN;
+    const HeadPlan p = head_plan(T, D, V, dtype, ldh, ldw, true);
+    if (!ws || ws_bytes < p.bytes || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    if (int rc = ensure_device_ready()) return rc;
+    const auto st = static_cast<hipStream_t>(stream);
+    char* base = static_cast<char*>(ws);
+    Operand16 h, w;
+    if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &h, &w)) return rc;
+    bf16* P = reinterpret_cast<bf16*>(base + p.p_at);
+    float* acc = reinterpret_cast<float*>(base + p.acc_at);
+    const Operand16 probs = {P, p.ldp, static_cast<int64_t>(T) * p.ldp};
+    const int64_t size = dtype_bytes(dtype);
+    for (int i = 0; i < p.n_pieces; ++i) {
+        const int v0 = i * p.piece, words = V - v0 < p.piece ? V - v0 : p.piece;
+        const Operand16 wp = {w.p + v0 * w.ld, w.ld, w.plane};
+        // P of this piece; its columns past the last word are zeros
+        Product16 g{};
+        head_segments(g, p.n_seg);
+        g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D;
+        g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
+        g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.P;
+        if (int rc = launch16(kEpiSoftmax, false, false, g, plan16(T, words, D, p.n_seg, false), st)) return rc;
+        // the piece's rows of dW
+        Product16 q{};
+        head_segments(q, p.n_seg);
+        q.A = probs, q.B = h, q.M = words, q.N = D, q.K = T;
+        q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
+        q.vec = D % 4 == 0;
+        q.part = reinterpret_cast<float*>(base + p.part_at);
+        Plan16 pl = plan16(words, D, T, p.n_seg, true);
+        if (pl.part_bytes > p.dw.part_bytes) pl = plan16(words, D, T, p.n_seg, false);
+        if (int rc = launch16(kEpiStore, true, true, q, pl, st)) return rc;
+        // its share of dH
+        const bool last = i + 1 == p.n_pieces;
+        Product16 s{};
+        head_segments(s, p.n_seg);
+        s.A = probs, s.B = wp, s.M = T, s.N = D, s.K = words;
+        s.add = i ? acc : nullptr;
+        s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16, s.vec = D % 4 == 0;
+        s.part = q.part;
+        pl = plan16(T, D, words, p.n_seg, true);
+        if (pl.part_bytes > p.dh.part_bytes) pl = plan16(T, D, words, p.n_seg, false);
+        if (int rc = launch16(kEpiStore, false, true, s, pl, st)) return rc;
+    }
+    return DAB_OK;
+}

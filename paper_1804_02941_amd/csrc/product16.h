@@ -1,0 +1,70 @@
+// Dense products of bf16 operands on the matrix cores, for the training side of the real-valued layers:
+//     C[m][n] = sum over pieces (a, b) and k of A_a[m][k] B_b[n][k],   fp32 accumulation.
+// Either operand may be held with k contiguous ([rows][k], rows = m or n) or with its rows contiguous ([k][rows]): the second form is
+// transposed on the way out of LDS (ds_read_b64_tr_b16), so that no operand is ever transposed in memory.  Operands of wider types are
+// several bf16 planes whose sum they are, and the product runs over a list of pairs of planes.
+//
+// A workgroup of WM x WN wavefronts owns a TM x TN tile of C.  A step is 64 k: both operands' tiles go from memory straight into LDS
+// (16 bytes a lane) while the step before is multiplied; two buffers, one barrier a step.  The product is taken with B as the
+// matrix core's left operand: register r of a lane is then column n = 4 (lane / 16) + r of row m = lane % 16, so that a lane stores four neighbouring columns, and
+// softmax sums over n stay in a lane but for two exchanges.
+#pragma once
+
+#include "real16.h"
+
+namespace dab {
+
+struct Operand16 {
+    const bf16* p;
+    int64_t ld;                      // elements between rows ([rows][k]) or between k ([k][rows]); a multiple of 8
+    int64_t plane;                   // elements between the planes
+};
+
+enum { kEpiStats = 0, kEpiSoftmax = 1, kEpiStore = 2 };
+
+constexpr int kStepK = 64;
+
+struct Product16 {
+    Operand16 A, B;
+    int M, N, K;
+    int n_seg;                       // pairs of planes
+    uint8_t seg_a[8], seg_b[8];
+    int tiles_m, tiles_n, per_xcd;   // tiles, and workgroups of an XCD
+    int splits, steps_per_split;     // shares of the sum, and steps of a share
+    int steps;                       // steps in all: n_seg * ceil(K / 64)
+    // kEpiStore: C (out_bf16 or fp32, rows ldc apart); with several shares their fp32 sums at part + share * M * N instead
+    void* C;
+    int64_t ldc;
+    int out_bf16, vec;               // vec: four neighbouring columns are one aligned store
+    const float* add;                // fp32 [M][N] added to the sum, or NULL
+    float* part;
+    // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece
+    const int64_t* targets;
+    int64_t ignore_index;
+    int n0, V;
+    float2* stats;                   // [ceil(N / stats_n)][M] maximum and sum of exponentials
+    float* target_logit;             // [M]
+    const float* lse;
+    const float* g;
+    bf16* P;                         // [planes][M][ldp]
+    int64_t ldp, p_plane;
+    int p_planes;
+};
+
+__device__ __forceinline__ bool no_loss(int64_t target, int64_t ignore, int V) { return target == ignore || target < 0 || target >= V; }
+
+// Tile, shares and steps of a product; the launch (product16.hip).
+struct Plan16 {
+    bool big;
+    int splits, steps_per_split, steps;
+    size_t part_bytes;
+};
+Plan16 plan16(int M, int N, int K, int n_seg, bool can_split);
+int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st);
+int stats_words16(const Plan16& pl);           // words of the vocabulary per pair of the stats
+int init_product16();
+// bf16 planes [P][rows][ldp] of X [rows][cols], zeros up to ldp; rows whose target has no loss are zeros (targets may be NULL)
+int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V,
+                    bf16* out, int64_t ldp, hipStream_t st);
+
+}  // namespace dab

@@ -1,0 +1,289 @@
+// Weights in 4 bits: laying out, reading back, and products of a few tokens with them.
+//
+// The product reads 0.53 bytes a weight and is bound by that.  A vector multiply-add per weight would
+// already exceed the vector units' rate at one token, so the matrix cores do it at any number of tokens: a wavefront holds 16 rows of
+// weights as the left operand of 16 x 16 x 32 products, converted from 4 bits to bf16 and scaled by one instruction per two weights, and up to
+// 16 columns of tokens as the right one.  A token whose numbers are wider than bf16 takes two or three columns, one per piece;
+// the columns of a token are added up at the end.  The layout (include/dab.h) gives every lane the 32 weights of one group,
+// so that a load is 16 bytes a lane and a kilobyte a wavefront, and a lane has one scale for them; the order of the weights within
+// the sum is then that of the lanes, which the tokens' loads follow.
+#include "real16.h"
+
+namespace dab {
+
+constexpr int kW4MaxWaves = 8;       // wavefronts per workgroup
+
+// ---------------------------------------------------------------- laying out
+// One wavefront: 16 rows x 512 weights, a lane per row and group.
+template <typename T>
+__global__ __launch_bounds__(64) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int vec, int Kt, int K4,
+                                                     uint8_t* __restrict__ Q, uint8_t* __restrict__ S) {
+    const int lane = threadIdx.x, tile = blockIdx.y, step = blockIdx.x;
+    const int row = tile * 16 + (lane & 15);
+    uint32_t codes = 0;
+    for (int j = 0; j < 4; ++j) {
+        const int kt = step * 4 + j;
+        int scale = 17;
+        if (kt < Kt) {
+            const int k0 = kt * 128 + (lane >> 4) * 32;
+            float v[4][8];
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (row < F && k0 + 8 * i < K) {
+                    load8(W + row * ldw, k0 + 8 * i, K, vec, v[i]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) v[i][u] = 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) m = max(m, __builtin_bit_cast(uint32_t, v[i][u]) & 0x7fffffffu);
+            }
+            const bool finite = m < 0x7f800000u;
+            const int e = group_exponent<2>(finite ? m : 0);
+            const float inv = pow2f(-e);
+            scale = finite ? e + 127 : 255;
+            v4u32 out;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t word = 0;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float a = fabsf(v[i][u] * inv);
+                    // to the nearest level, in the middle to the even code
+                    uint32_t code = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
+                    code |= (__builtin_bit_cast(uint32_t, v[i][u]) >> 31) << 3;
+                    word |= (finite ? code : 7u) << (4 * u);
+                }
+                out[i] = word;
+            }
+            *reinterpret_cast<v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16) = out;
+        }
+        codes |= static_cast<uint32_t>(scale) << (8 * j);
+    }
+    *reinterpret_cast<uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4) = codes;
+}
+
+// The scale of block j of four from its byte, as the conversions take it.
+__device__ __forceinline__ float scale_of(uint32_t codes, int j) {
+    const uint32_t s = (codes >> (8 * j)) & 255u;
+    return __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : s << 23);
+}
+
+__global__ __launch_bounds__(64) void w4_unpack_kernel(const uint8_t* __restrict__ Q, const uint8_t* __restrict__ S, int F, int K,
+                                                       int Kt, int K4, float* __restrict__ W) {
+    const int lane = threadIdx.x, tile = blockIdx.y, step = blockIdx.x;
+    const int row = tile * 16 + (lane & 15);
+    if (row >= F) return;
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4);
+    for (int j = 0; j < 4; ++j) {
+        const int kt = step * 4 + j;
+        if (kt >= Kt) break;
+        const v4u32 q = *reinterpret_cast<const v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16);
+        const uint32_t s = (codes >> (8 * j)) & 255u;
+        const float scale = s == 255u ? __builtin_nanf("") : pow2f(static_cast<int>(s) - 127);
+        const int k0 = kt * 128 + (lane >> 4) * 32;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t c = (q[i] >> (4 * u)) & 15u, m = c & 7u;
+                // 0, 1/2, then (2 + last bit) 2^(upper bits - 2)
+                const float a = m < 2 ? 0.5f * static_cast<float>(m)
+                                      : static_cast<float>(2u + (m & 1u)) * pow2f(static_cast<int>(m >> 1) - 2);
+                v[u] = (c & 8u ? -a : a) * scale;
+            }
+            if (k0 + 8 * i < K) store8(W + static_cast<int64_t>(row) * K, k0 + 8 * i, K, (K & 3) == 0, v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- tokens as bf16 pieces
+// [P][B][ldp] from X [B][K], zeros from K to ldp (a multiple of 8).
+template <typename T, int P>
+__global__ __launch_bounds__(256) void w4_pieces_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int vec, int ldp,
+                                                        bf16* __restrict__ out) {
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 8, b = blockIdx.y;
+    if (c >= ldp) return;
+    float v[8];
+    load8(X + b * ldx, c, K, vec, v);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        v8bf o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = piece_of(v[i], p);
+        *reinterpret_cast<v8bf*>(out + (static_cast<int64_t>(p) * B + b) * ldp + c) = o;
+    }
+}
+
+// ---------------------------------------------------------------- product
+struct W4Geom {
+    int F, Kt, K4, Kx;               // Kx: elements of a token's row in memory, a multiple of 8
+    int Ft, ks, tiles;               // 16-row tiles, wavefronts that share one, tiles of a workgroup
+    int B, nb, P;                    // tokens in all and per pass over the weights, pieces
+    int64_t ldx;                     // of the bf16 rows (piece p of token b: row p B + b)
+};
+
+// Eight weights as bf16, times a power of two.
+__device__ __forceinline__ v8bf weights8(uint32_t q, float scale) {
+    v8bf a;
+    const v2bf w0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 0), w1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 1);
+    const v2bf w2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 2), w3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, 3);
+    a[0] = w0[0], a[1] = w0[1], a[2] = w1[0], a[3] = w1[1], a[4] = w2[0], a[5] = w2[1], a[6] = w3[0], a[7] = w3[1];
+    return a;
+}
+
+template <typename T, int NCT>
+__global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16* __restrict__ X, const uint8_t* __restrict__ Q,
+                                                                     const uint8_t* __restrict__ S, W4Geom g, T* __restrict__ Y) {
+    extern __shared__ float sums[];                          // [wavefront][column][16 rows]
+    DAB_RESERVE_VGPRS();
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = blockIdx.x * g.tiles + wave / g.ks, part = wave % g.ks;
+    const int b0 = blockIdx.y * g.nb, nb = min(g.nb, g.B - b0), cols = nb * g.P;
+
+    v4f acc[NCT];
+    const bf16* xrow[NCT];
+    bool live[NCT];
+#pragma unroll
+    for (int t = 0; t < NCT; ++t) {
+        const int c = t * 16 + (lane & 15);
+        acc[t] = v4f{0.f, 0.f, 0.f, 0.f};
+        live[t] = c < cols;
+        const int p = live[t] ? c / nb : 0, b = live[t] ? c - p * nb : 0;
+        xrow[t] = X + (static_cast<int64_t>(p) * g.B + b0 + b) * g.ldx;
+    }
+    if (tile < g.Ft) {
+        const uint8_t* qt = Q + static_cast<int64_t>(tile) * g.Kt * 1024 + lane * 16;
+        const uint8_t* st = S + static_cast<int64_t>(tile) * g.K4 * 256 + lane * 4;
+        for (int s = part; s < g.K4; s += g.ks) {
+            const uint32_t codes = *reinterpret_cast<const uint32_t*>(st + s * 256);
+            v4u32 q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                q[j] = v4u32{0, 0, 0, 0};
+                if (4 * s + j < g.Kt) q[j] = *reinterpret_cast<const v4u32*>(qt + static_cast<int64_t>(4 * s + j) * 1024);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float scale = scale_of(codes, j);
+                const int k0 = (4 * s + j) * 128 + (lane >> 4) * 32;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const v8bf a = weights8(q[j][i], scale);
+#pragma unroll
+                    for (int t = 0; t < NCT; ++t) {
+                        v8bf x = {};
+                        if (live[t] && k0 + 8 * i < g.Kx) x = *reinterpret_cast<const v8bf*>(xrow[t] + k0 + 8 * i);
+                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, x, acc[t], 0, 0, 0);
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NCT; ++t)
+        *reinterpret_cast<v4f*>(sums + ((wave * NCT + t) * 16 + (lane & 15)) * 16 + (lane >> 4) * 4) = acc[t];
+    __syncthreads();
+    // the shares of a tile and the pieces of a token, added in a fixed order
+    for (int i = threadIdx.x; i < g.tiles * 16 * nb; i += blockDim.x) {
+        const int r = i & 15, tb = i >> 4, tl = tb / nb, b = tb - tl * nb;
+        const int f = (blockIdx.x * g.tiles + tl) * 16 + r;
+        float y = 0.f;
+        for (int p = g.P - 1; p >= 0; --p)
+            for (int u = 0; u < g.ks; ++u) y += sums[((tl * g.ks + u) * NCT * 16 + p * nb + b) * 16 + r];
+        if (f < g.F) Y[static_cast<int64_t>(b0 + b) * g.F + f] = static_cast<T>(y);
+    }
+}
+
+// Aligned bf16 tokens are read where they are; others as pieces from the workspace.
+static bool w4_direct(int32_t K, int32_t dtype, int64_t ldx) { return dtype == DAB_BF16 && K % 8 == 0 && ldx % 8 == 0; }
+
+template <typename T, int NCT>
+static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
+    const int waves = g.ks * g.tiles;
+    const dim3 grid(ceil_div(g.Ft, g.tiles), ceil_div(g.B, g.nb));
+    return launch(w4_matvec_kernel<T, NCT>, grid, dim3(64 * waves), static_cast<size_t>(waves) * NCT * 1024, st, X, Q, S, g,
+                  static_cast<T*>(Y));
+}
+template <typename T>
+static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
+    switch (ceil_div(g.nb * g.P, 16)) {
+        case 1: return launch_matvec<T, 1>(g, st, X, Q, S, Y);
+        case 2: return launch_matvec<T, 2>(g, st, X, Q, S, Y);
+        case 3: return launch_matvec<T, 3>(g, st, X, Q, S, Y);
+        default: return launch_matvec<T, 4>(g, st, X, Q, S, Y);
+    }
+}
+
+}  // namespace dab
+
+extern "C" int dab_w4_pack(const void* W, int32_t dtype, int32_t F, int32_t K, int64_t ldw, uint8_t* Q, uint8_t* S, void* stream) {
+    using namespace dab;
+    if (!W || !Q || !S) return DAB_ERR_NULL;
+    if (F < 1 || K < 1 || ldw < K) return DAB_ERR_SHAPE;
+    if (!real_dtype(dtype) || K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
+    const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4), vec = ldw * dtype_bytes(dtype) % 16 == 0;
+    const dim3 grid(K4, ceil_div(F, 16)), block(64);
+    const auto st = static_cast<hipStream_t>(stream);
+    if (dtype == DAB_F32) return launch(w4_pack_kernel<float>, grid, block, 0, st, static_cast<const float*>(W), F, K, ldw, vec, Kt, K4, Q, S);
+    if (dtype == DAB_BF16) return launch(w4_pack_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(W), F, K, ldw, vec, Kt, K4, Q, S);
+    return launch(w4_pack_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(W), F, K, ldw, vec, Kt, K4, Q, S);
+}
+
+extern "C" int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, float* W, void* stream) {
+    using namespace dab;
+    if (!W || !Q || !S) return DAB_ERR_NULL;
+    if (F < 1 || K < 1) return DAB_ERR_SHAPE;
+    if (K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
+    const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4);
+    return launch(w4_unpack_kernel, dim3(K4, ceil_div(F, 16)), dim3(64), 0, static_cast<hipStream_t>(stream), Q, S, F, K, Kt, K4, W);
+}
+
+extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
+    using namespace dab;
+    if (B < 1 || K < 1 || F < 1 || !real_dtype(dtype) || w4_direct(K, dtype, ldx)) return 0;
+    return static_cast<size_t>(dtype_pieces(dtype)) * B * round_up(K, 8) * 2;
+}
+
+extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K,
+                             int32_t F, void* Y, void* ws, size_t ws_bytes, void* stream) {
+    using namespace dab;
+    if (!X || !Q || !S || !Y) return DAB_ERR_NULL;
+    if (B < 1 || K < 1 || F < 1 || ldx < K) return DAB_ERR_SHAPE;
+    if (!real_dtype(dtype) || K > INT32_MAX - 512 || B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
+    const size_t need = dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx);
+    if (need && (!ws || ws_bytes < need || misaligned(ws, 256))) return DAB_ERR_WORKSPACE;
+    const auto st = static_cast<hipStream_t>(stream);
+
+    W4Geom g{};
+    g.F = F, g.Kt = ceil_div(K, 128), g.K4 = ceil_div(g.Kt, 4), g.Kx = static_cast<int>(round_up(K, 8));
+    g.Ft = ceil_div(F, 16), g.B = B, g.P = dtype_pieces(dtype);
+    const int passes = ceil_div(B, 64 / g.P);
+    g.nb = ceil_div(B, passes);
+    // shares of a row's sum: until every compute unit has eight wavefronts
+    g.ks = 1;
+    while (g.ks < 8 && g.ks < g.K4 && g.Ft * g.ks < 8 * kNumCU) g.ks *= 2;
+    g.tiles = 8 / g.ks;
+    const bf16* x = static_cast<const bf16*>(X);
+    g.ldx = ldx;
+    if (need) {
+        g.ldx = g.Kx;
+        bf16* out = static_cast<bf16*>(ws);
+        const dim3 grid(ceil_div(g.Kx, 2048), B), block(256);
+        const int vec = ldx * dtype_bytes(dtype) % 16 == 0;
+        int rc;
+        if (dtype == DAB_F32) rc = launch(w4_pieces_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), B, K, ldx, vec, g.Kx, out);
+        else if (dtype == DAB_F16) rc = launch(w4_pieces_kernel<f16, 2>, grid, block, 0, st, static_cast<const f16*>(X), B, K, ldx, vec, g.Kx, out);
+        else rc = launch(w4_pieces_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), B, K, ldx, vec, g.Kx, out);
+        if (rc) return rc;
+        x = out;
+    }
+    if (dtype == DAB_F32) return launch_matvec<float>(g, st, x, Q, S, Y);
+    if (dtype == DAB_BF16) return launch_matvec<bf16>(g, st, x, Q, S, Y);
+    return launch_matvec<f16>(g, st, x, Q, S, Y);
+}
