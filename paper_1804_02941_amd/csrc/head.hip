@@ -51,7 +51,7 @@ struct HeadPlan {
 };
 
 static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
-    return (dtype == DAB_BF16 || dtype == DAB_F32) && ldh < (1 << 23) && ldw < (1 << 23) && T < (1 << 30) && V < (1 << 30) &&
+    return (dtype == DAB_BF16 || dtype == DAB_F32) && ldh < (1 << 22) && ldw < (1 << 22) && T < (1 << 30) && V < (1 << 30) &&
            ceil_div64(T, 128) * ceil_div64(V, 128) < INT32_MAX / 64 && ceil_div64(T, 128) * ceil_div64(D, 128) < INT32_MAX / 1024;
 }
 
@@ -108,9 +108,8 @@ static int head_check(const void* H, int64_t ldh, const void* W, int64_t ldw, in
 
 static void head_segments(Product16& g, int n_seg) {
     // pairs of pieces in order of size; what is left out is below 2^-24 of a term
-    static const uint8_t a[6] = {0, 0, 1, 1, 0, 2}, b[6] = {0, 1, 0, 1, 2, 0};
     g.n_seg = n_seg;
-    for (int i = 0; i < n_seg; ++i) g.seg_a[i] = a[i], g.seg_b[i] = b[i];
+    if (n_seg > 1) g.seg_a = 0x201100, g.seg_b = 0x021010;
 }
 
 // The operands as bf16 planes, in the workspace where they are not already.

@@ -28,7 +28,7 @@ struct Product16 {
     Operand16 A, B;
     int M, N, K;
     int n_seg;                       // pairs of planes
-    uint8_t seg_a[8], seg_b[8];
+    uint32_t seg_a, seg_b;           // plane of each pair, four bits a pair
     int tiles_m, tiles_n, per_xcd;   // tiles, and workgroups of an XCD
     int splits, steps_per_split;     // shares of the sum, and steps of a share
     int steps;                       // steps in all: n_seg * ceil(K / 64)

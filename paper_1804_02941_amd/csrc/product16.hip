@@ -1,6 +1,8 @@
 // Host side of the bf16 products (product16.h): tile and split of a product, launches, and the kernels around it.
 #include "product16.h"
 
+#include <type_traits>
+
 namespace dab {
 
 // ---------------------------------------------------------------- the product
@@ -8,70 +10,63 @@ __device__ __forceinline__ void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-static __device__ const uint32_t g_zeros16[4] = {0, 0, 0, 0};
-
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
-typedef __attribute__((address_space(1))) const uint32_t glb_u32;
+// A byte offset past every tile: a load from there gives zeros.  What a tile's offsets reach stays below it (ld < 2^22).
+constexpr uint32_t kPast16 = 0x80000000u;
 
-// One operand's tile of ROWS x 64 k in LDS.
-template <int ROWS, bool RC, int NW>
-struct Tile16 {
-    static constexpr int kBytes = ROWS * kStepK * 2;
-    static constexpr int kCopies = kBytes / 1024 / NW;       // of one wavefront
-    static constexpr int kChunks = RC ? ROWS / 8 : 8;        // 16-byte pieces of a row of the tile in LDS
-    static constexpr int kLdsRows = 64 / kChunks;            // rows of it that one copy fills
-
-    // Where the lane's piece of copy c comes from: row and column in the tile (in elements of its two directions).
-    // A row's pieces are permuted so that the reads below meet no bank twice; a copy's lanes are in order in LDS, so the
-    // permutation is one of the addresses in memory.
-    static __device__ __forceinline__ void source(int copy, int lane, int* lds_row, int* elem) {
-        const int r = copy * kLdsRows + lane / kChunks, phys = lane % kChunks;
-        *lds_row = r;
-        if constexpr (RC) *elem = (phys ^ (((r & 3) | ((r >> 3) & 1) << 2) << 1)) * 8;
-        else *elem = (phys ^ ((r >> 1) & 7)) * 8;
-    }
-};
-
+// One operand's tile of ROWS x 64 k, from memory into LDS.
 template <int ROWS, bool RC, int NW>
 struct Loader16 {
-    using Tl = Tile16<ROWS, RC, NW>;
-    uint32_t off[Tl::kCopies];                               // bytes from the tile's origin, the same every step
-    int wave, lane;
+    static constexpr int kBytes = ROWS * kStepK * 2;
+    static constexpr int kCopies = kBytes / 1024 / NW;       // of one wavefront, a kilobyte each
+    static constexpr int kChunks = RC ? ROWS / 8 : 8;        // 16-byte pieces of a row of the tile in LDS
+    static constexpr int kLdsRows = 64 / kChunks;            // rows of it that one copy fills
+    uint32_t off[kCopies];                                   // bytes from the tile's origin, the same every step
+    uint64_t past[2];                                        // lanes whose k are past K in the last step, even and odd copies
+    __amdgpu_buffer_rsrc_t rsrc;
+    int wave;
 
-    // rows: how many of the operand's rows are left from the tile's first on; rows past them are read from the last one
-    // (their results are not used)
-    __device__ __forceinline__ void init(int w, int l, int64_t ld, int rows) {
-        wave = w, lane = l;
+    // A row's pieces are permuted in LDS so that the reads below meet no bank twice.  A copy's lanes are in order in LDS, so the
+    // permutation is one of the addresses in memory.  rows: how many of the operand's rows are left from the tile's first on.
+    __device__ __forceinline__ void init(int w, int lane, int64_t ld, int rows, int K) {
+        wave = w;
 #pragma unroll
-        for (int c = 0; c < Tl::kCopies; ++c) {
-            int r, e;
-            Tl::source(w * Tl::kCopies + c, l, &r, &e);
-            if constexpr (RC) off[c] = static_cast<uint32_t>((r * ld + min(e, (rows - 1) & ~7)) * 2);
-            else off[c] = static_cast<uint32_t>((min(r, rows - 1) * ld + e) * 2);
+        for (int c = 0; c < kCopies; ++c) {
+            const int r = (w * kCopies + c) * kLdsRows + lane / kChunks, phys = lane % kChunks;
+            int e;
+            if constexpr (RC) {
+                e = (phys ^ (((r & 3) | ((r >> 3) & 1) << 2) << 1)) * 8;
+                off[c] = e < rows ? static_cast<uint32_t>((r * ld + e) * 2) : kPast16;
+            } else {
+                e = (phys ^ ((r >> 1) & 7)) * 8;
+                off[c] = r < rows ? static_cast<uint32_t>((r * ld + e) * 2) : kPast16;
+                if (c < 2) past[c] = __ballot(K % kStepK != 0 && e >= K % kStepK);
+            }
         }
     }
-    // origin: the tile's first element of this step; k_left: k that are left from there on
-    __device__ __forceinline__ void copy(const bf16* origin, int k_left, char* lds) const {
-        const char* base = reinterpret_cast<const char*>(origin);
-#pragma unroll
-        for (int c = 0; c < Tl::kCopies; ++c) {
-            const char* src = base + off[c];
-            if (k_left < kStepK) {
-                int r, e;
-                Tl::source(wave * Tl::kCopies + c, lane, &r, &e);
-                if ((RC ? r : e) >= k_left) src = reinterpret_cast<const char*>(g_zeros16);
-            }
-            __builtin_amdgcn_global_load_lds((glb_u32*)src, (lds_u32*)(lds + (wave * Tl::kCopies + c) * 1024), 16, 0, 0);
-        }
+    // origin: the tile's first element of this step; left: bytes of the operand from there on ([k][rows]), or k (none: zeros).
+    // Rows past K are past the end of the buffer in one form, offsets of their own in the other.
+    __device__ __forceinline__ void aim(const bf16* origin, int64_t left) {
+        const uint32_t bytes = left <= 0 ? 0u : RC && left < kPast16 ? static_cast<uint32_t>(left) : kPast16;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(origin), 0, static_cast<int>(bytes), 0x00020000);
+    }
+    __device__ __forceinline__ void copy(int c, bool last_k, char* lds) const {
+        uint32_t o = off[c];
+        if constexpr (!RC) o = __builtin_amdgcn_inverse_ballot_w64(last_k ? past[c & 1] : 0) ? kPast16 : o;
+        // (in assembly because the compiler would have every later LDS read wait for the copy; what may be read is behind wait_and_meet())
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"               // (m0 is named as clobbered, which nothing else here uses)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     : : "s"(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_u32*)(lds + (wave * kCopies + c) * 1024)))), "v"(o), "s"(rsrc) : "m0");
+#pragma clang diagnostic pop
     }
 };
 
 // Fragments of 16 rows x 32 k: lane l holds row l % 16, k = 8 (l / 16) .. + 7.
-template <int ROWS, bool RC>
+template <int ROWS, bool RC, int NFRAG>
 struct Reader16 {
-    uint32_t at[RC ? 8 : 2];
+    uint32_t at[RC ? NFRAG : 2];
     // row0: this wavefront's first row in the tile
-    template <int NFRAG>
     __device__ __forceinline__ void init(int lane, int row0) {
         if constexpr (RC) {
             // a group of 16 lanes reads 4 k x 16 rows, a lane 4 neighbouring rows of one k, and gets the four k of its row
@@ -101,11 +96,11 @@ struct Reader16 {
 };
 
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
-__global__ __launch_bounds__(64 * WM * WN) void product16_kernel(Product16 g) {
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
-    using TA = Tile16<TM, ARC, NW>;
-    using TB = Tile16<TN, BRC, NW>;
-    constexpr int kBuf = TA::kBytes + TB::kBytes;
+    using LA = Loader16<TM, ARC, NW>;
+    using LB = Loader16<TN, BRC, NW>;
+    constexpr int kBuf = LA::kBytes + LB::kBytes;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -114,84 +109,137 @@ __global__ __launch_bounds__(64 * WM * WN) void product16_kernel(Product16 g) {
     const int unit = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);
     const int tiles = g.tiles_m * g.tiles_n;
     if (unit >= tiles * g.splits) return;
-    const int share = unit / tiles, tile = unit - share * tiles;
-    const int band = tile / (8 * g.tiles_n), in_band = tile - band * 8 * g.tiles_n;
+    // (quotients come from vector instructions; what is made of them here has to be scalar)
+    const int share = __builtin_amdgcn_readfirstlane(unit / tiles), tile = unit - share * tiles;
+    const int band = __builtin_amdgcn_readfirstlane(tile / (8 * g.tiles_n)), in_band = tile - band * 8 * g.tiles_n;
     const int bm = min(8, g.tiles_m - band * 8);
-    const int tn = in_band / bm, tm = band * 8 + in_band - tn * bm;
+    const int tn = __builtin_amdgcn_readfirstlane(in_band / bm), tm = band * 8 + in_band - tn * bm;
     const int m0 = tm * TM, n0 = tn * TN;
     const int wm = wave % WM, wn = wave / WM;
 
-    Loader16<TM, ARC, NW> la;
-    Loader16<TN, BRC, NW> lb;
-    la.init(wave, lane, g.A.ld, g.M - m0);
-    lb.init(wave, lane, g.B.ld, g.N - n0);
+    LA la;
+    LB lb;
+    la.init(wave, lane, g.A.ld, g.M - m0, g.K);
+    lb.init(wave, lane, g.B.ld, g.N - n0, g.K);
     const bf16* a0 = g.A.p + (ARC ? m0 : m0 * g.A.ld);
     const bf16* b0 = g.B.p + (BRC ? n0 : n0 * g.B.ld);
-    const int64_t ka = ARC ? g.A.ld : 1, kb = BRC ? g.B.ld : 1;
+    const int64_t ka = kStepK * (ARC ? g.A.ld : 1), kb = kStepK * (BRC ? g.B.ld : 1);   // a step further
 
     const int first = share * g.steps_per_split, last = min(first + g.steps_per_split, g.steps);
-    const int per_seg = g.steps / g.n_seg;
-    int seg = first / per_seg, k = (first - seg * per_seg) * kStepK;
+    const int per_seg = __builtin_amdgcn_readfirstlane(g.steps / g.n_seg);
+    // the step that is fetched next: how many are left, its pair of planes, its operands and k left there
+    int to_fetch = last - first, seg = __builtin_amdgcn_readfirstlane(first / per_seg), k_left = g.K - (first - seg * per_seg) * kStepK;
+    const bf16* pa = a0 + ((g.seg_a >> (4 * seg)) & 15) * g.A.plane + (first - seg * per_seg) * ka;
+    const bf16* pb = b0 + ((g.seg_b >> (4 * seg)) & 15) * g.B.plane + (first - seg * per_seg) * kb;
+    bool last_k = false;
+    auto aim = [&] {
+        const int left = to_fetch > 0 ? k_left : 0;
+        la.aim(pa, ARC ? left * g.A.ld * 2 : left);
+        lb.aim(pb, BRC ? left * g.B.ld * 2 : left);
+        last_k = k_left < kStepK;
+        --to_fetch, k_left -= kStepK, pa += ka, pb += kb;
+        if (k_left <= 0 && to_fetch > 0) {
+            ++seg, k_left = g.K;
+            pa = a0 + ((g.seg_a >> (4 * seg)) & 15) * g.A.plane;
+            pb = b0 + ((g.seg_b >> (4 * seg)) & 15) * g.B.plane;
+        }
+    };
     auto fetch = [&](char* buf) {
-        la.copy(a0 + g.seg_a[seg] * g.A.plane + k * ka, g.K - k, buf);
-        lb.copy(b0 + g.seg_b[seg] * g.B.plane + k * kb, g.K - k, buf + TA::kBytes);
-        k += kStepK;
-        if (k >= g.K) k = 0, ++seg;
+#pragma unroll
+        for (int c = 0; c < LA::kCopies; ++c) la.copy(c, last_k, buf);
+#pragma unroll
+        for (int c = 0; c < LB::kCopies; ++c) lb.copy(c, last_k, buf + LA::kBytes);
     };
 
-    Reader16<TM, ARC> ra;
-    Reader16<TN, BRC> rb;
-    ra.template init<FM>(lane, wm * FM * 16);
-    rb.template init<FN>(lane, wn * FN * 16);
+    Reader16<TM, ARC, FM> ra;
+    Reader16<TN, BRC, FN> rb;
+    ra.init(lane, wm * FM * 16);
+    rb.init(lane, wn * FN * 16);
 
     v4f acc[FN][FM];
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
         for (int j = 0; j < FM; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    v8bf a[2][FM], b[2][FN];
+    // Half a step: its products, and among them the reads of the next half's fragments (early, so that they have arrived by its
+    // end) and, COPY, the copies of a later step, one at a time: a burst of either would hold up the products behind it.
+    auto half = [&](auto copy_c, int set, const char* buf, int kk, char* to) {
+        constexpr bool COPY = decltype(copy_c)::value;
+        constexpr int kCopies = LA::kCopies + LB::kCopies, kEarly = FN / 2;
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            if constexpr (COPY)
+#pragma unroll
+                for (int c = kCopies * i / FN; c < kCopies * (i + 1) / FN; ++c) {
+                    if (c < LA::kCopies) la.copy(c, last_k, to);
+                    else lb.copy(c - LA::kCopies, last_k, to + LA::kBytes);
+                }
+            if (i < kEarly) {
+#pragma unroll
+                for (int j = FM * i / kEarly; j < FM * (i + 1) / kEarly; ++j) a[set ^ 1][j] = ra.read(buf, kk, j);
+#pragma unroll
+                for (int u = 2 * i; u < 2 * i + 2; ++u) b[set ^ 1][u] = rb.read(buf + LA::kBytes, kk, u);
+            }
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[set][i], a[set][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    using yes = std::integral_constant<bool, true>;
+    using no = std::integral_constant<bool, false>;
 
+    // Two buffers of 64 k.  While a half step is multiplied from registers, the next one's fragments are read; behind the one barrier of a
+    // step, in its middle, the step after has landed and its own buffer has been read by all, so the step after that is fetched into it.
+    aim();
     fetch(lds);
     wait_and_meet();
+    aim();
+    fetch(lds + kBuf);
+#pragma unroll
+    for (int j = 0; j < FM; ++j) a[0][j] = ra.read(lds, 0, j);
+#pragma unroll
+    for (int i = 0; i < FN; ++i) b[0][i] = rb.read(lds + LA::kBytes, 0, i);
     for (int s = first; s < last; ++s) {
         char* cur = lds + ((s - first) & 1) * kBuf;
-        if (s + 1 < last) fetch(lds + ((s + 1 - first) & 1) * kBuf);
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            v8bf a[FM], b[FN];
-#pragma unroll
-            for (int j = 0; j < FM; ++j) a[j] = ra.read(cur, kk, j);
-#pragma unroll
-            for (int i = 0; i < FN; ++i) b[i] = rb.read(cur + TA::kBytes, kk, i);
-#pragma unroll
-            for (int i = 0; i < FN; ++i)
-#pragma unroll
-                for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[i], a[j], acc[i][j], 0, 0, 0);
-        }
+        char* other = lds + ((s + 1 - first) & 1) * kBuf;
+        aim();
+        half(no{}, 0, cur, 1, cur);
         wait_and_meet();
+        half(yes{}, 1, other, 0, cur);
     }
+    // (copies and reads past the last step: zeros, and not used; the wavefront waits for them before it ends)
+    wait_and_meet();
 
     const int mw = m0 + wm * FM * 16 + (lane & 15), nw = n0 + wn * FN * 16 + (lane >> 4) * 4;
+    const bool full = n0 + TN <= g.N;                        // no column past the last one
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
         const int m = mw + j * 16;
         const bool in = m < g.M;
         if constexpr (EPI == kEpiStats) {
             // maximum and sum of exponentials of this wavefront's words, one pair per token
+            if (!full) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (nw + i * 16 + r >= g.N) acc[i][j][r] = -__builtin_inff();
+            }
             float big = -__builtin_inff();
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (nw + i * 16 + r < g.N) big = fmaxf(big, acc[i][j][r]);
+            for (int i = 0; i < FN; ++i) big = fmaxf(fmaxf(fmaxf(big, acc[i][j][0]), fmaxf(acc[i][j][1], acc[i][j][2])), acc[i][j][3]);
             big = fmaxf(big, __shfl_xor(big, 16));
             big = fmaxf(big, __shfl_xor(big, 32));
-            float sum = 0.f;
             const float at = big == -__builtin_inff() ? 0.f : big;
+            float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
+            for (int i = 0; i < FN; ++i) {
+                float four = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (nw + i * 16 + r < g.N) sum += __expf(acc[i][j][r] - at);
+                for (int r = 0; r < 4; ++r) four += __expf(acc[i][j][r] - at);
+                sum += four;
+            }
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (in && lane < 16) g.stats[static_cast<int64_t>(tn * WN + wn) * g.M + m] = float2{big, sum};
@@ -209,15 +257,25 @@ __global__ __launch_bounds__(64 * WM * WN) void product16_kernel(Product16 g) {
                 const int64_t t = g.targets[m];
                 const bool dead = no_loss(t, g.ignore_index, g.V);
                 const float lse = dead ? 0.f : g.lse[m], w = dead ? 0.f : g.g ? g.g[m] : 1.f;
-                const int d = dead ? -1 : static_cast<int>(t) - g.n0;
                 bf16* row = g.P + m * g.ldp + nw;
+                // the target's column, counted from this lane's first
+                const int64_t d64 = dead ? -1 : t - g.n0 - nw;
+                const int d = d64 < 0 || d64 >= FN * 16 ? -1 : static_cast<int>(d64);
+                const bool hit = __ballot(d >= 0) != 0;
 #pragma unroll
                 for (int i = 0; i < FN; ++i) {
                     float p[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int n = nw + i * 16 + r;
-                        p[r] = dead || n >= g.N ? 0.f : w * (__expf(acc[i][j][r] - lse) - (n == d ? 1.f : 0.f));
+                    for (int r = 0; r < 4; ++r) p[r] = __expf(acc[i][j][r] - lse);
+                    if (hit) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) p[r] -= d == i * 16 + r ? 1.f : 0.f;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[r] *= w;
+                    if (!full || dead) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) p[r] = dead || nw + i * 16 + r >= g.N ? 0.f : p[r];
                     }
                     typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
                     for (int q = 0; q < g.p_planes; ++q) {
@@ -399,7 +457,7 @@ static GradPlan grad_plan(int32_t rows, int32_t cols, int32_t F, int32_t dtype, 
     return p;
 }
 static bool grad_sizes(int32_t rows, int32_t cols, int32_t F, int32_t dtype, int64_t lddy) {
-    return real_dtype(dtype) && lddy < (1 << 23) && F < (1 << 23) && cols < (1 << 23) &&
+    return real_dtype(dtype) && lddy < (1 << 22) && F < (1 << 22) && cols < (1 << 22) &&
            ceil_div64(F, 128) * ceil_div64(cols, 128) < INT32_MAX / 64;
 }
 }  // namespace dab
@@ -435,7 +493,7 @@ extern "C" int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t 
     g.B = {x, p.ldx, 0};
     g.M = F, g.N = cols, g.K = rows;
     g.n_seg = dtype_pieces(dtype);
-    for (int i = 0; i < g.n_seg; ++i) g.seg_a[i] = static_cast<uint8_t>(i);
+    g.seg_a = 0x210;                 // pieces of dY in turn, with the one plane of X
     g.C = dW, g.ldc = cols, g.vec = cols % 4 == 0;
     g.part = reinterpret_cast<float*>(base + p.part_at);
     return launch16(kEpiStore, true, true, g, p.pl, st);

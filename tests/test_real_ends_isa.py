@@ -1,0 +1,41 @@
+"""Static checks over the ISA of the bf16 product kernel (hipcc -S, no GPU): its copies into LDS are inline assembly that the compiler
+knows nothing of."""
+import re
+
+import pytest
+
+from paper_1804_02941_amd import isa_checks as ic
+
+
+@pytest.fixture(scope="module")
+def product_kernels(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("isa") / "product16.s")
+    ic.compile_to_isa("product16.hip", out)
+    found = {n: lines for n, lines in ic.kernels(open(out).read()) if "product16_kernel" in n}
+    assert len(found) >= 8
+    return found
+
+
+def test_no_copy_reads_a_scalar_register_too_soon(product_kernels):
+    for name, lines in product_kernels.items():
+        assert any("buffer_load_dwordx4" in l and " lds" in l for l in lines), name
+        assert ic.scalar_read_hazards(lines) == [], name
+
+
+def test_copies_are_waited_for_at_the_barriers_and_nowhere_else_in_the_loop(product_kernels):
+    """Every barrier comes with a wait for the wavefront's own copies and reads; and no wait of the compiler's stands among the
+    products, where it would hold up the copies that are meant to be in flight."""
+    for name, lines in product_kernels.items():
+        text = [l.strip() for l in lines]
+        for i, l in enumerate(text):
+            if l.startswith("s_barrier"):
+                assert text[i - 1] == "s_waitcnt vmcnt(0) lgkmcnt(0)", name
+        products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
+        waits = [l for l in text[products[0]:products[-1]] if re.match(r"s_waitcnt.*vmcnt", l)]
+        assert waits == ["s_waitcnt vmcnt(0) lgkmcnt(0)"], (name, waits)
+
+
+def test_nothing_else_uses_the_register_of_the_copies_address(product_kernels):
+    for name, lines in product_kernels.items():
+        users = [l for l in lines if re.search(r"\bm0\b", l.split(";")[0])]
+        assert users and all(re.match(r"\s*s_mov_b32 m0, s\d+|\s*s_mov_b32 m0, ttmp", l) for l in users), (name, users[:3])
