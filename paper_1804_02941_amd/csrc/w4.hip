@@ -120,9 +120,10 @@ __global__ __launch_bounds__(256) void w4_pieces_kernel(const T* __restrict__ X,
 // ---------------------------------------------------------------- product
 struct W4Geom {
     int F, Kt, K4, Kx;               // Kx: elements of a token's row in memory, a multiple of 8
-    int Ft, ks, tiles;               // 16-row tiles, wavefronts that share one, tiles of a workgroup
+    int Ft, ks, groups;              // 16-row tiles, wavefronts that share a group of tiles, groups of a workgroup
     int B, nb, P;                    // tokens in all and per pass over the weights, pieces
     int64_t ldx;                     // of the bf16 rows (piece p of token b: row p B + b)
+    int dtype;                       // of the output
 };
 
 // Eight weights as bf16, times a power of two.
@@ -134,86 +135,117 @@ __device__ __forceinline__ v8bf weights8(uint32_t q, float scale) {
     return a;
 }
 
-template <typename T, int NCT>
+// A wavefront's share of a step: 512 weights of each of its TB tiles, five loads a tile.
+template <int TB>
+struct Step4 {
+    v4u32 q[TB][4];
+    uint32_t codes[TB];
+    __device__ __forceinline__ void load(const uint8_t* __restrict__ Q, const uint8_t* __restrict__ S, const W4Geom& g, int tile, int s,
+                                         int lane) {
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            const int64_t tl = min(tile + t, g.Ft - 1);      // (a tile past the last is read from the last and not used)
+            codes[t] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(S + (tl * g.K4 + s) * 256 + lane * 4));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int kt = min(4 * s + j, g.Kt - 1);     // (likewise: its tokens are zeros)
+                q[t][j] = __builtin_nontemporal_load(reinterpret_cast<const v4u32*>(Q + (tl * g.Kt + kt) * 1024 + lane * 16));
+            }
+        }
+    }
+};
+
+template <int NCT, int TB>
 __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16* __restrict__ X, const uint8_t* __restrict__ Q,
-                                                                     const uint8_t* __restrict__ S, W4Geom g, T* __restrict__ Y) {
-    extern __shared__ float sums[];                          // [wavefront][column][16 rows]
+                                                                     const uint8_t* __restrict__ S, W4Geom g, void* __restrict__ Y) {
+    extern __shared__ float sums[];                          // [wavefront][tile][column][16 rows]
     DAB_RESERVE_VGPRS();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = blockIdx.x * g.tiles + wave / g.ks, part = wave % g.ks;
+    const int group = __builtin_amdgcn_readfirstlane(wave / g.ks), part = wave - group * g.ks;
+    const int tile0 = blockIdx.x * g.groups * TB, tile = tile0 + group * TB;
     const int b0 = blockIdx.y * g.nb, nb = min(g.nb, g.B - b0), cols = nb * g.P;
 
-    v4f acc[NCT];
+    v4f acc[TB][NCT];
     const bf16* xrow[NCT];
     bool live[NCT];
 #pragma unroll
     for (int t = 0; t < NCT; ++t) {
         const int c = t * 16 + (lane & 15);
-        acc[t] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < TB; ++u) acc[u][t] = v4f{0.f, 0.f, 0.f, 0.f};
         live[t] = c < cols;
         const int p = live[t] ? c / nb : 0, b = live[t] ? c - p * nb : 0;
-        xrow[t] = X + (static_cast<int64_t>(p) * g.B + b0 + b) * g.ldx;
+        xrow[t] = X + (static_cast<int64_t>(p) * g.B + b0 + b) * g.ldx + (lane >> 4) * 32;
     }
-    if (tile < g.Ft) {
-        const uint8_t* qt = Q + static_cast<int64_t>(tile) * g.Kt * 1024 + lane * 16;
-        const uint8_t* st = S + static_cast<int64_t>(tile) * g.K4 * 256 + lane * 4;
+    if (tile < g.Ft && part < g.K4) {
+        Step4<TB> now, next;
+        now.load(Q, S, g, tile, part, lane);
         for (int s = part; s < g.K4; s += g.ks) {
-            const uint32_t codes = *reinterpret_cast<const uint32_t*>(st + s * 256);
-            v4u32 q[4];
+            const bool more = s + g.ks < g.K4;
+            if (more) next.load(Q, S, g, tile, s + g.ks, lane);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                q[j] = v4u32{0, 0, 0, 0};
-                if (4 * s + j < g.Kt) q[j] = *reinterpret_cast<const v4u32*>(qt + static_cast<int64_t>(4 * s + j) * 1024);
-            }
+                const int k0 = (4 * s + j) * 128;
+                v8bf x[4][NCT];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float scale = scale_of(codes, j);
-                const int k0 = (4 * s + j) * 128 + (lane >> 4) * 32;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const v8bf a = weights8(q[j][i], scale);
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int t = 0; t < NCT; ++t) {
-                        v8bf x = {};
-                        if (live[t] && k0 + 8 * i < g.Kx) x = *reinterpret_cast<const v8bf*>(xrow[t] + k0 + 8 * i);
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, x, acc[t], 0, 0, 0);
+                        x[i][t] = v8bf{};
+                        if (live[t] && k0 + (lane >> 4) * 32 + 8 * i < g.Kx) x[i][t] = *reinterpret_cast<const v8bf*>(xrow[t] + k0 + 8 * i);
+                    }
+#pragma unroll
+                for (int u = 0; u < TB; ++u) {
+                    const float scale = scale_of(now.codes[u], j);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const v8bf a = weights8(now.q[u][j][i], scale);
+#pragma unroll
+                        for (int t = 0; t < NCT; ++t) acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, x[i][t], acc[u][t], 0, 0, 0);
                     }
                 }
             }
+            if (more) now = next;
         }
     }
 #pragma unroll
-    for (int t = 0; t < NCT; ++t)
-        *reinterpret_cast<v4f*>(sums + ((wave * NCT + t) * 16 + (lane & 15)) * 16 + (lane >> 4) * 4) = acc[t];
+    for (int u = 0; u < TB; ++u)
+#pragma unroll
+        for (int t = 0; t < NCT; ++t)
+            *reinterpret_cast<v4f*>(sums + (((wave * TB + u) * NCT + t) * 16 + (lane & 15)) * 16 + (lane >> 4) * 4) = acc[u][t];
     __syncthreads();
     // the shares of a tile and the pieces of a token, added in a fixed order
-    for (int i = threadIdx.x; i < g.tiles * 16 * nb; i += blockDim.x) {
-        const int r = i & 15, tb = i >> 4, tl = tb / nb, b = tb - tl * nb;
-        const int f = (blockIdx.x * g.tiles + tl) * 16 + r;
+    const int rows = g.groups * TB * 16;
+    for (int i = threadIdx.x; i < rows * nb; i += blockDim.x) {
+        const int b = i / rows, row = i - b * rows, r = row & 15, tl = row >> 4, grp = tl / TB, u = tl - grp * TB;
+        const int f = tile0 * 16 + row;
         float y = 0.f;
         for (int p = g.P - 1; p >= 0; --p)
-            for (int u = 0; u < g.ks; ++u) y += sums[((tl * g.ks + u) * NCT * 16 + p * nb + b) * 16 + r];
-        if (f < g.F) Y[static_cast<int64_t>(b0 + b) * g.F + f] = static_cast<T>(y);
+            for (int k = 0; k < g.ks; ++k) y += sums[(((grp * g.ks + k) * TB + u) * NCT * 16 + p * nb + b) * 16 + r];
+        if (f >= g.F) continue;
+        const int64_t at = static_cast<int64_t>(b0 + b) * g.F + f;
+        if (g.dtype == DAB_F32) static_cast<float*>(Y)[at] = y;
+        else if (g.dtype == DAB_BF16) static_cast<bf16*>(Y)[at] = static_cast<bf16>(y);
+        else static_cast<f16*>(Y)[at] = static_cast<f16>(y);
     }
 }
 
 // Aligned bf16 tokens are read where they are; others as pieces from the workspace.
 static bool w4_direct(int32_t K, int32_t dtype, int64_t ldx) { return dtype == DAB_BF16 && K % 8 == 0 && ldx % 8 == 0; }
 
-template <typename T, int NCT>
+template <int NCT, int TB>
 static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
-    const int waves = g.ks * g.tiles;
-    const dim3 grid(ceil_div(g.Ft, g.tiles), ceil_div(g.B, g.nb));
-    return launch(w4_matvec_kernel<T, NCT>, grid, dim3(64 * waves), static_cast<size_t>(waves) * NCT * 1024, st, X, Q, S, g,
-                  static_cast<T*>(Y));
+    const int waves = g.ks * g.groups;
+    const dim3 grid(ceil_div(g.Ft, g.groups * TB), ceil_div(g.B, g.nb));
+    return launch(w4_matvec_kernel<NCT, TB>, grid, dim3(64 * waves), static_cast<size_t>(waves) * TB * NCT * 1024, st, X, Q, S, g, Y);
 }
-template <typename T>
+template <int TB>
 static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
     switch (ceil_div(g.nb * g.P, 16)) {
-        case 1: return launch_matvec<T, 1>(g, st, X, Q, S, Y);
-        case 2: return launch_matvec<T, 2>(g, st, X, Q, S, Y);
-        case 3: return launch_matvec<T, 3>(g, st, X, Q, S, Y);
-        default: return launch_matvec<T, 4>(g, st, X, Q, S, Y);
+        case 1: return launch_matvec<1, TB>(g, st, X, Q, S, Y);
+        case 2: return launch_matvec<2, TB>(g, st, X, Q, S, Y);
+        case 3: return launch_matvec<3, TB == 4 ? 2 : TB>(g, st, X, Q, S, Y);
+        default: return launch_matvec<4, TB == 4 ? 2 : TB>(g, st, X, Q, S, Y);
     }
 }
 
@@ -265,10 +297,17 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
     g.Ft = ceil_div(F, 16), g.B = B, g.P = dtype_pieces(dtype);
     const int passes = ceil_div(B, 64 / g.P);
     g.nb = ceil_div(B, passes);
-    // shares of a row's sum: until every compute unit has eight wavefronts
+    // Tiles of a wavefront: with one they are spread furthest, with more the tokens are loaded less often.  One token, 4096 weights a
+    // row: 16384 rows 12.4 us with one, 9.4 with two, 10.1 with four; 4096 rows of 9216 8.7, 9.9, 14.0.  Twenty-one columns: 4099 rows of
+    // 9111 31, 20, 25; thirty-two, 32768 rows of 4096: 68, 43, 31.  (Four tiles and three columns of tokens do not fit the registers.)
+    const int columns = ceil_div(g.nb * g.P, 16);
+    const int TB = columns == 1 ? (g.Ft >= 1024 ? 2 : 1) : columns == 2 && g.Ft >= 1024 ? 4 : g.Ft >= 128 ? 2 : 1;
+    // Shares of a row's sum: until there are 24 wavefronts for every compute unit (32768 rows of 4096, two tiles: 28 us with
+    // one share, 17.9, 17.1, 16.8 with eight; 131072 rows 58.3, 52.5 with two, 55.0, 57.6).
     g.ks = 1;
-    while (g.ks < 8 && g.ks < g.K4 && g.Ft * g.ks < 8 * kNumCU) g.ks *= 2;
-    g.tiles = 8 / g.ks;
+    while (g.ks < 8 && g.ks < g.K4 && g.Ft / TB * g.ks < 24 * kNumCU) g.ks *= 2;
+    g.groups = 8 / g.ks;
+    g.dtype = dtype;
     const bf16* x = static_cast<const bf16*>(X);
     g.ldx = ldx;
     if (need) {
@@ -283,7 +322,5 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
         if (rc) return rc;
         x = out;
     }
-    if (dtype == DAB_F32) return launch_matvec<float>(g, st, x, Q, S, Y);
-    if (dtype == DAB_BF16) return launch_matvec<bf16>(g, st, x, Q, S, Y);
-    return launch_matvec<f16>(g, st, x, Q, S, Y);
+    return TB == 4 ? launch_matvec<4>(g, st, x, Q, S, Y) : TB == 2 ? launch_matvec<2>(g, st, x, Q, S, Y) : launch_matvec<1>(g, st, x, Q, S, Y);
 }
