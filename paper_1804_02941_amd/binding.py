@@ -583,6 +583,9 @@ def _saved(Q, S, cols):
 
 def dab_ckpt8_save(X, out=None):
     """X [rows, cols] fp32, bf16 or f16 -> (Q int8 [rows, 32 ceil(cols/32)], S uint8 [rows, ceil(cols/32)])."""
+    done = (_native or native()).ckpt8_save(X, out)
+    if done is not None:
+        return done
     ptr, dtype, ld = _matrix(X, "X")
     rows, cols = X.shape
     Q, S = out if out is not None else ckpt8_outputs(rows, cols, X.device)
@@ -595,6 +598,10 @@ def dab_ckpt8_save(X, out=None):
 
 def dab_ckpt8_restore(Q, S, cols, dtype=torch.float32, out=None):
     """What dab_ckpt8_save() kept of `cols` channels, as a tensor [rows, cols] of dtype (or into `out`)."""
+    if out is None:
+        done = (_native or native()).ckpt8_restore(Q, S, cols, dtype)
+        if done is not None:
+            return done
     q, s, rows = _saved(Q, S, cols)
     X = out if out is not None else torch.empty((rows, cols), dtype=dtype, device=Q.device)
     ptr, code, ld = _matrix(_shaped(X, (rows, cols), "out"), "out")
@@ -604,6 +611,9 @@ def dab_ckpt8_restore(Q, S, cols, dtype=torch.float32, out=None):
 
 def dab_ckpt8_weight_gradient(dY, Q, S, cols, out=None, ws=None):
     """dW = dY^T X fp32 [F, cols] from dY [rows, F] (fp32, bf16 or f16) and what dab_ckpt8_save() kept of X [rows, cols]."""
+    done = (_native or native()).ckpt8_weight_gradient(dY, Q, S, cols, out, ws)
+    if done is not None:
+        return done
     ptr, dtype, ld = _matrix(dY, "dY")
     q, s, rows = _saved(Q, S, cols)
     F = _shaped(dY, (rows, dY.shape[1]), "dY").shape[1]
@@ -627,6 +637,9 @@ def _head(H, W, targets):
 
 def dab_head_loss(H, W, targets, ignore_index=-100, out=None, ws=None):
     """Softmax cross entropy of H [T, D] W [V, D]^T (bf16 or fp32) with targets int64 [T] -> (loss fp32 [T], lse fp32 [T])."""
+    done = (_native or native()).head_loss(H, W, targets, ignore_index, out, ws)
+    if done is not None:
+        return done
     h, ldh, w, ldw, dtype, t, T, D, V = _head(H, W, targets)
     loss, lse = out if out is not None else (None, None)
     loss, lse = _result(loss, (T,), torch.float32, H.device, "loss"), _result(lse, (T,), torch.float32, H.device, "lse")
@@ -638,6 +651,9 @@ def dab_head_loss(H, W, targets, ignore_index=-100, out=None, ws=None):
 
 def dab_head_loss_gradient(H, W, targets, lse, g=None, ignore_index=-100, out=None, ws=None):
     """(dH, dW) of sum_t g_t loss_t (g fp32 [T], or None for ones), with lse from dab_head_loss() for the same H, W and targets."""
+    done = (_native or native()).head_loss_gradient(H, W, targets, lse, g, ignore_index, out, ws)
+    if done is not None:
+        return done
     h, ldh, w, ldw, dtype, t, T, D, V = _head(H, W, targets)
     dH, dW = out if out is not None else (None, None)
     dH, dW = _result(dH, (T, D), H.dtype, H.device, "dH"), _result(dW, (V, D), H.dtype, H.device, "dW")
@@ -662,6 +678,9 @@ def _packed(Q, S, F, K):
 
 def dab_w4_pack(W, out=None):
     """W [F, K] fp32, bf16 or f16 -> (Q, S): 4-bit codes and scale bytes in the layout of include/dab.h."""
+    done = (_native or native()).w4_pack(W, out)
+    if done is not None:
+        return done
     ptr, dtype, ld = _matrix(W, "W")
     F, K = W.shape
     Q, S = out if out is not None else w4_outputs(F, K, W.device)
@@ -672,6 +691,9 @@ def dab_w4_pack(W, out=None):
 
 def dab_w4_unpack(Q, S, F, K, out=None):
     """The weights that dab_w4_pack()'s (Q, S) stand for, fp32 [F, K]."""
+    done = (_native or native()).w4_unpack(Q, S, F, K, out)
+    if done is not None:
+        return done
     q, s = _packed(Q, S, F, K)
     W = _result(out, (F, K), torch.float32, Q.device, "out")
     _check("dab_w4_unpack", lib().dab_w4_unpack(q, s, F, K, W.data_ptr(), _stream()))
@@ -680,6 +702,9 @@ def dab_w4_unpack(Q, S, F, K, out=None):
 
 def dab_w4_matvec(X, Q, S, F, out=None, ws=None):
     """X [B, K] (fp32, bf16 or f16) times the F packed rows -> Y [B, F] of X's type."""
+    done = (_native or native()).w4_matvec(X, Q, S, F, out, ws)
+    if done is not None:
+        return done
     ptr, dtype, ld = _matrix(X, "X")
     B, K = X.shape
     q, s = _packed(Q, S, F, K)

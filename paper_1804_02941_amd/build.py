@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdab_hip.so")
 CALL = os.path.join(PKG, "_dab_call.so")
 SOURCES = ("api.hip", "binconv.hip", "direct.hip", "wbin.hip", "pack.hip", "estimate.hip", "training.hip",
-           "ckpt.hip", "w4.hip", "product16.hip", "head.hip", "probe.hip")
+           "ckpt.hip", "w4.hip", "product16.hip", "small32.hip", "head.hip",
+           "probe.hip")
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

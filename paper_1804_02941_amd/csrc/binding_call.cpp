@@ -18,6 +18,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
@@ -382,6 +383,228 @@ PyObject* wbin_fc(PyObject*, PyObject* const* a, Py_ssize_t n) {
         });
     });
 }
+// ---------------------------------------------------------------- the real-valued ends of a network
+// The same for calls on matrices of three element types whose rows may lie apart, with one output or two.
+struct Matrix {
+    const at::Tensor* t;
+    void* p;
+    int32_t dtype, rows, cols;
+    int64_t ld;
+};
+int32_t real_type(at::ScalarType t) {
+    if (t == at::kFloat) return DAB_F32;
+    if (t == at::kBFloat16) return DAB_BF16;
+    if (t == at::kHalf) return DAB_F16;
+    throw Unusual{};
+}
+Matrix matrix(PyObject* o) {
+    if (!THPVariable_CheckExact(o)) throw Unusual{};
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.dim() != 2) throw Unusual{};
+    const int32_t rows = whole(t.size(0)), cols = whole(t.size(1));
+    if ((cols > 1 && t.stride(1) != 1) || (rows > 1 && t.stride(0) < cols)) throw Unusual{};
+    return {&t, t.data_ptr(), real_type(t.scalar_type()), rows, cols, rows > 1 ? t.stride(0) : cols};
+}
+template <size_t N>
+bool shaped(const at::Tensor& t, const std::array<int64_t, N>& shape) {
+    return t.sizes() == c10::IntArrayRef(shape.data(), N);
+}
+// A packed or saved operand, a vector: contiguous, of this type and shape.
+template <size_t N>
+void* packed(PyObject* o, at::ScalarType type, std::array<int64_t, N> shape) {
+    const at::Tensor& t = plain(o, type);
+    if (!shaped(t, shape)) throw Unusual{};
+    return t.data_ptr();
+}
+// Outputs and the workspace of a call.  item(): the i-th of the caller's outputs (a tuple of them where there are two).
+struct Outputs {
+    c10::Device device;
+    PyObject* given[2] = {nullptr, nullptr};
+    at::Tensor made[2], scratch;
+    c10::SmallVector<int64_t, 4> shape[2];
+    at::ScalarType type[2];
+    void *out[2] = {nullptr, nullptr}, *ws = nullptr;
+    size_t ws_bytes = 0;
+    int n = 0;
+
+    explicit Outputs(const at::Tensor& beside) : device(beside.device()) {}
+    template <size_t N>
+    Outputs& add(PyObject* o, at::ScalarType t, std::array<int64_t, N> s) {
+        for (const int64_t v : s) whole(v);
+        type[n] = t, shape[n].assign(s.begin(), s.end());
+        if (o != Py_None) given[n] = o, out[n] = packed(o, t, s);
+        ++n;
+        return *this;
+    }
+    Outputs& workspace(size_t nbytes, PyObject* o) {
+        ws_bytes = nbytes;
+        if (nbytes == 0 || o == Py_None) return *this;
+        if (!THPVariable_CheckExact(o)) throw Unusual{};
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda()) throw Unusual{};
+        if (t.nbytes() >= nbytes) ws = t.data_ptr();
+        return *this;
+    }
+    void allocate() {
+        for (int i = 0; i < n; ++i)
+            if (out[i] == nullptr) {
+                made[i] = at::empty(shape[i], at::TensorOptions().dtype(type[i]).device(device));
+                out[i] = made[i].data_ptr();
+            }
+        if (ws_bytes != 0 && ws == nullptr) {
+            scratch = at::empty({static_cast<int64_t>(ws_bytes)}, at::TensorOptions().dtype(at::kByte).device(device));
+            ws = scratch.data_ptr();
+        }
+    }
+    PyObject* item(int i) {
+        if (given[i] == nullptr) return THPVariable_Wrap(std::move(made[i]));
+        Py_INCREF(given[i]);
+        return given[i];
+    }
+    PyObject* result() {
+        if (n == 1) return item(0);
+        PyObject *a = item(0), *b = item(1);
+        return a && b ? Py_BuildValue("NN", a, b) : nullptr;
+    }
+};
+PyObject* item(PyObject* pair, int i) {
+    if (pair == Py_None) return Py_None;
+    if (!PyTuple_CheckExact(pair) || PyTuple_GET_SIZE(pair) != 2) throw Unusual{};
+    return PyTuple_GET_ITEM(pair, i);
+}
+int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m; }
+int64_t whole_number(PyObject* o) {
+    int overflow = 0;
+    if (!PyLong_CheckExact(o)) throw Unusual{};
+    const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
+    if (overflow) throw Unusual{};
+    return v;
+}
+
+// (X, out)
+PyObject* ckpt8_save(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<2>("dab_ckpt8_save", n, [&] {
+        const Matrix X = matrix(a[0]);
+        Outputs o(*X.t);
+        o.add(item(a[1], 0), at::kChar, std::array{int64_t{X.rows}, 32 * words(X.cols)}).add(item(a[1], 1), at::kByte, std::array{int64_t{X.rows}, words(X.cols)});
+        return std::pair(std::move(o), [X](const Outputs& b, void* st) {
+            return ::dab_ckpt8_save(X.p, X.dtype, X.rows, X.cols, X.ld, static_cast<int8_t*>(b.out[0]), static_cast<uint8_t*>(b.out[1]), st);
+        });
+    });
+}
+// What was saved of `cols` channels: (Q, S)
+std::pair<const int8_t*, const uint8_t*> saved(PyObject* Q, PyObject* S, int32_t cols, int32_t* rows) {
+    const at::Tensor& t = plain(Q, at::kChar);
+    if (t.dim() != 2 || cols < 1) throw Unusual{};
+    *rows = whole(t.size(0));
+    return {static_cast<const int8_t*>(packed(Q, at::kChar, std::array{int64_t{*rows}, 32 * words(cols)})),
+            static_cast<const uint8_t*>(packed(S, at::kByte, std::array{int64_t{*rows}, words(cols)}))};
+}
+// (Q, S, cols, dtype)
+PyObject* ckpt8_restore(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<4>("dab_ckpt8_restore", n, [&] {
+        const int32_t cols = small_int(a[2]);
+        int32_t rows = 0;
+        const auto [Q, S] = saved(a[0], a[1], cols, &rows);
+        if (!THPDtype_Check(a[3])) throw Unusual{};
+        const at::ScalarType type = reinterpret_cast<THPDtype*>(a[3])->scalar_type;
+        const int32_t dtype = real_type(type);
+        Outputs o(THPVariable_Unpack(a[0]));
+        o.add(Py_None, type, std::array{int64_t{rows}, int64_t{cols}});
+        return std::pair(std::move(o), [q = Q, s = S, rows, cols, dtype](const Outputs& b, void* st) {
+            return ::dab_ckpt8_restore(q, s, rows, cols, b.out[0], dtype, cols, st);
+        });
+    });
+}
+// (dY, Q, S, cols, out, ws)
+PyObject* ckpt8_weight_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<6>("dab_ckpt8_weight_gradient", n, [&] {
+        const Matrix dY = matrix(a[0]);
+        const int32_t cols = small_int(a[3]);
+        int32_t rows = 0;
+        const auto [Q, S] = saved(a[1], a[2], cols, &rows);
+        if (rows != dY.rows) throw Unusual{};
+        Outputs o(*dY.t);
+        o.add(a[4], at::kFloat, std::array{int64_t{dY.cols}, int64_t{cols}});
+        o.workspace(::dab_ckpt8_weight_gradient_workspace_bytes(rows, cols, dY.cols, dY.dtype, dY.ld), a[5]);
+        return std::pair(std::move(o), [dY, q = Q, s = S, rows, cols](const Outputs& b, void* st) {
+            return ::dab_ckpt8_weight_gradient(dY.p, dY.dtype, dY.ld, q, s, rows, cols, dY.cols, static_cast<float*>(b.out[0]), b.ws, b.ws_bytes, st);
+        });
+    });
+}
+// (H, W, targets, ignore_index, out, ws)
+PyObject* head_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<6>("dab_head_loss", n, [&] {
+        const Matrix H = matrix(a[0]), W = matrix(a[1]);
+        if (W.dtype != H.dtype || W.cols != H.cols) throw Unusual{};
+        const auto* t = static_cast<const int64_t*>(packed(a[2], at::kLong, std::array{int64_t{H.rows}}));
+        const int64_t ignore = whole_number(a[3]);
+        Outputs o(*H.t);
+        o.add(item(a[4], 0), at::kFloat, std::array{int64_t{H.rows}}).add(item(a[4], 1), at::kFloat, std::array{int64_t{H.rows}});
+        o.workspace(::dab_head_loss_workspace_bytes(H.rows, H.cols, W.rows, H.dtype, H.ld, W.ld), a[5]);
+        return std::pair(std::move(o), [=](const Outputs& b, void* st) {
+            return ::dab_head_loss(H.p, H.ld, W.p, W.ld, H.dtype, t, ignore, H.rows, H.cols, W.rows, static_cast<float*>(b.out[0]),
+                                   static_cast<float*>(b.out[1]), b.ws, b.ws_bytes, st);
+        });
+    });
+}
+// (H, W, targets, lse, g, ignore_index, out, ws)
+PyObject* head_loss_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<8>("dab_head_loss_gradient", n, [&] {
+        const Matrix H = matrix(a[0]), W = matrix(a[1]);
+        if (W.dtype != H.dtype || W.cols != H.cols) throw Unusual{};
+        const std::array tokens{int64_t{H.rows}};
+        const auto* t = static_cast<const int64_t*>(packed(a[2], at::kLong, tokens));
+        const auto* lse = static_cast<const float*>(packed(a[3], at::kFloat, tokens));
+        const auto* g = a[4] == Py_None ? nullptr : static_cast<const float*>(packed(a[4], at::kFloat, tokens));
+        const int64_t ignore = whole_number(a[5]);
+        Outputs o(*H.t);
+        const auto type = H.t->scalar_type();
+        o.add(item(a[6], 0), type, std::array{int64_t{H.rows}, int64_t{H.cols}}).add(item(a[6], 1), type, std::array{int64_t{W.rows}, int64_t{H.cols}});
+        o.workspace(::dab_head_loss_gradient_workspace_bytes(H.rows, H.cols, W.rows, H.dtype, H.ld, W.ld), a[7]);
+        return std::pair(std::move(o), [=](const Outputs& b, void* st) {
+            return ::dab_head_loss_gradient(H.p, H.ld, W.p, W.ld, H.dtype, t, ignore, lse, g, H.rows, H.cols, W.rows, b.out[0], b.out[1], b.ws,
+                                            b.ws_bytes, st);
+        });
+    });
+}
+std::array<int64_t, 4> w4_codes(int64_t F, int64_t K) { return {up(F, 16), up(K, 128), 64, 16}; }
+std::array<int64_t, 4> w4_scales(int64_t F, int64_t K) { return {up(F, 16), up(K, 512), 64, 4}; }
+// (W, out)
+PyObject* w4_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<2>("dab_w4_pack", n, [&] {
+        const Matrix W = matrix(a[0]);
+        Outputs o(*W.t);
+        o.add(item(a[1], 0), at::kByte, w4_codes(W.rows, W.cols)).add(item(a[1], 1), at::kByte, w4_scales(W.rows, W.cols));
+        return std::pair(std::move(o), [W](const Outputs& b, void* st) {
+            return ::dab_w4_pack(W.p, W.dtype, W.rows, W.cols, W.ld, static_cast<uint8_t*>(b.out[0]), static_cast<uint8_t*>(b.out[1]), st);
+        });
+    });
+}
+// (Q, S, F, K, out)
+PyObject* w4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<5>("dab_w4_unpack", n, [&] {
+        const int32_t F = whole(small_int(a[2])), K = whole(small_int(a[3]));
+        const auto *Q = static_cast<const uint8_t*>(packed(a[0], at::kByte, w4_codes(F, K))), *S = static_cast<const uint8_t*>(packed(a[1], at::kByte, w4_scales(F, K)));
+        Outputs o(THPVariable_Unpack(a[0]));
+        o.add(a[4], at::kFloat, std::array{int64_t{F}, int64_t{K}});
+        return std::pair(std::move(o), [=](const Outputs& b, void* st) { return ::dab_w4_unpack(Q, S, F, K, static_cast<float*>(b.out[0]), st); });
+    });
+}
+// (X, Q, S, F, out, ws)
+PyObject* w4_matvec(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<6>("dab_w4_matvec", n, [&] {
+        const Matrix X = matrix(a[0]);
+        const int32_t F = whole(small_int(a[3]));
+        const auto *Q = static_cast<const uint8_t*>(packed(a[1], at::kByte, w4_codes(F, X.cols))), *S = static_cast<const uint8_t*>(packed(a[2], at::kByte, w4_scales(F, X.cols)));
+        Outputs o(*X.t);
+        o.add(a[4], X.t->scalar_type(), std::array{int64_t{X.rows}, int64_t{F}});
+        o.workspace(::dab_w4_matvec_workspace_bytes(X.rows, X.cols, F, X.dtype, X.ld), a[5]);
+        return std::pair(std::move(o), [=](const Outputs& b, void* st) {
+            return ::dab_w4_matvec(X.p, X.dtype, X.ld, Q, S, X.rows, X.cols, F, b.out[0], b.ws, b.ws_bytes, st);
+        });
+    });
+}
 PyMethodDef whole_def(const char* name, PyObject* (*fn)(PyObject*, PyObject* const*, Py_ssize_t)) {
     return PyMethodDef{name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr};
 }
@@ -422,6 +645,9 @@ PyMethodDef* methods() {
         ENTRY(dab_weight_gradient, "W", _, _, "thr_val", "thr_idx", "alpha_is_upper", "upstream", "G_out"),
         whole_def("pack_activations", pack_activations), whole_def("binconv2d", binconv2d), whole_def("binconv2d_bits", binconv2d_bits),
         whole_def("binfc", binfc), whole_def("pool_bits", pool_bits), whole_def("wbin_conv2d", wbin_conv2d), whole_def("wbin_fc", wbin_fc),
+        whole_def("ckpt8_save", ckpt8_save), whole_def("ckpt8_restore", ckpt8_restore), whole_def("ckpt8_weight_gradient", ckpt8_weight_gradient),
+        whole_def("head_loss", head_loss), whole_def("head_loss_gradient", head_loss_gradient),
+        whole_def("w4_pack", w4_pack), whole_def("w4_unpack", w4_unpack), whole_def("w4_matvec", w4_matvec),
         {"setup", setup, METH_VARARGS, nullptr},
         {nullptr, nullptr, 0, nullptr},
     };

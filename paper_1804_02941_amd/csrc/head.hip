@@ -5,6 +5,7 @@
 // product again, now written out as P = g (softmax - onehot) in bf16, and the two products dW = P^T H (the piece's
 // rows of dW, finished) and dH += P W (fp32 until the last piece).  8 T D V flops, two of them for taking the logits twice.
 #include "product16.h"
+#include "small32.h"
 
 namespace dab {
 
@@ -40,6 +41,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2* __restrict
 }
 
 struct HeadPlan {
+    bool small;                      // small32.h
     int P;                           // planes
     int n_seg;
     bool h_direct, w_direct;
@@ -57,6 +59,24 @@ static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t l
 
 static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw, bool gradient) {
     HeadPlan p{};
+    size_t at = 0;
+    auto room = [&at](int64_t bytes) {
+        const size_t here = at;
+        at += static_cast<size_t>(round_up(bytes, 256));
+        return here;
+    };
+    p.small = small32(dtype, T, D, V);
+    if (p.small) {
+        if (gradient) {
+            p.ldp = round_up(V, 4);
+            p.p_at = room(T * p.ldp * 4);
+        } else {
+            p.stats_at = room(ceil_div64(V, kSmallTile) * T * 8);
+            p.target_at = room(static_cast<int64_t>(T) * 4);
+        }
+        p.bytes = at;
+        return p;
+    }
     p.P = dtype_pieces(dtype);
     p.n_seg = p.P == 1 ? 1 : 6;
     p.w_direct = dtype == DAB_BF16 && D % 8 == 0 && ldw % 8 == 0;
@@ -64,12 +84,6 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     p.h_direct = !gradient && dtype == DAB_BF16 && D % 8 == 0 && ldh % 8 == 0;
     p.ldh = p.h_direct ? ldh : round_up(D, 8);
     p.ldw = p.w_direct ? ldw : round_up(D, 8);
-    size_t at = 0;
-    auto room = [&at](int64_t bytes) {
-        const size_t here = at;
-        at += static_cast<size_t>(round_up(bytes, 256));
-        return here;
-    };
     p.h_at = p.h_direct ? 0 : room(static_cast<int64_t>(p.P) * T * p.ldh * 2);
     p.w_at = p.w_direct ? 0 : room(static_cast<int64_t>(p.P) * V * p.ldw * 2);
     if (!gradient) {
@@ -110,6 +124,17 @@ static void head_segments(Product16& g, int n_seg) {
     // pairs of pieces in order of size; what is left out is below 2^-24 of a term
     g.n_seg = n_seg;
     if (n_seg > 1) g.seg_a = 0x201100, g.seg_b = 0x021010;
+}
+
+// The logits of small sizes: operands as they are.
+static Small32 head_logits32(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets, int64_t ignore,
+                             int T, int D, int V) {
+    Small32 g{};
+    g.A = {H, ldh, T, ldh % 4 == 0, nullptr, 0, 0};
+    g.B = {W, ldw, V, ldw % 4 == 0, nullptr, 0, 0};
+    g.M = T, g.N = V, g.K = D, g.tiles_n = ceil_div(V, kSmallTile);
+    g.targets = targets, g.ignore_index = ignore;
+    return g;
 }
 
 // The operands as bf16 planes, in the workspace where they are not already.
@@ -156,13 +181,21 @@ extern "C" int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t 
     if (int rc = ensure_device_ready()) return rc;
     const auto st = static_cast<hipStream_t>(stream);
     char* base = static_cast<char*>(ws);
+    float2* stats = reinterpret_cast<float2*>(base + p.stats_at);
+    float* target_logit = reinterpret_cast<float*>(base + p.target_at);
+    if (p.small) {
+        Small32 g = head_logits32(H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V);
+        g.stats = stats, g.target_logit = target_logit;
+        if (int rc = launch_small_stats(g, dtype, st)) return rc;
+        return launch(head_join_kernel, dim3(ceil_div(T, 32)), dim3(256), 0, st, stats, target_logit, targets, ignore_index, T, V,
+                      ceil_div(V, kSmallTile), loss, lse);
+    }
     Product16 g{};
     if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &g.A, &g.B)) return rc;
     g.M = T, g.N = V, g.K = D, g.V = V;
     head_segments(g, p.n_seg);
     g.targets = targets, g.ignore_index = ignore_index;
-    g.stats = reinterpret_cast<float2*>(base + p.stats_at);
-    g.target_logit = reinterpret_cast<float*>(base + p.target_at);
+    g.stats = stats, g.target_logit = target_logit;
     if (int rc = launch16(kEpiStats, false, false, g, p.logits, st)) return rc;
     const int blocks = ceil_div(V, stats_words16(p.logits));
     return launch(head_join_kernel, dim3(ceil_div(T, 32)), dim3(256), 0, st, g.stats, g.target_logit, targets, ignore_index, T, V, blocks,
@@ -181,6 +214,18 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
     if (int rc = ensure_device_ready()) return rc;
     const auto st = static_cast<hipStream_t>(stream);
     char* base = static_cast<char*>(ws);
+    if (p.small) {
+        float* P = reinterpret_cast<float*>(base + p.p_at);
+        Small32 g = head_logits32(H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V);
+        g.C = P, g.ldc = p.ldp, g.lse = lse, g.g = grad;
+        if (int rc = launch_small_softmax(g, dtype, st)) return rc;
+        Small32 q{}, s{};
+        q.A = {P, p.ldp, V, 0, nullptr, 0, 0}, q.B = {H, ldh, D, 0, targets, ignore_index, V};
+        q.M = V, q.N = D, q.K = T, q.tiles_n = ceil_div(D, kSmallTile), q.C = dW, q.ldc = D, q.dtype = dtype;
+        s.A = {P, p.ldp, T, 1, nullptr, 0, 0}, s.B = {W, ldw, D, 0, nullptr, 0, 0};
+        s.M = T, s.N = D, s.K = V, s.tiles_n = q.tiles_n, s.C = dH, s.ldc = D, s.dtype = dtype;
+        return launch_small_gradients(q, s, dtype, st);
+    }
     Operand16 h, w;
     if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &h, &w)) return rc;
     bf16* P = reinterpret_cast<bf16*>(base + p.p_at);

@@ -29,15 +29,17 @@ struct Product16 {
     int M, N, K;
     int n_seg;                       // pairs of planes
     uint32_t seg_a, seg_b;           // plane of each pair, four bits a pair
-    int tiles_m, tiles_n, per_xcd;   // tiles, and workgroups of an XCD
-    int splits, steps_per_split;     // shares of the sum, and steps of a share
-    int steps;                       // steps in all: n_seg * ceil(K / 64)
-    // kEpiStore: C (out_bf16 or fp32, rows ldc apart); with several shares their fp32 sums at part + share * M * N instead
+    int tiles_m, tiles_n;
+    int steps;                       // steps of a sum: n_seg * ceil(K / 64)
+    int whole, whole_xcd;            // tiles whose sum one workgroup takes, and how many of them an XCD does
+    int rest, rest_xcd;              // the last tiles, in `shares` shares each, and shares an XCD takes
+    int shares, share_steps;
+    // kEpiStore: C (out_bf16 or fp32, rows ldc apart)
     void* C;
     int64_t ldc;
     int out_bf16, vec;               // vec: four neighbouring columns are one aligned store
     const float* add;                // fp32 [M][N] added to the sum, or NULL
-    float* part;
+    float* part;                     // [rest][shares][tile] sums of the shares, in the order of the accumulators
     // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece
     const int64_t* targets;
     int64_t ignore_index;
@@ -51,15 +53,14 @@ struct Product16 {
     int p_planes;
 };
 
-__device__ __forceinline__ bool no_loss(int64_t target, int64_t ignore, int V) { return target == ignore || target < 0 || target >= V; }
-
-// Tile, shares and steps of a product; the launch (product16.hip).
+// Tile of a product and how its sums are shared out (product16.hip).
 struct Plan16 {
     bool big;
-    int splits, steps_per_split, steps;
+    int steps, whole, rest, shares, share_steps;
     size_t part_bytes;
+    double us;                       // estimated time
 };
-Plan16 plan16(int M, int N, int K, int n_seg, bool can_split);
+Plan16 plan16(int M, int N, int K, int n_seg, bool can_share);
 int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st);
 int stats_words16(const Plan16& pl);           // words of the vocabulary per pair of the stats
 int init_product16();

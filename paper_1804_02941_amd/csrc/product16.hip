@@ -95,6 +95,25 @@ struct Reader16 {
     }
 };
 
+// Four neighbouring columns of the result.
+__device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v) {
+    typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+    if (n >= g.N) return;
+    if (g.vec) {
+        if (g.add) v += *reinterpret_cast<const v4f*>(g.add + static_cast<int64_t>(m) * g.N + n);
+        if (g.out_bf16) *reinterpret_cast<v4bf*>(static_cast<bf16*>(g.C) + m * g.ldc + n) = __builtin_convertvector(v, v4bf);
+        else *reinterpret_cast<v4f*>(static_cast<float*>(g.C) + m * g.ldc + n) = v;
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (n + r >= g.N) break;
+        if (g.add) v[r] += g.add[static_cast<int64_t>(m) * g.N + n + r];
+        if (g.out_bf16) static_cast<bf16*>(g.C)[m * g.ldc + n + r] = static_cast<bf16>(v[r]);
+        else static_cast<float*>(g.C)[m * g.ldc + n + r] = v[r];
+    }
+}
+
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
@@ -104,13 +123,20 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    // consecutive workgroups go to the XCDs in turn: each XCD gets neighbouring tiles, eight rows of tiles at a time, so
-    // that what runs on it together shares operands in its L2
-    const int unit = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);
-    const int tiles = g.tiles_m * g.tiles_n;
-    if (unit >= tiles * g.splits) return;
+    // Consecutive workgroups go to the XCDs in turn: each XCD gets neighbouring tiles, eight rows of tiles at a time, so
+    // that what runs on it together shares operands in its L2.  The tiles that would leave a last round half empty are taken in shares.
     // (quotients come from vector instructions; what is made of them here has to be scalar)
-    const int share = __builtin_amdgcn_readfirstlane(unit / tiles), tile = unit - share * tiles;
+    int tile, first = 0, last = g.steps, share = -1;
+    if (static_cast<int>(blockIdx.x) < 8 * g.whole_xcd) {
+        tile = (blockIdx.x & 7) * g.whole_xcd + (blockIdx.x >> 3);
+        if (tile >= g.whole) return;
+    } else {
+        const int b = blockIdx.x - 8 * g.whole_xcd, unit = (b & 7) * g.rest_xcd + (b >> 3);
+        if (unit >= g.rest * g.shares) return;
+        const int sh = __builtin_amdgcn_readfirstlane(unit / g.rest);
+        tile = g.whole + unit - sh * g.rest;
+        if (g.shares > 1) share = sh, first = sh * g.share_steps, last = min(first + g.share_steps, g.steps);
+    }
     const int band = __builtin_amdgcn_readfirstlane(tile / (8 * g.tiles_n)), in_band = tile - band * 8 * g.tiles_n;
     const int bm = min(8, g.tiles_m - band * 8);
     const int tn = __builtin_amdgcn_readfirstlane(in_band / bm), tm = band * 8 + in_band - tn * bm;
@@ -125,7 +151,6 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
     const bf16* b0 = g.B.p + (BRC ? n0 : n0 * g.B.ld);
     const int64_t ka = kStepK * (ARC ? g.A.ld : 1), kb = kStepK * (BRC ? g.B.ld : 1);   // a step further
 
-    const int first = share * g.steps_per_split, last = min(first + g.steps_per_split, g.steps);
     const int per_seg = __builtin_amdgcn_readfirstlane(g.steps / g.n_seg);
     // the step that is fetched next: how many are left, its pair of planes, its operands and k left there
     int to_fetch = last - first, seg = __builtin_amdgcn_readfirstlane(first / per_seg), k_left = g.K - (first - seg * per_seg) * kStepK;
@@ -286,46 +311,44 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
                     }
                 }
             }
-        } else {
-            if (in) {
+        } else if (share >= 0) {
 #pragma unroll
-                for (int i = 0; i < FN; ++i) {
-                    const int n = nw + i * 16;
-                    if (n >= g.N) continue;
-                    v4f v = acc[i][j];
-                    if (g.splits > 1) {
-                        float* to = g.part + (static_cast<int64_t>(share) * g.M + m) * g.N + n;
-                        if ((g.N & 3) == 0) *reinterpret_cast<v4f*>(to) = v;
-                        else
-                            for (int r = 0; r < 4; ++r)
-                                if (n + r < g.N) to[r] = v[r];
-                        continue;
-                    }
-                    if (g.add) {
-                        const float* from = g.add + static_cast<int64_t>(m) * g.N + n;
-                        for (int r = 0; r < 4; ++r)
-                            if (n + r < g.N) v[r] += from[r];
-                    }
-                    if (g.out_bf16) {
-                        bf16* to = static_cast<bf16*>(g.C) + m * g.ldc + n;
-                        typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
-                        if (g.vec) *reinterpret_cast<v4bf*>(to) = v4bf{static_cast<bf16>(v[0]), static_cast<bf16>(v[1]), static_cast<bf16>(v[2]), static_cast<bf16>(v[3])};
-                        else
-                            for (int r = 0; r < 4; ++r)
-                                if (n + r < g.N) to[r] = static_cast<bf16>(v[r]);
-                    } else {
-                        float* to = static_cast<float*>(g.C) + m * g.ldc + n;
-                        if (g.vec) *reinterpret_cast<v4f*>(to) = v;
-                        else
-                            for (int r = 0; r < 4; ++r)
-                                if (n + r < g.N) to[r] = v[r];
-                    }
-                }
-            }
+            for (int i = 0; i < FN; ++i)
+                *reinterpret_cast<v4f*>(g.part + ((static_cast<int64_t>(tile - g.whole) * g.shares + share) * (FN * FM) + i * FM + j) * (256 * NW) +
+                                        threadIdx.x * 4) = acc[i][j];
+        } else if (in) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) store16(g, m, nw + i * 16, acc[i][j]);
         }
     }
 }
 
+// The shares of a tile's sums, added in a fixed order.  A workgroup takes one 16 x 16 block of every wavefront; eight shares
+// are on their way at a time.
+template <int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void join16_kernel(Product16 g) {
+    DAB_RESERVE_VGPRS();
+    constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rest_tile = blockIdx.x / (FN * FM), block = blockIdx.x - rest_tile * (FN * FM), i = block / FM, j = block - i * FM;
+    const int tile = g.whole + rest_tile;
+    const int band = tile / (8 * g.tiles_n), in_band = tile - band * 8 * g.tiles_n, bm = min(8, g.tiles_m - band * 8);
+    const int tn = in_band / bm, tm = band * 8 + in_band - tn * bm;
+    const int n = tn * TN + (wave / WM * FN + i) * 16 + (lane >> 4) * 4, m = tm * TM + (wave % WM * FM + j) * 16 + (lane & 15);
+    if (m >= g.M || n >= g.N) return;
+    constexpr int64_t kNext = static_cast<int64_t>(FN * FM) * 256 * NW;
+    const float* from = g.part + static_cast<int64_t>(rest_tile) * g.shares * kNext + block * (256 * NW) + threadIdx.x * 4;
+    v4f v = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < g.shares; s += 8) {
+        v4f got[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) got[u] = *reinterpret_cast<const v4f*>(from + min(s + u, g.shares - 1) * kNext);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s + u < g.shares) v += got[u];
+    }
+    store16(g, m, n, v);
+}
 
 // ---------------------------------------------------------------- operands as bf16 planes
 template <typename T, int P>
@@ -359,38 +382,44 @@ int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld
     return launch(planes16_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), rows, cols, ld, vec, targets, ignore, V, out, l, chunks);
 }
 
-// ---------------------------------------------------------------- shares of a sum, added in a fixed order
-__global__ __launch_bounds__(256) void join16_kernel(const float* __restrict__ part, int splits, int64_t n, const float* add,
-                                                     void* C, int out_bf16) {
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
-        float v = add ? add[i] : 0.f;
-        for (int s = 0; s < splits; ++s) v += part[s * n + i];
-        if (out_bf16) static_cast<bf16*>(C)[i] = static_cast<bf16>(v);
-        else static_cast<float*>(C)[i] = v;
-    }
-}
-
 // ---------------------------------------------------------------- plan and launch
 constexpr int kBigM = 256, kBigN = 256, kBigWM = 4, kBigWN = 2;
 constexpr int kSmallM = 128, kSmallN = 128, kSmallWM = 2, kSmallWN = 2;
 constexpr size_t lds_bytes16(int tm, int tn) { return static_cast<size_t>(2) * (tm + tn) * kStepK * 2; }
 
-Plan16 plan16(int M, int N, int K, int n_seg, bool can_split) {
+// Time of a product in one tile size, in microseconds: rounds of workgroups over the compute units, the last of them in shares where
+// that takes less.  The figures are those of long sums on a full chip.
+static Plan16 plan16_of(bool big, int M, int N, int K, int n_seg, bool can_share) {
+    const double step = big ? 1.6 : 1.1, ends = big ? 5.0 : 3.0;    // of a step, and of a tile's beginning and end
+    const int slots = kNumCU * (big ? 1 : 2);                        // workgroups that run together
+    const int64_t tile_bytes = static_cast<int64_t>(big ? kBigM * kBigN : kSmallM * kSmallN) * 4;
     Plan16 pl{};
+    pl.big = big;
     pl.steps = n_seg * ceil_div(K, kStepK);
-    const int64_t big = static_cast<int64_t>(ceil_div(M, kBigM)) * ceil_div(N, kBigN);
-    pl.big = big >= kNumCU * 3 / 4;
-    pl.splits = 1;
-    if (!pl.big && can_split) {
-        const int64_t tiles = static_cast<int64_t>(ceil_div(M, kSmallM)) * ceil_div(N, kSmallN);
-        int64_t s = 2 * kNumCU / tiles;
-        if (s > pl.steps / 4) s = pl.steps / 4;
-        pl.splits = static_cast<int>(s < 1 ? 1 : s);
+    const int64_t tiles = static_cast<int64_t>(ceil_div(M, big ? kBigM : kSmallM)) * ceil_div(N, big ? kBigN : kSmallN);
+    const double round = pl.steps * step + ends;
+    const int64_t rounds = tiles / slots;
+    pl.whole = static_cast<int>(rounds * slots), pl.rest = static_cast<int>(tiles - pl.whole);
+    pl.shares = 1, pl.share_steps = pl.steps;
+    pl.us = rounds * round;
+    if (pl.rest == 0) return pl;
+    double best = round;
+    for (int s = 2; can_share && s <= 64 && pl.rest * s <= slots && s * 4 <= pl.steps; ++s) {
+        const int per = ceil_div(pl.steps, s), n = ceil_div(pl.steps, per);
+        if (n != s) continue;
+        // the join: a launch, and the sums written and read once
+        const double us = per * step + ends + 4.0 + 2.0 * pl.rest * s * tile_bytes / 4e6;
+        if (us < best) best = us, pl.shares = s, pl.share_steps = per;
     }
-    pl.steps_per_split = ceil_div(pl.steps, pl.splits);
-    pl.splits = ceil_div(pl.steps, pl.steps_per_split);
-    pl.part_bytes = pl.splits > 1 ? static_cast<size_t>(pl.splits) * M * N * sizeof(float) : 0;
+    pl.us += best;
+    if (pl.shares == 1) pl.whole = static_cast<int>(tiles), pl.rest = 0;
+    pl.part_bytes = pl.shares > 1 ? static_cast<size_t>(pl.rest) * pl.shares * tile_bytes : 0;
     return pl;
+}
+
+Plan16 plan16(int M, int N, int K, int n_seg, bool can_share) {
+    const Plan16 big = plan16_of(true, M, N, K, n_seg, can_share), small = plan16_of(false, M, N, K, n_seg, can_share);
+    return small.us < big.us ? small : big;
 }
 
 int stats_words16(const Plan16& pl) { return pl.big ? kBigN / kBigWN : kSmallN / kSmallWN; }
@@ -404,21 +433,20 @@ static auto kernel16(bool big) {
 int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st) {
     const int tm = pl.big ? kBigM : kSmallM, tn = pl.big ? kBigN : kSmallN;
     g.tiles_m = ceil_div(g.M, tm), g.tiles_n = ceil_div(g.N, tn);
-    g.splits = pl.splits, g.steps_per_split = pl.steps_per_split, g.steps = pl.steps;
-    const int64_t units = static_cast<int64_t>(g.tiles_m) * g.tiles_n * g.splits;
-    if (units > INT32_MAX / 2) return DAB_ERR_UNSUPPORTED;
-    g.per_xcd = static_cast<int>(ceil_div64(units, kNumXCD));
+    if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
+    g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
+    g.whole_xcd = ceil_div(g.whole, kNumXCD), g.rest_xcd = ceil_div(g.rest * g.shares, kNumXCD);
     const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.big)
                         : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.big)
                         : arc ? kernel16<kEpiStore, true, true>(pl.big)
                               : kernel16<kEpiStore, false, true>(pl.big);
     if (brc != (epi == kEpiStore)) return DAB_ERR_UNSUPPORTED;
     const int threads = 64 * (pl.big ? kBigWM * kBigWN : kSmallWM * kSmallWN);
-    if (int rc = launch(kernel, dim3(g.per_xcd * kNumXCD), dim3(threads), lds_bytes16(tm, tn), st, g)) return rc;
-    if (pl.splits == 1) return DAB_OK;
-    const int64_t n = static_cast<int64_t>(g.M) * g.N, blocks = ceil_div64(n, 256);
-    return launch(join16_kernel, dim3(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, g.part, g.splits, n,
-                  g.add, g.C, g.out_bf16);
+    if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(tm, tn), st, g)) return rc;
+    if (pl.shares == 1) return DAB_OK;
+    const int blocks = (pl.big ? kBigN * kBigM : kSmallN * kSmallM) / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
+    return launch(pl.big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
+                  dim3(g.rest * blocks), dim3(threads), 0, st, g);
 }
 
 int init_product16() {

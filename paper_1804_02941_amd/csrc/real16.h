@@ -86,6 +86,9 @@ __device__ __forceinline__ int group_exponent(uint32_t m) {
     return e;
 }
 
+// Whether a token has no part in the loss.
+__device__ __forceinline__ bool no_loss(int64_t target, int64_t ignore, int V) { return target == ignore || target < 0 || target >= V; }
+
 // Piece `which` of the bf16 numbers whose sum x is: x rounded, what is left rounded, what is left then.
 __device__ __forceinline__ bf16 piece_of(float x, int which) {
     const bf16 a = static_cast<bf16>(x);

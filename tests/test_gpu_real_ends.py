@@ -258,6 +258,31 @@ def test_head(dtype, T, D, V):
     check_head(*head_case(rng, T, D, V, dtype, 0.3))
 
 
+# sizes past what the kernels for small heads take (1024 or, in fp32, 4096 of anything), odd ones among them
+TILED = [(1, 64, 5000), (2, 8, 4099), (7, 33, 4500), (33, 64, 4257), (64, 100, 5300), (130, 72, 4615), (300, 40, 4129), (4097, 24, 40), (100, 4200, 33),
+         (1, 1, 4097), (129, 129, 4233)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,D,V", TILED)
+def test_head_on_tiles(dtype, T, D, V):
+    rng = np.random.default_rng(T + D + V)
+    H, W, t, g = head_case(rng, T, D, V, dtype, 0.3)
+    want = check_head(H, W, t, g)
+    got = check_head(strided(H, 5, 0), strided(W, 8, 8), t, g)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_head_on_tiles_ignored_tokens_hold_anything():
+    rng = np.random.default_rng(2)
+    H, W, t, g = head_case(rng, 300, 48, 4400, torch.bfloat16, 0.0)
+    t[5:9], t[20], t[280:] = -100, -100, -100
+    t[1], t[2] = 4400, -1
+    H[5], H[6], H[7, 3], H[20], H[299] = float("nan"), float("inf"), float("-inf"), float("nan"), float("inf")
+    loss, lse, dH, dW = check_head(H, W, t, g)
+    assert bool(torch.isfinite(dH).all()) and bool(torch.isfinite(dW).all()) and bool(torch.isnan(loss[1:3]).all())
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_head_of_many_tiles_and_pieces(dtype):
     """Large tiles, several shares; a second run gives the same bits."""
@@ -374,6 +399,19 @@ def test_head_of_a_matrix_whose_offsets_pass_32_bits():
     assert float((dW[-40:].float() - want).norm() / want.norm()) < 4e-3
     want = sum(P[:, i:i + 30000] @ W[i:i + 30000].float() for i in range(0, V, 30000))
     assert float((dH.float() - want).norm() / want.norm()) < 4e-3
+
+
+@pytest.mark.parametrize("rows,cols,F", [(20000, 40, 70), (1030, 520, 300), (512, 2600, 1300), (257, 4100, 4100), (6000, 260, 516)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_weight_gradient_of_shared_and_whole_tiles(dtype, rows, cols, F):
+    """Rounds of whole tiles, a last round in shares, long sums of few tiles: whole numbers, equal."""
+    rng = np.random.default_rng(rows)
+    x = rng.integers(-15, 16, (rows, cols)).astype(np.float64)
+    x[:, ::32] = 64
+    y = rng.integers(-3, 4, (rows, F)).astype(np.float64)
+    Q, S = dab.dab_ckpt8_save(on_gpu(x, torch.bfloat16))
+    dW = dab.dab_ckpt8_weight_gradient(on_gpu(y, dtype), Q, S, cols)
+    assert torch.equal(dW.double(), torch.mm(on_gpu(y, torch.float64).t().contiguous(), on_gpu(x, torch.float64)))
 
 
 # ------------------------------------------------------------------ streams, graphs, refusals
