@@ -549,7 +549,7 @@ int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, floa
 
 /*
  * dab_w4_matvec - Y[b][f] = sum_k X[b][k] W[f][k] with packed weights, for one token or a few (any B is right; the
- * weights are read once for every 64 bf16, 32 f16 or 21 fp32 tokens).  On the matrix cores in bf16, which hold a 4-bit weight times its
+ * weights are read once for every 48 bf16, 24 f16 or 16 fp32 tokens).  On the matrix cores in bf16, which hold a 4-bit weight times its
  * scale exactly; f16 inputs are sums of two bf16 numbers, fp32 ones of three: only the fp32 accumulation
  * rounds, and a 16-bit Y once more.
  *

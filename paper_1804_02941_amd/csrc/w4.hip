@@ -14,54 +14,76 @@ namespace dab {
 constexpr int kW4MaxWaves = 8;       // wavefronts per workgroup
 
 // ---------------------------------------------------------------- laying out
-// One wavefront: 16 rows x 512 weights, a lane per row and group.
+// Both directions: a wavefront takes 16 rows x 512 weights, a block of 128 at a time.  A lane holds four neighbouring weights of a row, 32 lanes a
+// row of the block, so that rows are read and written in whole lines; the packed block passes through LDS on its way.
+constexpr int kW4PackWaves = 4;
+struct W4Block {
+    uint16_t codes[512];             // [group][row][four weights]: a block's kilobyte
+    uint8_t scales[64][4];
+};
+
 template <typename T>
-__global__ __launch_bounds__(64) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int vec, int Kt, int K4,
-                                                     uint8_t* __restrict__ Q, uint8_t* __restrict__ S) {
-    const int lane = threadIdx.x, tile = blockIdx.y, step = blockIdx.x;
-    const int row = tile * 16 + (lane & 15);
-    uint32_t codes = 0;
+__device__ __forceinline__ v4f load4(const T* row, int c, int cols, bool vec) {
+    typedef T v4t __attribute__((ext_vector_type(4)));
+    v4f v = v4f{0.f, 0.f, 0.f, 0.f};
+    if (vec && c + 4 <= cols) return __builtin_convertvector(*reinterpret_cast<const v4t*>(row + c), v4f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c + i < cols) v[i] = static_cast<float>(row[c + i]);
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kW4PackWaves) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int vec, int Kt, int K4,
+                                                                    uint8_t* __restrict__ Q, uint8_t* __restrict__ S) {
+    __shared__ W4Block lds[kW4PackWaves];
+    DAB_RESERVE_VGPRS();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = blockIdx.y, step = blockIdx.x * kW4PackWaves + wave;
+    if (step >= K4) return;                                  // (a wavefront works alone: no barrier below)
+    W4Block& b = lds[wave];
+    reinterpret_cast<uint32_t*>(b.scales)[lane] = 17u * 0x01010101u;
     for (int j = 0; j < 4; ++j) {
         const int kt = step * 4 + j;
-        int scale = 17;
-        if (kt < Kt) {
-            const int k0 = kt * 128 + (lane >> 4) * 32;
-            float v[4][8];
+        if (kt >= Kt) break;
+        const int k = kt * 128 + (lane & 31) * 4, group = (lane & 31) >> 3;
+        v4f v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = tile * 16 + 2 * i + (lane >> 5);
+            v[i] = v4f{0.f, 0.f, 0.f, 0.f};
+            if (row < F) v[i] = load4(W + row * ldw, k, K, vec);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 2 * i + (lane >> 5);
+            // the largest magnitude, as bits, of the eight lanes of a group
             uint32_t m = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (row < F && k0 + 8 * i < K) {
-                    load8(W + row * ldw, k0 + 8 * i, K, vec, v[i]);
-                } else {
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) v[i][u] = 0.f;
-                }
-#pragma unroll
-                for (int u = 0; u < 8; ++u) m = max(m, __builtin_bit_cast(uint32_t, v[i][u]) & 0x7fffffffu);
-            }
+            for (int u = 0; u < 4; ++u) m = max(m, __float_as_uint(v[i][u]) & 0x7fffffffu);
+            m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0xB1, 0xf, 0xf, true)));    // lane ^ 1
+            m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x4E, 0xf, 0xf, true)));    // lane ^ 2
+            m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x141, 0xf, 0xf, true)));   // the other four
             const bool finite = m < 0x7f800000u;
             const int e = group_exponent<2>(finite ? m : 0);
             const float inv = pow2f(-e);
-            scale = finite ? e + 127 : 255;
-            v4u32 out;
+            uint32_t word = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t word = 0;
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const float a = fabsf(v[i][u] * inv);
-                    // to the nearest level, in the middle to the even code
-                    uint32_t code = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
-                    code |= (__builtin_bit_cast(uint32_t, v[i][u]) >> 31) << 3;
-                    word |= (finite ? code : 7u) << (4 * u);
-                }
-                out[i] = word;
+            for (int u = 0; u < 4; ++u) {
+                const float a = fabsf(v[i][u] * inv);
+                // to the nearest level, in the middle to the even code
+                uint32_t code = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
+                code |= (__float_as_uint(v[i][u]) >> 31) << 3;
+                word |= (finite ? code : 7u) << (4 * u);
             }
-            *reinterpret_cast<v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16) = out;
+            b.codes[(group * 16 + r) * 8 + (lane & 7)] = static_cast<uint16_t>(word);
+            if ((lane & 7) == 0) b.scales[group * 16 + r][j] = static_cast<uint8_t>(finite ? e + 127 : 255);
         }
-        codes |= static_cast<uint32_t>(scale) << (8 * j);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_nontemporal_store(reinterpret_cast<const v4u32*>(b.codes)[lane],
+                                    reinterpret_cast<v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16));
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    *reinterpret_cast<uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4) = codes;
+    *reinterpret_cast<uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4) = reinterpret_cast<const uint32_t*>(b.scales)[lane];
 }
 
 // The scale of block j of four from its byte, as the conversions take it.
@@ -70,32 +92,48 @@ __device__ __forceinline__ float scale_of(uint32_t codes, int j) {
     return __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : s << 23);
 }
 
-__global__ __launch_bounds__(64) void w4_unpack_kernel(const uint8_t* __restrict__ Q, const uint8_t* __restrict__ S, int F, int K,
-                                                       int Kt, int K4, float* __restrict__ W) {
-    const int lane = threadIdx.x, tile = blockIdx.y, step = blockIdx.x;
-    const int row = tile * 16 + (lane & 15);
-    if (row >= F) return;
-    const uint32_t codes = *reinterpret_cast<const uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4);
+__global__ __launch_bounds__(64 * kW4PackWaves) void w4_unpack_kernel(const uint8_t* __restrict__ Q, const uint8_t* __restrict__ S, int F,
+                                                                      int K, int Kt, int K4, float* __restrict__ W) {
+    __shared__ W4Block lds[kW4PackWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = blockIdx.y, step = blockIdx.x * kW4PackWaves + wave;
+    if (step >= K4) return;
+    W4Block& b = lds[wave];
+    reinterpret_cast<uint32_t*>(b.scales)[lane] = *reinterpret_cast<const uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4);
+    v4u32 q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        q[j] = *reinterpret_cast<const v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + min(step * 4 + j, Kt - 1)) * 64 + lane) * 16);
+#pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int kt = step * 4 + j;
         if (kt >= Kt) break;
-        const v4u32 q = *reinterpret_cast<const v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16);
-        const uint32_t s = (codes >> (8 * j)) & 255u;
-        const float scale = s == 255u ? __builtin_nanf("") : pow2f(static_cast<int>(s) - 127);
-        const int k0 = kt * 128 + (lane >> 4) * 32;
+        reinterpret_cast<v4u32*>(b.codes)[lane] = q[j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int k = kt * 128 + (lane & 31) * 4, group = (lane & 31) >> 3;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float v[8];
+        for (int i = 0; i < 8; ++i) {
+            const int r = 2 * i + (lane >> 5), row = tile * 16 + r;
+            const uint32_t word = b.codes[(group * 16 + r) * 8 + (lane & 7)], s = b.scales[group * 16 + r][j];
+            const float scale = s == 255u ? __builtin_nanf("") : pow2f(static_cast<int>(s) - 127);
+            v4f v;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const uint32_t c = (q[i] >> (4 * u)) & 15u, m = c & 7u;
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t c = word >> (4 * u), m = c & 7u;
                 // 0, 1/2, then (2 + last bit) 2^(upper bits - 2)
-                const float a = m < 2 ? 0.5f * static_cast<float>(m)
-                                      : static_cast<float>(2u + (m & 1u)) * pow2f(static_cast<int>(m >> 1) - 2);
+                const float a = m < 2 ? 0.5f * static_cast<float>(m) : static_cast<float>(2u + (m & 1u)) * pow2f(static_cast<int>(m >> 1) - 2);
                 v[u] = (c & 8u ? -a : a) * scale;
             }
-            if (k0 + 8 * i < K) store8(W + static_cast<int64_t>(row) * K, k0 + 8 * i, K, (K & 3) == 0, v);
+            if (row >= F) continue;
+            float* to = W + static_cast<int64_t>(row) * K;
+            if ((K & 3) == 0 && k + 4 <= K) {
+                *reinterpret_cast<v4f*>(to + k) = v;
+            } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (k + u < K) to[k + u] = v[u];
+            }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -167,33 +205,42 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
 
     v4f acc[TB][NCT];
     const bf16* xrow[NCT];
-    bool live[NCT];
 #pragma unroll
     for (int t = 0; t < NCT; ++t) {
         const int c = t * 16 + (lane & 15);
 #pragma unroll
         for (int u = 0; u < TB; ++u) acc[u][t] = v4f{0.f, 0.f, 0.f, 0.f};
-        live[t] = c < cols;
-        const int p = live[t] ? c / nb : 0, b = live[t] ? c - p * nb : 0;
-        xrow[t] = X + (static_cast<int64_t>(p) * g.B + b0 + b) * g.ldx + (lane >> 4) * 32;
+        const int p = c < cols ? c / nb : 0, b = c < cols ? c - p * nb : 0;
+        xrow[t] = X + (static_cast<int64_t>(p) * g.B + b0 + b) * g.ldx;
     }
     if (tile < g.Ft && part < g.K4) {
         Step4<TB> now, next;
         now.load(Q, S, g, tile, part, lane);
+        // columns past the last are read from the first (their results are not used), elements past the last from the end of the row
+        auto fetch = [&](v8bf (&x)[4][NCT], int kt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = min(kt * 128 + (lane >> 4) * 32 + 8 * i, g.Kx - 8);
+#pragma unroll
+                for (int t = 0; t < NCT; ++t) x[i][t] = *reinterpret_cast<const v8bf*>(xrow[t] + k);
+            }
+        };
         for (int s = part; s < g.K4; s += g.ks) {
             const bool more = s + g.ks < g.K4;
             if (more) next.load(Q, S, g, tile, s + g.ks, lane);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int k0 = (4 * s + j) * 128;
+                const int kt = 4 * s + j;
                 v8bf x[4][NCT];
+                fetch(x, kt);
+                if (kt * 128 + 128 > g.Kx) {
+                    // past the last element: zeros, whatever was loaded
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i)
+                        if (kt * 128 + (lane >> 4) * 32 + 8 * i >= g.Kx)
 #pragma unroll
-                    for (int t = 0; t < NCT; ++t) {
-                        x[i][t] = v8bf{};
-                        if (live[t] && k0 + (lane >> 4) * 32 + 8 * i < g.Kx) x[i][t] = *reinterpret_cast<const v8bf*>(xrow[t] + k0 + 8 * i);
-                    }
+                            for (int t = 0; t < NCT; ++t) x[i][t] = v8bf{};
+                }
 #pragma unroll
                 for (int u = 0; u < TB; ++u) {
                     const float scale = scale_of(now.codes[u], j);
@@ -244,8 +291,7 @@ static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const u
     switch (ceil_div(g.nb * g.P, 16)) {
         case 1: return launch_matvec<1, TB>(g, st, X, Q, S, Y);
         case 2: return launch_matvec<2, TB>(g, st, X, Q, S, Y);
-        case 3: return launch_matvec<3, TB == 4 ? 2 : TB>(g, st, X, Q, S, Y);
-        default: return launch_matvec<4, TB == 4 ? 2 : TB>(g, st, X, Q, S, Y);
+        default: return launch_matvec<3, TB == 4 ? 2 : TB>(g, st, X, Q, S, Y);
     }
 }
 
@@ -258,7 +304,7 @@ extern "C" int dab_w4_pack(const void* W, int32_t dtype, int32_t F, int32_t K, i
     if (!real_dtype(dtype) || K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
     const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4), vec = ldw * dtype_bytes(dtype) % 16 == 0;
-    const dim3 grid(K4, ceil_div(F, 16)), block(64);
+    const dim3 grid(ceil_div(K4, kW4PackWaves), ceil_div(F, 16)), block(64 * kW4PackWaves);
     const auto st = static_cast<hipStream_t>(stream);
     if (dtype == DAB_F32) return launch(w4_pack_kernel<float>, grid, block, 0, st, static_cast<const float*>(W), F, K, ldw, vec, Kt, K4, Q, S);
     if (dtype == DAB_BF16) return launch(w4_pack_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(W), F, K, ldw, vec, Kt, K4, Q, S);
@@ -272,7 +318,7 @@ extern "C" int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int3
     if (K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
     const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4);
-    return launch(w4_unpack_kernel, dim3(K4, ceil_div(F, 16)), dim3(64), 0, static_cast<hipStream_t>(stream), Q, S, F, K, Kt, K4, W);
+    return launch(w4_unpack_kernel, dim3(ceil_div(K4, kW4PackWaves), ceil_div(F, 16)), dim3(64 * kW4PackWaves), 0, static_cast<hipStream_t>(stream), Q, S, F, K, Kt, K4, W);
 }
 
 extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
@@ -295,18 +341,23 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
     W4Geom g{};
     g.F = F, g.Kt = ceil_div(K, 128), g.K4 = ceil_div(g.Kt, 4), g.Kx = static_cast<int>(round_up(K, 8));
     g.Ft = ceil_div(F, 16), g.B = B, g.P = dtype_pieces(dtype);
-    const int passes = ceil_div(B, 64 / g.P);
+    const int passes = ceil_div(B, 48 / g.P);
     g.nb = ceil_div(B, passes);
-    // Tiles of a wavefront: with one they are spread furthest, with more the tokens are loaded less often.  One token, 4096 weights a
-    // row: 16384 rows 12.4 us with one, 9.4 with two, 10.1 with four; 4096 rows of 9216 8.7, 9.9, 14.0.  Twenty-one columns: 4099 rows of
-    // 9111 31, 20, 25; thirty-two, 32768 rows of 4096: 68, 43, 31.  (Four tiles and three columns of tokens do not fit the registers.)
+    // Tiles of a wavefront: with one they are spread furthest, with more the tokens are loaded less often.  One token, 4096 weights a row:
+    // 4096 rows 4.0 us with one and 5.6 with two, 16384 rows 10.9 and 9.1, 131072 rows 63 and 51.7; twenty-one columns, 4099 rows of
+    // 9111: 26 with one, 19 with two, 24 with four; thirty-two, 32768 rows of 4096: 68, 41, 30; thirty-six, 4096 rows of 4096: 14.6
+    // and 16.0 (four tiles and three columns of tokens do not fit the registers).
     const int columns = ceil_div(g.nb * g.P, 16);
-    const int TB = columns == 1 ? (g.Ft >= 1024 ? 2 : 1) : columns == 2 && g.Ft >= 1024 ? 4 : g.Ft >= 128 ? 2 : 1;
-    // Shares of a row's sum: until there are 24 wavefronts for every compute unit (32768 rows of 4096, two tiles: 28 us with
-    // one share, 17.9, 17.1, 16.8 with eight; 131072 rows 58.3, 52.5 with two, 55.0, 57.6).
+    const int TB = columns == 1 ? (g.Ft >= 1024 ? 2 : 1) : columns == 2 ? (g.Ft >= 1024 ? 4 : g.Ft >= 128 ? 2 : 1) : g.Ft >= 512 ? 2 : 1;
+    // Shares of a row's sum: for one column of tokens until there are 24 wavefronts for every compute unit (131072 rows, two tiles: 57.8 us
+    // with one share, 51.7, 52.7, 54.9 with eight; 4096 rows, one tile: 7.9, 5.4, 4.2, 4.0), for more, which are bound by the tokens'
+    // loads, until there are four (60000 rows of 1500, twenty-four columns: 24.6, 20.8, 24.0).
+    const int enough = columns == 1 ? 24 * kNumCU : 4 * kNumCU;
     g.ks = 1;
-    while (g.ks < 8 && g.ks < g.K4 && g.Ft / TB * g.ks < 24 * kNumCU) g.ks *= 2;
+    while (g.ks < 8 && g.ks < g.K4 && g.Ft / TB * g.ks < enough) g.ks *= 2;
+    // groups of a workgroup: eight wavefronts, fewer where that leaves compute units without one (30 tokens, 1024 x 1024: 11.8 -> 5.6)
     g.groups = 8 / g.ks;
+    while (g.groups > 1 && ceil_div(g.Ft, g.groups * TB) < kNumCU) g.groups /= 2;
     g.dtype = dtype;
     const bf16* x = static_cast<const bf16*>(X);
     g.ldx = ldx;
