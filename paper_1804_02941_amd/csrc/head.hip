@@ -9,35 +9,56 @@
 
 namespace dab {
 
-// One workgroup: 32 tokens, eight threads each.
+// Maxima and sums of exponentials of two sets of words as those of both.  (A set of minus infinities alone adds nothing, and
+// exp of its difference would be undefined.)
+__device__ __forceinline__ float2 join_stats(float2 a, float2 b) {
+    const float top = fmaxf(a.x, b.x);
+    const float sa = a.x == -__builtin_inff() ? 0.f : a.y * expf(a.x - top), sb = b.x == -__builtin_inff() ? 0.f : b.y * expf(b.x - top);
+    return float2{top, sa + sb};
+}
+
+// TT tokens a workgroup, 256 / TT threads each, eight pairs on their way at a time: many tokens take whole lines of the pairs, few
+// the whole workgroup (one token, 131072 words: 100 us with eight threads).
+template <int TT>
 __global__ __launch_bounds__(256) void head_join_kernel(const float2* __restrict__ stats, const float* __restrict__ target_logit,
                                                         const int64_t* __restrict__ targets, int64_t ignore, int T, int V, int blocks,
                                                         float* __restrict__ loss, float* __restrict__ lse) {
-    __shared__ float2 part[8][32];
-    const int t = blockIdx.x * 32 + (threadIdx.x & 31), u = threadIdx.x >> 5;
-    float big = -__builtin_inff(), sum = 0.f;
+    constexpr int kParts = 256 / TT;
+    __shared__ float2 part[kParts][TT];
+    const int tt = threadIdx.x % TT, u = threadIdx.x / TT, t = blockIdx.x * TT + tt;
+    const float2 none = {-__builtin_inff(), 0.f};
+    float2 all = none;
     if (t < T)
-        for (int i = u; i < blocks; i += 8) {
-            const float2 s = stats[static_cast<int64_t>(i) * T + t];
-            const float top = fmaxf(big, s.x);
-            // (a block of minus infinities alone adds nothing, and exp of its difference would be undefined)
-            if (s.x != -__builtin_inff()) sum = (big == -__builtin_inff() ? 0.f : sum * expf(big - top)) + s.y * expf(s.x - top);
-            big = top;
+        for (int i = u; i < blocks; i += 8 * kParts) {
+            float2 s[8];
+            float top = all.x;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s[k] = i + k * kParts < blocks ? stats[static_cast<int64_t>(i + k * kParts) * T + t] : none;
+                top = fmaxf(top, s[k].x);
+            }
+            float sum = all.x == -__builtin_inff() ? 0.f : all.y * expf(all.x - top);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += s[k].x == -__builtin_inff() ? 0.f : s[k].y * expf(s[k].x - top);
+            all = float2{top, sum};
         }
-    part[u][threadIdx.x & 31] = float2{big, sum};
-    __syncthreads();
-    if (u != 0 || t >= T) return;
-    for (int i = 1; i < 8; ++i) {
-        const float2 s = part[i][threadIdx.x];
-        const float top = fmaxf(big, s.x);
-        if (s.x != -__builtin_inff()) sum = (big == -__builtin_inff() ? 0.f : sum * expf(big - top)) + s.y * expf(s.x - top);
-        big = top;
+    part[u][tt] = all;
+#pragma unroll
+    for (int n = kParts / 2; n > 0; n /= 2) {
+        __syncthreads();
+        if (u < n) part[u][tt] = all = join_stats(all, part[u + n][tt]);
     }
+    if (u != 0 || t >= T) return;
     const int64_t target = targets[t];
     const bool dead = no_loss(target, ignore, V);
-    const float l = big + logf(sum);
+    const float l = all.x + logf(all.y);
     lse[t] = dead ? 0.f : l;
     loss[t] = target == ignore ? 0.f : dead ? __builtin_nanf("") : l - target_logit[t];
+}
+static int launch_head_join(hipStream_t st, const float2* stats, const float* target_logit, const int64_t* targets, int64_t ignore, int T,
+                            int V, int blocks, float* loss, float* lse) {
+    if (T >= 2048) return launch(head_join_kernel<16>, dim3(ceil_div(T, 16)), dim3(256), 0, st, stats, target_logit, targets, ignore, T, V, blocks, loss, lse);
+    return launch(head_join_kernel<4>, dim3(ceil_div(T, 4)), dim3(256), 0, st, stats, target_logit, targets, ignore, T, V, blocks, loss, lse);
 }
 
 struct HeadPlan {
@@ -49,7 +70,7 @@ struct HeadPlan {
     int piece, n_pieces;             // words of a piece
     int64_t ldp;
     Plan16 logits, dh, dw;           // of a piece (the last one may be smaller)
-    size_t h_at, w_at, stats_at, target_at, p_at, acc_at, part_at, bytes;
+    size_t h_at, w_at, stats_at, target_at, p_at, acc_at, part_at, part_bytes, bytes;
 };
 
 static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
@@ -87,7 +108,7 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     p.h_at = p.h_direct ? 0 : room(static_cast<int64_t>(p.P) * T * p.ldh * 2);
     p.w_at = p.w_direct ? 0 : room(static_cast<int64_t>(p.P) * V * p.ldw * 2);
     if (!gradient) {
-        p.logits = plan16(T, V, D, p.n_seg, false);
+        p.logits = plan16(T, V, D, p.n_seg, 0);
         const int words = stats_words16(p.logits);
         p.stats_at = room((ceil_div64(V, words) + 8) * T * 8);
         p.target_at = room(static_cast<int64_t>(T) * 4);
@@ -100,12 +121,13 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         p.piece = static_cast<int>(round_up(ceil_div64(V, p.n_pieces), 256));
         p.n_pieces = ceil_div(V, p.piece);
         p.ldp = p.piece;
-        p.logits = plan16(T, p.piece, D, p.n_seg, false);
-        p.dh = plan16(T, D, p.piece, p.n_seg, true);
-        p.dw = plan16(p.piece, D, T, p.n_seg, true);
+        p.logits = plan16(T, p.piece, D, p.n_seg, 0);
+        p.dh = plan16(T, D, p.piece, p.n_seg, kAnyShares16);
+        p.dw = plan16(p.piece, D, T, p.n_seg, kAnyShares16);
         p.p_at = room(static_cast<int64_t>(p.P) * T * p.ldp * 2);
         p.acc_at = room(p.n_pieces > 1 ? static_cast<int64_t>(T) * D * 4 : 0);
-        p.part_at = room(static_cast<int64_t>(p.dh.part_bytes > p.dw.part_bytes ? p.dh.part_bytes : p.dw.part_bytes));
+        p.part_bytes = p.dh.part_bytes > p.dw.part_bytes ? p.dh.part_bytes : p.dw.part_bytes;
+        p.part_at = room(static_cast<int64_t>(p.part_bytes));
     }
     p.bytes = at;
     return p;
@@ -187,8 +209,7 @@ extern "C" int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t 
         Small32 g = head_logits32(H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V);
         g.stats = stats, g.target_logit = target_logit;
         if (int rc = launch_small_stats(g, dtype, st)) return rc;
-        return launch(head_join_kernel, dim3(ceil_div(T, 32)), dim3(256), 0, st, stats, target_logit, targets, ignore_index, T, V,
-                      ceil_div(V, kSmallTile), loss, lse);
+        return launch_head_join(st, stats, target_logit, targets, ignore_index, T, V, ceil_div(V, kSmallTile), loss, lse);
     }
     Product16 g{};
     if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &g.A, &g.B)) return rc;
@@ -198,8 +219,7 @@ extern "C" int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t 
     g.stats = stats, g.target_logit = target_logit;
     if (int rc = launch16(kEpiStats, false, false, g, p.logits, st)) return rc;
     const int blocks = ceil_div(V, stats_words16(p.logits));
-    return launch(head_join_kernel, dim3(ceil_div(T, 32)), dim3(256), 0, st, g.stats, g.target_logit, targets, ignore_index, T, V, blocks,
-                  loss, lse);
+    return launch_head_join(st, stats, target_logit, targets, ignore_index, T, V, blocks, loss, lse);
 }
 
 extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,
@@ -232,6 +252,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
     float* acc = reinterpret_cast<float*>(base + p.acc_at);
     const Operand16 probs = {P, p.ldp, static_cast<int64_t>(T) * p.ldp};
     const int64_t size = dtype_bytes(dtype);
+    const size_t shares = p.part_bytes;                      // room for sums in shares, of the last and smaller piece too
     for (int i = 0; i < p.n_pieces; ++i) {
         const int v0 = i * p.piece, words = V - v0 < p.piece ? V - v0 : p.piece;
         const Operand16 wp = {w.p + v0 * w.ld, w.ld, w.plane};
@@ -241,7 +262,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D;
         g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
         g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.P;
-        if (int rc = launch16(kEpiSoftmax, false, false, g, plan16(T, words, D, p.n_seg, false), st)) return rc;
+        if (int rc = launch16(kEpiSoftmax, false, false, g, plan16(T, words, D, p.n_seg, 0), st)) return rc;
         // the piece's rows of dW
         Product16 q{};
         head_segments(q, p.n_seg);
@@ -249,9 +270,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
         q.vec = D % 4 == 0;
         q.part = reinterpret_cast<float*>(base + p.part_at);
-        Plan16 pl = plan16(words, D, T, p.n_seg, true);
-        if (pl.part_bytes > p.dw.part_bytes) pl = plan16(words, D, T, p.n_seg, false);
-        if (int rc = launch16(kEpiStore, true, true, q, pl, st)) return rc;
+        if (int rc = launch16(kEpiStore, true, true, q, plan16(words, D, T, p.n_seg, shares), st)) return rc;
         // its share of dH
         const bool last = i + 1 == p.n_pieces;
         Product16 s{};
@@ -260,9 +279,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         s.add = i ? acc : nullptr;
         s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16, s.vec = D % 4 == 0;
         s.part = q.part;
-        pl = plan16(T, D, words, p.n_seg, true);
-        if (pl.part_bytes > p.dh.part_bytes) pl = plan16(T, D, words, p.n_seg, false);
-        if (int rc = launch16(kEpiStore, false, true, s, pl, st)) return rc;
+        if (int rc = launch16(kEpiStore, false, true, s, plan16(T, D, words, p.n_seg, shares), st)) return rc;
     }
     return DAB_OK;
 }

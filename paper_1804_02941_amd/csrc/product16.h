@@ -38,6 +38,7 @@ struct Product16 {
     void* C;
     int64_t ldc;
     int out_bf16, vec;               // vec: four neighbouring columns are one aligned store
+    int lines;                       // so are 16 bytes of a row
     const float* add;                // fp32 [M][N] added to the sum, or NULL
     float* part;                     // [rest][shares][tile] sums of the shares, in the order of the accumulators
     // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece
@@ -60,7 +61,9 @@ struct Plan16 {
     size_t part_bytes;
     double us;                       // estimated time
 };
-Plan16 plan16(int M, int N, int K, int n_seg, bool can_share);
+constexpr size_t kAnyShares16 = ~size_t{0};
+// share_bytes: room for the sums of shares (0: the whole sum in one workgroup)
+Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes);
 int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st);
 int stats_words16(const Plan16& pl);           // words of the vocabulary per pair of the stats
 int init_product16();
