@@ -264,6 +264,17 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
     const int mw = m0 + wm * FM * 16 + (lane & 15), nb = n0 + wn * FN * 16, nw = nb + (lane >> 4) * 4;
     const bool full = n0 + TN <= g.N;                        // no column past the last one
     char* mine = lds + wave * (16 * FN * 16 * 4);
+    // what a token's row needs, all of it requested before the first is used
+    int64_t target[FM];
+    float lse[FM], weight[FM];
+    if constexpr (EPI != kEpiStore) {
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            const int m = min(mw + j * 16, g.M - 1);
+            target[j] = g.targets[m];
+            if constexpr (EPI == kEpiSoftmax) lse[j] = g.lse[m], weight[j] = g.g ? g.g[m] : 1.f;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
         const int m = mw + j * 16, mj = m0 + wm * FM * 16 + j * 16;
@@ -294,7 +305,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (in && lane < 16) g.stats[static_cast<int64_t>(tn * WN + wn) * g.M + m] = float2{big, sum};
-            const int64_t t = in ? g.targets[m] : -1;
+            const int64_t t = target[j];
             if (in && t >= nw && t < g.N) {
                 const int d = static_cast<int>(t) - nw;
 #pragma unroll
@@ -304,9 +315,11 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
                         if (d == i * 16 + r) g.target_logit[m] = acc[i][j][r];
             }
         } else if constexpr (EPI == kEpiSoftmax) {
-            const int64_t t = in ? g.targets[m] : -1;
+            const int64_t t = target[j];
             const bool dead = !in || no_loss(t, g.ignore_index, g.V);
-            const float lse = dead ? 0.f : g.lse[m], w = dead ? 0.f : g.g ? g.g[m] : 1.f;
+            const float base = dead ? 0.f : lse[j], w = dead ? 0.f : weight[j];
+            constexpr float kLog2e = 1.44269504f;
+            const float base2 = -base * kLog2e;
             // the target's column, counted from this lane's first
             const int64_t d64 = dead ? -1 : t - g.n0 - nw;
             const int d = d64 < 0 || d64 >= FN * 16 ? -1 : static_cast<int>(d64);
@@ -314,8 +327,14 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
 #pragma unroll
             for (int i = 0; i < FN; ++i) {
                 v4f p;
+                // rounded to bf16 below, the exponent may be formed with one rounding more; as planes it may not
+                if (g.p_planes == 1) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = __expf(acc[i][j][r] - lse);
+                    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, base2));
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[r] = __expf(acc[i][j][r] - base);
+                }
                 if (hit) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) p[r] -= d == i * 16 + r ? 1.f : 0.f;
@@ -332,8 +351,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
 #pragma unroll
                 for (int i = 0; i < FN; ++i) {
                     out.put(i, acc[i][j]);
+                    if (q + 1 < g.p_planes)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] -= static_cast<float>(static_cast<bf16>(acc[i][j][r]));
+                        for (int r = 0; r < 4; ++r) acc[i][j][r] -= static_cast<float>(static_cast<bf16>(acc[i][j][r]));
                 }
                 out.flush(g.P + q * g.p_plane + mj * g.ldp + nb, g.ldp, g.M - mj, FN * 16);
             }
