@@ -61,10 +61,18 @@ static int launch_head_join(hipStream_t st, const float2* stats, const float* ta
     return launch(head_join_kernel<4>, dim3(ceil_div(T, 4)), dim3(256), 0, st, stats, target_logit, targets, ignore, T, V, blocks, loss, lse);
 }
 
+// dH from the products with P's two planes.
+__global__ __launch_bounds__(256) void head_unstack_kernel(const float* __restrict__ acc, int n, bf16* __restrict__ dH) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) dH[i] = static_cast<bf16>(acc[i] + acc[n + i]);
+}
+
 struct HeadPlan {
     bool small;                      // small32.h
     int P;                           // planes
     int n_seg;
+    int prob_planes;                 // planes of P
+    bool stacked;                    // bf16, few tokens: P's two planes as twice the tokens in dH, and as two pairs in dW
     bool h_direct, w_direct;
     int64_t ldh, ldw;
     int piece, n_pieces;             // words of a piece
@@ -113,19 +121,26 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         p.stats_at = room((ceil_div64(V, words) + 8) * T * 8);
         p.target_at = room(static_cast<int64_t>(T) * 4);
     } else {
-        // pieces of up to 256 MB of P, which is about what the memory-side cache holds, of equal size
-        int64_t words = (int64_t{256} << 20) / (int64_t{2} * p.P * T) / 1024 * 1024;
+        // With many tokens the roundings of P to bf16 average out beside those of dH and dW; with few a row's largest entry is most of it, and
+        // one rounding of that shows (relative error of one token's dH 0.4 % instead of 0.17 %).  Its second eight bits cost nothing there: the
+        // products are bound by reading W and writing dW.
+        p.stacked = p.P == 1 && T <= 128;
+        p.prob_planes = p.stacked ? 2 : p.P;
+        // pieces of up to 256 MB of P, which is about what the memory-side cache holds, of equal size; rows of P stay within the
+        // offsets of the product's copies
+        int64_t words = (int64_t{256} << 20) / (int64_t{2} * p.prob_planes * T) / 1024 * 1024;
         if (words < 1024) words = 1024;
+        if (words > (1 << 20)) words = 1 << 20;
         if (words > V) words = V;
         p.n_pieces = static_cast<int>(ceil_div64(V, words));
         p.piece = static_cast<int>(round_up(ceil_div64(V, p.n_pieces), 256));
         p.n_pieces = ceil_div(V, p.piece);
         p.ldp = p.piece;
         p.logits = plan16(T, p.piece, D, p.n_seg, 0);
-        p.dh = plan16(T, D, p.piece, p.n_seg, kAnyShares16);
-        p.dw = plan16(p.piece, D, T, p.n_seg, kAnyShares16);
-        p.p_at = room(static_cast<int64_t>(p.P) * T * p.ldp * 2);
-        p.acc_at = room(p.n_pieces > 1 ? static_cast<int64_t>(T) * D * 4 : 0);
+        p.dh = plan16(p.stacked ? 2 * T : T, D, p.piece, p.n_seg, kAnyShares16);
+        p.dw = plan16(p.piece, D, T, p.stacked ? 2 : p.n_seg, kAnyShares16);
+        p.p_at = room(static_cast<int64_t>(p.prob_planes) * T * p.ldp * 2);
+        p.acc_at = room(p.stacked ? int64_t{2} * T * D * 4 : p.n_pieces > 1 ? static_cast<int64_t>(T) * D * 4 : 0);
         p.part_bytes = p.dh.part_bytes > p.dw.part_bytes ? p.dh.part_bytes : p.dw.part_bytes;
         p.part_at = room(static_cast<int64_t>(p.part_bytes));
     }
@@ -261,25 +276,27 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         head_segments(g, p.n_seg);
         g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D;
         g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
-        g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.P;
+        g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.prob_planes;
         if (int rc = launch16(kEpiSoftmax, false, false, g, plan16(T, words, D, p.n_seg, 0), st)) return rc;
         // the piece's rows of dW
         Product16 q{};
         head_segments(q, p.n_seg);
+        if (p.stacked) q.n_seg = 2, q.seg_a = 0x10, q.seg_b = 0;
         q.A = probs, q.B = h, q.M = words, q.N = D, q.K = T;
         q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
         q.vec = D % 4 == 0;
         q.part = reinterpret_cast<float*>(base + p.part_at);
-        if (int rc = launch16(kEpiStore, true, true, q, plan16(words, D, T, p.n_seg, shares), st)) return rc;
+        if (int rc = launch16(kEpiStore, true, true, q, plan16(words, D, T, q.n_seg, shares), st)) return rc;
         // its share of dH
-        const bool last = i + 1 == p.n_pieces;
+        const bool last = i + 1 == p.n_pieces && !p.stacked;
         Product16 s{};
         head_segments(s, p.n_seg);
-        s.A = probs, s.B = wp, s.M = T, s.N = D, s.K = words;
+        s.A = probs, s.B = wp, s.M = p.stacked ? 2 * T : T, s.N = D, s.K = words;
         s.add = i ? acc : nullptr;
         s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16, s.vec = D % 4 == 0;
         s.part = q.part;
-        if (int rc = launch16(kEpiStore, false, true, s, plan16(T, D, words, p.n_seg, shares), st)) return rc;
+        if (int rc = launch16(kEpiStore, false, true, s, plan16(s.M, D, words, p.n_seg, shares), st)) return rc;
     }
-    return DAB_OK;
+    if (!p.stacked) return DAB_OK;
+    return launch(head_unstack_kernel, dim3(ceil_div(T * D, 256)), dim3(256), 0, st, acc, T * D, static_cast<bf16*>(dH));
 }
