@@ -554,7 +554,8 @@ int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, floa
  * rounds, and a 16-bit Y once more.
  *
  *   X   [B][K] of dtype, rows ldx apart;  Y  [B][F] of dtype out
- *   ws  dab_w4_matvec_workspace_bytes(...) bytes, 256-byte aligned (0 for aligned bf16 inputs)
+ *   ws  dab_w4_matvec_workspace_bytes(...) bytes, 256-byte aligned (0 for up to 16 bf16
+ *       tokens whose rows are 16-byte aligned)
  */
 size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx);
 int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F,

@@ -137,30 +137,32 @@ __global__ __launch_bounds__(64 * kW4PackWaves) void w4_unpack_kernel(const uint
     }
 }
 
-// ---------------------------------------------------------------- tokens as bf16 pieces
-// [P][B][ldp] from X [B][K], zeros from K to ldp (a multiple of 8).
-template <typename T, int P>
-__global__ __launch_bounds__(256) void w4_pieces_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int vec, int ldp,
-                                                        bf16* __restrict__ out) {
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 8, b = blockIdx.y;
-    if (c >= ldp) return;
-    float v[8];
-    load8(X + b * ldx, c, K, vec, v);
+// ---------------------------------------------------------------- tokens as the matrix cores take them
+// [pass][block of 128 k][i][column tile][lane] pieces of 16 bytes: column c = 16 tile + lane % 16 is piece c / nb of token c % nb of the pass, and
+// the piece holds its k = 128 block + 32 (lane / 16) + 8 i .. + 7; zeros past the last column and the last k.  A wavefront's load of them is a
+// kilobyte in a row; from the tokens' own rows it would touch 16 rows in four places each.
+template <typename T>
+__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int vec, int Kt, int nb, int P,
+                                                        int tiles, bf16* __restrict__ out) {
+    const int at = blockIdx.x * 256 + threadIdx.x, lane = at & 63, frag = at >> 6;
+    const int i4 = frag / tiles, t = frag - i4 * tiles, kt = i4 >> 2, i = i4 & 3;
+    if (kt >= Kt) return;
+    const int b0 = blockIdx.y * nb, n = min(nb, B - b0), c = t * 16 + (lane & 15), p = c / n, b = c - p * n;
+    float v[8] = {};
+    const int k = kt * 128 + (lane >> 4) * 32 + 8 * i;
+    if (p < P && k < K) load8(X + (b0 + b) * ldx, k, K, vec, v);
+    v8bf o;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        v8bf o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = piece_of(v[i], p);
-        *reinterpret_cast<v8bf*>(out + (static_cast<int64_t>(p) * B + b) * ldp + c) = o;
-    }
+    for (int u = 0; u < 8; ++u) o[u] = piece_of(v[u], p);
+    *reinterpret_cast<v8bf*>(out + ((static_cast<int64_t>(blockIdx.y) * Kt * 4 * tiles + frag) * 64 + lane) * 8) = o;
 }
 
 // ---------------------------------------------------------------- product
 struct W4Geom {
-    int F, Kt, K4, Kx;               // Kx: elements of a token's row in memory, a multiple of 8
+    int F, K, Kt, K4;
     int Ft, ks, groups;              // 16-row tiles, wavefronts that share a group of tiles, groups of a workgroup
     int B, nb, P;                    // tokens in all and per pass over the weights, pieces
-    int64_t ldx;                     // of the bf16 rows (piece p of token b: row p B + b)
+    int64_t ldx;                     // of tokens that are read where they are
     int dtype;                       // of the output
 };
 
@@ -193,7 +195,8 @@ struct Step4 {
     }
 };
 
-template <int NCT, int TB>
+// ROWS: bf16 tokens in rows of their own, X; else as w4_tokens_kernel lays them out.
+template <int NCT, int TB, bool ROWS>
 __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16* __restrict__ X, const uint8_t* __restrict__ Q,
                                                                      const uint8_t* __restrict__ S, W4Geom g, void* __restrict__ Y) {
     extern __shared__ float sums[];                          // [wavefront][tile][column][16 rows]
@@ -204,27 +207,16 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
     const int b0 = blockIdx.y * g.nb, nb = min(g.nb, g.B - b0), cols = nb * g.P;
 
     v4f acc[TB][NCT];
-    const bf16* xrow[NCT];
 #pragma unroll
-    for (int t = 0; t < NCT; ++t) {
-        const int c = t * 16 + (lane & 15);
+    for (int t = 0; t < NCT; ++t)
 #pragma unroll
         for (int u = 0; u < TB; ++u) acc[u][t] = v4f{0.f, 0.f, 0.f, 0.f};
-        const int p = c < cols ? c / nb : 0, b = c < cols ? c - p * nb : 0;
-        xrow[t] = X + (static_cast<int64_t>(p) * g.B + b0 + b) * g.ldx;
-    }
+    // (columns past the last read the first one's token; their results are not used)
+    const bf16* x0 = ROWS ? X + (b0 + ((lane & 15) < cols ? lane & 15 : 0)) * g.ldx
+                          : X + static_cast<int64_t>(blockIdx.y) * g.Kt * (4 * NCT * 512) + lane * 8;
     if (tile < g.Ft && part < g.K4) {
         Step4<TB> now, next;
         now.load(Q, S, g, tile, part, lane);
-        // columns past the last are read from the first (their results are not used), elements past the last from the end of the row
-        auto fetch = [&](v8bf (&x)[4][NCT], int kt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = min(kt * 128 + (lane >> 4) * 32 + 8 * i, g.Kx - 8);
-#pragma unroll
-                for (int t = 0; t < NCT; ++t) x[i][t] = *reinterpret_cast<const v8bf*>(xrow[t] + k);
-            }
-        };
         for (int s = part; s < g.K4; s += g.ks) {
             const bool more = s + g.ks < g.K4;
             if (more) next.load(Q, S, g, tile, s + g.ks, lane);
@@ -232,14 +224,27 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
             for (int j = 0; j < 4; ++j) {
                 const int kt = 4 * s + j;
                 v8bf x[4][NCT];
-                fetch(x, kt);
-                if (kt * 128 + 128 > g.Kx) {
-                    // past the last element: zeros, whatever was loaded
+                if constexpr (ROWS) {
+                    const int k = kt * 128 + (lane >> 4) * 32;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i][0] = *reinterpret_cast<const v8bf*>(x0 + min(k + 8 * i, g.K - 8));
+                    if (kt * 128 + 128 > g.K) {
+                        // past the last element: zeros, whatever was loaded
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (k + 8 * i >= g.K) x[i][0] = v8bf{};
+                    }
+                } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (kt * 128 + (lane >> 4) * 32 + 8 * i >= g.Kx)
+#pragma unroll
+                        for (int t = 0; t < NCT; ++t) x[i][t] = *reinterpret_cast<const v8bf*>(x0 + (static_cast<int64_t>(min(kt, g.Kt - 1)) * 4 + i) * (NCT * 512) + t * 512);
+                    if (kt >= g.Kt) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
                             for (int t = 0; t < NCT; ++t) x[i][t] = v8bf{};
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < TB; ++u) {
@@ -277,21 +282,25 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
     }
 }
 
-// Aligned bf16 tokens are read where they are; others as pieces from the workspace.
-static bool w4_direct(int32_t K, int32_t dtype, int64_t ldx) { return dtype == DAB_BF16 && K % 8 == 0 && ldx % 8 == 0; }
+// Columns of tokens that a pass over the weights takes, and its tokens.
+constexpr int kW4Columns = 48;
+static int w4_tokens(int B, int P) { return ceil_div(B, ceil_div(B, kW4Columns / P)); }
+// Aligned bf16 tokens of one column tile are read where they are, others from the workspace.
+static bool w4_rows(int32_t B, int32_t K, int32_t dtype, int64_t ldx) { return dtype == DAB_BF16 && B <= 16 && K % 8 == 0 && ldx % 8 == 0; }
 
-template <int NCT, int TB>
+template <int NCT, int TB, bool ROWS>
 static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
     const int waves = g.ks * g.groups;
     const dim3 grid(ceil_div(g.Ft, g.groups * TB), ceil_div(g.B, g.nb));
-    return launch(w4_matvec_kernel<NCT, TB>, grid, dim3(64 * waves), static_cast<size_t>(waves) * TB * NCT * 1024, st, X, Q, S, g, Y);
+    return launch(w4_matvec_kernel<NCT, TB, ROWS>, grid, dim3(64 * waves), static_cast<size_t>(waves) * TB * NCT * 1024, st, X, Q, S, g, Y);
 }
 template <int TB>
-static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
+static int launch_matvec(const W4Geom& g, bool rows, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
+    if (rows) return launch_matvec<1, TB, true>(g, st, X, Q, S, Y);
     switch (ceil_div(g.nb * g.P, 16)) {
-        case 1: return launch_matvec<1, TB>(g, st, X, Q, S, Y);
-        case 2: return launch_matvec<2, TB>(g, st, X, Q, S, Y);
-        default: return launch_matvec<3, TB == 4 ? 2 : TB>(g, st, X, Q, S, Y);
+        case 1: return launch_matvec<1, TB, false>(g, st, X, Q, S, Y);
+        case 2: return launch_matvec<2, TB, false>(g, st, X, Q, S, Y);
+        default: return launch_matvec<3, TB == 4 ? 2 : TB, false>(g, st, X, Q, S, Y);
     }
 }
 
@@ -323,8 +332,9 @@ extern "C" int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int3
 
 extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
     using namespace dab;
-    if (B < 1 || K < 1 || F < 1 || !real_dtype(dtype) || w4_direct(K, dtype, ldx)) return 0;
-    return static_cast<size_t>(dtype_pieces(dtype)) * B * round_up(K, 8) * 2;
+    if (B < 1 || K < 1 || F < 1 || !real_dtype(dtype) || w4_rows(B, K, dtype, ldx)) return 0;
+    const int P = dtype_pieces(dtype), nb = w4_tokens(B, P);
+    return static_cast<size_t>(ceil_div(B, nb)) * ceil_div(K, 128) * 4 * ceil_div(nb * P, 16) * 1024;
 }
 
 extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K,
@@ -332,46 +342,46 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
     using namespace dab;
     if (!X || !Q || !S || !Y) return DAB_ERR_NULL;
     if (B < 1 || K < 1 || F < 1 || ldx < K) return DAB_ERR_SHAPE;
-    if (!real_dtype(dtype) || K > INT32_MAX - 512 || B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
+    if (!real_dtype(dtype) || K > (1 << 26) || B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
     const size_t need = dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx);
     if (need && (!ws || ws_bytes < need || misaligned(ws, 256))) return DAB_ERR_WORKSPACE;
     const auto st = static_cast<hipStream_t>(stream);
 
     W4Geom g{};
-    g.F = F, g.Kt = ceil_div(K, 128), g.K4 = ceil_div(g.Kt, 4), g.Kx = static_cast<int>(round_up(K, 8));
-    g.Ft = ceil_div(F, 16), g.B = B, g.P = dtype_pieces(dtype);
-    const int passes = ceil_div(B, 48 / g.P);
-    g.nb = ceil_div(B, passes);
+    g.F = F, g.K = K, g.Kt = ceil_div(K, 128), g.K4 = ceil_div(g.Kt, 4);
+    g.Ft = ceil_div(F, 16), g.B = B, g.P = dtype_pieces(dtype), g.nb = w4_tokens(B, g.P);
     // Tiles of a wavefront: with one they are spread furthest, with more the tokens are loaded less often.  One token, 4096 weights a row:
-    // 4096 rows 4.0 us with one and 5.6 with two, 16384 rows 10.9 and 9.1, 131072 rows 63 and 51.7; twenty-one columns, 4099 rows of
-    // 9111: 26 with one, 19 with two, 24 with four; thirty-two, 32768 rows of 4096: 68, 41, 30; thirty-six, 4096 rows of 4096: 14.6
-    // and 16.0 (four tiles and three columns of tokens do not fit the registers).
+    // 4096 rows 3.9 us with one and 5.5 with two, 16384 rows 10.8 and 9.1, 131072 rows 63 and 52.4; two columns of tokens, 4096 rows
+    // of 4096: 8.0, 9.8 with two, 4099 rows of 9111 19.9, 15.4, 20.4 with four, 32768 rows of 4096 34, 26, 24.5; three, 4096 rows of 4096
+    // 9.6 and 10.8, (four tiles and three columns do not fit the registers).
     const int columns = ceil_div(g.nb * g.P, 16);
-    const int TB = columns == 1 ? (g.Ft >= 1024 ? 2 : 1) : columns == 2 ? (g.Ft >= 1024 ? 4 : g.Ft >= 128 ? 2 : 1) : g.Ft >= 512 ? 2 : 1;
-    // Shares of a row's sum: for one column of tokens until there are 24 wavefronts for every compute unit (131072 rows, two tiles: 57.8 us
-    // with one share, 51.7, 52.7, 54.9 with eight; 4096 rows, one tile: 7.9, 5.4, 4.2, 4.0), for more, which are bound by the tokens'
-    // loads, until there are four (60000 rows of 1500, twenty-four columns: 24.6, 20.8, 24.0).
-    const int enough = columns == 1 ? 24 * kNumCU : 4 * kNumCU;
+    const int TB = columns == 1   ? (g.Ft >= 1024 ? 2 : 1)
+                   : columns == 2 ? (g.Ft >= 1024 ? 4 : g.Ft >= 128 && g.K4 > 8 ? 2 : 1)
+                                  : (g.Ft >= 512 ? 2 : 1);
+    // Shares of a row's sum: for one column of tokens until there are 24 wavefronts for every compute unit (131072 rows, two tiles: 58.6 us
+    // with one share, 52.4, 53.7, 54.8 with eight; 4096 rows, one tile: 7.7, 5.3, 4.1, 3.9), for more, which are bound by the tokens'
+    // loads, until there are eight (32768 rows of 4096, two columns: 43, 28, 24.5, 27.4; 65536 of 8192 124, 129, 138, 160).
+    const int enough = columns == 1 ? 24 * kNumCU : 8 * kNumCU;
     g.ks = 1;
-    while (g.ks < 8 && g.ks < g.K4 && g.Ft / TB * g.ks < enough) g.ks *= 2;
-    // groups of a workgroup: eight wavefronts, fewer where that leaves compute units without one (30 tokens, 1024 x 1024: 11.8 -> 5.6)
+    while (g.ks < 8 && g.ks * 2 <= g.K4 && g.Ft / TB * g.ks < enough) g.ks *= 2;
+    // groups of a workgroup: eight wavefronts, fewer where that leaves compute units without one (30 tokens, 1024 x 1024: 11.8 -> 7.1)
     g.groups = 8 / g.ks;
     while (g.groups > 1 && ceil_div(g.Ft, g.groups * TB) < kNumCU) g.groups /= 2;
     g.dtype = dtype;
     const bf16* x = static_cast<const bf16*>(X);
     g.ldx = ldx;
     if (need) {
-        g.ldx = g.Kx;
         bf16* out = static_cast<bf16*>(ws);
-        const dim3 grid(ceil_div(g.Kx, 2048), B), block(256);
+        const int64_t frags = static_cast<int64_t>(g.Kt) * 4 * columns;
+        const dim3 grid(static_cast<unsigned>(ceil_div64(frags, 4)), ceil_div(B, g.nb)), block(256);
         const int vec = ldx * dtype_bytes(dtype) % 16 == 0;
         int rc;
-        if (dtype == DAB_F32) rc = launch(w4_pieces_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), B, K, ldx, vec, g.Kx, out);
-        else if (dtype == DAB_F16) rc = launch(w4_pieces_kernel<f16, 2>, grid, block, 0, st, static_cast<const f16*>(X), B, K, ldx, vec, g.Kx, out);
-        else rc = launch(w4_pieces_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), B, K, ldx, vec, g.Kx, out);
+        if (dtype == DAB_F32) rc = launch(w4_tokens_kernel<float>, grid, block, 0, st, static_cast<const float*>(X), B, K, ldx, vec, g.Kt, g.nb, g.P, columns, out);
+        else if (dtype == DAB_F16) rc = launch(w4_tokens_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(X), B, K, ldx, vec, g.Kt, g.nb, g.P, columns, out);
+        else rc = launch(w4_tokens_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(X), B, K, ldx, vec, g.Kt, g.nb, g.P, columns, out);
         if (rc) return rc;
         x = out;
     }
-    return TB == 4 ? launch_matvec<4>(g, st, x, Q, S, Y) : TB == 2 ? launch_matvec<2>(g, st, x, Q, S, Y) : launch_matvec<1>(g, st, x, Q, S, Y);
+    return TB == 4 ? launch_matvec<4>(g, !need, st, x, Q, S, Y) : TB == 2 ? launch_matvec<2>(g, !need, st, x, Q, S, Y) : launch_matvec<1>(g, !need, st, x, Q, S, Y);
 }
