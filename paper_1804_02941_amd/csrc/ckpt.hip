@@ -1,4 +1,4 @@
-// A layer's input in 8 bits: save, restore (the weight gradient from it: head.hip's neighbour product16.h).
+// A layer's input in 8 bits: save, restore (the weight gradient from it: product16.hip).
 //
 // Both are one pass over memory: save reads size bytes a value and writes 1 + 1/32, restore the other way round.  Four lanes
 // hold a group of 32, eight values each, so that a lane's load is 16 or 32 bytes and its store 8, and the group's largest magnitude is two
@@ -14,7 +14,6 @@ struct Rows8 {
     int lanes_log2;                  // lanes that share a row within a wavefront
     int row_parts;                   // pieces of 64 lanes that a row takes
     int64_t ld;
-    int vec;
 };
 
 // Row and first column of this lane's eight values; false past the end.
@@ -35,7 +34,7 @@ __global__ __launch_bounds__(64 * kSaveWaves) void ckpt8_save_kernel(const T* __
     int row, c;
     const bool in = my_eight(g, &row, &c);                   // whole groups are in or out, and the exchange stays in a group
     float v[8] = {};
-    if (in) load8(X + row * g.ld, c, g.cols, g.vec, v);
+    if (in) load8(X + row * g.ld, c, g.cols, v);
     const uint32_t m = group_max(v);
     if (!in) return;
     uint64_t word = 0;
@@ -67,13 +66,12 @@ __global__ __launch_bounds__(64 * kSaveWaves) void ckpt8_restore_kernel(const in
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(static_cast<int8_t>(word >> (8 * i))) * scale;
-    store8(X + row * g.ld, c, g.cols, g.vec, v);
+    store8(X + row * g.ld, c, g.cols, v);
 }
 
-static Rows8 rows8_of(int rows, int cols, int64_t ld, int64_t size) {
+static Rows8 rows8_of(int rows, int cols, int64_t ld) {
     Rows8 g{};
     g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ld = ld;
-    g.vec = ld * size % 16 == 0;
     const int lanes = g.groups * 4;
     g.lanes_log2 = 2;
     while (g.lanes_log2 < 6 && (1 << g.lanes_log2) < lanes) ++g.lanes_log2;
@@ -102,7 +100,7 @@ extern "C" int dab_ckpt8_save(const void* X, int32_t dtype, int32_t rows, int32_
                               void* stream) {
     using namespace dab;
     if (int rc = check_rows(X, dtype, rows, cols, ldx, Q, S)) return rc;
-    const Rows8 g = rows8_of(rows, cols, ldx, dtype_bytes(dtype));
+    const Rows8 g = rows8_of(rows, cols, ldx);
     const unsigned grid = save_grid(g);
     if (grid == 0) return DAB_ERR_UNSUPPORTED;
     const auto st = static_cast<hipStream_t>(stream);
@@ -116,7 +114,7 @@ extern "C" int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows
                                  void* stream) {
     using namespace dab;
     if (int rc = check_rows(X, dtype, rows, cols, ldx, Q, S)) return rc;
-    const Rows8 g = rows8_of(rows, cols, ldx, dtype_bytes(dtype));
+    const Rows8 g = rows8_of(rows, cols, ldx);
     const unsigned grid = save_grid(g);
     if (grid == 0) return DAB_ERR_UNSUPPORTED;
     const auto st = static_cast<hipStream_t>(stream);

@@ -167,8 +167,8 @@ static void head_segments(Product16& g, int n_seg) {
 static Small32 head_logits32(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets, int64_t ignore,
                              int T, int D, int V) {
     Small32 g{};
-    g.A = {H, ldh, T, ldh % 4 == 0, nullptr, 0, 0};
-    g.B = {W, ldw, V, ldw % 4 == 0, nullptr, 0, 0};
+    g.A = {H, ldh, T, nullptr, 0, 0};
+    g.B = {W, ldw, V, nullptr, 0, 0};
     g.M = T, g.N = V, g.K = D, g.tiles_n = ceil_div(V, kSmallTile);
     g.targets = targets, g.ignore_index = ignore;
     return g;
@@ -255,9 +255,9 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         g.C = P, g.ldc = p.ldp, g.lse = lse, g.g = grad;
         if (int rc = launch_small_softmax(g, dtype, st)) return rc;
         Small32 q{}, s{};
-        q.A = {P, p.ldp, V, 0, nullptr, 0, 0}, q.B = {H, ldh, D, 0, targets, ignore_index, V};
+        q.A = {P, p.ldp, V, nullptr, 0, 0}, q.B = {H, ldh, D, targets, ignore_index, V};
         q.M = V, q.N = D, q.K = T, q.tiles_n = ceil_div(D, kSmallTile), q.C = dW, q.ldc = D, q.dtype = dtype;
-        s.A = {P, p.ldp, T, 1, nullptr, 0, 0}, s.B = {W, ldw, D, 0, nullptr, 0, 0};
+        s.A = {P, p.ldp, T, nullptr, 0, 0}, s.B = {W, ldw, D, nullptr, 0, 0};
         s.M = T, s.N = D, s.K = V, s.tiles_n = q.tiles_n, s.C = dH, s.ldc = D, s.dtype = dtype;
         return launch_small_gradients(q, s, dtype, st);
     }
@@ -284,7 +284,6 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         if (p.stacked) q.n_seg = 2, q.seg_a = 0x10, q.seg_b = 0;
         q.A = probs, q.B = h, q.M = words, q.N = D, q.K = T;
         q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
-        q.vec = D % 4 == 0;
         q.part = reinterpret_cast<float*>(base + p.part_at);
         if (int rc = launch16(kEpiStore, true, true, q, plan16(words, D, T, q.n_seg, shares), st)) return rc;
         // its share of dH
@@ -293,7 +292,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         head_segments(s, p.n_seg);
         s.A = probs, s.B = wp, s.M = p.stacked ? 2 * T : T, s.N = D, s.K = words;
         s.add = i ? acc : nullptr;
-        s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16, s.vec = D % 4 == 0;
+        s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16;
         s.part = q.part;
         if (int rc = launch16(kEpiStore, false, true, s, plan16(s.M, D, words, p.n_seg, shares), st)) return rc;
     }

@@ -37,8 +37,7 @@ struct Product16 {
     // kEpiStore: C (out_bf16 or fp32, rows ldc apart)
     void* C;
     int64_t ldc;
-    int out_bf16, vec;               // vec: four neighbouring columns are one aligned store
-    int lines;                       // so are 16 bytes of a row
+    int out_bf16;
     const float* add;                // fp32 [M][N] added to the sum, or NULL
     float* part;                     // [rest][shares][tile] sums of the shares, in the order of the accumulators
     // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece

@@ -96,22 +96,27 @@ struct Reader16 {
 };
 
 // Four neighbouring columns of the result.
-__device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v) {
-    typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
-    if (n >= g.N) return;
-    if (g.vec) {
-        if (g.add) v += *reinterpret_cast<const v4f*>(g.add + static_cast<int64_t>(m) * g.N + n);
-        if (g.out_bf16) *reinterpret_cast<v4bf*>(static_cast<bf16*>(g.C) + m * g.ldc + n) = __builtin_convertvector(v, v4bf);
-        else *reinterpret_cast<v4f*>(static_cast<float*>(g.C) + m * g.ldc + n) = v;
+template <typename T>
+__device__ __forceinline__ void store4(T* to, v4f v, int columns) {
+    typedef T v4t __attribute__((ext_vector_type(4)));
+    const v4t out = __builtin_convertvector(v, v4t);
+    if (columns >= 4) {
+        *reinterpret_cast<typename Unaligned<T, 4>::type*>(to) = out;
         return;
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (n + r >= g.N) break;
-        if (g.add) v[r] += g.add[static_cast<int64_t>(m) * g.N + n + r];
-        if (g.out_bf16) static_cast<bf16*>(g.C)[m * g.ldc + n + r] = static_cast<bf16>(v[r]);
-        else static_cast<float*>(g.C)[m * g.ldc + n + r] = v[r];
+    for (int r = 0; r < 4; ++r)
+        if (r < columns) to[r] = out[r];
+}
+__device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v) {
+    if (n >= g.N) return;
+    if (g.add) {
+        const float* from = g.add + static_cast<int64_t>(m) * g.N + n;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += n + r < g.N ? from[r] : 0.f;
     }
+    if (g.out_bf16) store4(static_cast<bf16*>(g.C) + m * g.ldc + n, v, g.N - n);
+    else store4(static_cast<float*>(g.C) + m * g.ldc + n, v, g.N - n);
 }
 
 // 16 rows of a wavefront's result through LDS (its own part, 16 rows x FN x 16 columns), so that rows are stored in whole lines instead of
@@ -134,7 +139,23 @@ struct Rows16 {
         for (int r0 = 0; r0 < 16; r0 += 64 / kLanes) {
             const int r = r0 + lane / kLanes;
             const v4u32 v = *reinterpret_cast<const v4u32*>(lds + r * kRow + ((c ^ r) & (kChunks - 1)) * 16);
-            if (r < rows && c * (16 / static_cast<int>(sizeof(T))) < columns) *reinterpret_cast<v4u32*>(row0 + r * ld + c * (16 / sizeof(T))) = v;
+            constexpr int kElems = 16 / static_cast<int>(sizeof(T));
+            const int left = columns - c * kElems;
+            T* to = row0 + r * ld + c * kElems;
+            if (r >= rows) continue;
+            if (left >= kElems) {
+                *reinterpret_cast<Unaligned<uint32_t, 4>::type*>(to) = v;
+            } else {
+                // the last columns of a row whose number is no multiple of a piece's
+#pragma unroll
+                for (int u = 0; u < kElems; ++u) {
+                    const uint32_t bits = sizeof(T) == 4 ? v[u & 3] : v[(u >> 1) & 3] >> (16 * (u & 1));
+                    if (u < left) {
+                        if constexpr (sizeof(T) == 4) to[u] = __uint_as_float(bits);
+                        else to[u] = __builtin_bit_cast(T, static_cast<uint16_t>(bits));
+                    }
+                }
+            }
         }
     }
 };
@@ -362,7 +383,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
             for (int i = 0; i < FN; ++i)
                 *reinterpret_cast<v4f*>(g.part + ((static_cast<int64_t>(tile - g.whole) * g.shares + share) * (FN * FM) + i * FM + j) * (256 * NW) +
                                         threadIdx.x * 4) = acc[i][j];
-        } else if (g.lines && !g.add) {
+        } else if (!g.add) {
             if (g.out_bf16) {
                 const Rows16<bf16, FN> out{mine, lane};
 #pragma unroll
@@ -410,7 +431,7 @@ __global__ __launch_bounds__(64 * WM * WN) void join16_kernel(Product16 g) {
 
 // ---------------------------------------------------------------- operands as bf16 planes
 template <typename T, int P>
-__global__ __launch_bounds__(256) void planes16_kernel(const T* __restrict__ X, int rows, int cols, int64_t ld, int vec,
+__global__ __launch_bounds__(256) void planes16_kernel(const T* __restrict__ X, int rows, int cols, int64_t ld,
                                                        const int64_t* __restrict__ targets, int64_t ignore, int V,
                                                        bf16* __restrict__ out, int ldp, int64_t chunks) {
     const int per_row = ldp >> 3;
@@ -418,7 +439,7 @@ __global__ __launch_bounds__(256) void planes16_kernel(const T* __restrict__ X, 
         const int64_t row = i / per_row;
         const int c = static_cast<int>(i - row * per_row) * 8;
         float v[8] = {};
-        if (!targets || !no_loss(targets[row], ignore, V)) load8(X + row * ld, c, cols, vec, v);
+        if (!targets || !no_loss(targets[row], ignore, V)) load8(X + row * ld, c, cols, v);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             v8bf o;
@@ -434,10 +455,10 @@ int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld
     const int64_t chunks = rows * (ldp >> 3);
     const int64_t blocks = ceil_div64(chunks, 256);
     const dim3 grid(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), block(256);
-    const int vec = ld * dtype_bytes(dtype) % 16 == 0, l = static_cast<int>(ldp);
-    if (dtype == DAB_F32) return launch(planes16_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), rows, cols, ld, vec, targets, ignore, V, out, l, chunks);
-    if (dtype == DAB_F16) return launch(planes16_kernel<f16, 2>, grid, block, 0, st, static_cast<const f16*>(X), rows, cols, ld, vec, targets, ignore, V, out, l, chunks);
-    return launch(planes16_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), rows, cols, ld, vec, targets, ignore, V, out, l, chunks);
+    const int l = static_cast<int>(ldp);
+    if (dtype == DAB_F32) return launch(planes16_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
+    if (dtype == DAB_F16) return launch(planes16_kernel<f16, 2>, grid, block, 0, st, static_cast<const f16*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
+    return launch(planes16_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
 }
 
 // ---------------------------------------------------------------- plan and launch
@@ -493,7 +514,6 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
     g.tiles_m = ceil_div(g.M, tm), g.tiles_n = ceil_div(g.N, tn);
     if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
     g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
-    g.lines = g.ldc * (g.out_bf16 ? 2 : 4) % 16 == 0 && g.N % (g.out_bf16 ? 8 : 4) == 0;
     g.whole_xcd = ceil_div(g.whole, kNumXCD), g.rest_xcd = ceil_div(g.rest * g.shares, kNumXCD);
     const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.big)
                         : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.big)
@@ -524,6 +544,42 @@ int init_product16() {
 
 // ---------------------------------------------------------------- the weight gradient from a saved input
 namespace dab {
+
+// Both operands of it in one launch: the saved input as bf16 [rows][32 groups], which is exact, by the first `x_blocks` workgroups; dY as P
+// planes by the others (none where it is read as it is).
+template <typename T, int P>
+__global__ __launch_bounds__(256) void grad_operands_kernel(const int8_t* __restrict__ Q, const uint8_t* __restrict__ S, int64_t x_chunks,
+                                                            bf16* __restrict__ X, unsigned x_blocks, const T* __restrict__ dY, int rows, int F,
+                                                            int64_t ld, bf16* __restrict__ Y, int ldp) {
+    if (blockIdx.x < x_blocks) {
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < x_chunks; i += static_cast<int64_t>(x_blocks) * 256) {
+            const uint64_t word = reinterpret_cast<const uint64_t*>(Q)[i];
+            const int code = S[i >> 2];
+            const float scale = code == 255 ? __builtin_nanf("") : pow2f(code - 127);
+            v8bf o;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = static_cast<bf16>(static_cast<float>(static_cast<int8_t>(word >> (8 * u))) * scale);
+            reinterpret_cast<v8bf*>(X)[i] = o;
+        }
+        return;
+    }
+    const int per_row = ldp >> 3;
+    const int64_t chunks = static_cast<int64_t>(rows) * per_row, step = static_cast<int64_t>(gridDim.x - x_blocks) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x - x_blocks) * 256 + threadIdx.x; i < chunks; i += step) {
+        const int64_t row = i / per_row;
+        const int c = static_cast<int>(i - row * per_row) * 8;
+        float v[8];
+        load8(dY + row * ld, c, F, v);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            v8bf o;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = piece_of(v[u], p);
+            *reinterpret_cast<v8bf*>(Y + p * (static_cast<int64_t>(rows) * ldp) + row * ldp + c) = o;
+        }
+    }
+}
+
 struct GradPlan {
     Plan16 pl;
     bool direct;                     // dY is read where it is
@@ -568,20 +624,26 @@ extern "C" int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t 
     const auto st = static_cast<hipStream_t>(stream);
     char* base = static_cast<char*>(ws);
     bf16* x = reinterpret_cast<bf16*>(base + p.x_at);
-    if (int rc = dab_ckpt8_restore(Q, S, rows, cols, x, DAB_BF16, p.ldx, stream)) return rc;
     const bf16* y = static_cast<const bf16*>(dY);
-    if (!p.direct) {
-        bf16* out = reinterpret_cast<bf16*>(base + p.y_at);
-        if (int rc = launch_planes16(dY, dtype, rows, F, lddy, nullptr, 0, 0, out, p.ldy, st)) return rc;
-        y = out;
-    }
+    bf16* out = reinterpret_cast<bf16*>(base + p.y_at);
+    const int64_t x_chunks = rows * (p.ldx / 8), y_chunks = p.direct ? 0 : rows * (p.ldy / 8);
+    auto blocks = [](int64_t chunks) { return static_cast<unsigned>(ceil_div64(chunks, 256) < 8192 ? ceil_div64(chunks, 256) : 8192); };
+    const unsigned x_blocks = blocks(x_chunks);
+    const dim3 grid(x_blocks + blocks(y_chunks)), block(256);
+    const int ldy = static_cast<int>(p.ldy);
+    int rc;
+    if (dtype == DAB_F32) rc = launch(grad_operands_kernel<float, 3>, grid, block, 0, st, Q, S, x_chunks, x, x_blocks, static_cast<const float*>(dY), rows, F, lddy, out, ldy);
+    else if (dtype == DAB_F16) rc = launch(grad_operands_kernel<f16, 2>, grid, block, 0, st, Q, S, x_chunks, x, x_blocks, static_cast<const f16*>(dY), rows, F, lddy, out, ldy);
+    else rc = launch(grad_operands_kernel<bf16, 1>, grid, block, 0, st, Q, S, x_chunks, x, x_blocks, static_cast<const bf16*>(dY), rows, F, lddy, out, ldy);
+    if (rc) return rc;
+    if (!p.direct) y = out;
     Product16 g{};
     g.A = {y, p.ldy, static_cast<int64_t>(rows) * p.ldy};
     g.B = {x, p.ldx, 0};
     g.M = F, g.N = cols, g.K = rows;
     g.n_seg = dtype_pieces(dtype);
     g.seg_a = 0x210;                 // pieces of dY in turn, with the one plane of X
-    g.C = dW, g.ldc = cols, g.vec = cols % 4 == 0;
+    g.C = dW, g.ldc = cols;
     g.part = reinterpret_cast<float*>(base + p.part_at);
     return launch16(kEpiStore, true, true, g, p.pl, st);
 }

@@ -24,16 +24,24 @@ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // 2^e as fp32 for -126 <= e <= 127.
 __device__ __forceinline__ float pow2f(int e) { return __builtin_bit_cast(float, static_cast<uint32_t>(e + 127) << 23); }
 
-// Eight elements of a row from column c on as fp32, zeros past the row's end.  vec: rows are 16-byte aligned.
+// Vectors of elements at any address of theirs: the memory system takes 16 bytes a lane at any alignment (rows whose distance is odd cost a
+// line more here and there, not eight loads for one).
+template <typename T, int N>
+struct Unaligned {
+    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// Eight elements of a row from column c on as fp32, zeros past the row's end.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int c, int cols, bool vec, float (&v)[8]) {
-    if (vec && c + 8 <= cols) {
+__device__ __forceinline__ void load8(const T* row, int c, int cols, float (&v)[8]) {
+    if (c + 8 <= cols) {
+        typedef typename Unaligned<T, 4>::type v4t;
+        typedef typename Unaligned<T, 8>::type v8t;
         if constexpr (sizeof(T) == 4) {
-            const v4f a = *reinterpret_cast<const v4f*>(row + c), b = *reinterpret_cast<const v4f*>(row + c + 4);
+            const v4t a = *reinterpret_cast<const v4t*>(row + c), b = *reinterpret_cast<const v4t*>(row + c + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
         } else {
-            typedef T v8t __attribute__((ext_vector_type(8)));
             const v8t a = *reinterpret_cast<const v8t*>(row + c);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(a[i]);
@@ -46,13 +54,14 @@ __device__ __forceinline__ void load8(const T* row, int c, int cols, bool vec, f
 
 // The same eight back; what lies past the row's end is not written.
 template <typename T>
-__device__ __forceinline__ void store8(T* row, int c, int cols, bool vec, const float (&v)[8]) {
-    if (vec && c + 8 <= cols) {
+__device__ __forceinline__ void store8(T* row, int c, int cols, const float (&v)[8]) {
+    if (c + 8 <= cols) {
+        typedef typename Unaligned<T, 4>::type v4t;
+        typedef typename Unaligned<T, 8>::type v8t;
         if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<v4f*>(row + c) = v4f{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<v4f*>(row + c + 4) = v4f{v[4], v[5], v[6], v[7]};
+            *reinterpret_cast<v4t*>(row + c) = v4t{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<v4t*>(row + c + 4) = v4t{v[4], v[5], v[6], v[7]};
         } else {
-            typedef T v8t __attribute__((ext_vector_type(8)));
             v8t a;
 #pragma unroll
             for (int i = 0; i < 8; ++i) a[i] = static_cast<T>(v[i]);

@@ -12,7 +12,7 @@ namespace dab {
 struct Source32 {
     const void* p;
     int64_t ld;                      // elements between rows ([rows][k]) or between k ([k][rows])
-    int rows, vec;                   // vec: four k of a row are one aligned load
+    int rows;
     const int64_t* targets;          // k whose target has no loss are zeros (NULL: none)
     int64_t ignore_index;
     int V;

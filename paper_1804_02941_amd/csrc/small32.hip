@@ -16,9 +16,10 @@ __device__ __forceinline__ v4f four(const Source32& o, int row, int k, int K) {
                 v[c] = static_cast<float>(static_cast<const T*>(o.p)[(k + c) * o.ld + row]);
     } else {
         const T* from = static_cast<const T*>(o.p) + row * o.ld + k;
-        if (o.vec && k + 4 <= K) {
+        if (k + 4 <= K) {
             typedef T v4t __attribute__((ext_vector_type(4)));
-            v = __builtin_convertvector(*reinterpret_cast<const v4t*>(from), v4f);
+            const v4t got = *reinterpret_cast<const typename Unaligned<T, 4>::type*>(from);
+            v = __builtin_convertvector(got, v4f);
         } else {
 #pragma unroll
             for (int c = 0; c < 4; ++c)

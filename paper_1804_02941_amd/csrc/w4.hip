@@ -23,10 +23,13 @@ struct W4Block {
 };
 
 template <typename T>
-__device__ __forceinline__ v4f load4(const T* row, int c, int cols, bool vec) {
+__device__ __forceinline__ v4f load4(const T* row, int c, int cols) {
     typedef T v4t __attribute__((ext_vector_type(4)));
     v4f v = v4f{0.f, 0.f, 0.f, 0.f};
-    if (vec && c + 4 <= cols) return __builtin_convertvector(*reinterpret_cast<const v4t*>(row + c), v4f);
+    if (c + 4 <= cols) {
+        const v4t got = *reinterpret_cast<const typename Unaligned<T, 4>::type*>(row + c);
+        return __builtin_convertvector(got, v4f);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (c + i < cols) v[i] = static_cast<float>(row[c + i]);
@@ -34,7 +37,7 @@ __device__ __forceinline__ v4f load4(const T* row, int c, int cols, bool vec) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(64 * kW4PackWaves) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int vec, int Kt, int K4,
+__global__ __launch_bounds__(64 * kW4PackWaves) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int Kt, int K4,
                                                                     uint8_t* __restrict__ Q, uint8_t* __restrict__ S) {
     __shared__ W4Block lds[kW4PackWaves];
     DAB_RESERVE_VGPRS();
@@ -51,7 +54,7 @@ __global__ __launch_bounds__(64 * kW4PackWaves) void w4_pack_kernel(const T* __r
         for (int i = 0; i < 8; ++i) {
             const int row = tile * 16 + 2 * i + (lane >> 5);
             v[i] = v4f{0.f, 0.f, 0.f, 0.f};
-            if (row < F) v[i] = load4(W + row * ldw, k, K, vec);
+            if (row < F) v[i] = load4(W + row * ldw, k, K);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -125,8 +128,8 @@ __global__ __launch_bounds__(64 * kW4PackWaves) void w4_unpack_kernel(const uint
             }
             if (row >= F) continue;
             float* to = W + static_cast<int64_t>(row) * K;
-            if ((K & 3) == 0 && k + 4 <= K) {
-                *reinterpret_cast<v4f*>(to + k) = v;
+            if (k + 4 <= K) {
+                *reinterpret_cast<Unaligned<float, 4>::type*>(to + k) = v;
             } else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(64 * kW4PackWaves) void w4_unpack_kernel(const uint
 // the piece holds its k = 128 block + 32 (lane / 16) + 8 i .. + 7; zeros past the last column and the last k.  A wavefront's load of them is a
 // kilobyte in a row; from the tokens' own rows it would touch 16 rows in four places each.
 template <typename T>
-__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int vec, int Kt, int nb, int P,
+__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int Kt, int nb, int P,
                                                         int tiles, bf16* __restrict__ out) {
     const int at = blockIdx.x * 256 + threadIdx.x, lane = at & 63, frag = at >> 6;
     const int i4 = frag / tiles, t = frag - i4 * tiles, kt = i4 >> 2, i = i4 & 3;
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X,
     const int b0 = blockIdx.y * nb, n = min(nb, B - b0), c = t * 16 + (lane & 15), p = c / n, b = c - p * n;
     float v[8] = {};
     const int k = kt * 128 + (lane >> 4) * 32 + 8 * i;
-    if (p < P && k < K) load8(X + (b0 + b) * ldx, k, K, vec, v);
+    if (p < P && k < K) load8(X + (b0 + b) * ldx, k, K, v);
     v8bf o;
 #pragma unroll
     for (int u = 0; u < 8; ++u) o[u] = piece_of(v[u], p);
@@ -312,12 +315,12 @@ extern "C" int dab_w4_pack(const void* W, int32_t dtype, int32_t F, int32_t K, i
     if (F < 1 || K < 1 || ldw < K) return DAB_ERR_SHAPE;
     if (!real_dtype(dtype) || K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
-    const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4), vec = ldw * dtype_bytes(dtype) % 16 == 0;
+    const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4);
     const dim3 grid(ceil_div(K4, kW4PackWaves), ceil_div(F, 16)), block(64 * kW4PackWaves);
     const auto st = static_cast<hipStream_t>(stream);
-    if (dtype == DAB_F32) return launch(w4_pack_kernel<float>, grid, block, 0, st, static_cast<const float*>(W), F, K, ldw, vec, Kt, K4, Q, S);
-    if (dtype == DAB_BF16) return launch(w4_pack_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(W), F, K, ldw, vec, Kt, K4, Q, S);
-    return launch(w4_pack_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(W), F, K, ldw, vec, Kt, K4, Q, S);
+    if (dtype == DAB_F32) return launch(w4_pack_kernel<float>, grid, block, 0, st, static_cast<const float*>(W), F, K, ldw, Kt, K4, Q, S);
+    if (dtype == DAB_BF16) return launch(w4_pack_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(W), F, K, ldw, Kt, K4, Q, S);
+    return launch(w4_pack_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(W), F, K, ldw, Kt, K4, Q, S);
 }
 
 extern "C" int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, float* W, void* stream) {
@@ -375,11 +378,10 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
         bf16* out = static_cast<bf16*>(ws);
         const int64_t frags = static_cast<int64_t>(g.Kt) * 4 * columns;
         const dim3 grid(static_cast<unsigned>(ceil_div64(frags, 4)), ceil_div(B, g.nb)), block(256);
-        const int vec = ldx * dtype_bytes(dtype) % 16 == 0;
         int rc;
-        if (dtype == DAB_F32) rc = launch(w4_tokens_kernel<float>, grid, block, 0, st, static_cast<const float*>(X), B, K, ldx, vec, g.Kt, g.nb, g.P, columns, out);
-        else if (dtype == DAB_F16) rc = launch(w4_tokens_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(X), B, K, ldx, vec, g.Kt, g.nb, g.P, columns, out);
-        else rc = launch(w4_tokens_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(X), B, K, ldx, vec, g.Kt, g.nb, g.P, columns, out);
+        if (dtype == DAB_F32) rc = launch(w4_tokens_kernel<float>, grid, block, 0, st, static_cast<const float*>(X), B, K, ldx, g.Kt, g.nb, g.P, columns, out);
+        else if (dtype == DAB_F16) rc = launch(w4_tokens_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(X), B, K, ldx, g.Kt, g.nb, g.P, columns, out);
+        else rc = launch(w4_tokens_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(X), B, K, ldx, g.Kt, g.nb, g.P, columns, out);
         if (rc) return rc;
         x = out;
     }
