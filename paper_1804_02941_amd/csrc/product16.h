@@ -54,8 +54,9 @@ struct Product16 {
 };
 
 // Tile of a product and how its sums are shared out (product16.hip).
+enum class Tiles16 { kSmall, kDeep, kBig };
 struct Plan16 {
-    bool big;
+    Tiles16 tiles;
     int steps, whole, rest, shares, share_steps;
     size_t part_bytes;
     double us;                       // estimated time

@@ -6,8 +6,10 @@
 namespace dab {
 
 // ---------------------------------------------------------------- the product
+// Waits until no more than N of the wavefront's copies are on their way and its LDS reads have arrived, and for the other wavefronts.
+template <int N = 0>
 __device__ __forceinline__ void wait_and_meet() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
@@ -160,8 +162,9 @@ struct Rows16 {
     }
 };
 
-template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
+// NS: steps in LDS.
+template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS>
+__device__ __forceinline__ void product16(const Product16& g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
     using LA = Loader16<TM, ARC, NW>;
     using LB = Loader16<TN, BRC, NW>;
@@ -260,23 +263,34 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
     using yes = std::integral_constant<bool, true>;
     using no = std::integral_constant<bool, false>;
 
-    // Two buffers of 64 k.  While a half step is multiplied from registers, the next one's fragments are read; behind the one barrier of a
-    // step, in its middle, the step after has landed and its own buffer has been read by all, so the step after that is fetched into it.
-    aim();
-    fetch(lds);
-    wait_and_meet();
-    aim();
-    fetch(lds + kBuf);
+    // NS buffers of 64 k.  While a half step is multiplied from registers, the next one's fragments are read; behind the one barrier of a
+    // step, in its middle, the next step has landed (those after it may be on their way) and its own buffer has been read by all, so step NS further on
+    // is fetched into it.
+    constexpr int kInFlight = LA::kCopies + LB::kCopies;     // copies of a wavefront for a step
+    if constexpr (NS == 2) {
+        aim();
+        fetch(lds);
+        wait_and_meet();
+        aim();
+        fetch(lds + kBuf);
+    } else {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            aim();
+            fetch(lds + i * kBuf);
+        }
+        wait_and_meet<(NS - 1) * kInFlight>();
+    }
 #pragma unroll
     for (int j = 0; j < FM; ++j) a[0][j] = ra.read(lds, 0, j);
 #pragma unroll
     for (int i = 0; i < FN; ++i) b[0][i] = rb.read(lds + LA::kBytes, 0, i);
     for (int s = first; s < last; ++s) {
-        char* cur = lds + ((s - first) & 1) * kBuf;
-        char* other = lds + ((s + 1 - first) & 1) * kBuf;
+        char* cur = lds + ((s - first) & (NS - 1)) * kBuf;
+        char* other = lds + ((s + 1 - first) & (NS - 1)) * kBuf;
         aim();
         half(no{}, 0, cur, 1, cur);
-        wait_and_meet();
+        wait_and_meet<(NS - 2) * kInFlight>();
         half(yes{}, 1, other, 0, cur);
     }
     // (copies and reads past the last step: zeros, and not used; the wavefront waits for them before it ends)
@@ -402,6 +416,17 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Pr
     }
 }
 
+template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
+    product16<EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
+}
+// For no more tiles than compute units: with one workgroup on each, a step of the small tile takes as long as its copies, so four
+// steps are on their way instead of two.
+template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_deep_kernel(Product16 g) {
+    product16<EPI, TM, TN, WM, WN, ARC, BRC, 4>(g);
+}
+
 // The shares of a tile's sums, added in a fixed order.  A workgroup takes one 16 x 16 block of every wavefront; eight shares
 // are on their way at a time.
 template <int TM, int TN, int WM, int WN>
@@ -464,16 +489,19 @@ int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld
 // ---------------------------------------------------------------- plan and launch
 constexpr int kBigM = 256, kBigN = 256, kBigWM = 4, kBigWN = 2;
 constexpr int kSmallM = 128, kSmallN = 128, kSmallWM = 2, kSmallWN = 2;
-constexpr size_t lds_bytes16(int tm, int tn) { return static_cast<size_t>(2) * (tm + tn) * kStepK * 2; }
+constexpr size_t lds_bytes16(Tiles16 kind) {
+    return kind == Tiles16::kBig ? size_t{2} * (kBigM + kBigN) * kStepK * 2 : (kind == Tiles16::kDeep ? size_t{4} : size_t{2}) * (kSmallM + kSmallN) * kStepK * 2;
+}
 
-// Time of a product in one tile size, in microseconds: rounds of workgroups over the compute units, the last of them in shares where
-// that takes less.  The figures are those of long sums on a full chip.
-static Plan16 plan16_of(bool big, int M, int N, int K, int n_seg, size_t share_bytes) {
-    const double step = big ? 1.6 : 1.1, ends = big ? 5.0 : 3.0;    // of a step, and of a tile's beginning and end
-    const int slots = kNumCU * (big ? 1 : 2);                        // workgroups that run together
+// Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares where
+// that takes less.  The figures are those of long sums on a full chip; of the deep form, of few tiles.
+static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t share_bytes) {
+    const bool big = kind == Tiles16::kBig, deep = kind == Tiles16::kDeep;
+    const double step = big ? 1.6 : deep ? 0.6 : 1.1, ends = big ? 5.0 : deep ? 4.0 : 3.0;    // of a step, and of a tile's beginning and end
+    const int slots = kNumCU * (big || deep ? 1 : 2);                // workgroups that run together
     const int64_t tile_bytes = static_cast<int64_t>(big ? kBigM * kBigN : kSmallM * kSmallN) * 4;
     Plan16 pl{};
-    pl.big = big;
+    pl.tiles = kind;
     pl.steps = n_seg * ceil_div(K, kStepK);
     const int64_t tiles = static_cast<int64_t>(ceil_div(M, big ? kBigM : kSmallM)) * ceil_div(N, big ? kBigN : kSmallN);
     const double round = pl.steps * step + ends;
@@ -481,6 +509,7 @@ static Plan16 plan16_of(bool big, int M, int N, int K, int n_seg, size_t share_b
     pl.whole = static_cast<int>(rounds * slots), pl.rest = static_cast<int>(tiles - pl.whole);
     pl.shares = 1, pl.share_steps = pl.steps;
     pl.us = rounds * round;
+    if (deep && rounds > 0) pl.us = 1e30;
     if (pl.rest == 0) return pl;
     double best = round;
     for (int s = 2; s <= 64 && pl.rest * s <= slots && s * 4 <= pl.steps && static_cast<size_t>(pl.rest * s * tile_bytes) <= share_bytes; ++s) {
@@ -497,44 +526,49 @@ static Plan16 plan16_of(bool big, int M, int N, int K, int n_seg, size_t share_b
 }
 
 Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes) {
-    const Plan16 big = plan16_of(true, M, N, K, n_seg, share_bytes), small = plan16_of(false, M, N, K, n_seg, share_bytes);
-    return small.us < big.us ? small : big;
+    Plan16 best = plan16_of(Tiles16::kBig, M, N, K, n_seg, share_bytes);
+    for (const Tiles16 kind : {Tiles16::kSmall, Tiles16::kDeep}) {
+        const Plan16 pl = plan16_of(kind, M, N, K, n_seg, share_bytes);
+        if (pl.us < best.us) best = pl;
+    }
+    return best;
 }
 
-int stats_words16(const Plan16& pl) { return pl.big ? kBigN / kBigWN : kSmallN / kSmallWN; }
+int stats_words16(const Plan16& pl) { return pl.tiles == Tiles16::kBig ? kBigN / kBigWN : kSmallN / kSmallWN; }
 
 template <int EPI, bool ARC, bool BRC>
-static auto kernel16(bool big) {
-    return big ? product16_kernel<EPI, kBigM, kBigN, kBigWM, kBigWN, ARC, BRC>
-               : product16_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN, ARC, BRC>;
+static auto kernel16(Tiles16 kind) {
+    return kind == Tiles16::kBig    ? product16_kernel<EPI, kBigM, kBigN, kBigWM, kBigWN, ARC, BRC>
+           : kind == Tiles16::kDeep ? product16_deep_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN, ARC, BRC>
+                                    : product16_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN, ARC, BRC>;
 }
 
 int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st) {
-    const int tm = pl.big ? kBigM : kSmallM, tn = pl.big ? kBigN : kSmallN;
+    const bool big = pl.tiles == Tiles16::kBig;
+    const int tm = big ? kBigM : kSmallM, tn = big ? kBigN : kSmallN;
     g.tiles_m = ceil_div(g.M, tm), g.tiles_n = ceil_div(g.N, tn);
     if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
     g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
     g.whole_xcd = ceil_div(g.whole, kNumXCD), g.rest_xcd = ceil_div(g.rest * g.shares, kNumXCD);
-    const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.big)
-                        : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.big)
-                        : arc ? kernel16<kEpiStore, true, true>(pl.big)
-                              : kernel16<kEpiStore, false, true>(pl.big);
+    const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.tiles)
+                        : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.tiles)
+                        : arc ? kernel16<kEpiStore, true, true>(pl.tiles)
+                              : kernel16<kEpiStore, false, true>(pl.tiles);
     if (brc != (epi == kEpiStore)) return DAB_ERR_UNSUPPORTED;
-    const int threads = 64 * (pl.big ? kBigWM * kBigWN : kSmallWM * kSmallWN);
-    if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(tm, tn), st, g)) return rc;
+    const int threads = 64 * (big ? kBigWM * kBigWN : kSmallWM * kSmallWN);
+    if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(pl.tiles), st, g)) return rc;
     if (pl.shares == 1) return DAB_OK;
-    const int blocks = (pl.big ? kBigN * kBigM : kSmallN * kSmallM) / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
-    return launch(pl.big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
+    const int blocks = (big ? kBigN * kBigM : kSmallN * kSmallM) / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
+    return launch(big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
                   dim3(g.rest * blocks), dim3(threads), 0, st, g);
 }
 
 int init_product16() {
-    for (int big = 0; big < 2; ++big)
-        for (const auto k : {kernel16<kEpiStats, false, false>(big), kernel16<kEpiSoftmax, false, false>(big),
-                             kernel16<kEpiStore, true, true>(big), kernel16<kEpiStore, false, true>(big)}) {
-            const size_t lds = big ? lds_bytes16(kBigM, kBigN) : lds_bytes16(kSmallM, kSmallN);
+    for (const Tiles16 kind : {Tiles16::kSmall, Tiles16::kDeep, Tiles16::kBig})
+        for (const auto k : {kernel16<kEpiStats, false, false>(kind), kernel16<kEpiSoftmax, false, false>(kind),
+                             kernel16<kEpiStore, true, true>(kind), kernel16<kEpiStore, false, true>(kind)}) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                     static_cast<int>(lds));
+                                                     static_cast<int>(lds_bytes16(kind)));
             if (e != hipSuccess) return hip_failed(e);
         }
     return DAB_OK;

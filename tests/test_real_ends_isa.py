@@ -39,3 +39,19 @@ def test_nothing_else_uses_the_register_of_the_copies_address(product_kernels):
     for name, lines in product_kernels.items():
         users = [l for l in lines if re.search(r"\bm0\b", l.split(";")[0])]
         assert users and all(re.match(r"\s*s_mov_b32 m0, s\d+|\s*s_mov_b32 m0, ttmp", l) for l in users), (name, users[:3])
+
+
+def test_the_deep_form_leaves_two_steps_of_copies_on_their_way(tmp_path):
+    """Four steps in LDS: its barriers wait for all but the copies of two steps (eight each), the first one for all but those of three; and
+    no wait of the compiler's for all of them stands among the products."""
+    out = str(tmp_path / "product16.s")
+    ic.compile_to_isa("product16.hip", out)
+    found = [(n, l) for n, l in ic.kernels(open(out).read()) if "product16_deep_kernel" in n]
+    assert len(found) == 4
+    for name, lines in found:
+        assert ic.scalar_read_hazards(lines) == [], name
+        text = [l.strip() for l in lines]
+        waits = [text[i - 1] for i, l in enumerate(text) if l.startswith("s_barrier")]
+        assert waits == [f"s_waitcnt vmcnt({n}) lgkmcnt(0)" for n in (24, 16, 0)], (name, waits)
+        products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
+        assert [l for l in text[products[0]:products[-1]] if re.match(r"s_waitcnt.*vmcnt", l)] == ["s_waitcnt vmcnt(16) lgkmcnt(0)"], name
