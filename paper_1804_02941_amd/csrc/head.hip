@@ -1,9 +1,11 @@
 // Softmax cross entropy over a large vocabulary and its gradient, without the logits.
 //
 // loss: one product H W^T whose tiles leave only each token's maximum and sum of exponentials over a block of words, and the
-// target's logit; a second, small kernel joins the blocks.  gradient: a piece of the vocabulary at a time, the
-// product again, now written out as P = g (softmax - onehot) in bf16, and the two products dW = P^T H (the piece's
-// rows of dW, finished) and dH += P W (fp32 until the last piece).  8 T D V flops, two of them for taking the logits twice.
+// target's logit; a second, small kernel joins the blocks.  gradient: a piece of the vocabulary at a time, the product again, now
+// written out as P = g (softmax - onehot), and the two products dW = P^T H (the piece's rows of dW, finished) and dH += P W
+// (fp32 until the last piece).  8 T D V flops, two of them for taking the logits twice.  Bound by the matrix cores from a few hundred
+// tokens on (8192 x 2048 -> 131072 in 13.4 ms, 1310 TFLOP/s over all four products), by reading W three times and writing dW once below
+// (one token, 4096 -> 131072, 0.88 ms: 4.9 TB/s).  Small heads: small32.h.
 #include "product16.h"
 #include "small32.h"
 
@@ -69,6 +71,7 @@ __global__ __launch_bounds__(256) void head_unstack_kernel(const float* __restri
 
 struct HeadPlan {
     bool small;                      // small32.h
+    bool wide;                       // fp32 operands as they are
     int P;                           // planes
     int n_seg;
     int prob_planes;                 // planes of P
@@ -84,6 +87,24 @@ struct HeadPlan {
 static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
     return (dtype == DAB_BF16 || dtype == DAB_F32) && ldh < (1 << 22) && ldw < (1 << 22) && T < (1 << 30) && V < (1 << 30) &&
            ceil_div64(T, 128) * ceil_div64(V, 128) < INT32_MAX / 64 && ceil_div64(T, 128) * ceil_div64(D, 128) < INT32_MAX / 1024;
+}
+
+// Tokens up to which fp32 operands are multiplied as they are.  Loss and gradients, as they are and as planes (tokens x width x words): 64 x
+// 2048 x 64000 632 us and 1734, 64 x 512 x 8000 78 and 116, 256 x 1024 x 16000 281 and 283, 512 x 1024 x 16000 527 and 422,
+// 2048 x 1024 x 32000 3931 and 2495.
+constexpr int kWideTokens = 256;
+
+// Pieces of up to 256 MB of P (`bytes` an entry), which is about what the memory-side cache holds, of equal size; rows of P stay within
+// the offsets of the product's copies.
+static void head_pieces(HeadPlan& p, int32_t T, int32_t D, int32_t V, int bytes) {
+    int64_t words = (int64_t{256} << 20) / (static_cast<int64_t>(bytes) * T) / 1024 * 1024;
+    if (words < 1024) words = 1024;
+    if (words > (1 << 20)) words = 1 << 20;
+    if (words > V) words = V;
+    p.n_pieces = static_cast<int>(ceil_div64(V, words));
+    p.piece = static_cast<int>(round_up(ceil_div64(V, p.n_pieces), 256));
+    p.n_pieces = ceil_div(V, p.piece);
+    p.ldp = p.piece;
 }
 
 static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw, bool gradient) {
@@ -102,6 +123,29 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         } else {
             p.stats_at = room(ceil_div64(V, kSmallTile) * T * 8);
             p.target_at = room(static_cast<int64_t>(T) * 4);
+        }
+        p.bytes = at;
+        return p;
+    }
+    p.wide = dtype == DAB_F32 && T <= kWideTokens;
+    if (p.wide) {
+        p.P = p.n_seg = p.prob_planes = 1;
+        p.h_direct = !gradient && D % 4 == 0 && ldh % 4 == 0, p.w_direct = D % 4 == 0 && ldw % 4 == 0;
+        p.ldh = p.h_direct ? ldh : round_up(D, 4), p.ldw = p.w_direct ? ldw : round_up(D, 4);
+        p.h_at = p.h_direct ? 0 : room(T * p.ldh * 4);
+        p.w_at = p.w_direct ? 0 : room(V * p.ldw * 4);
+        if (!gradient) {
+            p.logits = plan32(T, V, D, 0);
+            p.stats_at = room((ceil_div64(V, stats_words16(p.logits)) + 8) * T * 8);
+            p.target_at = room(static_cast<int64_t>(T) * 4);
+        } else {
+            head_pieces(p, T, D, V, 4);
+            p.logits = plan32(T, p.piece, D, 0);
+            p.dh = plan32(T, D, p.piece, kAnyShares16), p.dw = plan32(p.piece, D, T, kAnyShares16);
+            p.p_at = room(static_cast<int64_t>(T) * p.ldp * 4);
+            p.acc_at = room(p.n_pieces > 1 ? static_cast<int64_t>(T) * D * 4 : 0);
+            p.part_bytes = p.dh.part_bytes > p.dw.part_bytes ? p.dh.part_bytes : p.dw.part_bytes;
+            p.part_at = room(static_cast<int64_t>(p.part_bytes));
         }
         p.bytes = at;
         return p;
@@ -126,16 +170,7 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         // products are bound by reading W and writing dW.
         p.stacked = p.P == 1 && T <= 128;
         p.prob_planes = p.stacked ? 2 : p.P;
-        // pieces of up to 256 MB of P, which is about what the memory-side cache holds, of equal size; rows of P stay within the
-        // offsets of the product's copies
-        int64_t words = (int64_t{256} << 20) / (int64_t{2} * p.prob_planes * T) / 1024 * 1024;
-        if (words < 1024) words = 1024;
-        if (words > (1 << 20)) words = 1 << 20;
-        if (words > V) words = V;
-        p.n_pieces = static_cast<int>(ceil_div64(V, words));
-        p.piece = static_cast<int>(round_up(ceil_div64(V, p.n_pieces), 256));
-        p.n_pieces = ceil_div(V, p.piece);
-        p.ldp = p.piece;
+        head_pieces(p, T, D, V, 2 * p.prob_planes);
         p.logits = plan16(T, p.piece, D, p.n_seg, 0);
         p.dh = plan16(p.stacked ? 2 * T : T, D, p.piece, p.n_seg, kAnyShares16);
         p.dw = plan16(p.piece, D, T, p.stacked ? 2 : p.n_seg, kAnyShares16);
@@ -177,8 +212,21 @@ static Small32 head_logits32(const void* H, int64_t ldh, const void* W, int64_t 
 // The operands as bf16 planes, in the workspace where they are not already.
 static int head_operands(const HeadPlan& p, const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype,
                          const int64_t* targets, int64_t ignore, int T, int D, int V, char* ws, hipStream_t st, Operand16* h, Operand16* w) {
-    *h = {static_cast<const bf16*>(H), p.ldh, static_cast<int64_t>(T) * p.ldh};
-    *w = {static_cast<const bf16*>(W), p.ldw, static_cast<int64_t>(V) * p.ldw};
+    *h = {H, p.ldh, static_cast<int64_t>(T) * p.ldh};
+    *w = {W, p.ldw, static_cast<int64_t>(V) * p.ldw};
+    if (p.wide) {
+        if (!p.h_direct) {
+            float* out = reinterpret_cast<float*>(ws + p.h_at);
+            if (int rc = launch_rows32(static_cast<const float*>(H), T, D, ldh, targets, ignore, V, out, p.ldh, st)) return rc;
+            h->p = out;
+        }
+        if (!p.w_direct) {
+            float* out = reinterpret_cast<float*>(ws + p.w_at);
+            if (int rc = launch_rows32(static_cast<const float*>(W), V, D, ldw, nullptr, 0, 0, out, p.ldw, st)) return rc;
+            w->p = out;
+        }
+        return DAB_OK;
+    }
     if (!p.h_direct) {
         bf16* out = reinterpret_cast<bf16*>(ws + p.h_at);
         if (int rc = launch_planes16(H, dtype, T, D, ldh, targets, ignore, V, out, p.ldh, st)) return rc;
@@ -263,21 +311,23 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
     }
     Operand16 h, w;
     if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &h, &w)) return rc;
-    bf16* P = reinterpret_cast<bf16*>(base + p.p_at);
+    void* P = base + p.p_at;
     float* acc = reinterpret_cast<float*>(base + p.acc_at);
     const Operand16 probs = {P, p.ldp, static_cast<int64_t>(T) * p.ldp};
     const int64_t size = dtype_bytes(dtype);
+    const int64_t w_size = p.wide ? 4 : 2;
+    auto plan = [&](int M, int N, int K, int n_seg, size_t room) { return p.wide ? plan32(M, N, K, room) : plan16(M, N, K, n_seg, room); };
     const size_t shares = p.part_bytes;                      // room for sums in shares, of the last and smaller piece too
     for (int i = 0; i < p.n_pieces; ++i) {
         const int v0 = i * p.piece, words = V - v0 < p.piece ? V - v0 : p.piece;
-        const Operand16 wp = {w.p + v0 * w.ld, w.ld, w.plane};
+        const Operand16 wp = {static_cast<const char*>(w.p) + v0 * w.ld * w_size, w.ld, w.plane};
         // P of this piece; its columns past the last word are zeros
         Product16 g{};
         head_segments(g, p.n_seg);
         g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D;
         g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
         g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.prob_planes;
-        if (int rc = launch16(kEpiSoftmax, false, false, g, plan16(T, words, D, p.n_seg, 0), st)) return rc;
+        if (int rc = launch16(kEpiSoftmax, false, false, g, plan(T, words, D, p.n_seg, 0), st)) return rc;
         // the piece's rows of dW
         Product16 q{};
         head_segments(q, p.n_seg);
@@ -285,7 +335,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         q.A = probs, q.B = h, q.M = words, q.N = D, q.K = T;
         q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
         q.part = reinterpret_cast<float*>(base + p.part_at);
-        if (int rc = launch16(kEpiStore, true, true, q, plan16(words, D, T, q.n_seg, shares), st)) return rc;
+        if (int rc = launch16(kEpiStore, true, true, q, plan(words, D, T, q.n_seg, shares), st)) return rc;
         // its share of dH
         const bool last = i + 1 == p.n_pieces && !p.stacked;
         Product16 s{};
@@ -294,7 +344,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         s.add = i ? acc : nullptr;
         s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16;
         s.part = q.part;
-        if (int rc = launch16(kEpiStore, false, true, s, plan16(s.M, D, words, p.n_seg, shares), st)) return rc;
+        if (int rc = launch16(kEpiStore, false, true, s, plan(s.M, D, words, p.n_seg, shares), st)) return rc;
     }
     if (!p.stacked) return DAB_OK;
     return launch(head_unstack_kernel, dim3(ceil_div(T * D, 256)), dim3(256), 0, st, acc, T * D, static_cast<bf16*>(dH));

@@ -1,13 +1,20 @@
-// Dense products of bf16 operands on the matrix cores, for the training side of the real-valued layers:
+// Dense products on the matrix cores, for the training side of the real-valued layers:
 //     C[m][n] = sum over pieces (a, b) and k of A_a[m][k] B_b[n][k],   fp32 accumulation.
 // Either operand may be held with k contiguous ([rows][k], rows = m or n) or with its rows contiguous ([k][rows]): the second form is
-// transposed on the way out of LDS (ds_read_b64_tr_b16), so that no operand is ever transposed in memory.  Operands of wider types are
-// several bf16 planes whose sum they are, and the product runs over a list of pairs of planes.
+// transposed on the way out of LDS (ds_read_b64_tr_b16), so that no operand is ever transposed in memory.  Operands are bf16, or fp32 in one
+// of two forms: several bf16 planes whose sum they are, the product running over a list of pairs of planes (six for all of 24 bits), or as
+// they are on the fp32 matrix instruction.  The first reaches 190 TFLOP/s of fp32 products, 1.4 times the second, but has the planes to write
+// and read: it is for many rows.
 //
-// A workgroup of WM x WN wavefronts owns a TM x TN tile of C.  A step is 64 k: both operands' tiles go from memory straight into LDS
-// (16 bytes a lane) while the step before is multiplied; two buffers, one barrier a step.  The product is taken with B as the
-// matrix core's left operand: register r of a lane is then column n = 4 (lane / 16) + r of row m = lane % 16, so that a lane stores four neighbouring columns, and
-// softmax sums over n stay in a lane but for two exchanges.
+// A workgroup of WM x WN wavefronts owns a TM x TN tile of C.  A step is 128 bytes of k: both operands' tiles go from memory straight into
+// LDS (16 bytes a lane) while the steps before are multiplied; two buffers, one barrier a step (four buffers for a few tiles, which would wait
+// for each step's copies).  The product is taken with B as the matrix core's left operand: register r of a lane is then column
+// n = 4 (lane / 16) + r of row m = lane % 16, so that softmax sums over n stay in a lane but for two exchanges.
+//
+// Bound by the matrix cores at the clock that their power leaves (1.7 - 2.0 GHz in long products): 256 x 256 tiles of eight wavefronts, 64 x 128
+// each, read 192 KB of LDS a step against 2048 clocks of products, 75 % of its bandwidth.  Measured: 16384 x 4096 -> 4096 from two
+// operands in the form [k][rows] 410 us, 1340 TFLOP/s; logits of 8192 x 2048 -> 131072 with their softmax statistics 3.3 ms, 1330; a step that
+// waited for its own LDS reads, its copies in a burst behind the barrier and addresses from vector registers had each cost 10 - 15 %.
 #pragma once
 
 #include "real16.h"
@@ -15,14 +22,14 @@
 namespace dab {
 
 struct Operand16 {
-    const bf16* p;
-    int64_t ld;                      // elements between rows ([rows][k]) or between k ([k][rows]); a multiple of 8
+    const void* p;                   // bf16, or fp32 where the plan says so
+    int64_t ld;                      // elements between rows ([rows][k]) or between k ([k][rows]), whole 16 bytes
     int64_t plane;                   // elements between the planes
 };
 
 enum { kEpiStats = 0, kEpiSoftmax = 1, kEpiStore = 2 };
 
-constexpr int kStepK = 64;
+constexpr int kStepK = 64;           // k of a step of bf16 operands
 
 struct Product16 {
     Operand16 A, B;
@@ -30,7 +37,7 @@ struct Product16 {
     int n_seg;                       // pairs of planes
     uint32_t seg_a, seg_b;           // plane of each pair, four bits a pair
     int tiles_m, tiles_n;
-    int steps;                       // steps of a sum: n_seg * ceil(K / 64)
+    int steps;                       // steps of a sum: n_seg * ceil(K / 64), fp32 ceil(K / 32)
     int whole, whole_xcd;            // tiles whose sum one workgroup takes, and how many of them an XCD does
     int rest, rest_xcd;              // the last tiles, in `shares` shares each, and shares an XCD takes
     int shares, share_steps;
@@ -44,17 +51,18 @@ struct Product16 {
     const int64_t* targets;
     int64_t ignore_index;
     int n0, V;
-    float2* stats;                   // [ceil(N / stats_n)][M] maximum and sum of exponentials
+    float2* stats;                   // [ceil(N / stats_words16())][M] maximum and sum of exponentials
     float* target_logit;             // [M]
     const float* lse;
     const float* g;
-    bf16* P;                         // [planes][M][ldp]
+    void* P;                         // bf16 [planes][M][ldp], or fp32 [M][ldp]
     int64_t ldp, p_plane;
     int p_planes;
 };
 
-// Tile of a product and how its sums are shared out (product16.hip).
-enum class Tiles16 { kSmall, kDeep, kBig };
+// Tile of a product and how its sums are shared out (product16.hip).  kSmall 128 x 128, two workgroups on a compute unit; kDeep the same, one, four
+// steps in LDS; kBig 256 x 256; of fp32 operands kF32 64 x 128, three workgroups, and kFew 32 x 128 for up to 32 rows.
+enum class Tiles16 { kSmall, kDeep, kBig, kF32, kFew };
 struct Plan16 {
     Tiles16 tiles;
     int steps, whole, rest, shares, share_steps;
@@ -64,9 +72,14 @@ struct Plan16 {
 constexpr size_t kAnyShares16 = ~size_t{0};
 // share_bytes: room for the sums of shares (0: the whole sum in one workgroup)
 Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes);
+// The same for fp32 operands.
+Plan16 plan32(int M, int N, int K, size_t share_bytes);
 int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st);
 int stats_words16(const Plan16& pl);           // words of the vocabulary per pair of the stats
 int init_product16();
+// fp32 rows ldp apart (a multiple of 4, zeros behind the last element), those of tokens without a loss cleared (targets may be NULL)
+int launch_rows32(const float* X, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V, float* out, int64_t ldp,
+                  hipStream_t st);
 // bf16 planes [P][rows][ldp] of X [rows][cols], zeros up to ldp; rows whose target has no loss are zeros (targets may be NULL)
 int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V,
                     bf16* out, int64_t ldp, hipStream_t st);

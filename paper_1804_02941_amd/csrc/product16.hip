@@ -1,4 +1,5 @@
-// Host side of the bf16 products (product16.h): tile and split of a product, launches, and the kernels around it.
+// The products of product16.h: kernels, their tiles and shares, launches, the operands they need laid out, and the weight gradient
+// from a saved input, which is one of them.
 #include "product16.h"
 
 #include <type_traits>
@@ -16,13 +17,15 @@ typedef __attribute__((address_space(3))) uint32_t lds_u32;
 // A byte offset past every tile: a load from there gives zeros.  What a tile's offsets reach stays below it (ld < 2^22).
 constexpr uint32_t kPast16 = 0x80000000u;
 
-// One operand's tile of ROWS x 64 k, from memory into LDS.
-template <int ROWS, bool RC, int NW>
+// One operand's tile of ROWS x 128 bytes of k (64 bf16 or 32 fp32), from memory into LDS.
+template <typename E, int ROWS, bool RC, int NW>
 struct Loader16 {
-    static constexpr int kBytes = ROWS * kStepK * 2;
+    static constexpr int kE = sizeof(E), kPer = 16 / kE, kStep = 128 / kE;
+    static constexpr int kBytes = ROWS * 128;
     static constexpr int kCopies = kBytes / 1024 / NW;       // of one wavefront, a kilobyte each
-    static constexpr int kChunks = RC ? ROWS / 8 : 8;        // 16-byte pieces of a row of the tile in LDS
+    static constexpr int kChunks = RC ? ROWS / kPer : 8;     // 16-byte pieces of a row of the tile in LDS
     static constexpr int kLdsRows = 64 / kChunks;            // rows of it that one copy fills
+    static_assert(RC || kCopies == 1 || kCopies % 2 == 0, "the permutation of a row's pieces repeats every second copy");
     uint32_t off[kCopies];                                   // bytes from the tile's origin, the same every step
     uint64_t past[2];                                        // lanes whose k are past K in the last step, even and odd copies
     __amdgpu_buffer_rsrc_t rsrc;
@@ -37,20 +40,21 @@ struct Loader16 {
             const int r = (w * kCopies + c) * kLdsRows + lane / kChunks, phys = lane % kChunks;
             int e;
             if constexpr (RC) {
-                e = (phys ^ (((r & 3) | ((r >> 3) & 1) << 2) << 1)) * 8;
-                off[c] = e < rows ? static_cast<uint32_t>((r * ld + e) * 2) : kPast16;
+                const int key = kE == 2 ? ((r & 3) | ((r >> 3) & 1) << 2) << 1 : ((r >> 2) & 3) << 2;
+                e = (phys ^ key) * kPer;
+                off[c] = e < rows ? static_cast<uint32_t>((r * ld + e) * kE) : kPast16;
             } else {
-                e = (phys ^ ((r >> 1) & 7)) * 8;
-                off[c] = r < rows ? static_cast<uint32_t>((r * ld + e) * 2) : kPast16;
-                if (c < 2) past[c] = __ballot(K % kStepK != 0 && e >= K % kStepK);
+                e = (phys ^ ((r >> 1) & 7)) * kPer;
+                off[c] = r < rows ? static_cast<uint32_t>((r * ld + e) * kE) : kPast16;
+                if (c < 2) past[c] = __ballot(K % kStep != 0 && e >= K % kStep);
             }
         }
     }
     // origin: the tile's first element of this step; left: bytes of the operand from there on ([k][rows]), or k (none: zeros).
     // Rows past K are past the end of the buffer in one form, offsets of their own in the other.
-    __device__ __forceinline__ void aim(const bf16* origin, int64_t left) {
+    __device__ __forceinline__ void aim(const E* origin, int64_t left) {
         const uint32_t bytes = left <= 0 ? 0u : RC && left < kPast16 ? static_cast<uint32_t>(left) : kPast16;
-        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(origin), 0, static_cast<int>(bytes), 0x00020000);
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(origin), 0, static_cast<int>(bytes), 0x00020000);
     }
     __device__ __forceinline__ void copy(int c, bool last_k, char* lds) const {
         uint32_t o = off[c];
@@ -64,38 +68,59 @@ struct Loader16 {
     }
 };
 
-// Fragments of 16 rows x 32 k: lane l holds row l % 16, k = 8 (l / 16) .. + 7.
-template <int ROWS, bool RC, int NFRAG>
+// Fragments of 16 rows, half a step of k: lane l holds row l % 16 and 16 bytes of k from piece l / 16 of the half on, eight bf16 or four fp32.
+template <typename E, int ROWS, bool RC, int NFRAG>
 struct Reader16 {
+    static constexpr bool kWide = sizeof(E) == 4;
+    using Frag = std::conditional_t<kWide, v4f, v8bf>;
+    static constexpr int kPitch = ROWS * static_cast<int>(sizeof(E));   // bytes of a k in the form [k][rows]
     uint32_t at[RC ? NFRAG : 2];
     // row0: this wavefront's first row in the tile
     __device__ __forceinline__ void init(int lane, int row0) {
+        const int s = lane & 15, g = lane >> 4;
         if constexpr (RC) {
-            // a group of 16 lanes reads 4 k x 16 rows, a lane 4 neighbouring rows of one k, and gets the four k of its row
-            const int s = lane & 15, g = lane >> 4, key = (s >> 2) | (g & 1) << 2;
 #pragma unroll
-            for (int j = 0; j < NFRAG; ++j)
-                at[j] = (g * 8 + (s >> 2)) * (ROWS * 2) + (((row0 >> 4) + j) ^ key) * 32 + (s & 3) * 8;
+            for (int j = 0; j < NFRAG; ++j) {
+                const int block = (row0 >> 4) + j;
+                if constexpr (kWide) {
+                    at[j] = g * 4 * kPitch + (block ^ g) * 64 + s * 4;
+                } else {
+                    // a group of 16 lanes reads 4 k x 16 rows, a lane 4 neighbouring rows of one k, and gets the four k of its row
+                    at[j] = (g * 8 + (s >> 2)) * kPitch + (block ^ ((s >> 2) | (g & 1) << 2)) * 32 + (s & 3) * 8;
+                }
+            }
         } else {
-            const int row = row0 + (lane & 15), key = (lane & 15) >> 1;
+            const int row = row0 + s, key = s >> 1;
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) at[kk] = row * 128 + (((kk * 4 + (lane >> 4)) ^ key) * 16);
+            for (int kk = 0; kk < 2; ++kk) at[kk] = row * 128 + (((kk * 4 + g) ^ key) * 16);
         }
     }
-    __device__ __forceinline__ v8bf read(const char* lds, int kk, int j) const {
-        if constexpr (RC) {
+    __device__ __forceinline__ Frag read(const char* lds, int kk, int j) const {
+        if constexpr (RC && kWide) {
+            v4f v;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = *reinterpret_cast<const float*>(lds + at[j] + (kk * 16 + c) * kPitch);
+            return v;
+        } else if constexpr (RC) {
             typedef short v4s __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) v4s lds_v4s;
             union { v4s h[2]; v8bf v; } u;
-            const char* p = lds + at[j] + kk * 32 * (ROWS * 2);
+            const char* p = lds + at[j] + kk * 32 * kPitch;
             u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
-            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * (ROWS * 2)));
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * kPitch));
             return u.v;
         } else {
-            return *reinterpret_cast<const v8bf*>(lds + at[kk] + j * 16 * 128);
+            return *reinterpret_cast<const Frag*>(lds + at[kk] + j * 16 * 128);
         }
     }
 };
+// One half step's product of two fragments (which k a lane holds does not matter as long as both operands agree).
+__device__ __forceinline__ v4f multiply16(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v4f multiply16(v4f a, v4f b, v4f c) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u], b[u], c, 0, 0, 0);
+    return c;
+}
 
 // Four neighbouring columns of the result.
 template <typename T>
@@ -163,11 +188,12 @@ struct Rows16 {
 };
 
 // NS: steps in LDS.
-template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS>
+template <typename E, int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS>
 __device__ __forceinline__ void product16(const Product16& g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
-    using LA = Loader16<TM, ARC, NW>;
-    using LB = Loader16<TN, BRC, NW>;
+    using LA = Loader16<E, TM, ARC, NW>;
+    using LB = Loader16<E, TN, BRC, NW>;
+    constexpr int kStep = LA::kStep, kE = sizeof(E);
     constexpr int kBuf = LA::kBytes + LB::kBytes;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -196,22 +222,22 @@ __device__ __forceinline__ void product16(const Product16& g) {
     LB lb;
     la.init(wave, lane, g.A.ld, g.M - m0, g.K);
     lb.init(wave, lane, g.B.ld, g.N - n0, g.K);
-    const bf16* a0 = g.A.p + (ARC ? m0 : m0 * g.A.ld);
-    const bf16* b0 = g.B.p + (BRC ? n0 : n0 * g.B.ld);
-    const int64_t ka = kStepK * (ARC ? g.A.ld : 1), kb = kStepK * (BRC ? g.B.ld : 1);   // a step further
+    const E* a0 = static_cast<const E*>(g.A.p) + (ARC ? m0 : m0 * g.A.ld);
+    const E* b0 = static_cast<const E*>(g.B.p) + (BRC ? n0 : n0 * g.B.ld);
+    const int64_t ka = kStep * (ARC ? g.A.ld : 1), kb = kStep * (BRC ? g.B.ld : 1);   // a step further
 
     const int per_seg = __builtin_amdgcn_readfirstlane(g.steps / g.n_seg);
     // the step that is fetched next: how many are left, its pair of planes, its operands and k left there
-    int to_fetch = last - first, seg = __builtin_amdgcn_readfirstlane(first / per_seg), k_left = g.K - (first - seg * per_seg) * kStepK;
-    const bf16* pa = a0 + ((g.seg_a >> (4 * seg)) & 15) * g.A.plane + (first - seg * per_seg) * ka;
-    const bf16* pb = b0 + ((g.seg_b >> (4 * seg)) & 15) * g.B.plane + (first - seg * per_seg) * kb;
+    int to_fetch = last - first, seg = __builtin_amdgcn_readfirstlane(first / per_seg), k_left = g.K - (first - seg * per_seg) * kStep;
+    const E* pa = a0 + ((g.seg_a >> (4 * seg)) & 15) * g.A.plane + (first - seg * per_seg) * ka;
+    const E* pb = b0 + ((g.seg_b >> (4 * seg)) & 15) * g.B.plane + (first - seg * per_seg) * kb;
     bool last_k = false;
     auto aim = [&] {
         const int left = to_fetch > 0 ? k_left : 0;
-        la.aim(pa, ARC ? left * g.A.ld * 2 : left);
-        lb.aim(pb, BRC ? left * g.B.ld * 2 : left);
-        last_k = k_left < kStepK;
-        --to_fetch, k_left -= kStepK, pa += ka, pb += kb;
+        la.aim(pa, ARC ? left * g.A.ld * kE : left);
+        lb.aim(pb, BRC ? left * g.B.ld * kE : left);
+        last_k = k_left < kStep;
+        --to_fetch, k_left -= kStep, pa += ka, pb += kb;
         if (k_left <= 0 && to_fetch > 0) {
             ++seg, k_left = g.K;
             pa = a0 + ((g.seg_a >> (4 * seg)) & 15) * g.A.plane;
@@ -225,8 +251,8 @@ __device__ __forceinline__ void product16(const Product16& g) {
         for (int c = 0; c < LB::kCopies; ++c) lb.copy(c, last_k, buf + LA::kBytes);
     };
 
-    Reader16<TM, ARC, FM> ra;
-    Reader16<TN, BRC, FN> rb;
+    Reader16<E, TM, ARC, FM> ra;
+    Reader16<E, TN, BRC, FN> rb;
     ra.init(lane, wm * FM * 16);
     rb.init(lane, wn * FN * 16);
 
@@ -235,7 +261,7 @@ __device__ __forceinline__ void product16(const Product16& g) {
     for (int i = 0; i < FN; ++i)
 #pragma unroll
         for (int j = 0; j < FM; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    v8bf a[2][FM], b[2][FN];
+    typename decltype(ra)::Frag a[2][FM], b[2][FN];
     // Half a step: its products, and among them the reads of the next half's fragments (early, so that they have arrived by its
     // end) and, COPY, the copies of a later step, one at a time: a burst of either would hold up the products behind it.
     auto half = [&](auto copy_c, int set, const char* buf, int kk, char* to) {
@@ -256,14 +282,14 @@ __device__ __forceinline__ void product16(const Product16& g) {
                 for (int u = 2 * i; u < 2 * i + 2; ++u) b[set ^ 1][u] = rb.read(buf + LA::kBytes, kk, u);
             }
 #pragma unroll
-            for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[set][i], a[set][j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < FM; ++j) acc[i][j] = multiply16(b[set][i], a[set][j], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     using yes = std::integral_constant<bool, true>;
     using no = std::integral_constant<bool, false>;
 
-    // NS buffers of 64 k.  While a half step is multiplied from registers, the next one's fragments are read; behind the one barrier of a
+    // NS buffers of a step.  While a half step is multiplied from registers, the next one's fragments are read; behind the one barrier of a
     // step, in its middle, the next step has landed (those after it may be on their way) and its own buffer has been read by all, so step NS further on
     // is fetched into it.
     constexpr int kInFlight = LA::kCopies + LB::kCopies;     // copies of a wavefront for a step
@@ -363,7 +389,7 @@ __device__ __forceinline__ void product16(const Product16& g) {
             for (int i = 0; i < FN; ++i) {
                 v4f p;
                 // rounded to bf16 below, the exponent may be formed with one rounding more; as planes it may not
-                if (g.p_planes == 1) {
+                if (kE == 2 && g.p_planes == 1) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, base2));
                 } else {
@@ -381,6 +407,13 @@ __device__ __forceinline__ void product16(const Product16& g) {
                 }
                 acc[i][j] = p;
             }
+            if constexpr (kE == 4) {
+                const Rows16<float, FN> out{mine, lane};
+#pragma unroll
+                for (int i = 0; i < FN; ++i) out.put(i, acc[i][j]);
+                out.flush(static_cast<float*>(g.P) + mj * g.ldp + nb, g.ldp, g.M - mj, FN * 16);
+                continue;
+            }
             const Rows16<bf16, FN> out{mine, lane};
             for (int q = 0; q < g.p_planes; ++q) {
 #pragma unroll
@@ -390,7 +423,7 @@ __device__ __forceinline__ void product16(const Product16& g) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) acc[i][j][r] -= static_cast<float>(static_cast<bf16>(acc[i][j][r]));
                 }
-                out.flush(g.P + q * g.p_plane + mj * g.ldp + nb, g.ldp, g.M - mj, FN * 16);
+                out.flush(static_cast<bf16*>(g.P) + q * g.p_plane + mj * g.ldp + nb, g.ldp, g.M - mj, FN * 16);
             }
         } else if (share >= 0) {
 #pragma unroll
@@ -418,13 +451,18 @@ __device__ __forceinline__ void product16(const Product16& g) {
 
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
-    product16<EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
+    product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
 }
 // For no more tiles than compute units: with one workgroup on each, a step of the small tile takes as long as its copies, so four
 // steps are on their way instead of two.
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_deep_kernel(Product16 g) {
-    product16<EPI, TM, TN, WM, WN, ARC, BRC, 4>(g);
+    product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 4>(g);
+}
+// fp32 operands as they are, on the matrix cores' fp32 form.
+template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product32_kernel(Product16 g) {
+    product16<float, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
 }
 
 // The shares of a tile's sums, added in a fixed order.  A workgroup takes one 16 x 16 block of every wavefront; eight shares
@@ -482,28 +520,65 @@ int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld
     const dim3 grid(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), block(256);
     const int l = static_cast<int>(ldp);
     if (dtype == DAB_F32) return launch(planes16_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
-    if (dtype == DAB_F16) return launch(planes16_kernel<f16, 2>, grid, block, 0, st, static_cast<const f16*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
     return launch(planes16_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
+}
+
+// fp32 rows [rows][cols] as they are, ldp apart (a multiple of 4, zeros behind the last element); those of tokens without a loss cleared
+// (targets may be NULL).
+__global__ __launch_bounds__(256) void rows32_kernel(const float* __restrict__ X, int cols, int64_t ld, const int64_t* __restrict__ targets,
+                                                     int64_t ignore, int V, float* __restrict__ out, int ldp, int64_t chunks) {
+    const int per_row = ldp >> 2;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < chunks; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = i / per_row;
+        const int c = static_cast<int>(i - row * per_row) * 4;
+        const float* from = X + row * ld + c;
+        v4f v = v4f{0.f, 0.f, 0.f, 0.f};
+        if (!targets || !no_loss(targets[row], ignore, V)) {
+            if (c + 4 <= cols) {
+                v = *reinterpret_cast<const Unaligned<float, 4>::type*>(from);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (c + u < cols) v[u] = from[u];
+            }
+        }
+        *reinterpret_cast<v4f*>(out + row * ldp + c) = v;
+    }
+}
+int launch_rows32(const float* X, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V, float* out, int64_t ldp,
+                  hipStream_t st) {
+    const int64_t chunks = rows * (ldp >> 2), blocks = ceil_div64(chunks, 256);
+    return launch(rows32_kernel, dim3(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, X, cols, ld, targets, ignore, V,
+                  out, static_cast<int>(ldp), chunks);
 }
 
 // ---------------------------------------------------------------- plan and launch
 constexpr int kBigM = 256, kBigN = 256, kBigWM = 4, kBigWN = 2;
 constexpr int kSmallM = 128, kSmallN = 128, kSmallWM = 2, kSmallWN = 2;
-constexpr size_t lds_bytes16(Tiles16 kind) {
-    return kind == Tiles16::kBig ? size_t{2} * (kBigM + kBigN) * kStepK * 2 : (kind == Tiles16::kDeep ? size_t{4} : size_t{2}) * (kSmallM + kSmallN) * kStepK * 2;
+constexpr int kF32M = 64, kF32N = 128, kF32WM = 2, kF32WN = 2;
+constexpr int kFewM = 32, kFewN = 128, kFewWM = 1, kFewWN = 4;   // of up to 32 rows (one token, 64000 x 2048: with 64 rows 142 us, the matrix cores')
+constexpr bool wide16(Tiles16 kind) { return kind == Tiles16::kF32 || kind == Tiles16::kFew; }
+constexpr int tile_m16(Tiles16 kind) {
+    return kind == Tiles16::kBig ? kBigM : kind == Tiles16::kF32 ? kF32M : kind == Tiles16::kFew ? kFewM : kSmallM;
 }
+constexpr int tile_n16(Tiles16 kind) {
+    return kind == Tiles16::kBig ? kBigN : kind == Tiles16::kF32 ? kF32N : kind == Tiles16::kFew ? kFewN : kSmallN;
+}
+constexpr size_t lds_bytes16(Tiles16 kind) { return (kind == Tiles16::kDeep ? size_t{4} : size_t{2}) * (tile_m16(kind) + tile_n16(kind)) * 128; }
 
 // Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares where
 // that takes less.  The figures are those of long sums on a full chip; of the deep form, of few tiles.
 static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t share_bytes) {
-    const bool big = kind == Tiles16::kBig, deep = kind == Tiles16::kDeep;
-    const double step = big ? 1.6 : deep ? 0.6 : 1.1, ends = big ? 5.0 : deep ? 4.0 : 3.0;    // of a step, and of a tile's beginning and end
-    const int slots = kNumCU * (big || deep ? 1 : 2);                // workgroups that run together
-    const int64_t tile_bytes = static_cast<int64_t>(big ? kBigM * kBigN : kSmallM * kSmallN) * 4;
+    const bool deep = kind == Tiles16::kDeep;
+    // of a step, and of a tile's beginning and end; workgroups that a compute unit runs together
+    const double step = kind == Tiles16::kBig ? 1.6 : deep ? 0.6 : kind == Tiles16::kF32 ? 3.0 : kind == Tiles16::kFew ? 1.8 : 1.1;
+    const double ends = kind == Tiles16::kBig ? 5.0 : deep || wide16(kind) ? 4.0 : 3.0;
+    const int slots = kNumCU * (kind == Tiles16::kBig || deep ? 1 : wide16(kind) ? 3 : 2);
+    const int64_t tile_bytes = static_cast<int64_t>(tile_m16(kind)) * tile_n16(kind) * 4;
     Plan16 pl{};
     pl.tiles = kind;
-    pl.steps = n_seg * ceil_div(K, kStepK);
-    const int64_t tiles = static_cast<int64_t>(ceil_div(M, big ? kBigM : kSmallM)) * ceil_div(N, big ? kBigN : kSmallN);
+    pl.steps = n_seg * ceil_div(K, wide16(kind) ? kStepK / 2 : kStepK);
+    const int64_t tiles = static_cast<int64_t>(ceil_div(M, tile_m16(kind))) * ceil_div(N, tile_n16(kind));
     const double round = pl.steps * step + ends;
     const int64_t rounds = tiles / slots;
     pl.whole = static_cast<int>(rounds * slots), pl.rest = static_cast<int>(tiles - pl.whole);
@@ -534,18 +609,24 @@ Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes) {
     return best;
 }
 
-int stats_words16(const Plan16& pl) { return pl.tiles == Tiles16::kBig ? kBigN / kBigWN : kSmallN / kSmallWN; }
+Plan16 plan32(int M, int N, int K, size_t share_bytes) { return plan16_of(M <= kFewM ? Tiles16::kFew : Tiles16::kF32, M, N, K, 1, share_bytes); }
+
+int stats_words16(const Plan16& pl) {
+    return pl.tiles == Tiles16::kF32 ? kF32N / kF32WN : pl.tiles == Tiles16::kFew ? kFewN / kFewWN : pl.tiles == Tiles16::kBig ? kBigN / kBigWN : kSmallN / kSmallWN;
+}
 
 template <int EPI, bool ARC, bool BRC>
 static auto kernel16(Tiles16 kind) {
-    return kind == Tiles16::kBig    ? product16_kernel<EPI, kBigM, kBigN, kBigWM, kBigWN, ARC, BRC>
+    return kind == Tiles16::kF32    ? product32_kernel<EPI, kF32M, kF32N, kF32WM, kF32WN, ARC, BRC>
+           : kind == Tiles16::kFew  ? product32_kernel<EPI, kFewM, kFewN, kFewWM, kFewWN, ARC, BRC>
+           : kind == Tiles16::kBig  ? product16_kernel<EPI, kBigM, kBigN, kBigWM, kBigWN, ARC, BRC>
            : kind == Tiles16::kDeep ? product16_deep_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN, ARC, BRC>
                                     : product16_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN, ARC, BRC>;
 }
 
 int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st) {
     const bool big = pl.tiles == Tiles16::kBig;
-    const int tm = big ? kBigM : kSmallM, tn = big ? kBigN : kSmallN;
+    const int tm = tile_m16(pl.tiles), tn = tile_n16(pl.tiles);
     g.tiles_m = ceil_div(g.M, tm), g.tiles_n = ceil_div(g.N, tn);
     if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
     g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
@@ -558,13 +639,13 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
     const int threads = 64 * (big ? kBigWM * kBigWN : kSmallWM * kSmallWN);
     if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(pl.tiles), st, g)) return rc;
     if (pl.shares == 1) return DAB_OK;
-    const int blocks = (big ? kBigN * kBigM : kSmallN * kSmallM) / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
-    return launch(big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
+    const int blocks = tm * tn / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
+    return launch(pl.tiles == Tiles16::kF32 ? join16_kernel<kF32M, kF32N, kF32WM, kF32WN> : pl.tiles == Tiles16::kFew ? join16_kernel<kFewM, kFewN, kFewWM, kFewWN> : big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
                   dim3(g.rest * blocks), dim3(threads), 0, st, g);
 }
 
 int init_product16() {
-    for (const Tiles16 kind : {Tiles16::kSmall, Tiles16::kDeep, Tiles16::kBig})
+    for (const Tiles16 kind : {Tiles16::kSmall, Tiles16::kDeep, Tiles16::kBig, Tiles16::kF32, Tiles16::kFew})
         for (const auto k : {kernel16<kEpiStats, false, false>(kind), kernel16<kEpiSoftmax, false, false>(kind),
                              kernel16<kEpiStore, true, true>(kind), kernel16<kEpiStore, false, true>(kind)}) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize,

@@ -297,14 +297,15 @@ static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const u
     const dim3 grid(ceil_div(g.Ft, g.groups * TB), ceil_div(g.B, g.nb));
     return launch(w4_matvec_kernel<NCT, TB, ROWS>, grid, dim3(64 * waves), static_cast<size_t>(waves) * TB * NCT * 1024, st, X, Q, S, g, Y);
 }
-template <int TB>
-static int launch_matvec(const W4Geom& g, bool rows, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
-    if (rows) return launch_matvec<1, TB, true>(g, st, X, Q, S, Y);
-    switch (ceil_div(g.nb * g.P, 16)) {
-        case 1: return launch_matvec<1, TB, false>(g, st, X, Q, S, Y);
-        case 2: return launch_matvec<2, TB, false>(g, st, X, Q, S, Y);
-        default: return launch_matvec<3, TB == 4 ? 2 : TB, false>(g, st, X, Q, S, Y);
-    }
+static int launch_matvec(const W4Geom& g, int columns, int TB, bool rows, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S,
+                         void* Y) {
+    if (rows) return TB == 2 ? launch_matvec<1, 2, true>(g, st, X, Q, S, Y) : launch_matvec<1, 1, true>(g, st, X, Q, S, Y);
+    if (columns == 1) return TB == 2 ? launch_matvec<1, 2, false>(g, st, X, Q, S, Y) : launch_matvec<1, 1, false>(g, st, X, Q, S, Y);
+    if (columns == 2)
+        return TB == 4   ? launch_matvec<2, 4, false>(g, st, X, Q, S, Y)
+               : TB == 2 ? launch_matvec<2, 2, false>(g, st, X, Q, S, Y)
+                         : launch_matvec<2, 1, false>(g, st, X, Q, S, Y);
+    return TB == 2 ? launch_matvec<3, 2, false>(g, st, X, Q, S, Y) : launch_matvec<3, 1, false>(g, st, X, Q, S, Y);
 }
 
 }  // namespace dab
@@ -385,5 +386,5 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
         if (rc) return rc;
         x = out;
     }
-    return TB == 4 ? launch_matvec<4>(g, !need, st, x, Q, S, Y) : TB == 2 ? launch_matvec<2>(g, !need, st, x, Q, S, Y) : launch_matvec<1>(g, !need, st, x, Q, S, Y);
+    return launch_matvec(g, columns, TB, !need, st, x, Q, S, Y);
 }
