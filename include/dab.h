@@ -496,8 +496,8 @@ int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t lddy, const
  *     lse_t = log sum_v exp(L_tv),   loss_t = lse_t - L_t,target(t).
  * The products run on the matrix cores a block of the vocabulary at a time; of a block only its rows'
  * maxima and sums and the targets' logits leave the compute unit.  Sums and logits are fp32.  fp32
- * inputs are multiplied as sums of three bf16 numbers (six products of pieces, what is left out is
- * below 2^-24 of a term).
+ * inputs are multiplied as they are where tokens are few, else as sums of three bf16 numbers (six
+ * products of pieces, what is left out is below 2^-24 of a term).
  *
  *   H        [T][D] of dtype (DAB_BF16 or DAB_F32; DAB_F16 -> DAB_ERR_UNSUPPORTED: softmax gradients leave its
  *            range), rows ldh apart
@@ -516,9 +516,10 @@ int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_
 /*
  * dab_head_loss_gradient - its gradient.  With g_t the gradient with respect to loss_t,
  *     P_tv = g_t (exp(L_tv - lse_t) - [v = target(t)]),   dH = P W,   dW = P^T H,
- * the logits recomputed a piece of the vocabulary at a time.  P is rounded to bf16 where H and W are bf16 (as those
- * are: the products stay on the matrix cores, and dH and dW are rounded to bf16 themselves); for fp32 it is
- * held as three bf16 numbers like them.  Sums are fp32; no atomics: the same inputs give the same bits.
+ * the logits recomputed a piece of the vocabulary at a time.  Where H and W are bf16 P is rounded to bf16 (as those
+ * are: the products stay on the matrix cores, and dH and dW are rounded to bf16 themselves, so that their error is
+ * about 1.4 times that of the rounding alone), of up to 128 tokens to 16 bits and of small heads not at all; for fp32 it is held
+ * as the operands are.  Sums are fp32; no atomics: the same inputs give the same bits.
  *
  *   lse      [T] fp32 of dab_head_loss for the same H, W, targets
  *   g        [T] fp32, or NULL for 1

@@ -89,10 +89,21 @@ static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t l
            ceil_div64(T, 128) * ceil_div64(V, 128) < INT32_MAX / 64 && ceil_div64(T, 128) * ceil_div64(D, 128) < INT32_MAX / 1024;
 }
 
-// Tokens up to which fp32 operands are multiplied as they are.  Loss and gradients, as they are and as planes (tokens x width x words): 64 x
-// 2048 x 64000 632 us and 1734, 64 x 512 x 8000 78 and 116, 256 x 1024 x 16000 281 and 283, 512 x 1024 x 16000 527 and 422,
-// 2048 x 1024 x 32000 3931 and 2495.
-constexpr int kWideTokens = 256;
+// How the products of a head are done.  Measured, loss and gradients (tokens x width x words), small kernels, fp32 operands as they are, planes:
+// fp32 256 x 512 x 250 27 us, 65, 95; 299 x 1504 x 628 75, 150, 194; 64 x 2048 x 64000 -, 632, 1734; 256 x 1024 x 16000 -, 281, 283;
+// 1024 x 1024 x 16000 -, 1017, 664; 2048 x 1024 x 32000 -, 3931, 2495.  bf16 256 x 512 x 250 29 small and 42 on tiles, 256 x 512 x 1000
+// 47 and 44, 64 x 512 x 4000 116 and 47.
+enum class Route { kSmall, kWide, kPlanes };
+static Route head_route(int32_t dtype, int64_t T, int64_t D, int64_t V) {
+    const int t = static_cast<int>(T), d = static_cast<int>(D), v = static_cast<int>(V);
+    if (dtype == DAB_BF16) return T <= 1024 && D <= 1024 && V <= 1024 && T * D * V <= (1 << 26) ? Route::kSmall : Route::kPlanes;
+    const double small = small32_us(T, D, V);
+    const double wide = 15.0 + 2 * plan32(t, v, d, 0).us + plan32(v, d, t, kAnyShares16).us + plan32(t, d, v, kAnyShares16).us;
+    // (both calls write and read the planes of H and W)
+    const double planes = 20.0 + 2 * plan16(t, v, d, 6, 0).us + plan16(v, d, t, 6, kAnyShares16).us + plan16(t, d, v, 6, kAnyShares16).us +
+                          2.0 * static_cast<double>((T + V) * D) * 10 / 4e6;
+    return small <= wide && small <= planes ? Route::kSmall : wide <= planes ? Route::kWide : Route::kPlanes;
+}
 
 // Pieces of up to 256 MB of P (`bytes` an entry), which is about what the memory-side cache holds, of equal size; rows of P stay within
 // the offsets of the product's copies.
@@ -115,7 +126,8 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         at += static_cast<size_t>(round_up(bytes, 256));
         return here;
     };
-    p.small = small32(dtype, T, D, V);
+    const Route route = head_route(dtype, T, D, V);
+    p.small = route == Route::kSmall;
     if (p.small) {
         if (gradient) {
             p.ldp = round_up(V, 4);
@@ -127,7 +139,7 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         p.bytes = at;
         return p;
     }
-    p.wide = dtype == DAB_F32 && T <= kWideTokens;
+    p.wide = route == Route::kWide;
     if (p.wide) {
         p.P = p.n_seg = p.prob_planes = 1;
         p.h_direct = !gradient && D % 4 == 0 && ldh % 4 == 0, p.w_direct = D % 4 == 0 && ldw % 4 == 0;

@@ -61,7 +61,7 @@ struct Product16 {
 };
 
 // Tile of a product and how its sums are shared out (product16.hip).  kSmall 128 x 128, two workgroups on a compute unit; kDeep the same, one, four
-// steps in LDS; kBig 256 x 256; of fp32 operands kF32 64 x 128, three workgroups, and kFew 32 x 128 for up to 32 rows.
+// steps in LDS; kBig 256 x 256; of fp32 operands kF32 64 x 128, three workgroups, and kFew 32 x 128 for up to 32 rows and for few tiles.
 enum class Tiles16 { kSmall, kDeep, kBig, kF32, kFew };
 struct Plan16 {
     Tiles16 tiles;

@@ -25,6 +25,7 @@ struct Loader16 {
     static constexpr int kCopies = kBytes / 1024 / NW;       // of one wavefront, a kilobyte each
     static constexpr int kChunks = RC ? ROWS / kPer : 8;     // 16-byte pieces of a row of the tile in LDS
     static constexpr int kLdsRows = 64 / kChunks;            // rows of it that one copy fills
+    static_assert((ROWS & (ROWS - 1)) == 0 && (kE == 4 || ROWS >= 128), "the permutation stays within a row's pieces");
     static_assert(RC || kCopies == 1 || kCopies % 2 == 0, "the permutation of a row's pieces repeats every second copy");
     uint32_t off[kCopies];                                   // bytes from the tile's origin, the same every step
     uint64_t past[2];                                        // lanes whose k are past K in the last step, even and odd copies
@@ -40,7 +41,7 @@ struct Loader16 {
             const int r = (w * kCopies + c) * kLdsRows + lane / kChunks, phys = lane % kChunks;
             int e;
             if constexpr (RC) {
-                const int key = kE == 2 ? ((r & 3) | ((r >> 3) & 1) << 2) << 1 : ((r >> 2) & 3) << 2;
+                const int key = (kE == 2 ? ((r & 3) | ((r >> 3) & 1) << 2) << 1 : ((r >> 2) & 3) << 2) & (kChunks - 1);
                 e = (phys ^ key) * kPer;
                 off[c] = e < rows ? static_cast<uint32_t>((r * ld + e) * kE) : kPast16;
             } else {
@@ -83,7 +84,7 @@ struct Reader16 {
             for (int j = 0; j < NFRAG; ++j) {
                 const int block = (row0 >> 4) + j;
                 if constexpr (kWide) {
-                    at[j] = g * 4 * kPitch + (block ^ g) * 64 + s * 4;
+                    at[j] = g * 4 * kPitch + (block ^ (g & (ROWS / 16 - 1))) * 64 + s * 4;
                 } else {
                     // a group of 16 lanes reads 4 k x 16 rows, a lane 4 neighbouring rows of one k, and gets the four k of its row
                     at[j] = (g * 8 + (s >> 2)) * kPitch + (block ^ ((s >> 2) | (g & 1) << 2)) * 32 + (s & 3) * 8;
@@ -556,7 +557,7 @@ int launch_rows32(const float* X, int rows, int cols, int64_t ld, const int64_t*
 constexpr int kBigM = 256, kBigN = 256, kBigWM = 4, kBigWN = 2;
 constexpr int kSmallM = 128, kSmallN = 128, kSmallWM = 2, kSmallWN = 2;
 constexpr int kF32M = 64, kF32N = 128, kF32WM = 2, kF32WN = 2;
-constexpr int kFewM = 32, kFewN = 128, kFewWM = 1, kFewWN = 4;   // of up to 32 rows (one token, 64000 x 2048: with 64 rows 142 us, the matrix cores')
+constexpr int kFewM = 32, kFewN = 128, kFewWM = 1, kFewWN = 4;   // of up to 32 rows, and of few tiles (one token's logits, 64000 x 2048: with 64 rows 142 us, which is the matrix cores', with these 88)
 constexpr bool wide16(Tiles16 kind) { return kind == Tiles16::kF32 || kind == Tiles16::kFew; }
 constexpr int tile_m16(Tiles16 kind) {
     return kind == Tiles16::kBig ? kBigM : kind == Tiles16::kF32 ? kF32M : kind == Tiles16::kFew ? kFewM : kSmallM;
@@ -567,31 +568,42 @@ constexpr int tile_n16(Tiles16 kind) {
 constexpr size_t lds_bytes16(Tiles16 kind) { return (kind == Tiles16::kDeep ? size_t{4} : size_t{2}) * (tile_m16(kind) + tile_n16(kind)) * 128; }
 
 // Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares where
-// that takes less.  The figures are those of long sums on a full chip; of the deep form, of few tiles.
+// that takes less.
 static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t share_bytes) {
-    const bool deep = kind == Tiles16::kDeep;
-    // of a step, and of a tile's beginning and end; workgroups that a compute unit runs together
-    const double step = kind == Tiles16::kBig ? 1.6 : deep ? 0.6 : kind == Tiles16::kF32 ? 3.0 : kind == Tiles16::kFew ? 1.8 : 1.1;
-    const double ends = kind == Tiles16::kBig ? 5.0 : deep || wide16(kind) ? 4.0 : 3.0;
-    const int slots = kNumCU * (kind == Tiles16::kBig || deep ? 1 : wide16(kind) ? 3 : 2);
+    // Workgroups that a compute unit runs together; a step's time with all of them there, that of one alone (fp32 products are bound by the
+    // matrix cores, which the workgroups share), and that of a tile's beginning and end: those of long sums on a full chip, of
+    // the deep form of few tiles.
+    struct Cost {
+        int together;
+        double step, alone, ends;
+    };
+    const Cost cost = kind == Tiles16::kBig    ? Cost{1, 1.6, 1.6, 5.0}
+                      : kind == Tiles16::kDeep ? Cost{1, 0.6, 0.6, 4.0}
+                      : kind == Tiles16::kF32  ? Cost{3, 3.0, 1.1, 4.0}
+                      : kind == Tiles16::kFew  ? Cost{3, 1.6, 0.7, 4.0}
+                                               : Cost{2, 1.1, 1.1, 3.0};
+    const int slots = kNumCU * cost.together;
     const int64_t tile_bytes = static_cast<int64_t>(tile_m16(kind)) * tile_n16(kind) * 4;
     Plan16 pl{};
     pl.tiles = kind;
     pl.steps = n_seg * ceil_div(K, wide16(kind) ? kStepK / 2 : kStepK);
     const int64_t tiles = static_cast<int64_t>(ceil_div(M, tile_m16(kind))) * ceil_div(N, tile_n16(kind));
-    const double round = pl.steps * step + ends;
+    auto round = [&](int64_t units, int steps) {
+        const int on_one = ceil_div(static_cast<int>(units), kNumCU);
+        return steps * (on_one >= cost.together ? cost.step : cost.alone + (cost.step - cost.alone) * (on_one - 1) / cost.together) + cost.ends;
+    };
     const int64_t rounds = tiles / slots;
     pl.whole = static_cast<int>(rounds * slots), pl.rest = static_cast<int>(tiles - pl.whole);
     pl.shares = 1, pl.share_steps = pl.steps;
-    pl.us = rounds * round;
-    if (deep && rounds > 0) pl.us = 1e30;
+    pl.us = rounds * round(slots, pl.steps);
+    if (kind == Tiles16::kDeep && rounds > 0) pl.us = 1e30;
     if (pl.rest == 0) return pl;
-    double best = round;
+    double best = round(pl.rest, pl.steps);
     for (int s = 2; s <= 64 && pl.rest * s <= slots && s * 4 <= pl.steps && static_cast<size_t>(pl.rest * s * tile_bytes) <= share_bytes; ++s) {
         const int per = ceil_div(pl.steps, s), n = ceil_div(pl.steps, per);
         if (n != s) continue;
         // the join: a launch, and the sums written and read once
-        const double us = per * step + ends + 4.0 + 2.0 * pl.rest * s * tile_bytes / 4e6;
+        const double us = round(pl.rest * s, per) + 4.0 + 2.0 * pl.rest * s * tile_bytes / 4e6;
         if (us < best) best = us, pl.shares = s, pl.share_steps = per;
     }
     pl.us += best;
@@ -609,7 +621,10 @@ Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes) {
     return best;
 }
 
-Plan16 plan32(int M, int N, int K, size_t share_bytes) { return plan16_of(M <= kFewM ? Tiles16::kFew : Tiles16::kF32, M, N, K, 1, share_bytes); }
+Plan16 plan32(int M, int N, int K, size_t share_bytes) {
+    const Plan16 few = plan16_of(Tiles16::kFew, M, N, K, 1, share_bytes), all = plan16_of(Tiles16::kF32, M, N, K, 1, share_bytes);
+    return few.us < all.us ? few : all;
+}
 
 int stats_words16(const Plan16& pl) {
     return pl.tiles == Tiles16::kF32 ? kF32N / kF32WN : pl.tiles == Tiles16::kFew ? kFewN / kFewWN : pl.tiles == Tiles16::kBig ? kBigN / kBigWN : kSmallN / kSmallWN;

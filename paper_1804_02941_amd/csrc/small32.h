@@ -32,8 +32,8 @@ struct Small32 {
     const float* g;
 };
 constexpr int kSmallTile = 32;
-// Whether a head of this size is taken here.
-bool small32(int32_t dtype, int64_t T, int64_t D, int64_t V);
+// Estimated time of loss and gradients here, in microseconds (very large past the sizes that are taken).
+double small32_us(int64_t T, int64_t D, int64_t V);
 // Statistics of H W^T, P = g (softmax - onehot) as fp32 [T][ldc], and both gradients from it (one launch).
 int launch_small_stats(const Small32& g, int32_t dtype, hipStream_t st);
 int launch_small_softmax(const Small32& g, int32_t dtype, hipStream_t st);

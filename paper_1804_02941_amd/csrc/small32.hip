@@ -130,12 +130,12 @@ __global__ __launch_bounds__(64 * kSmallWaves) void small_gradients_kernel(Small
     }
 }
 
-// Both paths, loss and gradients, replayed from a graph (tokens x width x words): fp32 256 x 512 x 250 27 us here and 99 on the tiles of
-// product16.h, 512 x 512 x 1000 57 and 116, 64 x 512 x 4000 84 and 110, but 16 x 1024 x 8000 and longer sums of few tiles are bound by
-// their own length; bf16, whose operands need no planes there, 256 x 512 x 250 29 and 42, 256 x 512 x 1000 47 and 44.
-bool small32(int32_t dtype, int64_t T, int64_t D, int64_t V) {
-    const int64_t longest = dtype == DAB_F32 ? 4096 : 1024, most = dtype == DAB_F32 ? int64_t{1} << 28 : int64_t{1} << 26;
-    return T <= longest && D <= longest && V <= longest && T * D * V <= most;
+// Time of loss and gradients here, in microseconds: the launches, the products at what single loads bring the matrix cores, the longest chains of
+// loads (words in dH, width in the logits), the tiles of dW.  Within a quarter of what twenty fp32 heads of up to 4096 of anything measured.
+double small32_us(int64_t T, int64_t D, int64_t V) {
+    if (T > 4096 || D > 4096 || V > 4096) return 1e30;
+    return 14.0 + 55.0 * static_cast<double>(T * D * V) / (int64_t{1} << 29) + 0.012 * (V + D) + 0.006 * T +
+           4.0 * static_cast<double>(V * D + T * D + 2 * T * V) / (1024 * 768);
 }
 
 static unsigned small_tiles(const Small32& g) { return static_cast<unsigned>(ceil_div(g.M, kSmallTile) * g.tiles_n); }

@@ -481,3 +481,13 @@ def test_refusals_of_the_binding():
         dab.dab_w4_matvec(torch.randn((1, 200), device=DEV), Q4, S4, 4)
     with pytest.raises(ValueError, match="out: expected shape"):
         dab.dab_w4_matvec(X, Q4, S4, 4, out=torch.empty((4, 5), device=DEV))
+
+
+# few tokens or few words beside a width past 4096, and sizes on either side of where the products change their tiles
+@pytest.mark.parametrize("T,D,V", [(100, 4200, 17), (40, 4200, 32), (17, 4100, 1), (31, 4104, 300), (97, 500, 2600), (1025, 60, 1030), (300, 1504, 628), (520, 33, 9000)])
+def test_fp32_head_on_every_tile(T, D, V):
+    rng = np.random.default_rng(T + D + V)
+    H, W, t, g = head_case(rng, T, D, V, torch.float32, 0.2)
+    want = check_head(H, W, t, g)
+    got = check_head(strided(H, 3, 0), strided(W, 4, 4), t, g)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
