@@ -380,8 +380,6 @@ __device__ __forceinline__ void product16(const Product16& g) {
             const int64_t t = target[j];
             const bool dead = !in || no_loss(t, g.ignore_index, g.V);
             const float base = dead ? 0.f : lse[j], w = dead ? 0.f : weight[j];
-            constexpr float kLog2e = 1.44269504f;
-            const float base2 = -base * kLog2e;
             // the target's column, counted from this lane's first
             const int64_t d64 = dead ? -1 : t - g.n0 - nw;
             const int d = d64 < 0 || d64 >= FN * 16 ? -1 : static_cast<int>(d64);
@@ -389,14 +387,8 @@ __device__ __forceinline__ void product16(const Product16& g) {
 #pragma unroll
             for (int i = 0; i < FN; ++i) {
                 v4f p;
-                // rounded to bf16 below, the exponent may be formed with one rounding more; as planes it may not
-                if (kE == 2 && g.p_planes == 1) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, base2));
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) p[r] = __expf(acc[i][j][r] - base);
-                }
+                for (int r = 0; r < 4; ++r) p[r] = __expf(acc[i][j][r] - base);
                 if (hit) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) p[r] -= d == i * 16 + r ? 1.f : 0.f;

@@ -491,3 +491,11 @@ def test_fp32_head_on_every_tile(T, D, V):
     want = check_head(H, W, t, g)
     got = check_head(strided(H, 3, 0), strided(W, 4, 4), t, g)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,D", [(1, 40), (100, 8), (189, 4534), (1094, 8), (4100, 24)])
+def test_head_of_one_word_has_nothing_to_learn(dtype, T, D):
+    rng = np.random.default_rng(T + D)
+    loss, _, dH, dW = check_head(*head_case(rng, T, D, 1, dtype, 0.2))
+    assert not loss.any() and not dH.any() and not dW.any()        # p = exp(0) exactly
