@@ -142,10 +142,9 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     p.wide = route == Route::kWide;
     if (p.wide) {
         p.P = p.n_seg = p.prob_planes = 1;
-        p.h_direct = !gradient && D % 4 == 0 && ldh % 4 == 0, p.w_direct = D % 4 == 0 && ldw % 4 == 0;
-        p.ldh = p.h_direct ? ldh : round_up(D, 4), p.ldw = p.w_direct ? ldw : round_up(D, 4);
+        p.h_direct = !gradient && D % 4 == 0 && ldh % 4 == 0, p.w_direct = true;
+        p.ldh = p.h_direct ? ldh : round_up(D, 4), p.ldw = ldw;
         p.h_at = p.h_direct ? 0 : room(T * p.ldh * 4);
-        p.w_at = p.w_direct ? 0 : room(V * p.ldw * 4);
         if (!gradient) {
             p.logits = plan32(T, V, D, 0);
             p.stats_at = room((ceil_div64(V, stats_words16(p.logits)) + 8) * T * 8);
@@ -164,7 +163,10 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     }
     p.P = dtype_pieces(dtype);
     p.n_seg = p.P == 1 ? 1 : 6;
-    p.w_direct = dtype == DAB_BF16 && D % 8 == 0 && ldw % 8 == 0;
+    // Rows of whole words are read where they are, though pieces of 16 bytes that cross lines cost the products more than aligned ones: loss
+    // and gradients, copied | as they are: 100 x 1002 x 50000 249 | 157 us, 500 x 1002 x 50000 368 | 288, 2000 x 2050 x 32768 1183 | 1081,
+    // 4000 x 1022 x 50000 1644 | 1652, 8000 x 1022 x 50000 3173 | 3287.
+    p.w_direct = dtype == DAB_BF16 && ((D % 8 == 0 && ldw % 8 == 0) || (D % 2 == 0 && ldw % 2 == 0 && T <= 4096));
     // (a gradient reads H with the rows of ignored tokens cleared, whatever they hold)
     p.h_direct = !gradient && dtype == DAB_BF16 && D % 8 == 0 && ldh % 8 == 0;
     p.ldh = p.h_direct ? ldh : round_up(D, 8);
@@ -231,11 +233,6 @@ static int head_operands(const HeadPlan& p, const void* H, int64_t ldh, const vo
             float* out = reinterpret_cast<float*>(ws + p.h_at);
             if (int rc = launch_rows32(static_cast<const float*>(H), T, D, ldh, targets, ignore, V, out, p.ldh, st)) return rc;
             h->p = out;
-        }
-        if (!p.w_direct) {
-            float* out = reinterpret_cast<float*>(ws + p.w_at);
-            if (int rc = launch_rows32(static_cast<const float*>(W), V, D, ldw, nullptr, 0, 0, out, p.ldw, st)) return rc;
-            w->p = out;
         }
         return DAB_OK;
     }

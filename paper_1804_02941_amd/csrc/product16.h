@@ -23,7 +23,7 @@ namespace dab {
 
 struct Operand16 {
     const void* p;                   // bf16, or fp32 where the plan says so
-    int64_t ld;                      // elements between rows ([rows][k]) or between k ([k][rows]), whole 16 bytes
+    int64_t ld;                      // elements between rows ([rows][k]) or between k ([k][rows]), whole words of 32 bits
     int64_t plane;                   // elements between the planes
 };
 

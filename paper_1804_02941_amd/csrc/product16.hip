@@ -29,13 +29,18 @@ struct Loader16 {
     static_assert(RC || kCopies == 1 || kCopies % 2 == 0, "the permutation of a row's pieces repeats every second copy");
     uint32_t off[kCopies];                                   // bytes from the tile's origin, the same every step
     uint64_t past[2];                                        // lanes whose k are past K in the last step, even and odd copies
+    uint32_t reach;                                          // bytes of a k's rows ([k][rows]), or of all rows but the last
     __amdgpu_buffer_rsrc_t rsrc;
     int wave;
 
+    // Bytes of n elements, in whole words of 32 bits (an odd number of bf16 has room behind it).
+    static __device__ __forceinline__ uint32_t words(uint32_t n) { return kE == 4 ? n * 4 : (n + 1) / 2 * 4; }
     // A row's pieces are permuted in LDS so that the reads below meet no bank twice.  A copy's lanes are in order in LDS, so the
     // permutation is one of the addresses in memory.  rows: how many of the operand's rows are left from the tile's first on.
     __device__ __forceinline__ void init(int w, int lane, int64_t ld, int rows, int K) {
         wave = w;
+        const int n = rows < ROWS ? rows : ROWS;
+        reach = RC ? words(n) : (n - 1) * static_cast<uint32_t>(ld) * kE;
 #pragma unroll
         for (int c = 0; c < kCopies; ++c) {
             const int r = (w * kCopies + c) * kLdsRows + lane / kChunks, phys = lane % kChunks;
@@ -51,10 +56,11 @@ struct Loader16 {
             }
         }
     }
-    // origin: the tile's first element of this step; left: bytes of the operand from there on ([k][rows]), or k (none: zeros).
-    // Rows past K are past the end of the buffer in one form, offsets of their own in the other.
-    __device__ __forceinline__ void aim(const E* origin, int64_t left) {
-        const uint32_t bytes = left <= 0 ? 0u : RC && left < kPast16 ? static_cast<uint32_t>(left) : kPast16;
+    // origin: the tile's first element of this step; left: k from there on (none: zeros).
+    // Nothing behind the operand's last word is read.  Rows past K are past the end of the buffer in one form, offsets of their own in the other.
+    __device__ __forceinline__ void aim(const E* origin, int left, int64_t ld) {
+        const uint32_t end = RC ? (left - 1) * (static_cast<uint32_t>(ld) * kE) + reach : reach + words(left);
+        const uint32_t bytes = left <= 0 ? 0u : left <= kStep ? end : kPast16;
         rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(origin), 0, static_cast<int>(bytes), 0x00020000);
     }
     __device__ __forceinline__ void copy(int c, bool last_k, char* lds) const {
@@ -235,8 +241,8 @@ __device__ __forceinline__ void product16(const Product16& g) {
     bool last_k = false;
     auto aim = [&] {
         const int left = to_fetch > 0 ? k_left : 0;
-        la.aim(pa, ARC ? left * g.A.ld * kE : left);
-        lb.aim(pb, BRC ? left * g.B.ld * kE : left);
+        la.aim(pa, left, g.A.ld);
+        lb.aim(pb, left, g.B.ld);
         last_k = k_left < kStep;
         --to_fetch, k_left -= kStep, pa += ka, pb += kb;
         if (k_left <= 0 && to_fetch > 0) {
@@ -250,6 +256,18 @@ __device__ __forceinline__ void product16(const Product16& g) {
         for (int c = 0; c < LA::kCopies; ++c) la.copy(c, last_k, buf);
 #pragma unroll
         for (int c = 0; c < LB::kCopies; ++c) lb.copy(c, last_k, buf + LA::kBytes);
+    };
+
+    // An operand that is read where it is has rows of whole words, not of whole pieces: what the last piece of a row holds behind K is
+    // cleared in LDS (the other operand's zeros would not do: it may be a NaN).
+    const int tail = BRC || last < g.steps ? 0 : static_cast<int>(LB::words(g.K % LB::kPer) / 4);
+    auto clear = [&](char* buf) {
+        const int piece = g.K % kStep / LB::kPer;
+        for (int r = threadIdx.x; r < TN; r += 64 * NW) {
+            uint32_t* at = reinterpret_cast<uint32_t*>(buf + LA::kBytes + r * 128 + (piece ^ ((r >> 1) & 7)) * 16);
+            for (int u = tail; u < 4; ++u) at[u] = 0;
+        }
+        __syncthreads();
     };
 
     Reader16<E, TM, ARC, FM> ra;
@@ -308,18 +326,25 @@ __device__ __forceinline__ void product16(const Product16& g) {
         }
         wait_and_meet<(NS - 1) * kInFlight>();
     }
+    if (!BRC && tail && last - first == 1) clear(lds);
 #pragma unroll
     for (int j = 0; j < FM; ++j) a[0][j] = ra.read(lds, 0, j);
 #pragma unroll
     for (int i = 0; i < FN; ++i) b[0][i] = rb.read(lds + LA::kBytes, 0, i);
-    for (int s = first; s < last; ++s) {
+    auto step = [&](auto end_c, int s) {
         char* cur = lds + ((s - first) & (NS - 1)) * kBuf;
         char* other = lds + ((s + 1 - first) & (NS - 1)) * kBuf;
         aim();
         half(no{}, 0, cur, 1, cur);
         wait_and_meet<(NS - 2) * kInFlight>();
+        if (decltype(end_c)::value && tail && s + 2 == last) clear(other);
         half(yes{}, 1, other, 0, cur);
-    }
+    };
+    int s = first;
+    for (; s < last - (BRC ? 0 : 2); ++s) step(no{}, s);
+    // (apart from the others: with the question in all of them the logits' products took 3 % longer)
+    if (!BRC)
+        for (; s < last; ++s) step(yes{}, s);
     // (copies and reads past the last step: zeros, and not used; the wavefront waits for them before it ends)
     wait_and_meet();
 

@@ -499,3 +499,21 @@ def test_head_of_one_word_has_nothing_to_learn(dtype, T, D):
     rng = np.random.default_rng(T + D)
     loss, _, dH, dW = check_head(*head_case(rng, T, D, 1, dtype, 0.2))
     assert not loss.any() and not dH.any() and not dW.any()        # p = exp(0) exactly
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 40, 150, 1100])
+@pytest.mark.parametrize("D", [1, 2, 33, 34, 38, 66, 100, 191])
+def test_head_between_whatever_lies_behind_its_rows(dtype, T, D):
+    """Rows of any number of words, each followed by what is no number: none of it is multiplied."""
+    rng = np.random.default_rng(T + D)
+    V = 4101
+    H, W, t, g = head_case(rng, T, D, V, dtype, 0.1)
+    want = check_head(H, W, t, g)
+    for behind in (1, 2, 8 - D % 8):
+        wide = torch.full((V, D + behind), float("nan"), dtype=dtype, device=DEV)
+        wide[:, :D] = W
+        last = torch.full((T, D + behind), float("inf"), dtype=dtype, device=DEV)
+        last[:, :D] = H
+        got = check_head(last[:, :D], wide[:, :D], t, g)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
