@@ -91,13 +91,18 @@ static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t l
 
 // How the products of a head are done.  Measured, loss and gradients (tokens x width x words), small kernels, fp32 operands as they are, planes:
 // fp32 256 x 512 x 250 27 us, 65, 95; 299 x 1504 x 628 75, 150, 194; 64 x 2048 x 64000 -, 632, 1734; 256 x 1024 x 16000 -, 281, 283;
-// 1024 x 1024 x 16000 -, 1017, 664; 2048 x 1024 x 32000 -, 3931, 2495.  bf16 256 x 512 x 250 29 small and 42 on tiles, 256 x 512 x 1000
-// 47 and 44, 64 x 512 x 4000 116 and 47.
+// 1024 x 1024 x 16000 -, 1017, 664; 2048 x 1024 x 32000 -, 3931, 2495.  bf16, small kernels and tiles: 256 x 512 x 250 29 us, 42; 1 x 2083 x 256
+// 54, 71; 75 x 931 x 901 51, 64; 51 x 1272 x 2602 130, 59; 1050 x 464 x 1060 113, 61.
 enum class Route { kSmall, kWide, kPlanes };
 static Route head_route(int32_t dtype, int64_t T, int64_t D, int64_t V) {
     const int t = static_cast<int>(T), d = static_cast<int>(D), v = static_cast<int>(V);
-    if (dtype == DAB_BF16) return T <= 1024 && D <= 1024 && V <= 1024 && T * D * V <= (1 << 26) ? Route::kSmall : Route::kPlanes;
-    const double small = small32_us(T, D, V);
+    const double small = small32_us(dtype, T, D, V);
+    if (dtype == DAB_BF16) {
+        const int planes = T <= 128 ? 2 : 1;                 // of P (head_plan)
+        const double sums = 2 * plan16(t, v, d, 1, 0).us + plan16(v, d, t, planes, kAnyShares16).us + plan16(planes * t, d, v, 1, kAnyShares16).us;
+        // (the estimates are those of a full chip, where steps take longer; H is copied)
+        return small <= 22.5 + 0.78 * sums + 12e-6 * static_cast<double>(T * D) ? Route::kSmall : Route::kPlanes;
+    }
     const double wide = 15.0 + 2 * plan32(t, v, d, 0).us + plan32(v, d, t, kAnyShares16).us + plan32(t, d, v, kAnyShares16).us;
     // (both calls write and read the planes of H and W)
     const double planes = 20.0 + 2 * plan16(t, v, d, 6, 0).us + plan16(v, d, t, 6, kAnyShares16).us + plan16(t, d, v, 6, kAnyShares16).us +

@@ -33,7 +33,7 @@ struct Small32 {
 };
 constexpr int kSmallTile = 32;
 // Estimated time of loss and gradients here, in microseconds (very large past the sizes that are taken).
-double small32_us(int64_t T, int64_t D, int64_t V);
+double small32_us(int32_t dtype, int64_t T, int64_t D, int64_t V);
 // Statistics of H W^T, P = g (softmax - onehot) as fp32 [T][ldc], and both gradients from it (one launch).
 int launch_small_stats(const Small32& g, int32_t dtype, hipStream_t st);
 int launch_small_softmax(const Small32& g, int32_t dtype, hipStream_t st);

@@ -131,11 +131,13 @@ __global__ __launch_bounds__(64 * kSmallWaves) void small_gradients_kernel(Small
 }
 
 // Time of loss and gradients here, in microseconds: the launches, the products at what single loads bring the matrix cores, the longest chains of
-// loads (words in dH, width in the logits), the tiles of dW.  Within a quarter of what twenty fp32 heads of up to 4096 of anything measured.
-double small32_us(int64_t T, int64_t D, int64_t V) {
+// loads (words in dH, width in the logits), the tiles of dW and of the rest.  Fitted to 25 fp32 and 44 bf16 heads of up to 4096 of anything,
+// all of them within a quarter.
+double small32_us(int32_t dtype, int64_t T, int64_t D, int64_t V) {
     if (T > 4096 || D > 4096 || V > 4096) return 1e30;
-    return 14.0 + 55.0 * static_cast<double>(T * D * V) / (int64_t{1} << 29) + 0.012 * (V + D) + 0.006 * T +
-           4.0 * static_cast<double>(V * D + T * D + 2 * T * V) / (1024 * 768);
+    const double products = static_cast<double>(T * D * V) / (int64_t{1} << 29), tiles = static_cast<double>(V * D + T * D + 2 * T * V) / (1024 * 768);
+    if (dtype == DAB_BF16) return 14.5 + 17.0 * products + 0.011 * (V + D) + 0.014 * T + 13.0 * tiles;
+    return 14.0 + 55.0 * products + 0.012 * (V + D) + 0.006 * T + 4.0 * tiles;
 }
 
 static unsigned small_tiles(const Small32& g) { return static_cast<unsigned>(ceil_div(g.M, kSmallTile) * g.tiles_n); }

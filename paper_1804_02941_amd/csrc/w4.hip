@@ -14,12 +14,19 @@ namespace dab {
 constexpr int kW4MaxWaves = 8;       // wavefronts per workgroup
 
 // ---------------------------------------------------------------- laying out
-// Both directions: a wavefront takes 16 rows x 512 weights, a block of 128 at a time.  A lane holds four neighbouring weights of a row, 32 lanes a
-// row of the block, so that rows are read and written in whole lines; the packed block passes through LDS on its way.
-constexpr int kW4PackWaves = 4;
-struct W4Block {
-    uint16_t codes[512];             // [group][row][four weights]: a block's kilobyte
-    uint8_t scales[64][4];
+// Both directions: a workgroup takes 16 rows x 512 weights, a wavefront 128 of them.  A lane holds four neighbouring weights of a row, 32 lanes a
+// row of the block, so that rows are read and written in whole lines; the packed block passes through LDS on its way.  (A wavefront that
+// takes the 512 by itself waits four times as long for its loads: 1836 x 624 bf16 laid out and read back, 17 + 11 us instead of 6 + 5.)  Rows
+// of one or two blocks: four or two times 16 of them.
+constexpr int kW4PackWaves = 4;      // blocks that share a word of scales
+struct W4Place {
+    int tile, step, j, kt, slot;     // 16 rows, 512 weights of them, which 128 of those and of all; the tile's place in the workgroup
+    __device__ __forceinline__ W4Place(int Kt) {
+        const int wave = threadIdx.x >> 6, shift = Kt == 1 ? 0 : Kt == 2 ? 1 : 2;
+        slot = wave >> shift, tile = blockIdx.y * (kW4PackWaves >> shift) + slot, step = blockIdx.x;
+        j = wave & ((1 << shift) - 1), kt = step * kW4PackWaves + j;
+    }
+    static dim3 grid(int F, int Kt) { return dim3(ceil_div(Kt, kW4PackWaves), ceil_div(F, Kt == 1 ? 64 : Kt == 2 ? 32 : 16)); }
 };
 
 template <typename T>
@@ -36,18 +43,16 @@ __device__ __forceinline__ v4f load4(const T* row, int c, int cols) {
     return v;
 }
 
+// (eight wavefronts on a SIMD, or else the compiler takes all rows at once, in 238 registers)
 template <typename T>
-__global__ __launch_bounds__(64 * kW4PackWaves) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int Kt, int K4,
+__global__ __launch_bounds__(64 * kW4PackWaves, 6) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int Kt, int K4,
                                                                     uint8_t* __restrict__ Q, uint8_t* __restrict__ S) {
-    __shared__ W4Block lds[kW4PackWaves];
-    DAB_RESERVE_VGPRS();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = blockIdx.y, step = blockIdx.x * kW4PackWaves + wave;
-    if (step >= K4) return;                                  // (a wavefront works alone: no barrier below)
-    W4Block& b = lds[wave];
-    reinterpret_cast<uint32_t*>(b.scales)[lane] = 17u * 0x01010101u;
-    for (int j = 0; j < 4; ++j) {
-        const int kt = step * 4 + j;
-        if (kt >= Kt) break;
+    __shared__ __attribute__((aligned(16))) uint16_t codes[kW4PackWaves][512];     // [group][row][four weights]: a block's kilobyte
+    __shared__ __attribute__((aligned(4))) uint8_t scales[kW4PackWaves][64][kW4PackWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const W4Place at(Kt);
+    const int tile = at.tile, kt = at.kt;
+    if (kt < Kt && tile * 16 < F) {
         const int k = kt * 128 + (lane & 31) * 4, group = (lane & 31) >> 3;
         v4f v[8];
 #pragma unroll
@@ -78,15 +83,21 @@ __global__ __launch_bounds__(64 * kW4PackWaves) void w4_pack_kernel(const T* __r
                 code |= (__float_as_uint(v[i][u]) >> 31) << 3;
                 word |= (finite ? code : 7u) << (4 * u);
             }
-            b.codes[(group * 16 + r) * 8 + (lane & 7)] = static_cast<uint16_t>(word);
-            if ((lane & 7) == 0) b.scales[group * 16 + r][j] = static_cast<uint8_t>(finite ? e + 127 : 255);
+            codes[wave][(group * 16 + r) * 8 + (lane & 7)] = static_cast<uint16_t>(word);
+            if ((lane & 7) == 0) scales[at.slot][group * 16 + r][at.j] = static_cast<uint8_t>(finite ? e + 127 : 255);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_nontemporal_store(reinterpret_cast<const v4u32*>(b.codes)[lane],
+        __builtin_nontemporal_store(reinterpret_cast<const v4u32*>(codes[wave])[lane],
                                     reinterpret_cast<v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16));
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    *reinterpret_cast<uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4) = reinterpret_cast<const uint32_t*>(b.scales)[lane];
+    __syncthreads();
+    if (at.j == 0 && tile * 16 < F) {
+        // (17, the scale of zeros, for blocks past the last one)
+        const uint32_t all = *reinterpret_cast<const uint32_t*>(scales[at.slot][lane]);
+        const int n = Kt - at.step * kW4PackWaves;
+        const uint32_t past = n >= kW4PackWaves ? 0u : ~0u << (8 * n);
+        *reinterpret_cast<uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + at.step) * 64 + lane) * 4) = (all & ~past) | (17u * 0x01010101u & past);
+    }
 }
 
 // The scale of block j of four from its byte, as the conversions take it.
@@ -97,46 +108,39 @@ __device__ __forceinline__ float scale_of(uint32_t codes, int j) {
 
 __global__ __launch_bounds__(64 * kW4PackWaves) void w4_unpack_kernel(const uint8_t* __restrict__ Q, const uint8_t* __restrict__ S, int F,
                                                                       int K, int Kt, int K4, float* __restrict__ W) {
-    __shared__ W4Block lds[kW4PackWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = blockIdx.y, step = blockIdx.x * kW4PackWaves + wave;
-    if (step >= K4) return;
-    W4Block& b = lds[wave];
-    reinterpret_cast<uint32_t*>(b.scales)[lane] = *reinterpret_cast<const uint32_t*>(S + ((static_cast<int64_t>(tile) * K4 + step) * 64 + lane) * 4);
-    v4u32 q[4];
+    __shared__ __attribute__((aligned(16))) uint16_t codes[kW4PackWaves][512];
+    __shared__ uint8_t scales[kW4PackWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const W4Place at(Kt);
+    const int tile = at.tile, kt = at.kt;
+    if (kt >= Kt || tile * 16 >= F) return;                  // (a wavefront works alone: no barrier below)
+    const v4u32 q = *reinterpret_cast<const v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + kt) * 64 + lane) * 16);
+    scales[wave][lane] = S[((static_cast<int64_t>(tile) * K4 + at.step) * 64 + lane) * 4 + at.j];
+    reinterpret_cast<v4u32*>(codes[wave])[lane] = q;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int k = kt * 128 + (lane & 31) * 4, group = (lane & 31) >> 3;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        q[j] = *reinterpret_cast<const v4u32*>(Q + ((static_cast<int64_t>(tile) * Kt + min(step * 4 + j, Kt - 1)) * 64 + lane) * 16);
+    for (int i = 0; i < 8; ++i) {
+        const int r = 2 * i + (lane >> 5), row = tile * 16 + r;
+        const uint32_t word = codes[wave][(group * 16 + r) * 8 + (lane & 7)], s = scales[wave][group * 16 + r];
+        const float scale = s == 255u ? __builtin_nanf("") : pow2f(static_cast<int>(s) - 127);
+        v4f v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int kt = step * 4 + j;
-        if (kt >= Kt) break;
-        reinterpret_cast<v4u32*>(b.codes)[lane] = q[j];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const int k = kt * 128 + (lane & 31) * 4, group = (lane & 31) >> 3;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = 2 * i + (lane >> 5), row = tile * 16 + r;
-            const uint32_t word = b.codes[(group * 16 + r) * 8 + (lane & 7)], s = b.scales[group * 16 + r][j];
-            const float scale = s == 255u ? __builtin_nanf("") : pow2f(static_cast<int>(s) - 127);
-            v4f v;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t c = word >> (4 * u), m = c & 7u;
-                // 0, 1/2, then (2 + last bit) 2^(upper bits - 2)
-                const float a = m < 2 ? 0.5f * static_cast<float>(m) : static_cast<float>(2u + (m & 1u)) * pow2f(static_cast<int>(m >> 1) - 2);
-                v[u] = (c & 8u ? -a : a) * scale;
-            }
-            if (row >= F) continue;
-            float* to = W + static_cast<int64_t>(row) * K;
-            if (k + 4 <= K) {
-                *reinterpret_cast<Unaligned<float, 4>::type*>(to + k) = v;
-            } else {
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (k + u < K) to[k + u] = v[u];
-            }
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t c = word >> (4 * u), m = c & 7u;
+            // 0, 1/2, then (2 + last bit) 2^(upper bits - 2)
+            const float a = m < 2 ? 0.5f * static_cast<float>(m) : static_cast<float>(2u + (m & 1u)) * pow2f(static_cast<int>(m >> 1) - 2);
+            v[u] = (c & 8u ? -a : a) * scale;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (row >= F) continue;
+        float* to = W + static_cast<int64_t>(row) * K;
+        if (k + 4 <= K) {
+            *reinterpret_cast<Unaligned<float, 4>::type*>(to + k) = v;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (k + u < K) to[k + u] = v[u];
+        }
     }
 }
 
@@ -317,7 +321,7 @@ extern "C" int dab_w4_pack(const void* W, int32_t dtype, int32_t F, int32_t K, i
     if (!real_dtype(dtype) || K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
     const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4);
-    const dim3 grid(ceil_div(K4, kW4PackWaves), ceil_div(F, 16)), block(64 * kW4PackWaves);
+    const dim3 grid = W4Place::grid(F, Kt), block(64 * kW4PackWaves);
     const auto st = static_cast<hipStream_t>(stream);
     if (dtype == DAB_F32) return launch(w4_pack_kernel<float>, grid, block, 0, st, static_cast<const float*>(W), F, K, ldw, Kt, K4, Q, S);
     if (dtype == DAB_BF16) return launch(w4_pack_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(W), F, K, ldw, Kt, K4, Q, S);
@@ -331,7 +335,7 @@ extern "C" int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int3
     if (K > INT32_MAX - 512 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(W, 16) || misaligned(Q, 16) || misaligned(S, 16)) return DAB_ERR_ALIGN;
     const int Kt = ceil_div(K, 128), K4 = ceil_div(Kt, 4);
-    return launch(w4_unpack_kernel, dim3(ceil_div(K4, kW4PackWaves), ceil_div(F, 16)), dim3(64 * kW4PackWaves), 0, static_cast<hipStream_t>(stream), Q, S, F, K, Kt, K4, W);
+    return launch(w4_unpack_kernel, W4Place::grid(F, Kt), dim3(64 * kW4PackWaves), 0, static_cast<hipStream_t>(stream), Q, S, F, K, Kt, K4, W);
 }
 
 extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
