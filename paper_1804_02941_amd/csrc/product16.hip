@@ -16,6 +16,7 @@ __device__ __forceinline__ void wait_and_meet() {
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
 // A byte offset past every tile: a load from there gives zeros.  What a tile's offsets reach stays below it (ld < 2^22).
 constexpr uint32_t kPast16 = 0x80000000u;
+constexpr int kParts16 = 4;          // of a big tile in the last round of a product whose sums are not shared out
 
 // One operand's tile of ROWS x 128 bytes of k (64 bf16 or 32 fp32), from memory into LDS.
 template <typename E, int ROWS, bool RC, int NW>
@@ -25,7 +26,7 @@ struct Loader16 {
     static constexpr int kCopies = kBytes / 1024 / NW;       // of one wavefront, a kilobyte each
     static constexpr int kChunks = RC ? ROWS / kPer : 8;     // 16-byte pieces of a row of the tile in LDS
     static constexpr int kLdsRows = 64 / kChunks;            // rows of it that one copy fills
-    static_assert((ROWS & (ROWS - 1)) == 0 && (kE == 4 || ROWS >= 128), "the permutation stays within a row's pieces");
+    static_assert((ROWS & (ROWS - 1)) == 0 && (!RC || kE == 4 || ROWS >= 128), "the permutation stays within a row's pieces");
     static_assert(RC || kCopies == 1 || kCopies % 2 == 0, "the permutation of a row's pieces repeats every second copy");
     uint32_t off[kCopies];                                   // bytes from the tile's origin, the same every step
     uint64_t past[2];                                        // lanes whose k are past K in the last step, even and odd copies
@@ -194,8 +195,8 @@ struct Rows16 {
     }
 };
 
-// NS: steps in LDS.
-template <typename E, int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS>
+// NS: steps in LDS.  PARTS: the tile is one of that many, one above the other, of a tile of the last round.
+template <typename E, int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS, int PARTS = 1>
 __device__ __forceinline__ void product16(const Product16& g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
     using LA = Loader16<E, TM, ARC, NW>;
@@ -208,8 +209,8 @@ __device__ __forceinline__ void product16(const Product16& g) {
     // Consecutive workgroups go to the XCDs in turn: each XCD gets neighbouring tiles, eight rows of tiles at a time, so
     // that what runs on it together shares operands in its L2.  The tiles that would leave a last round half empty are taken in shares.
     // (quotients come from vector instructions; what is made of them here has to be scalar)
-    int tile, first = 0, last = g.steps, share = -1;
-    if (static_cast<int>(blockIdx.x) < 8 * g.whole_xcd) {
+    int tile, first = 0, last = g.steps, share = -1, part = 0;
+    if (PARTS == 1 && static_cast<int>(blockIdx.x) < 8 * g.whole_xcd) {
         tile = (blockIdx.x & 7) * g.whole_xcd + (blockIdx.x >> 3);
         if (tile >= g.whole) return;
     } else {
@@ -217,12 +218,14 @@ __device__ __forceinline__ void product16(const Product16& g) {
         if (unit >= g.rest * g.shares) return;
         const int sh = __builtin_amdgcn_readfirstlane(unit / g.rest);
         tile = g.whole + unit - sh * g.rest;
-        if (g.shares > 1) share = sh, first = sh * g.share_steps, last = min(first + g.share_steps, g.steps);
+        if (PARTS > 1) part = sh;
+        else if (g.shares > 1) share = sh, first = sh * g.share_steps, last = min(first + g.share_steps, g.steps);
     }
     const int band = __builtin_amdgcn_readfirstlane(tile / (8 * g.tiles_n)), in_band = tile - band * 8 * g.tiles_n;
     const int bm = min(8, g.tiles_m - band * 8);
     const int tn = __builtin_amdgcn_readfirstlane(in_band / bm), tm = band * 8 + in_band - tn * bm;
-    const int m0 = tm * TM, n0 = tn * TN;
+    const int m0 = (tm * PARTS + part) * TM, n0 = tn * TN;
+    if (PARTS > 1 && m0 >= g.M) return;
     const int wm = wave % WM, wn = wave / WM;
 
     LA la;
@@ -469,6 +472,12 @@ __device__ __forceinline__ void product16(const Product16& g) {
 
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
+    // Sums that a row's softmax needs whole are not shared out: big tiles of the last round are taken in four parts instead.
+    if constexpr (EPI != kEpiStore && TM == 256)
+        if (static_cast<int>(blockIdx.x) >= 8 * g.whole_xcd) {
+            product16<bf16, EPI, TM / kParts16, TN, WM, WN, ARC, BRC, 2, kParts16>(g);
+            return;
+        }
     product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
 }
 // For no more tiles than compute units: with one workgroup on each, a step of the small tile takes as long as its copies, so four
@@ -584,8 +593,8 @@ constexpr int tile_n16(Tiles16 kind) {
 }
 constexpr size_t lds_bytes16(Tiles16 kind) { return (kind == Tiles16::kDeep ? size_t{4} : size_t{2}) * (tile_m16(kind) + tile_n16(kind)) * 128; }
 
-// Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares where
-// that takes less.
+// Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares (or, with
+// no room for those, parts of tiles) where that takes less.
 static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t share_bytes) {
     // Workgroups that a compute unit runs together; a step's time with all of them there, that of one alone (fp32 products are bound by the
     // matrix cores, which the workgroups share), and that of a tile's beginning and end: those of long sums on a full chip, of
@@ -623,9 +632,14 @@ static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t sha
         const double us = round(pl.rest * s, per) + 4.0 + 2.0 * pl.rest * s * tile_bytes / 4e6;
         if (us < best) best = us, pl.shares = s, pl.share_steps = per;
     }
+    if (kind == Tiles16::kBig && share_bytes == 0) {
+        // a quarter of a tile: two fifths of its time, as all its columns are fetched and read
+        const double us = ceil_div(pl.rest * kParts16, slots) * (pl.steps * 0.65 + 4.0);
+        if (us < best) best = us, pl.shares = kParts16;
+    }
     pl.us += best;
     if (pl.shares == 1) pl.whole = static_cast<int>(tiles), pl.rest = 0;
-    pl.part_bytes = pl.shares > 1 ? static_cast<size_t>(pl.rest) * pl.shares * tile_bytes : 0;
+    pl.part_bytes = pl.shares > 1 && share_bytes ? static_cast<size_t>(pl.rest) * pl.shares * tile_bytes : 0;
     return pl;
 }
 
@@ -670,7 +684,7 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
     if (brc != (epi == kEpiStore)) return DAB_ERR_UNSUPPORTED;
     const int threads = 64 * (big ? kBigWM * kBigWN : kSmallWM * kSmallWN);
     if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(pl.tiles), st, g)) return rc;
-    if (pl.shares == 1) return DAB_OK;
+    if (pl.shares == 1 || epi != kEpiStore) return DAB_OK;
     const int blocks = tm * tn / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
     return launch(pl.tiles == Tiles16::kF32 ? join16_kernel<kF32M, kF32N, kF32WM, kF32WN> : pl.tiles == Tiles16::kFew ? join16_kernel<kFewM, kFewN, kFewWM, kFewWN> : big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
                   dim3(g.rest * blocks), dim3(threads), 0, st, g);
