@@ -195,8 +195,8 @@ struct Rows16 {
     }
 };
 
-// NS: steps in LDS.  PARTS: the tile is one of that many, one above the other, of a tile of the last round.
-template <typename E, int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS, int PARTS = 1>
+// NS: steps in LDS.  TAIL: B's rows may hold anything behind K.  PARTS: the tile is one of that many, one above the other, of a tile of the last round.
+template <typename E, int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS, bool TAIL = false, int PARTS = 1>
 __device__ __forceinline__ void product16(const Product16& g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
     using LA = Loader16<E, TM, ARC, NW>;
@@ -263,14 +263,14 @@ __device__ __forceinline__ void product16(const Product16& g) {
 
     // An operand that is read where it is has rows of whole words, not of whole pieces: what the last piece of a row holds behind K is
     // cleared in LDS (the other operand's zeros would not do: it may be a NaN).
-    const int tail = BRC || last < g.steps ? 0 : static_cast<int>(LB::words(g.K % LB::kPer) / 4);
+    const int tail = TAIL && g.b_tail && last == g.steps ? static_cast<int>(LB::words(g.K % LB::kPer) / 4) : 0;
     auto clear = [&](char* buf) {
         const int piece = g.K % kStep / LB::kPer;
         for (int r = threadIdx.x; r < TN; r += 64 * NW) {
             uint32_t* at = reinterpret_cast<uint32_t*>(buf + LA::kBytes + r * 128 + (piece ^ ((r >> 1) & 7)) * 16);
             for (int u = tail; u < 4; ++u) at[u] = 0;
         }
-        __syncthreads();
+        wait_and_meet<(NS - 2) * (LA::kCopies + LB::kCopies)>();
     };
 
     Reader16<E, TM, ARC, FM> ra;
@@ -329,7 +329,7 @@ __device__ __forceinline__ void product16(const Product16& g) {
         }
         wait_and_meet<(NS - 1) * kInFlight>();
     }
-    if (!BRC && tail && last - first == 1) clear(lds);
+    if (TAIL && tail && last - first == 1) clear(lds);
 #pragma unroll
     for (int j = 0; j < FM; ++j) a[0][j] = ra.read(lds, 0, j);
 #pragma unroll
@@ -344,9 +344,9 @@ __device__ __forceinline__ void product16(const Product16& g) {
         half(yes{}, 1, other, 0, cur);
     };
     int s = first;
-    for (; s < last - (BRC ? 0 : 2); ++s) step(no{}, s);
+    for (; s < last - (TAIL ? 2 : 0); ++s) step(no{}, s);
     // (apart from the others: with the question in all of them the logits' products took 3 % longer)
-    if (!BRC)
+    if (TAIL)
         for (; s < last; ++s) step(yes{}, s);
     // (copies and reads past the last step: zeros, and not used; the wavefront waits for them before it ends)
     wait_and_meet();
@@ -472,13 +472,18 @@ __device__ __forceinline__ void product16(const Product16& g) {
 
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
-    // Sums that a row's softmax needs whole are not shared out: big tiles of the last round are taken in four parts instead.
-    if constexpr (EPI != kEpiStore && TM == 256)
+    product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
+}
+// Logits whose words' rows may hold anything behind K; and, as sums that a softmax needs whole are not shared out, whose big tiles of the last round
+// are taken in four parts.
+template <int EPI, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_ends_kernel(Product16 g) {
+    if constexpr (TM == 256)
         if (static_cast<int>(blockIdx.x) >= 8 * g.whole_xcd) {
-            product16<bf16, EPI, TM / kParts16, TN, WM, WN, ARC, BRC, 2, kParts16>(g);
+            product16<bf16, EPI, TM / kParts16, TN, WM, WN, false, false, 2, true, kParts16>(g);
             return;
         }
-    product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
+    product16<bf16, EPI, TM, TN, WM, WN, false, false, 2, true>(g);
 }
 // For no more tiles than compute units: with one workgroup on each, a step of the small tile takes as long as its copies, so four
 // steps are on their way instead of two.
@@ -486,10 +491,14 @@ template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_deep_kernel(Product16 g) {
     product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 4>(g);
 }
+template <int EPI, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_deep_ends_kernel(Product16 g) {
+    product16<bf16, EPI, TM, TN, WM, WN, false, false, 4, true>(g);
+}
 // fp32 operands as they are, on the matrix cores' fp32 form.
 template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product32_kernel(Product16 g) {
-    product16<float, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
+    product16<float, EPI, TM, TN, WM, WN, ARC, BRC, 2, !BRC>(g);
 }
 
 // The shares of a tile's sums, added in a fixed order.  A workgroup takes one 16 x 16 block of every wavefront; eight shares
@@ -663,7 +672,12 @@ int stats_words16(const Plan16& pl) {
 }
 
 template <int EPI, bool ARC, bool BRC>
-static auto kernel16(Tiles16 kind) {
+static auto kernel16(Tiles16 kind, bool ends) {
+    if constexpr (EPI != kEpiStore)
+        if (ends && !wide16(kind))
+            return kind == Tiles16::kBig    ? product16_ends_kernel<EPI, kBigM, kBigN, kBigWM, kBigWN>
+                   : kind == Tiles16::kDeep ? product16_deep_ends_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN>
+                                            : product16_ends_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN>;
     return kind == Tiles16::kF32    ? product32_kernel<EPI, kF32M, kF32N, kF32WM, kF32WN, ARC, BRC>
            : kind == Tiles16::kFew  ? product32_kernel<EPI, kFewM, kFewN, kFewWM, kFewWN, ARC, BRC>
            : kind == Tiles16::kBig  ? product16_kernel<EPI, kBigM, kBigN, kBigWM, kBigWN, ARC, BRC>
@@ -678,10 +692,11 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
     if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
     g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
     g.whole_xcd = ceil_div(g.whole, kNumXCD), g.rest_xcd = ceil_div(g.rest * g.shares, kNumXCD);
-    const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.tiles)
-                        : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.tiles)
-                        : arc ? kernel16<kEpiStore, true, true>(pl.tiles)
-                              : kernel16<kEpiStore, false, true>(pl.tiles);
+    const bool ends = g.b_tail || g.shares > 1;
+    const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.tiles, ends)
+                        : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.tiles, ends)
+                        : arc ? kernel16<kEpiStore, true, true>(pl.tiles, false)
+                              : kernel16<kEpiStore, false, true>(pl.tiles, false);
     if (brc != (epi == kEpiStore)) return DAB_ERR_UNSUPPORTED;
     const int threads = 64 * (big ? kBigWM * kBigWN : kSmallWM * kSmallWN);
     if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(pl.tiles), st, g)) return rc;
@@ -693,8 +708,9 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
 
 int init_product16() {
     for (const Tiles16 kind : {Tiles16::kSmall, Tiles16::kDeep, Tiles16::kBig, Tiles16::kF32, Tiles16::kFew})
-        for (const auto k : {kernel16<kEpiStats, false, false>(kind), kernel16<kEpiSoftmax, false, false>(kind),
-                             kernel16<kEpiStore, true, true>(kind), kernel16<kEpiStore, false, true>(kind)}) {
+        for (const auto k : {kernel16<kEpiStats, false, false>(kind, false), kernel16<kEpiSoftmax, false, false>(kind, false),
+                             kernel16<kEpiStats, false, false>(kind, true), kernel16<kEpiSoftmax, false, false>(kind, true),
+                             kernel16<kEpiStore, true, true>(kind, false), kernel16<kEpiStore, false, true>(kind, false)}) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                      static_cast<int>(lds_bytes16(kind)));
             if (e != hipSuccess) return hip_failed(e);

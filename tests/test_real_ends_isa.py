@@ -55,3 +55,25 @@ def test_the_deep_form_leaves_two_steps_of_copies_on_their_way(tmp_path):
         assert waits == [f"s_waitcnt vmcnt({n}) lgkmcnt(0)" for n in (24, 16, 0)], (name, waits)
         products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
         assert [l for l in text[products[0]:products[-1]] if re.match(r"s_waitcnt.*vmcnt", l)] == ["s_waitcnt vmcnt(16) lgkmcnt(0)"], name
+
+
+def test_kernels_that_clear_what_lies_behind_a_row(tmp_path):
+    """The forms whose words' rows may hold anything behind the width, and the fp32 ones: every barrier comes with the wait for copies and reads
+    (what is cleared in LDS included), and among the products of one tile there is no other wait for copies."""
+    out = str(tmp_path / "product16.s")
+    ic.compile_to_isa("product16.hip", out)
+    found = [(n, l) for n, l in ic.kernels(open(out).read()) if "ends_kernel" in n or "product32_kernel" in n]
+    assert len(found) == 6 + 8
+    for name, lines in found:
+        assert ic.scalar_read_hazards(lines) == [], name
+        text = [l.strip() for l in lines]
+        allowed = (24, 16, 0) if "deep" in name else (0,)
+        for i, l in enumerate(text):
+            if l.startswith("s_barrier"):
+                assert text[i - 1] in [f"s_waitcnt vmcnt({n}) lgkmcnt(0)" for n in allowed], (name, text[i - 1])
+        if "ELi256ELi256" in name:                                # (two tiles' code, an end between them)
+            continue
+        products = [i for i, l in enumerate(text) if l.startswith("v_mfma")]
+        for i in range(products[0], products[-1]):
+            if re.match(r"s_waitcnt.*vmcnt", text[i]):
+                assert text[i + 1].startswith("s_barrier"), (name, text[i])
