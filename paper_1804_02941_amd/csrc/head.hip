@@ -77,7 +77,7 @@ struct HeadPlan {
     int prob_planes;                 // planes of P
     bool stacked;                    // bf16, few tokens: P's two planes as twice the tokens in dH, and as two pairs in dW
     bool h_direct, w_direct;
-    bool w_tail;                     // W's rows are read where they are and are no whole pieces of 16 bytes
+    bool tail;                       // rows that are read where they are and are no whole pieces of 16 bytes
     int64_t ldh, ldw;
     int piece, n_pieces;             // words of a piece
     int64_t ldp;
@@ -148,7 +148,7 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     p.wide = route == Route::kWide;
     if (p.wide) {
         p.P = p.n_seg = p.prob_planes = 1;
-        p.h_direct = !gradient && D % 4 == 0 && ldh % 4 == 0, p.w_direct = true, p.w_tail = D % 4 != 0;
+        p.h_direct = !gradient, p.w_direct = true, p.tail = D % 4 != 0;
         p.ldh = p.h_direct ? ldh : round_up(D, 4), p.ldw = ldw;
         p.h_at = p.h_direct ? 0 : room(T * p.ldh * 4);
         if (!gradient) {
@@ -172,10 +172,11 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     // Rows of whole words are read where they are, though pieces of 16 bytes that cross lines cost the products more than aligned ones: loss
     // and gradients, copied | as they are: 100 x 1002 x 50000 249 | 157 us, 500 x 1002 x 50000 368 | 288, 2000 x 2050 x 32768 1183 | 1081,
     // 4000 x 1022 x 50000 1644 | 1652, 8000 x 1022 x 50000 3173 | 3287.
-    p.w_direct = dtype == DAB_BF16 && ((D % 8 == 0 && ldw % 8 == 0) || (D % 2 == 0 && ldw % 2 == 0 && T <= 4096));
-    p.w_tail = p.w_direct && D % 8 != 0;
+    auto direct = [&](int64_t ld) { return dtype == DAB_BF16 && ((D % 8 == 0 && ld % 8 == 0) || (D % 2 == 0 && ld % 2 == 0 && T <= 4096)); };
+    p.w_direct = direct(ldw);
     // (a gradient reads H with the rows of ignored tokens cleared, whatever they hold)
-    p.h_direct = !gradient && dtype == DAB_BF16 && D % 8 == 0 && ldh % 8 == 0;
+    p.h_direct = !gradient && direct(ldh);
+    p.tail = D % 8 != 0 && (p.w_direct || p.h_direct);
     p.ldh = p.h_direct ? ldh : round_up(D, 8);
     p.ldw = p.w_direct ? ldw : round_up(D, 8);
     p.h_at = p.h_direct ? 0 : room(static_cast<int64_t>(p.P) * T * p.ldh * 2);
@@ -292,7 +293,7 @@ extern "C" int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t 
     }
     Product16 g{};
     if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &g.A, &g.B)) return rc;
-    g.M = T, g.N = V, g.K = D, g.V = V, g.b_tail = p.w_tail;
+    g.M = T, g.N = V, g.K = D, g.V = V, g.tail = p.tail;
     head_segments(g, p.n_seg);
     g.targets = targets, g.ignore_index = ignore_index;
     g.stats = stats, g.target_logit = target_logit;
@@ -340,7 +341,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         // P of this piece; its columns past the last word are zeros
         Product16 g{};
         head_segments(g, p.n_seg);
-        g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D, g.b_tail = p.w_tail;
+        g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D, g.tail = p.tail;
         g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
         g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.prob_planes;
         if (int rc = launch16(kEpiSoftmax, false, false, g, plan(T, words, D, p.n_seg, 0), st)) return rc;

@@ -34,7 +34,7 @@ constexpr int kStepK = 64;           // k of a step of bf16 operands
 struct Product16 {
     Operand16 A, B;
     int M, N, K;
-    int b_tail;                      // kEpiStats, kEpiSoftmax: B's rows end behind K with what may be anything, not zeros up to 16 bytes
+    int tail;                        // kEpiStats, kEpiSoftmax: rows may hold anything behind K, not zeros up to 16 bytes
     int n_seg;                       // pairs of planes
     uint32_t seg_a, seg_b;           // plane of each pair, four bits a pair
     int tiles_m, tiles_n;

@@ -195,7 +195,7 @@ struct Rows16 {
     }
 };
 
-// NS: steps in LDS.  TAIL: B's rows may hold anything behind K.  PARTS: the tile is one of that many, one above the other, of a tile of the last round.
+// NS: steps in LDS.  TAIL: the operands' rows may hold anything behind K.  PARTS: the tile is one of that many, one above the other, of a tile of the last round.
 template <typename E, int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC, int NS, bool TAIL = false, int PARTS = 1>
 __device__ __forceinline__ void product16(const Product16& g) {
     constexpr int NW = WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
@@ -262,12 +262,13 @@ __device__ __forceinline__ void product16(const Product16& g) {
     };
 
     // An operand that is read where it is has rows of whole words, not of whole pieces: what the last piece of a row holds behind K is
-    // cleared in LDS (the other operand's zeros would not do: it may be a NaN).
-    const int tail = TAIL && g.b_tail && last == g.steps ? static_cast<int>(LB::words(g.K % LB::kPer) / 4) : 0;
+    // cleared in LDS, in both operands (one's zeros would not do: the other's may be a NaN).
+    const int tail = TAIL && g.tail && last == g.steps ? static_cast<int>(LB::words(g.K % LB::kPer) / 4) : 0;
     auto clear = [&](char* buf) {
         const int piece = g.K % kStep / LB::kPer;
-        for (int r = threadIdx.x; r < TN; r += 64 * NW) {
-            uint32_t* at = reinterpret_cast<uint32_t*>(buf + LA::kBytes + r * 128 + (piece ^ ((r >> 1) & 7)) * 16);
+        for (int r = threadIdx.x; r < TM + TN; r += 64 * NW) {
+            // (B's rows follow A's, and both begin a permutation: TM is a multiple of 16)
+            uint32_t* at = reinterpret_cast<uint32_t*>(buf + r * 128 + (piece ^ ((r >> 1) & 7)) * 16);
             for (int u = tail; u < 4; ++u) at[u] = 0;
         }
         wait_and_meet<(NS - 2) * (LA::kCopies + LB::kCopies)>();
@@ -474,7 +475,7 @@ template <int EPI, int TM, int TN, int WM, int WN, bool ARC, bool BRC>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_kernel(Product16 g) {
     product16<bf16, EPI, TM, TN, WM, WN, ARC, BRC, 2>(g);
 }
-// Logits whose words' rows may hold anything behind K; and, as sums that a softmax needs whole are not shared out, whose big tiles of the last round
+// Logits whose operands' rows may hold anything behind K; and, as sums that a softmax needs whole are not shared out, whose big tiles of the last round
 // are taken in four parts.
 template <int EPI, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN / 4) void product16_ends_kernel(Product16 g) {
@@ -593,7 +594,8 @@ int launch_rows32(const float* X, int rows, int cols, int64_t ld, const int64_t*
 constexpr int kBigM = 256, kBigN = 256, kBigWM = 4, kBigWN = 2;
 constexpr int kSmallM = 128, kSmallN = 128, kSmallWM = 2, kSmallWN = 2;
 constexpr int kF32M = 64, kF32N = 128, kF32WM = 2, kF32WN = 2;
-constexpr int kFewM = 32, kFewN = 128, kFewWM = 1, kFewWN = 4;   // of up to 32 rows, and of few tiles (one token's logits, 64000 x 2048: with 64 rows 142 us, which is the matrix cores', with these 88)
+// of up to 32 rows, and of few tiles (one token's logits, 64000 x 2048: with 64 rows 142 us, which is the matrix cores', with these 88)
+constexpr int kFewM = 32, kFewN = 128, kFewWM = 1, kFewWN = 4;
 constexpr bool wide16(Tiles16 kind) { return kind == Tiles16::kF32 || kind == Tiles16::kFew; }
 constexpr int tile_m16(Tiles16 kind) {
     return kind == Tiles16::kBig ? kBigM : kind == Tiles16::kF32 ? kF32M : kind == Tiles16::kFew ? kFewM : kSmallM;
@@ -692,7 +694,7 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
     if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
     g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
     g.whole_xcd = ceil_div(g.whole, kNumXCD), g.rest_xcd = ceil_div(g.rest * g.shares, kNumXCD);
-    const bool ends = g.b_tail || g.shares > 1;
+    const bool ends = g.tail || g.shares > 1;
     const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.tiles, ends)
                         : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.tiles, ends)
                         : arc ? kernel16<kEpiStore, true, true>(pl.tiles, false)
