@@ -4,7 +4,8 @@
 // target's logit; a second, small kernel joins the blocks.  gradient: a piece of the vocabulary at a time, the product again, now
 // written out as P = g (softmax - onehot), and the two products dW = P^T H (the piece's rows of dW, finished) and dH += P W
 // (fp32 until the last piece).  8 T D V flops, two of them for taking the logits twice.  Bound by the matrix cores from a few hundred
-// tokens on (8192 x 2048 -> 131072 in 13.4 ms, 1310 TFLOP/s over all four products; the library's own plain ones of these sizes reach 1140 to 1380), by reading W three times and writing dW once below
+// tokens on (8192 x 2048 -> 131072 in 13.4 ms, 1310 TFLOP/s over all four products; the library's own plain
+// ones of these sizes reach 1140 to 1380), by reading W three times and writing dW once below
 // (one token, 4096 -> 131072, 0.88 ms: 4.9 TB/s).  Small heads: small32.h.
 #include "product16.h"
 #include "small32.h"

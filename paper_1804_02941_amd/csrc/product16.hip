@@ -670,7 +670,10 @@ Plan16 plan32(int M, int N, int K, size_t share_bytes) {
 }
 
 int stats_words16(const Plan16& pl) {
-    return pl.tiles == Tiles16::kF32 ? kF32N / kF32WN : pl.tiles == Tiles16::kFew ? kFewN / kFewWN : pl.tiles == Tiles16::kBig ? kBigN / kBigWN : kSmallN / kSmallWN;
+    return pl.tiles == Tiles16::kF32   ? kF32N / kF32WN
+           : pl.tiles == Tiles16::kFew ? kFewN / kFewWN
+           : pl.tiles == Tiles16::kBig ? kBigN / kBigWN
+                                       : kSmallN / kSmallWN;
 }
 
 template <int EPI, bool ARC, bool BRC>
@@ -704,8 +707,11 @@ int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStre
     if (int rc = launch(kernel, dim3((g.whole_xcd + g.rest_xcd) * kNumXCD), dim3(threads), lds_bytes16(pl.tiles), st, g)) return rc;
     if (pl.shares == 1 || epi != kEpiStore) return DAB_OK;
     const int blocks = tm * tn / 256 / (threads / 64);   // 16 x 16 blocks of a wavefront
-    return launch(pl.tiles == Tiles16::kF32 ? join16_kernel<kF32M, kF32N, kF32WM, kF32WN> : pl.tiles == Tiles16::kFew ? join16_kernel<kFewM, kFewN, kFewWM, kFewWN> : big ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN> : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>,
-                  dim3(g.rest * blocks), dim3(threads), 0, st, g);
+    const auto join = pl.tiles == Tiles16::kF32   ? join16_kernel<kF32M, kF32N, kF32WM, kF32WN>
+                      : pl.tiles == Tiles16::kFew ? join16_kernel<kFewM, kFewN, kFewWM, kFewWN>
+                      : big                       ? join16_kernel<kBigM, kBigN, kBigWM, kBigWN>
+                                                  : join16_kernel<kSmallM, kSmallN, kSmallWM, kSmallWN>;
+    return launch(join, dim3(g.rest * blocks), dim3(threads), 0, st, g);
 }
 
 int init_product16() {
