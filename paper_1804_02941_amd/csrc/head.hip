@@ -101,13 +101,13 @@ static Route head_route(int32_t dtype, int64_t T, int64_t D, int64_t V) {
     const double small = small32_us(dtype, T, D, V);
     if (dtype == DAB_BF16) {
         const int planes = T <= 128 ? 2 : 1;                 // of P (head_plan)
-        const double sums = 2 * plan16(t, v, d, 1, 0).us + plan16(v, d, t, planes, kAnyShares16).us + plan16(planes * t, d, v, 1, kAnyShares16).us;
+        const double sums = 2 * plan16_logits(t, v, d, 1).us + plan16(v, d, t, planes, kAnyShares16).us + plan16(planes * t, d, v, 1, kAnyShares16).us;
         // (the estimates are those of a full chip, where steps take longer; H is copied)
         return small <= 22.5 + 0.78 * sums + 12e-6 * static_cast<double>(T * D) ? Route::kSmall : Route::kPlanes;
     }
-    const double wide = 15.0 + 2 * plan32(t, v, d, 0).us + plan32(v, d, t, kAnyShares16).us + plan32(t, d, v, kAnyShares16).us;
+    const double wide = 15.0 + 2 * plan32_logits(t, v, d).us + plan32(v, d, t, kAnyShares16).us + plan32(t, d, v, kAnyShares16).us;
     // (both calls write and read the planes of H and W)
-    const double planes = 20.0 + 2 * plan16(t, v, d, 6, 0).us + plan16(v, d, t, 6, kAnyShares16).us + plan16(t, d, v, 6, kAnyShares16).us +
+    const double planes = 20.0 + 2 * plan16_logits(t, v, d, 6).us + plan16(v, d, t, 6, kAnyShares16).us + plan16(t, d, v, 6, kAnyShares16).us +
                           2.0 * static_cast<double>((T + V) * D) * 10 / 4e6;
     return small <= wide && small <= planes ? Route::kSmall : wide <= planes ? Route::kWide : Route::kPlanes;
 }
@@ -153,12 +153,12 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         p.ldh = p.h_direct ? ldh : round_up(D, 4), p.ldw = ldw;
         p.h_at = p.h_direct ? 0 : room(T * p.ldh * 4);
         if (!gradient) {
-            p.logits = plan32(T, V, D, 0);
+            p.logits = plan32_logits(T, V, D);
             p.stats_at = room((ceil_div64(V, stats_words16(p.logits)) + 8) * T * 8);
             p.target_at = room(static_cast<int64_t>(T) * 4);
         } else {
             head_pieces(p, T, D, V, 4);
-            p.logits = plan32(T, p.piece, D, 0);
+            p.logits = plan32_logits(T, p.piece, D);
             p.dh = plan32(T, D, p.piece, kAnyShares16), p.dw = plan32(p.piece, D, T, kAnyShares16);
             p.p_at = room(static_cast<int64_t>(T) * p.ldp * 4);
             p.acc_at = room(p.n_pieces > 1 ? static_cast<int64_t>(T) * D * 4 : 0);
@@ -183,7 +183,7 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
     p.h_at = p.h_direct ? 0 : room(static_cast<int64_t>(p.P) * T * p.ldh * 2);
     p.w_at = p.w_direct ? 0 : room(static_cast<int64_t>(p.P) * V * p.ldw * 2);
     if (!gradient) {
-        p.logits = plan16(T, V, D, p.n_seg, 0);
+        p.logits = plan16_logits(T, V, D, p.n_seg);
         const int words = stats_words16(p.logits);
         p.stats_at = room((ceil_div64(V, words) + 8) * T * 8);
         p.target_at = room(static_cast<int64_t>(T) * 4);
@@ -194,7 +194,7 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         p.stacked = p.P == 1 && T <= 128;
         p.prob_planes = p.stacked ? 2 : p.P;
         head_pieces(p, T, D, V, 2 * p.prob_planes);
-        p.logits = plan16(T, p.piece, D, p.n_seg, 0);
+        p.logits = plan16_logits(T, p.piece, D, p.n_seg);
         p.dh = plan16(p.stacked ? 2 * T : T, D, p.piece, p.n_seg, kAnyShares16);
         p.dw = plan16(p.piece, D, T, p.stacked ? 2 : p.n_seg, kAnyShares16);
         p.p_at = room(static_cast<int64_t>(p.prob_planes) * T * p.ldp * 2);
@@ -298,7 +298,7 @@ extern "C" int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t 
     head_segments(g, p.n_seg);
     g.targets = targets, g.ignore_index = ignore_index;
     g.stats = stats, g.target_logit = target_logit;
-    if (int rc = launch16(kEpiStats, false, false, g, p.logits, st)) return rc;
+    if (int rc = launch16(kEpiStats, false, false, g, p.logits, 0, st)) return rc;
     const int blocks = ceil_div(V, stats_words16(p.logits));
     return launch_head_join(st, stats, target_logit, targets, ignore_index, T, V, blocks, loss, lse);
 }
@@ -334,8 +334,8 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
     const Operand16 probs = {P, p.ldp, static_cast<int64_t>(T) * p.ldp};
     const int64_t size = dtype_bytes(dtype);
     const int64_t w_size = p.wide ? 4 : 2;
-    auto plan = [&](int M, int N, int K, int n_seg, size_t room) { return p.wide ? plan32(M, N, K, room) : plan16(M, N, K, n_seg, room); };
-    const size_t shares = p.part_bytes;                      // room for sums in shares, of the last and smaller piece too
+    // (the last, smaller piece has its own plans; their shares have the room that the others' take)
+    auto plan = [&](int M, int N, int K, int n_seg) { return p.wide ? plan32(M, N, K, p.part_bytes) : plan16(M, N, K, n_seg, p.part_bytes); };
     for (int i = 0; i < p.n_pieces; ++i) {
         const int v0 = i * p.piece, words = V - v0 < p.piece ? V - v0 : p.piece;
         const Operand16 wp = {static_cast<const char*>(w.p) + v0 * w.ld * w_size, w.ld, w.plane};
@@ -345,7 +345,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D, g.tail = p.tail;
         g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
         g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.prob_planes;
-        if (int rc = launch16(kEpiSoftmax, false, false, g, plan(T, words, D, p.n_seg, 0), st)) return rc;
+        if (int rc = launch16(kEpiSoftmax, false, false, g, p.wide ? plan32_logits(T, words, D) : plan16_logits(T, words, D, p.n_seg), 0, st)) return rc;
         // the piece's rows of dW
         Product16 q{};
         head_segments(q, p.n_seg);
@@ -353,7 +353,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         q.A = probs, q.B = h, q.M = words, q.N = D, q.K = T;
         q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
         q.part = reinterpret_cast<float*>(base + p.part_at);
-        if (int rc = launch16(kEpiStore, true, true, q, plan(words, D, T, q.n_seg, shares), st)) return rc;
+        if (int rc = launch16(kEpiStore, true, true, q, plan(words, D, T, q.n_seg), p.part_bytes, st)) return rc;
         // its share of dH
         const bool last = i + 1 == p.n_pieces && !p.stacked;
         Product16 s{};
@@ -362,7 +362,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         s.add = i ? acc : nullptr;
         s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16;
         s.part = q.part;
-        if (int rc = launch16(kEpiStore, false, true, s, plan(s.M, D, words, p.n_seg, shares), st)) return rc;
+        if (int rc = launch16(kEpiStore, false, true, s, plan(s.M, D, words, p.n_seg), p.part_bytes, st)) return rc;
     }
     if (!p.stacked) return DAB_OK;
     return launch(head_unstack_kernel, dim3(ceil_div(T * D, 256)), dim3(256), 0, st, acc, T * D, static_cast<bf16*>(dH));

@@ -71,11 +71,15 @@ struct Plan16 {
     double us;                       // estimated time
 };
 constexpr size_t kAnyShares16 = ~size_t{0};
-// share_bytes: room for the sums of shares (0: the whole sum in one workgroup)
+// Of a product whose result is stored; share_bytes: room for the sums of shares (0: every sum whole in one workgroup).
 Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes);
-// The same for fp32 operands.
+// Of logits: a softmax needs its sums whole, and its kernels take the last round's big tiles in parts (kParts16) instead.
+Plan16 plan16_logits(int M, int N, int K, int n_seg);
+// The same two for fp32 operands.
 Plan16 plan32(int M, int N, int K, size_t share_bytes);
-int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st);
+inline Plan16 plan32_logits(int M, int N, int K) { return plan32(M, N, K, 0); }
+// part_bytes: room at g.part; DAB_ERR_UNSUPPORTED if the plan's shares do not fit it.
+int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, size_t part_bytes, hipStream_t st);
 int stats_words16(const Plan16& pl);           // words of the vocabulary per pair of the stats
 int init_product16();
 // fp32 rows ldp apart (a multiple of 4, zeros behind the last element), those of tokens without a loss cleared (targets may be NULL)

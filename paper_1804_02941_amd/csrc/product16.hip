@@ -605,9 +605,9 @@ constexpr int tile_n16(Tiles16 kind) {
 }
 constexpr size_t lds_bytes16(Tiles16 kind) { return (kind == Tiles16::kDeep ? size_t{4} : size_t{2}) * (tile_m16(kind) + tile_n16(kind)) * 128; }
 
-// Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares (or, with
-// no room for those, parts of tiles) where that takes less.
-static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t share_bytes) {
+// Time of a product in one kind of tiles, in microseconds: rounds of workgroups over the compute units, the last of them in shares (or, of
+// logits, parts of tiles) where that takes less.
+static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t share_bytes, bool logits) {
     // Workgroups that a compute unit runs together; a step's time with all of them there, that of one alone (fp32 products are bound by the
     // matrix cores, which the workgroups share), and that of a tile's beginning and end: those of long sums on a full chip, of
     // the deep form of few tiles.
@@ -644,28 +644,30 @@ static Plan16 plan16_of(Tiles16 kind, int M, int N, int K, int n_seg, size_t sha
         const double us = round(pl.rest * s, per) + 4.0 + 2.0 * pl.rest * s * tile_bytes / 4e6;
         if (us < best) best = us, pl.shares = s, pl.share_steps = per;
     }
-    if (kind == Tiles16::kBig && share_bytes == 0) {
+    if (kind == Tiles16::kBig && logits) {
         // a quarter of a tile: two fifths of its time, as all its columns are fetched and read
         const double us = ceil_div(pl.rest * kParts16, slots) * (pl.steps * 0.65 + 4.0);
         if (us < best) best = us, pl.shares = kParts16;
     }
     pl.us += best;
     if (pl.shares == 1) pl.whole = static_cast<int>(tiles), pl.rest = 0;
-    pl.part_bytes = pl.shares > 1 && share_bytes ? static_cast<size_t>(pl.rest) * pl.shares * tile_bytes : 0;
+    pl.part_bytes = pl.shares > 1 && !logits ? static_cast<size_t>(pl.rest) * pl.shares * tile_bytes : 0;
     return pl;
 }
 
-Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes) {
-    Plan16 best = plan16_of(Tiles16::kBig, M, N, K, n_seg, share_bytes);
+static Plan16 plan16_best(int M, int N, int K, int n_seg, size_t share_bytes, bool logits) {
+    Plan16 best = plan16_of(Tiles16::kBig, M, N, K, n_seg, share_bytes, logits);
     for (const Tiles16 kind : {Tiles16::kSmall, Tiles16::kDeep}) {
-        const Plan16 pl = plan16_of(kind, M, N, K, n_seg, share_bytes);
+        const Plan16 pl = plan16_of(kind, M, N, K, n_seg, share_bytes, logits);
         if (pl.us < best.us) best = pl;
     }
     return best;
 }
+Plan16 plan16(int M, int N, int K, int n_seg, size_t share_bytes) { return plan16_best(M, N, K, n_seg, share_bytes, false); }
+Plan16 plan16_logits(int M, int N, int K, int n_seg) { return plan16_best(M, N, K, n_seg, 0, true); }
 
 Plan16 plan32(int M, int N, int K, size_t share_bytes) {
-    const Plan16 few = plan16_of(Tiles16::kFew, M, N, K, 1, share_bytes), all = plan16_of(Tiles16::kF32, M, N, K, 1, share_bytes);
+    const Plan16 few = plan16_of(Tiles16::kFew, M, N, K, 1, share_bytes, false), all = plan16_of(Tiles16::kF32, M, N, K, 1, share_bytes, false);
     return few.us < all.us ? few : all;
 }
 
@@ -690,13 +692,15 @@ static auto kernel16(Tiles16 kind, bool ends) {
                                     : product16_kernel<EPI, kSmallM, kSmallN, kSmallWM, kSmallWN, ARC, BRC>;
 }
 
-int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, hipStream_t st) {
+int launch16(int epi, bool arc, bool brc, Product16 g, const Plan16& pl, size_t part_bytes, hipStream_t st) {
     const bool big = pl.tiles == Tiles16::kBig;
     const int tm = tile_m16(pl.tiles), tn = tile_n16(pl.tiles);
     g.tiles_m = ceil_div(g.M, tm), g.tiles_n = ceil_div(g.N, tn);
     if (static_cast<int64_t>(g.tiles_m) * g.tiles_n > INT32_MAX / 64) return DAB_ERR_UNSUPPORTED;
     g.steps = pl.steps, g.whole = pl.whole, g.rest = pl.rest, g.shares = pl.shares, g.share_steps = pl.share_steps;
     g.whole_xcd = ceil_div(g.whole, kNumXCD), g.rest_xcd = ceil_div(g.rest * g.shares, kNumXCD);
+    // (the sums of shares go to g.part: never past the room that the caller has there)
+    if (epi == kEpiStore && g.shares > 1 && static_cast<uint64_t>(g.rest) * g.shares * tm * tn * 4 > part_bytes) return DAB_ERR_UNSUPPORTED;
     const bool ends = g.tail || g.shares > 1;
     const auto kernel = epi == kEpiStats ? kernel16<kEpiStats, false, false>(pl.tiles, ends)
                         : epi == kEpiSoftmax ? kernel16<kEpiSoftmax, false, false>(pl.tiles, ends)
@@ -831,5 +835,5 @@ extern "C" int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t 
     g.seg_a = 0x210;                 // pieces of dY in turn, with the one plane of X
     g.C = dW, g.ldc = cols;
     g.part = reinterpret_cast<float*>(base + p.part_at);
-    return launch16(kEpiStore, true, true, g, p.pl, st);
+    return launch16(kEpiStore, true, true, g, p.pl, p.bytes - p.part_at, st);
 }
