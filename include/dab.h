@@ -507,6 +507,8 @@ int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t lddy, const
  *            NaN, and its token no part in any gradient.
  *   loss     [T] fp32 out, lse [T] fp32 out (0 for an ignored token)
  *   ws       dab_head_loss_workspace_bytes(...) bytes, 256-byte aligned
+ * A NaN in a token's row of H, or in any row of W, gives that token (every token) a loss and an lse of NaN.  Words whose logits are minus
+ * infinity have probability 0; but where fp32 inputs are multiplied as pieces an infinity in H or W gives NaN.
  */
 size_t dab_head_loss_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw);
 int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,

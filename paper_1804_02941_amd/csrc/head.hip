@@ -12,12 +12,13 @@
 
 namespace dab {
 
-// Maxima and sums of exponentials of two sets of words as those of both.  (A set of minus infinities alone adds nothing, and
-// exp of its difference would be undefined.)
+// The sum of exponentials of a set of words, from its own maximum to `top`.  A set without a maximum keeps its sum, which is 0 if all of
+// its logits are minus infinity (exp of the difference would be undefined) and NaN if one of them is: maxima drop NaNs, sums never.
+__device__ __forceinline__ float sum_at(float2 s, float top) { return s.x == -__builtin_inff() ? s.y : s.y * expf(s.x - top); }
+// Maxima and sums of exponentials of two sets of words as those of both.
 __device__ __forceinline__ float2 join_stats(float2 a, float2 b) {
     const float top = fmaxf(a.x, b.x);
-    const float sa = a.x == -__builtin_inff() ? 0.f : a.y * expf(a.x - top), sb = b.x == -__builtin_inff() ? 0.f : b.y * expf(b.x - top);
-    return float2{top, sa + sb};
+    return float2{top, sum_at(a, top) + sum_at(b, top)};
 }
 
 // TT tokens a workgroup, 256 / TT threads each, eight pairs on their way at a time: many tokens take whole lines of the pairs, few
@@ -40,9 +41,9 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2* __restrict
                 s[k] = i + k * kParts < blocks ? stats[static_cast<int64_t>(i + k * kParts) * T + t] : none;
                 top = fmaxf(top, s[k].x);
             }
-            float sum = all.x == -__builtin_inff() ? 0.f : all.y * expf(all.x - top);
+            float sum = sum_at(all, top);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += s[k].x == -__builtin_inff() ? 0.f : s[k].y * expf(s[k].x - top);
+            for (int k = 0; k < 8; ++k) sum += sum_at(s[k], top);
             all = float2{top, sum};
         }
     part[u][tt] = all;
