@@ -525,7 +525,7 @@ int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_
  *
  *   lse      [T] fp32 of dab_head_loss for the same H, W, targets
  *   g        [T] fp32, or NULL for 1
- *   dH       [T][D] of dtype out (zero rows for ignored tokens), dW [V][D] of dtype out
+ *   dH       [T][D] of dtype out (zero rows for tokens without a loss, whatever W holds), dW [V][D] of dtype out
  */
 size_t dab_head_loss_gradient_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw);
 int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,

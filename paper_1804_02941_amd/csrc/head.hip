@@ -65,10 +65,11 @@ static int launch_head_join(hipStream_t st, const float2* stats, const float* ta
     return launch(head_join_kernel<4>, dim3(ceil_div(T, 4)), dim3(256), 0, st, stats, target_logit, targets, ignore, T, V, blocks, loss, lse);
 }
 
-// dH from the products with P's two planes.
-__global__ __launch_bounds__(256) void head_unstack_kernel(const float* __restrict__ acc, int n, bf16* __restrict__ dH) {
+// dH from the products with P's two planes, n entries of D a token.
+__global__ __launch_bounds__(256) void head_unstack_kernel(const float* __restrict__ acc, int n, bf16* __restrict__ dH, int D,
+                                                           const int64_t* __restrict__ targets, int64_t ignore, int V) {
     const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n) dH[i] = static_cast<bf16>(acc[i] + acc[n + i]);
+    if (i < n) dH[i] = static_cast<bf16>(no_loss(targets[i / D], ignore, V) ? 0.f : acc[i] + acc[n + i]);
 }
 
 struct HeadPlan {
@@ -326,6 +327,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         q.M = V, q.N = D, q.K = T, q.tiles_n = ceil_div(D, kSmallTile), q.C = dW, q.ldc = D, q.dtype = dtype;
         s.A = {P, p.ldp, T, nullptr, 0, 0}, s.B = {W, ldw, D, nullptr, 0, 0};
         s.M = T, s.N = D, s.K = V, s.tiles_n = q.tiles_n, s.C = dH, s.ldc = D, s.dtype = dtype;
+        s.targets = targets, s.ignore_index = ignore_index;
         return launch_small_gradients(q, s, dtype, st);
     }
     Operand16 h, w;
@@ -362,9 +364,10 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         s.A = probs, s.B = wp, s.M = p.stacked ? 2 * T : T, s.N = D, s.K = words;
         s.add = i ? acc : nullptr;
         s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16;
+        if (last) s.targets = targets, s.ignore_index = ignore_index, s.V = V;
         s.part = q.part;
         if (int rc = launch16(kEpiStore, false, true, s, plan(s.M, D, words, p.n_seg), p.part_bytes, st)) return rc;
     }
     if (!p.stacked) return DAB_OK;
-    return launch(head_unstack_kernel, dim3(ceil_div(T * D, 256)), dim3(256), 0, st, acc, T * D, static_cast<bf16*>(dH));
+    return launch(head_unstack_kernel, dim3(ceil_div(T * D, 256)), dim3(256), 0, st, acc, T * D, static_cast<bf16*>(dH), D, targets, ignore_index, V);
 }

@@ -47,6 +47,7 @@ struct Product16 {
     int64_t ldc;
     int out_bf16;
     const float* add;                // fp32 [M][N] added to the sum, or NULL
+                                     // (and `targets`, or NULL: rows m of tokens without a loss are stored as zeros)
     float* part;                     // [rest][shares][tile] sums of the shares, in the order of the accumulators
     // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece
     const int64_t* targets;

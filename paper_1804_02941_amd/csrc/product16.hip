@@ -150,6 +150,8 @@ __device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v)
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] += n + r < g.N ? from[r] : 0.f;
     }
+    // (not their products: P's zeros times a word that is no number are not 0)
+    if (g.targets && no_loss(g.targets[m], g.ignore_index, g.V)) v = v4f{0.f, 0.f, 0.f, 0.f};
     if (g.out_bf16) store4(static_cast<bf16*>(g.C) + m * g.ldc + n, v, g.N - n);
     else store4(static_cast<float*>(g.C) + m * g.ldc + n, v, g.N - n);
 }
@@ -453,6 +455,10 @@ __device__ __forceinline__ void product16(const Product16& g) {
                 *reinterpret_cast<v4f*>(g.part + ((static_cast<int64_t>(tile - g.whole) * g.shares + share) * (FN * FM) + i * FM + j) * (256 * NW) +
                                         threadIdx.x * 4) = acc[i][j];
         } else if (!g.add) {
+            if (g.targets && no_loss(g.targets[min(m, g.M - 1)], g.ignore_index, g.V)) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+            }
             if (g.out_bf16) {
                 const Rows16<bf16, FN> out{mine, lane};
 #pragma unroll

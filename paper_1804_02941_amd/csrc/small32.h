@@ -24,7 +24,7 @@ struct Small32 {
     void* C;                         // results of dtype (DAB_F32 or DAB_BF16), rows ldc apart
     int64_t ldc;
     int dtype;
-    // softmax: m is a token, n a word
+    // softmax: m is a token, n a word; gradients: m is a token, k a word, and rows of tokens without a loss are stored as zeros (NULL: none)
     const int64_t* targets;
     int64_t ignore_index;
     float2* stats;                   // [ceil(N / 32)][M]

@@ -108,6 +108,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void small_softmax_kernel(Small32
 __device__ __forceinline__ void small_store(const Small32& g, int m0, int n0, float2 v) {
     const int m = m0 + (threadIdx.x >> 4), n = n0 + (threadIdx.x & 15) * 2;
     if (m >= g.M) return;
+    // (not its product: P's zeros times a word that is no number are not 0)
+    if (g.targets && no_loss(g.targets[m], g.ignore_index, g.K)) v = float2{0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         if (n + u >= g.N) return;

@@ -100,6 +100,7 @@ void product(const std::string& k, const std::vector<int>& t, const Product16& g
         if (g.shares > 1) write(k, range(g.part, 1ull * g.rest * g.shares * TM * TN * 4, "sums of shares"));
         if (g.rest && (g.share_steps < 1 || 1ll * g.share_steps * g.shares < g.steps || 1ll * g.share_steps * (g.shares - 1) >= g.steps)) fault(k, "shares that do not cover the sum once");
         if (g.add) read(k, range(g.add, 4ull * M * N, "sums of the pieces before"));
+        if (g.targets) read(k, range(g.targets, 8ull * M, "targets"));
         if (g.whole || g.shares == 1) write(k, range(g.C, (1ull * (M - 1) * static_cast<unsigned long long>(g.ldc) + N) * (g.out_bf16 ? 2 : 4), "result"));
         return;
     }
@@ -158,6 +159,7 @@ void launched(const void* f, dim3 grid, dim3 block, void** a) {
     } else if (is("head_unstack_kernel")) {
         const unsigned long long n = argument<int>(a, 1);
         read(k, range(argument<void*>(a, 0), 8 * n, "sums of both planes"));
+        read(k, range(argument<void*>(a, 4), 8 * (n / argument<int>(a, 3)), "targets"));
         write(k, range(argument<void*>(a, 2), 2 * n, "dH"));
     } else if (is("small_stats_kernel") || is("small_softmax_kernel")) {
         const Small32 g = argument<Small32>(a, 0);
@@ -172,6 +174,7 @@ void launched(const void* f, dim3 grid, dim3 block, void** a) {
         for (int i = 0; i < 2; ++i) {
             const Small32 g = argument<Small32>(a, i);
             small(k, g, 4, i == 0, f32 ? 4 : 2, true);
+            if (g.targets) read(k, range(g.targets, 8ull * g.M, "targets"));
             write(k, range(g.C, (g.dtype == DAB_F32 ? 4ull : 2ull) * (static_cast<unsigned long long>(g.M - 1) * g.ldc + g.N), "result"));
         }
     } else if (is("grad_operands_kernel")) {

@@ -81,3 +81,22 @@ def test_infinities_among_fp32_words_never_give_a_wrong_number():
     """Products of pieces have no infinite logits: an infinity's products with the pieces of a number have both signs, or are undefined."""
     loss, lse, want, ref, tol = no_weight(torch.float32, MANY)
     assert bool((((lse - ref).abs() <= tol) | torch.isnan(lse)).all()) and bool((((loss - want).abs() <= tol) | torch.isnan(loss)).all())
+
+
+# and a vocabulary in several pieces, with and without shares of dH's sums
+IGNORED = CASES + [(torch.bfloat16, (4100, 64, 70001)), (torch.bfloat16, (70000, 40, 4099)), (torch.bfloat16, (129, 2000, 9001)), (torch.float32, (4100, 64, 70001))]
+
+
+@pytest.mark.parametrize("value", [NAN, float("inf")])
+@pytest.mark.parametrize("dtype,sizes", IGNORED)
+def test_tokens_without_a_loss_have_no_gradient_whatever_the_words_hold(dtype, sizes, value):
+    T, D, V = sizes
+    H, W, t = case(dtype, sizes)
+    t[2::7] = V
+    t[3::11] = -1
+    t[-1] = -100
+    W[V // 3] = value
+    _, lse = dab.dab_head_loss(H, W, t)
+    dH, _ = dab.dab_head_loss_gradient(H, W, t, lse)
+    dead = (t < 0) | (t >= V)
+    assert not bool(dH[dead].any()) and not bool(torch.isfinite(dH[~dead]).any())
