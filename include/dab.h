@@ -482,7 +482,8 @@ int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows, int32_t c
  * input: dW[f][c] = sum over rows of dY[row][f] * (q 2^e)[row][c], which is what dab_weight_gradient takes as
  * `upstream` for a binarized layer.  On the matrix cores in bf16: the saved values are bf16 numbers, a
  * bf16 gradient is used as it is, an f16 one as the sum of two bf16 numbers and an fp32 one as the sum of
- * three, so that every product is exact and only the fp32 accumulation rounds.
+ * three, so that every product is exact (pieces have steps of 2^-133) and only the fp32 accumulation rounds.  Infinities and NaN in dY come
+ * out as in the sum itself.
  *
  *   dY   [rows][F] of dtype, rows lddy apart;   dW  fp32 [F][cols] out
  *   ws   dab_ckpt8_weight_gradient_workspace_bytes(...) bytes, 256-byte aligned
@@ -508,7 +509,7 @@ int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t lddy, const
  *   loss     [T] fp32 out, lse [T] fp32 out (0 for an ignored token)
  *   ws       dab_head_loss_workspace_bytes(...) bytes, 256-byte aligned
  * A NaN in a token's row of H, or in any row of W, gives that token (every token) a loss and an lse of NaN.  Words whose logits are minus
- * infinity have probability 0; but where fp32 inputs are multiplied as pieces an infinity in H or W gives NaN.
+ * infinity have probability 0; but where fp32 inputs are multiplied as pieces an infinity in H or W may give NaN.
  */
 size_t dab_head_loss_workspace_bytes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw);
 int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype, const int64_t* targets,
@@ -554,7 +555,7 @@ int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, floa
  * dab_w4_matvec - Y[b][f] = sum_k X[b][k] W[f][k] with packed weights, for one token or a few (any B is right; the
  * weights are read once for every 48 bf16, 24 f16 or 16 fp32 tokens).  On the matrix cores in bf16, which hold a 4-bit weight times its
  * scale exactly; f16 inputs are sums of two bf16 numbers, fp32 ones of three: only the fp32 accumulation
- * rounds, and a 16-bit Y once more.
+ * rounds, and a 16-bit Y once more.  Infinities and NaN in X come out as in the sum itself.
  *
  *   X   [B][K] of dtype, rows ldx apart;  Y  [B][F] of dtype out
  *   ws  dab_w4_matvec_workspace_bytes(...) bytes, 256-byte aligned (0 for up to 16 bf16

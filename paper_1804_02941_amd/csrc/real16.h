@@ -98,12 +98,18 @@ __device__ __forceinline__ int group_exponent(uint32_t m) {
 // Whether a token has no part in the loss.
 __device__ __forceinline__ bool no_loss(int64_t target, int64_t ignore, int V) { return target == ignore || target < 0 || target >= V; }
 
-// Piece `which` of the bf16 numbers whose sum x is: x rounded, what is left rounded, what is left then.
+// x without what a bf16 number does not hold.
+__device__ __forceinline__ float cut16(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+// Piece `which` of the bf16 numbers whose sum x is: x rounded, what is left rounded, what is left then.  Numbers that would round to infinity are
+// cut instead, and so is what is left of them, so that no sum of their pieces passes fp32's last number; of an infinity and of a NaN nothing
+// is left behind the first piece (their difference would be undefined).
 __device__ __forceinline__ bf16 piece_of(float x, int which) {
-    const bf16 a = static_cast<bf16>(x);
+    const uint32_t size = __float_as_uint(x) & 0x7fffffffu;
+    const bool finite = size < 0x7f800000u, last = finite && size >= 0x7f7f8000u;
+    const bf16 a = static_cast<bf16>(last ? cut16(x) : x);
     if (which == 0) return a;
-    const float r = x - static_cast<float>(a);
-    const bf16 b = static_cast<bf16>(r);
+    const float r = finite ? x - static_cast<float>(a) : 0.f;
+    const bf16 b = static_cast<bf16>(last ? cut16(r) : r);
     if (which == 1) return b;
     return static_cast<bf16>(r - static_cast<float>(b));
 }
