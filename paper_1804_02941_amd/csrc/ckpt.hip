@@ -19,7 +19,7 @@ struct Rows8 {
 
 // Row and first column of this lane's eight values; false past the end.
 __device__ __forceinline__ bool my_eight(const Rows8& g, int* row, int* c) {
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kSaveWaves + (threadIdx.x >> 6);
+    const int64_t unit = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kSaveWaves + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     const int64_t block = unit / g.row_parts;
     const int part = static_cast<int>(unit - block * g.row_parts);
@@ -88,11 +88,13 @@ static int check_rows(const void* X, int32_t dtype, int32_t rows, int32_t cols, 
     return DAB_OK;
 }
 
-// Workgroups of a pass; 0 if they are more than a launch takes.
-static unsigned save_grid(const Rows8& g) {
+// Workgroups of a pass, in lines (a grid has fewer than 2^32 threads along its first dimension); of no threads if they are more than a launch
+// takes.
+static dim3 save_grid(const Rows8& g) {
+    constexpr int64_t kLine = 1 << 23;
     const int64_t units = ceil_div64(g.rows, int64_t{1} << (6 - g.lanes_log2)) * g.row_parts;
-    const int64_t n = ceil_div64(units, kSaveWaves);
-    return n <= INT32_MAX ? static_cast<unsigned>(n) : 0;
+    const int64_t n = ceil_div64(units, kSaveWaves), lines = ceil_div64(n, kLine);
+    return lines <= 65535 ? dim3(static_cast<unsigned>(n < kLine ? n : kLine), static_cast<unsigned>(lines)) : dim3(0);
 }
 
 }  // namespace dab
@@ -102,13 +104,13 @@ extern "C" int dab_ckpt8_save(const void* X, int32_t dtype, int32_t rows, int32_
     using namespace dab;
     if (int rc = check_rows(X, dtype, rows, cols, ldx, Q, S)) return rc;
     const Rows8 g = rows8_of(rows, cols, ldx);
-    const unsigned grid = save_grid(g);
-    if (grid == 0) return DAB_ERR_UNSUPPORTED;
+    const dim3 grid = save_grid(g);
+    if (grid.x == 0) return DAB_ERR_UNSUPPORTED;
     const auto st = static_cast<hipStream_t>(stream);
     const dim3 block(64 * kSaveWaves);
-    if (dtype == DAB_F32) return launch(ckpt8_save_kernel<float>, dim3(grid), block, 0, st, static_cast<const float*>(X), g, Q, S);
-    if (dtype == DAB_BF16) return launch(ckpt8_save_kernel<bf16>, dim3(grid), block, 0, st, static_cast<const bf16*>(X), g, Q, S);
-    return launch(ckpt8_save_kernel<f16>, dim3(grid), block, 0, st, static_cast<const f16*>(X), g, Q, S);
+    if (dtype == DAB_F32) return launch(ckpt8_save_kernel<float>, grid, block, 0, st, static_cast<const float*>(X), g, Q, S);
+    if (dtype == DAB_BF16) return launch(ckpt8_save_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(X), g, Q, S);
+    return launch(ckpt8_save_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(X), g, Q, S);
 }
 
 extern "C" int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows, int32_t cols, void* X, int32_t dtype, int64_t ldx,
@@ -116,11 +118,11 @@ extern "C" int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows
     using namespace dab;
     if (int rc = check_rows(X, dtype, rows, cols, ldx, Q, S)) return rc;
     const Rows8 g = rows8_of(rows, cols, ldx);
-    const unsigned grid = save_grid(g);
-    if (grid == 0) return DAB_ERR_UNSUPPORTED;
+    const dim3 grid = save_grid(g);
+    if (grid.x == 0) return DAB_ERR_UNSUPPORTED;
     const auto st = static_cast<hipStream_t>(stream);
     const dim3 block(64 * kSaveWaves);
-    if (dtype == DAB_F32) return launch(ckpt8_restore_kernel<float>, dim3(grid), block, 0, st, Q, S, g, static_cast<float*>(X));
-    if (dtype == DAB_BF16) return launch(ckpt8_restore_kernel<bf16>, dim3(grid), block, 0, st, Q, S, g, static_cast<bf16*>(X));
-    return launch(ckpt8_restore_kernel<f16>, dim3(grid), block, 0, st, Q, S, g, static_cast<f16*>(X));
+    if (dtype == DAB_F32) return launch(ckpt8_restore_kernel<float>, grid, block, 0, st, Q, S, g, static_cast<float*>(X));
+    if (dtype == DAB_BF16) return launch(ckpt8_restore_kernel<bf16>, grid, block, 0, st, Q, S, g, static_cast<bf16*>(X));
+    return launch(ckpt8_restore_kernel<f16>, grid, block, 0, st, Q, S, g, static_cast<f16*>(X));
 }

@@ -19,10 +19,13 @@ inline int hip_failed(hipError_t e) {
 }
 
 // Enqueues one kernel and returns the status of that launch call itself (not the thread's last
-// error, which may stem from HIP work that is not this library's).
+// error, which may stem from HIP work that is not this library's).  A launch has fewer than 2^32 threads along a dimension: one of
+// more is refused here, as the runtime takes it and runs only what is left of the number in 32 bits.
 template <typename... KArgs, typename... Args>
 inline int launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t lds_bytes, hipStream_t st, const Args&... args) {
     static_assert(sizeof...(KArgs) == sizeof...(Args), "one argument per kernel parameter");
+    if ((static_cast<uint64_t>(grid.x) * block.x | static_cast<uint64_t>(grid.y) * block.y | static_cast<uint64_t>(grid.z) * block.z) >> 32)
+        return DAB_ERR_UNSUPPORTED;
     std::tuple<KArgs...> vals(static_cast<KArgs>(args)...);
     return std::apply(
         [&](auto&... v) {

@@ -274,6 +274,19 @@ int matvec(int B, int K, int F, int dtype, long long ldx) {
     begin(text, {X}, {Y}, n);
     return finish(dab_w4_matvec(at(X), dtype, ldx, reinterpret_cast<uint8_t*>(1ull << 47), reinterpret_cast<uint8_t*>(3ull << 47), B, K, F, at(Y), n ? at(now.ws) : nullptr, n, nullptr));
 }
+// Launches of 2^32 threads along a dimension are refused, those of fewer are not.
+void kernel_of_nothing() {}
+int too_many_threads() {
+    int bad = 0;
+    for (const dim3 grid : {dim3(1u << 24), dim3(1, 1u << 24), dim3((1u << 24) + 3, 2), dim3(0xffffffffu)}) {
+        now = Call{};
+        bad += dab::launch(kernel_of_nothing, grid, dim3(256, 256), 0, nullptr) != DAB_ERR_UNSUPPORTED || now.launches != 0;
+    }
+    now = Call{};
+    bad += dab::launch(kernel_of_nothing, dim3((1u << 24) - 1, 65535), dim3(256), 0, nullptr) != DAB_OK || now.launches != 1;
+    if (bad) std::printf("launches of too many threads: %d\n", bad);
+    return bad;
+}
 // A plan whose shares have less room than they need is refused before anything is launched.
 int refusal() {
     const dab::Plan16 pl = dab::plan16(300, 300, 100000, 1, dab::kAnyShares16);
@@ -296,7 +309,7 @@ int main(int argc, char** argv) {
     }
     const int cases = argc > 1 ? num(1) : 20000;
     g_state = 977ull * static_cast<unsigned long long>(argc > 2 ? num(2) : 1) + 1;
-    int bad = refusal();
+    int bad = refusal() + too_many_threads();
     for (int i = 0; i < cases; ++i) {
         const int T = whole(1, 32768), D = whole(1, 16384), V = whole(1, 262144), dtype = uniform() < 0.6 ? DAB_BF16 : DAB_F32;
         auto apart = [&](int n) { return uniform() < 0.7 ? static_cast<long long>(n) : n + whole(1, 200); };

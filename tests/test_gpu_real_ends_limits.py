@@ -1,0 +1,23 @@
+"""Saved inputs of more rows than one launch has threads for (2^32 along a grid's first dimension)."""
+import pytest
+import torch
+
+from paper_1804_02941_amd import binding as dab
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def test_save_and_restore_of_more_rows_than_a_grid_has_along_one_dimension():
+    rows = (1 << 30) + 70                                          # 64 rows of one channel a workgroup of 256
+    X = torch.empty((rows, 1), dtype=torch.bfloat16, device=DEV).normal_()
+    Q, S = dab.dab_ckpt8_save(X)
+    back = dab.dab_ckpt8_restore(Q, S, 1, torch.bfloat16)
+    # a lone number is kept to 7 bits, halves to even: as the same rows are in calls of few
+    for at in range(0, rows, 1 << 27):
+        part = slice(at, min(at + (1 << 27), rows))
+        q, s = dab.dab_ckpt8_save(X[part])
+        assert torch.equal(Q[part], q) and torch.equal(S[part], s)
+        assert torch.equal(back[part], dab.dab_ckpt8_restore(q, s, 1, torch.bfloat16))
+    assert float((back.float() - X.float()).abs().max()) <= 2.0 ** -7 * float(X.abs().max())
