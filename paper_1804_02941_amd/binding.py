@@ -535,6 +535,13 @@ def dab_wbin_fc(X, E_packed, alpha, beta, out=None, ws=None):
 _REAL = {torch.float32: DAB_F32, torch.bfloat16: DAB_BF16, torch.float16: DAB_F16}
 
 
+def _counted(t, name):
+    """t, a matrix whose rows and columns the C calls' 32-bit sizes count (ctypes would pass the lower bits of larger ones)."""
+    if max(t.shape) > 2 ** 31 - 1:
+        raise ValueError(f"{name}: expected at most {2 ** 31 - 1} rows and columns, got {tuple(t.shape)}")
+    return t
+
+
 def _matrix(t, name):
     """(address, element type, distance of the rows) of a matrix on the GPU whose rows are contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -546,6 +553,7 @@ def _matrix(t, name):
     rows, cols = t.shape
     if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
         raise ValueError(f"{name}: the elements of a row must be contiguous and rows apart")
+    _counted(t, name)
     return t.data_ptr(), _REAL[t.dtype], t.stride(0) if rows > 1 else cols
 
 
@@ -577,7 +585,7 @@ def ckpt8_outputs(rows, cols, dev):
 
 def _saved(Q, S, cols):
     rows, groups = Q.shape[0], (cols + 31) // 32
-    _shaped(Q, (rows, 32 * groups), "Q"), _shaped(S, (rows, groups), "S")
+    _counted(_shaped(Q, (rows, 32 * groups), "Q"), "Q"), _shaped(S, (rows, groups), "S")
     return _ptr(Q, torch.int8, "Q"), _ptr(S, torch.uint8, "S"), rows
 
 

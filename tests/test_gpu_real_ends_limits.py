@@ -21,3 +21,16 @@ def test_save_and_restore_of_more_rows_than_a_grid_has_along_one_dimension():
         assert torch.equal(Q[part], q) and torch.equal(S[part], s)
         assert torch.equal(back[part], dab.dab_ckpt8_restore(q, s, 1, torch.bfloat16))
     assert float((back.float() - X.float()).abs().max()) <= 2.0 ** -7 * float(X.abs().max())
+
+
+def test_matrices_of_more_rows_than_32_bits_count_are_refused():
+    """Not taken for one of as many rows as the number's lower 32 bits say."""
+    X = torch.empty(((1 << 32) + 4, 1), dtype=torch.bfloat16, device=DEV)
+    few = torch.zeros((4, 1), dtype=torch.bfloat16, device=DEV)
+    t = torch.zeros((4,), dtype=torch.int64, device=DEV)
+    for call in (lambda: dab.dab_head_loss(few, X, t), lambda: dab.dab_w4_pack(X), lambda: dab.dab_ckpt8_save(X)):
+        with pytest.raises(ValueError, match="at most 2147483647 rows"):
+            call()
+    Q, S = torch.empty(((1 << 32) + 4, 32), dtype=torch.int8, device=DEV), torch.empty(((1 << 32) + 4, 1), dtype=torch.uint8, device=DEV)
+    with pytest.raises(ValueError, match="at most 2147483647 rows"):
+        dab.dab_ckpt8_restore(Q, S, 1, out=X)
