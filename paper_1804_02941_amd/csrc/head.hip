@@ -79,13 +79,14 @@ struct HeadPlan {
     int n_seg;
     int prob_planes;                 // planes of P
     bool stacked;                    // bf16, few tokens: P's two planes as twice the tokens in dH, and as two pairs in dW
+    bool factored;                   // bf16, many tokens: the weights' factor (product16.h)
     bool h_direct, w_direct;
     bool tail;                       // rows that are read where they are and are no whole pieces of 16 bytes
     int64_t ldh, ldw;
     int piece, n_pieces;             // words of a piece
     int64_t ldp;
     Plan16 logits, dh, dw;           // of a piece (the last one may be smaller)
-    size_t h_at, w_at, stats_at, target_at, p_at, acc_at, part_at, part_bytes, bytes;
+    size_t h_at, w_at, factor_at, stats_at, target_at, p_at, acc_at, part_at, part_bytes, bytes;
 };
 
 static bool head_sizes(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_t ldh, int64_t ldw) {
@@ -194,6 +195,11 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         // one rounding of that shows (relative error of one token's dH 0.4 % instead of 0.17 %).  Its second eight bits cost nothing there: the
         // products are bound by reading W and writing dW.
         p.stacked = p.P == 1 && T <= 128;
+        // Of many tokens the weights are rounded with P, and one weight for all of them, a mean's 1 / N, is no bf16 number: the targets' terms,
+        // -g but for little, would all be off by the same, up to 2^-8 of them.  So P is made with g over the significand of one of
+        // them, powers of two then, and dH and dW are multiplied by it in fp32.
+        p.factored = p.P == 1 && !p.stacked;
+        p.factor_at = p.factored ? room(4) : 0;
         p.prob_planes = p.stacked ? 2 : p.P;
         head_pieces(p, T, D, V, 2 * p.prob_planes);
         p.logits = plan16_logits(T, p.piece, D, p.n_seg);
@@ -236,7 +242,8 @@ static Small32 head_logits32(const void* H, int64_t ldh, const void* W, int64_t 
 
 // The operands as bf16 planes, in the workspace where they are not already.
 static int head_operands(const HeadPlan& p, const void* H, int64_t ldh, const void* W, int64_t ldw, int32_t dtype,
-                         const int64_t* targets, int64_t ignore, int T, int D, int V, char* ws, hipStream_t st, Operand16* h, Operand16* w) {
+                         const int64_t* targets, int64_t ignore, int T, int D, int V, char* ws, hipStream_t st, Operand16* h, Operand16* w,
+                         const float* g = nullptr) {
     *h = {H, p.ldh, static_cast<int64_t>(T) * p.ldh};
     *w = {W, p.ldw, static_cast<int64_t>(V) * p.ldw};
     if (p.wide) {
@@ -249,7 +256,8 @@ static int head_operands(const HeadPlan& p, const void* H, int64_t ldh, const vo
     }
     if (!p.h_direct) {
         bf16* out = reinterpret_cast<bf16*>(ws + p.h_at);
-        if (int rc = launch_planes16(H, dtype, T, D, ldh, targets, ignore, V, out, p.ldh, st)) return rc;
+        float* factor = g && p.factored ? reinterpret_cast<float*>(ws + p.factor_at) : nullptr;
+        if (int rc = launch_planes16(H, dtype, T, D, ldh, targets, ignore, V, out, p.ldh, st, g, factor)) return rc;
         h->p = out;
     }
     if (!p.w_direct) {
@@ -331,7 +339,8 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         return launch_small_gradients(q, s, dtype, st);
     }
     Operand16 h, w;
-    if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &h, &w)) return rc;
+    if (int rc = head_operands(p, H, ldh, W, ldw, dtype, targets, ignore_index, T, D, V, base, st, &h, &w, grad)) return rc;
+    const float* factor = grad && p.factored ? reinterpret_cast<const float*>(base + p.factor_at) : nullptr;
     void* P = base + p.p_at;
     float* acc = reinterpret_cast<float*>(base + p.acc_at);
     const Operand16 probs = {P, p.ldp, static_cast<int64_t>(T) * p.ldp};
@@ -346,7 +355,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         Product16 g{};
         head_segments(g, p.n_seg);
         g.A = h, g.B = wp, g.M = T, g.N = words, g.K = D, g.tail = p.tail;
-        g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad;
+        g.targets = targets, g.ignore_index = ignore_index, g.n0 = v0, g.V = V, g.lse = lse, g.g = grad, g.factor = factor;
         g.P = P, g.ldp = p.ldp, g.p_plane = probs.plane, g.p_planes = p.prob_planes;
         if (int rc = launch16(kEpiSoftmax, false, false, g, p.wide ? plan32_logits(T, words, D) : plan16_logits(T, words, D, p.n_seg), 0, st)) return rc;
         // the piece's rows of dW
@@ -355,6 +364,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         if (p.stacked) q.n_seg = 2, q.seg_a = 0x10, q.seg_b = 0;
         q.A = probs, q.B = h, q.M = words, q.N = D, q.K = T;
         q.C = static_cast<char*>(dW) + v0 * static_cast<int64_t>(D) * size, q.ldc = D, q.out_bf16 = dtype == DAB_BF16;
+        q.factor = factor;
         q.part = reinterpret_cast<float*>(base + p.part_at);
         if (int rc = launch16(kEpiStore, true, true, q, plan(words, D, T, q.n_seg), p.part_bytes, st)) return rc;
         // its share of dH
@@ -364,7 +374,7 @@ extern "C" int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W,
         s.A = probs, s.B = wp, s.M = p.stacked ? 2 * T : T, s.N = D, s.K = words;
         s.add = i ? acc : nullptr;
         s.C = last ? dH : acc, s.ldc = D, s.out_bf16 = last && dtype == DAB_BF16;
-        if (last) s.targets = targets, s.ignore_index = ignore_index, s.V = V;
+        if (last) s.targets = targets, s.ignore_index = ignore_index, s.V = V, s.factor = factor;
         s.part = q.part;
         if (int rc = launch16(kEpiStore, false, true, s, plan(s.M, D, words, p.n_seg), p.part_bytes, st)) return rc;
     }

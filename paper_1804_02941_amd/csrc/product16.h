@@ -48,6 +48,7 @@ struct Product16 {
     int out_bf16;
     const float* add;                // fp32 [M][N] added to the sum, or NULL
                                      // (and `targets`, or NULL: rows m of tokens without a loss are stored as zeros)
+    const float* factor;             // what is stored is multiplied by it, P is made with g over it; or NULL
     float* part;                     // [rest][shares][tile] sums of the shares, in the order of the accumulators
     // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece
     const int64_t* targets;
@@ -86,8 +87,9 @@ int init_product16();
 // fp32 rows ldp apart (a multiple of 4, zeros behind the last element), those of tokens without a loss cleared (targets may be NULL)
 int launch_rows32(const float* X, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V, float* out, int64_t ldp,
                   hipStream_t st);
-// bf16 planes [P][rows][ldp] of X [rows][cols], zeros up to ldp; rows whose target has no loss are zeros (targets may be NULL)
+// bf16 planes [P][rows][ldp] of X [rows][cols], zeros up to ldp; rows whose target has no loss are zeros (targets may be NULL).  And, with
+// `factor`, the significand (1 .. 2) of the first of the weights g of tokens with a loss that is no 0 and finite (1 if none is).
 int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V,
-                    bf16* out, int64_t ldp, hipStream_t st);
+                    bf16* out, int64_t ldp, hipStream_t st, const float* g = nullptr, float* factor = nullptr);
 
 }  // namespace dab

@@ -150,6 +150,7 @@ __device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v)
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] += n + r < g.N ? from[r] : 0.f;
     }
+    if (g.factor) v *= *g.factor;
     // (not their products: P's zeros times a word that is no number are not 0)
     if (g.targets && no_loss(g.targets[m], g.ignore_index, g.V)) v = v4f{0.f, 0.f, 0.f, 0.f};
     if (g.out_bf16) store4(static_cast<bf16*>(g.C) + m * g.ldc + n, v, g.N - n);
@@ -281,6 +282,13 @@ __device__ __forceinline__ void product16(const Product16& g) {
     ra.init(lane, wm * FM * 16);
     rb.init(lane, wn * FN * 16);
 
+    // (a scalar load: an earlier launch has written it)
+    auto factor_of = [&] {
+        typedef const __attribute__((address_space(4))) float scalar_f32;
+        return g.factor ? *reinterpret_cast<scalar_f32*>(reinterpret_cast<uintptr_t>(g.factor)) : 1.f;
+    };
+    float factor = EPI == kEpiStore ? factor_of() : 1.f;
+
     v4f acc[FN][FM];
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -332,6 +340,7 @@ __device__ __forceinline__ void product16(const Product16& g) {
         }
         wait_and_meet<(NS - 1) * kInFlight>();
     }
+    if constexpr (EPI == kEpiStore) asm volatile("" : "+s"(factor));   // (arrived by now; the compiler would load it at the end)
     if (TAIL && tail && last - first == 1) clear(lds);
 #pragma unroll
     for (int j = 0; j < FM; ++j) a[0][j] = ra.read(lds, 0, j);
@@ -361,11 +370,12 @@ __device__ __forceinline__ void product16(const Product16& g) {
     int64_t target[FM];
     float lse[FM], weight[FM];
     if constexpr (EPI != kEpiStore) {
+        if constexpr (EPI == kEpiSoftmax) factor = factor_of();
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
             const int m = min(mw + j * 16, g.M - 1);
             target[j] = g.targets[m];
-            if constexpr (EPI == kEpiSoftmax) lse[j] = g.lse[m], weight[j] = g.g ? g.g[m] : 1.f;
+            if constexpr (EPI == kEpiSoftmax) lse[j] = g.lse[m], weight[j] = g.g ? g.g[m] / factor : 1.f;
         }
     }
 #pragma unroll
@@ -455,6 +465,10 @@ __device__ __forceinline__ void product16(const Product16& g) {
                 *reinterpret_cast<v4f*>(g.part + ((static_cast<int64_t>(tile - g.whole) * g.shares + share) * (FN * FM) + i * FM + j) * (256 * NW) +
                                         threadIdx.x * 4) = acc[i][j];
         } else if (!g.add) {
+            if (g.factor) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i) acc[i][j] *= factor;
+            }
             if (g.targets && no_loss(g.targets[min(m, g.M - 1)], g.ignore_index, g.V)) {
 #pragma unroll
                 for (int i = 0; i < FN; ++i) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -536,13 +550,44 @@ __global__ __launch_bounds__(64 * WM * WN) void join16_kernel(Product16 g) {
 }
 
 // ---------------------------------------------------------------- operands as bf16 planes
-// (bound by memory: 8192 x 2048 bf16 rows with some cleared 12 us, 5.5 TB/s)
+// (bound by memory: 8192 x 2048 bf16 rows with some cleared 12 us, 5.5 TB/s; the weights' factor is found by a workgroup of its own beside the
+// others, 1024 tokens at a time)
+__device__ __forceinline__ void weights_factor(const float* __restrict__ g, const int64_t* __restrict__ targets, int64_t ignore, int V, int rows,
+                                               float* __restrict__ factor) {
+    __shared__ int found[4];
+    float by = 1.f;
+    for (int64_t t0 = 0; t0 < rows; t0 += 1024) {
+        int first = INT32_MAX;
+#pragma unroll
+        for (int u = 3; u >= 0; --u) {
+            const int t = static_cast<int>(min(t0 + u * 256 + threadIdx.x, static_cast<int64_t>(rows) - 1));
+            const uint32_t size = __float_as_uint(g[t]) & 0x7fffffffu;
+            // (0, subnormal numbers, infinities and NaN have no significand to divide by)
+            if (!no_loss(targets[t], ignore, V) && size >= 0x00800000u && size < 0x7f800000u) first = t;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) first = min(first, __shfl_xor(first, d));
+        if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = first;
+        __syncthreads();
+        first = min(min(found[0], found[1]), min(found[2], found[3]));
+        __syncthreads();
+        if (first == INT32_MAX) continue;
+        by = __uint_as_float((__float_as_uint(g[first]) & 0x007fffffu) | 0x3f800000u);
+        break;
+    }
+    if (threadIdx.x == 0) *factor = by;
+}
 template <typename T, int P>
 __global__ __launch_bounds__(256) void planes16_kernel(const T* __restrict__ X, int rows, int cols, int64_t ld,
                                                        const int64_t* __restrict__ targets, int64_t ignore, int V,
-                                                       bf16* __restrict__ out, int ldp, int64_t chunks) {
+                                                       bf16* __restrict__ out, int ldp, int64_t chunks, unsigned blocks,
+                                                       const float* __restrict__ g, float* __restrict__ factor) {
+    if (blockIdx.x == blocks) {
+        weights_factor(g, targets, ignore, V, rows, factor);
+        return;
+    }
     const int per_row = ldp >> 3;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < chunks; i += static_cast<int64_t>(gridDim.x) * 256) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < chunks; i += static_cast<int64_t>(blocks) * 256) {
         const int64_t row = i / per_row;
         const int c = static_cast<int>(i - row * per_row) * 8;
         float v[8] = {};
@@ -558,13 +603,13 @@ __global__ __launch_bounds__(256) void planes16_kernel(const T* __restrict__ X, 
 }
 
 int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V,
-                    bf16* out, int64_t ldp, hipStream_t st) {
+                    bf16* out, int64_t ldp, hipStream_t st, const float* g, float* factor) {
     const int64_t chunks = rows * (ldp >> 3);
-    const int64_t blocks = ceil_div64(chunks, 256);
-    const dim3 grid(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), block(256);
+    const unsigned blocks = static_cast<unsigned>(ceil_div64(chunks, 256) < 8192 ? ceil_div64(chunks, 256) : 8192);
+    const dim3 grid(blocks + (factor ? 1 : 0)), block(256);
     const int l = static_cast<int>(ldp);
-    if (dtype == DAB_F32) return launch(planes16_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
-    return launch(planes16_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks);
+    if (dtype == DAB_F32) return launch(planes16_kernel<float, 3>, grid, block, 0, st, static_cast<const float*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks, blocks, g, factor);
+    return launch(planes16_kernel<bf16, 1>, grid, block, 0, st, static_cast<const bf16*>(X), rows, cols, ld, targets, ignore, V, out, l, chunks, blocks, g, factor);
 }
 
 // fp32 rows [rows][cols] as they are, ldp apart (a multiple of 4, zeros behind the last element); those of tokens without a loss cleared
