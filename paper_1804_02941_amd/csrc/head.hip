@@ -197,9 +197,9 @@ static HeadPlan head_plan(int32_t T, int32_t D, int32_t V, int32_t dtype, int64_
         p.stacked = p.P == 1 && T <= 128;
         // Of many tokens the weights are rounded with P, and one weight for all of them, a mean's 1 / N, is no bf16 number: the targets' terms,
         // -g but for little, would all be off by the same, up to 2^-8 of them.  So P is made with g over the significand of one of
-        // them, powers of two then, and dH and dW are multiplied by it in fp32.
+        // them, powers of two then (but for a last bit of fp32), and dH and dW are multiplied by it in fp32.
         p.factored = p.P == 1 && !p.stacked;
-        p.factor_at = p.factored ? room(4) : 0;
+        p.factor_at = p.factored ? room(8) : 0;
         p.prob_planes = p.stacked ? 2 : p.P;
         head_pieces(p, T, D, V, 2 * p.prob_planes);
         p.logits = plan16_logits(T, p.piece, D, p.n_seg);

@@ -48,7 +48,7 @@ struct Product16 {
     int out_bf16;
     const float* add;                // fp32 [M][N] added to the sum, or NULL
                                      // (and `targets`, or NULL: rows m of tokens without a loss are stored as zeros)
-    const float* factor;             // what is stored is multiplied by it, P is made with g over it; or NULL
+    const float* factor;             // [2] what is stored is multiplied by the first, in P the weights by the second; or NULL
     float* part;                     // [rest][shares][tile] sums of the shares, in the order of the accumulators
     // kEpiStats, kEpiSoftmax: m is a token, n a word of the vocabulary, n0 the first word of this piece
     const int64_t* targets;
@@ -88,7 +88,8 @@ int init_product16();
 int launch_rows32(const float* X, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V, float* out, int64_t ldp,
                   hipStream_t st);
 // bf16 planes [P][rows][ldp] of X [rows][cols], zeros up to ldp; rows whose target has no loss are zeros (targets may be NULL).  And, with
-// `factor`, the significand (1 .. 2) of the first of the weights g of tokens with a loss that is no 0 and finite (1 if none is).
+// `factor`, the significand (1 .. 2) of the first of the weights g of tokens with a loss that is no 0 and finite (1 if none is),
+// and 1 over it.
 int launch_planes16(const void* X, int32_t dtype, int rows, int cols, int64_t ld, const int64_t* targets, int64_t ignore, int V,
                     bf16* out, int64_t ldp, hipStream_t st, const float* g = nullptr, float* factor = nullptr);
 

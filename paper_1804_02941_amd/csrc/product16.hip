@@ -143,16 +143,22 @@ __device__ __forceinline__ void store4(T* to, v4f v, int columns) {
     for (int r = 0; r < 4; ++r)
         if (r < columns) to[r] = out[r];
 }
-__device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v) {
+// What a row's sums become as they are stored: times the factor, or zeros, of a token without a loss (not its products: P's zeros times a word
+// that is no number are not 0).
+struct RowEnd {
+    float factor;
+    bool none;
+    __device__ __forceinline__ RowEnd(const Product16& g, int m)
+        : factor(g.factor ? *g.factor : 1.f), none(g.targets && no_loss(g.targets[m], g.ignore_index, g.V)) {}
+};
+__device__ __forceinline__ void store16(const Product16& g, int m, int n, v4f v, RowEnd end) {
     if (n >= g.N) return;
     if (g.add) {
         const float* from = g.add + static_cast<int64_t>(m) * g.N + n;
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] += n + r < g.N ? from[r] : 0.f;
     }
-    if (g.factor) v *= *g.factor;
-    // (not their products: P's zeros times a word that is no number are not 0)
-    if (g.targets && no_loss(g.targets[m], g.ignore_index, g.V)) v = v4f{0.f, 0.f, 0.f, 0.f};
+    v = end.none ? v4f{0.f, 0.f, 0.f, 0.f} : v * end.factor;
     if (g.out_bf16) store4(static_cast<bf16*>(g.C) + m * g.ldc + n, v, g.N - n);
     else store4(static_cast<float*>(g.C) + m * g.ldc + n, v, g.N - n);
 }
@@ -283,11 +289,11 @@ __device__ __forceinline__ void product16(const Product16& g) {
     rb.init(lane, wn * FN * 16);
 
     // (a scalar load: an earlier launch has written it)
-    auto factor_of = [&] {
+    auto factor_of = [&](int which) {
         typedef const __attribute__((address_space(4))) float scalar_f32;
-        return g.factor ? *reinterpret_cast<scalar_f32*>(reinterpret_cast<uintptr_t>(g.factor)) : 1.f;
+        return g.factor ? reinterpret_cast<scalar_f32*>(reinterpret_cast<uintptr_t>(g.factor))[which] : 1.f;
     };
-    float factor = EPI == kEpiStore ? factor_of() : 1.f;
+    float factor = EPI == kEpiStore ? factor_of(0) : 1.f;
 
     v4f acc[FN][FM];
 #pragma unroll
@@ -370,12 +376,12 @@ __device__ __forceinline__ void product16(const Product16& g) {
     int64_t target[FM];
     float lse[FM], weight[FM];
     if constexpr (EPI != kEpiStore) {
-        if constexpr (EPI == kEpiSoftmax) factor = factor_of();
+        if constexpr (EPI == kEpiSoftmax) factor = factor_of(1);
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
             const int m = min(mw + j * 16, g.M - 1);
             target[j] = g.targets[m];
-            if constexpr (EPI == kEpiSoftmax) lse[j] = g.lse[m], weight[j] = g.g ? g.g[m] / factor : 1.f;
+            if constexpr (EPI == kEpiSoftmax) lse[j] = g.lse[m], weight[j] = g.g ? g.g[m] * factor : 1.f;
         }
     }
 #pragma unroll
@@ -485,8 +491,9 @@ __device__ __forceinline__ void product16(const Product16& g) {
                 out.flush(static_cast<float*>(g.C) + mj * g.ldc + nb, g.ldc, g.M - mj, g.N - nb);
             }
         } else if (in) {
+            const RowEnd end(g, m);
 #pragma unroll
-            for (int i = 0; i < FN; ++i) store16(g, m, nw + i * 16, acc[i][j]);
+            for (int i = 0; i < FN; ++i) store16(g, m, nw + i * 16, acc[i][j], end);
         }
     }
 }
@@ -535,6 +542,7 @@ __global__ __launch_bounds__(64 * WM * WN) void join16_kernel(Product16 g) {
     const int tn = in_band / bm, tm = band * 8 + in_band - tn * bm;
     const int n = tn * TN + (wave / WM * FN + i) * 16 + (lane >> 4) * 4, m = tm * TM + (wave % WM * FM + j) * 16 + (lane & 15);
     if (m >= g.M || n >= g.N) return;
+    const RowEnd end(g, m);                                  // (requested before the sums)
     constexpr int64_t kNext = static_cast<int64_t>(FN * FM) * 256 * NW;
     const float* from = g.part + static_cast<int64_t>(rest_tile) * g.shares * kNext + block * (256 * NW) + threadIdx.x * 4;
     v4f v = v4f{0.f, 0.f, 0.f, 0.f};
@@ -546,12 +554,12 @@ __global__ __launch_bounds__(64 * WM * WN) void join16_kernel(Product16 g) {
         for (int u = 0; u < 8; ++u)
             if (s + u < g.shares) v += got[u];
     }
-    store16(g, m, n, v);
+    store16(g, m, n, v, end);
 }
 
 // ---------------------------------------------------------------- operands as bf16 planes
-// (bound by memory: 8192 x 2048 bf16 rows with some cleared 12 us, 5.5 TB/s; the weights' factor is found by a workgroup of its own beside the
-// others, 1024 tokens at a time)
+// (bound by memory: 8192 x 2048 bf16 rows with some cleared 12 us, 5.5 TB/s; the weights' factor is found by a workgroup of its own in front of
+// the others, 1024 tokens at a time: behind them it ended last, 14.5 us)
 __device__ __forceinline__ void weights_factor(const float* __restrict__ g, const int64_t* __restrict__ targets, int64_t ignore, int V, int rows,
                                                float* __restrict__ factor) {
     __shared__ int found[4];
@@ -575,19 +583,20 @@ __device__ __forceinline__ void weights_factor(const float* __restrict__ g, cons
         by = __uint_as_float((__float_as_uint(g[first]) & 0x007fffffu) | 0x3f800000u);
         break;
     }
-    if (threadIdx.x == 0) *factor = by;
+    if (threadIdx.x == 0) factor[0] = by, factor[1] = 1.f / by;
 }
 template <typename T, int P>
 __global__ __launch_bounds__(256) void planes16_kernel(const T* __restrict__ X, int rows, int cols, int64_t ld,
                                                        const int64_t* __restrict__ targets, int64_t ignore, int V,
                                                        bf16* __restrict__ out, int ldp, int64_t chunks, unsigned blocks,
                                                        const float* __restrict__ g, float* __restrict__ factor) {
-    if (blockIdx.x == blocks) {
+    const unsigned lead = gridDim.x - blocks;
+    if (blockIdx.x < lead) {
         weights_factor(g, targets, ignore, V, rows, factor);
         return;
     }
     const int per_row = ldp >> 3;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < chunks; i += static_cast<int64_t>(blocks) * 256) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x - lead) * 256 + threadIdx.x; i < chunks; i += static_cast<int64_t>(blocks) * 256) {
         const int64_t row = i / per_row;
         const int c = static_cast<int>(i - row * per_row) * 8;
         float v[8] = {};

@@ -101,7 +101,7 @@ void product(const std::string& k, const std::vector<int>& t, const Product16& g
         if (g.rest && (g.share_steps < 1 || 1ll * g.share_steps * g.shares < g.steps || 1ll * g.share_steps * (g.shares - 1) >= g.steps)) fault(k, "shares that do not cover the sum once");
         if (g.add) read(k, range(g.add, 4ull * M * N, "sums of the pieces before"));
         if (g.targets) read(k, range(g.targets, 8ull * M, "targets"));
-        if (g.factor) read(k, range(g.factor, 4, "weights' factor"));
+        if (g.factor) read(k, range(g.factor, 8, "weights' factor"));
         if (g.whole || g.shares == 1) write(k, range(g.C, (1ull * (M - 1) * static_cast<unsigned long long>(g.ldc) + N) * (g.out_bf16 ? 2 : 4), "result"));
         return;
     }
@@ -114,7 +114,7 @@ void product(const std::string& k, const std::vector<int>& t, const Product16& g
     } else {
         read(k, range(g.lse, 4ull * M, "lse"));
         if (g.g) read(k, range(g.g, 4ull * M, "weights"));
-        if (g.factor) read(k, range(g.factor, 4, "weights' factor"));
+        if (g.factor) read(k, range(g.factor, 8, "weights' factor"));
         if (1ll * g.tiles_n * TN > g.ldp) fault(k, "rows of P that run into each other");
         const unsigned long long elems = 1ull * (g.p_planes - 1) * static_cast<unsigned long long>(g.p_plane) + 1ull * (M - 1) * static_cast<unsigned long long>(g.ldp) + 1ull * g.tiles_n * TN;
         write(k, range(g.P, elems * size, "P"));
@@ -152,7 +152,7 @@ void launched(const void* f, dim3 grid, dim3 block, void** a) {
         if (void* factor = argument<void*>(a, 12)) {
             if (grid.x != argument<unsigned>(a, 10) + 1) fault(k, "no workgroup for the factor");
             read(k, range(argument<void*>(a, 11), 4 * rows, "weights"));
-            write(k, range(factor, 4, "weights' factor"));
+            write(k, range(factor, 8, "weights' factor"));
         } else if (grid.x != argument<unsigned>(a, 10)) {
             fault(k, "grid");
         }
