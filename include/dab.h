@@ -448,9 +448,10 @@ int dab_weight_gradient(const float* W, int32_t F, int32_t n, const float* thr_v
  * largest matrices.
  *
  * Element types of these calls, and the strides of their inputs: a matrix [rows][cols] is given with
- * the distance ld of its rows in elements (ld >= cols, any alignment of the rows), so that a slice of
- * columns needs no copy.  Outputs are contiguous.  Offsets are 64-bit.  Base pointers are 16-byte aligned
- * (DAB_ERR_ALIGN), fp32 vectors, scale bytes and targets as their type wants.
+ * the distance ld of its rows in elements (ld >= cols), so that a slice of columns whose first element is 16-byte
+ * aligned needs no copy: base pointers are 16-byte aligned (DAB_ERR_ALIGN), the rows behind the first one at any
+ * element.  fp32 vectors, scale bytes and targets are aligned as their type wants.  Outputs are contiguous.  Offsets are 64-bit.
+ * Larger sizes than each call names are DAB_ERR_UNSUPPORTED.
  */
 typedef enum dab_dtype {
     DAB_F32 = 0,
@@ -463,13 +464,15 @@ typedef enum dab_dtype {
  * A group is 32 neighbouring channels of a row (the last one may be short).  With a the largest
  * magnitude of a group and f = floor(log2 a), its exponent is e = f - 6, or f - 5 where a 2^-e would
  * lie at or above 127.5; a value is q = x 2^-e rounded to the nearest integer, ties to even, so |q| <= 127 and
- * |x - q 2^e| <= 2^(e-1) < a/127.  f - 6 is kept within -110 .. 120, and |q| at 127.  The scale is a
+ * |x - q 2^e| <= 2^(e-1) < a/127, for groups with a from 2^-104 to 127.5 2^121.  f - 6 is kept within -110 .. 120 and |q| at
+ * 127: below, steps are 2^-110 and a group loses its digits; above, at the end of fp32's range, e is 121 and
+ * magnitudes are cut to 127 steps, by less than one of them.  The scale is a
  * power of two because undoing it is then exact in every type that has 8 significant bits: a
  * restored value is a bf16 number.
  *
  *   X    [rows][cols] of dtype, rows ldx apart
  *   Q    int8 [rows][32*ceil(cols/32)] out, zeros behind the last channel
- *   S    uint8 [rows][ceil(cols/32)] out: e + 127; a group of zeros has 17; a group with an
+ *   S    uint8 [rows][ceil(cols/32)] out: e + 127 (17 .. 248); a group of zeros has 17; a group with an
  *        infinity or a NaN has 255, and is restored as NaN throughout
  * restore writes [rows][cols] of dtype, rows ldx apart (f16: rounded to nearest, infinite where too large).
  */
@@ -485,7 +488,7 @@ int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows, int32_t c
  * three, so that every product is exact (pieces have steps of 2^-133) and only the fp32 accumulation rounds.  Infinities and NaN in dY come
  * out as in the sum itself.
  *
- *   dY   [rows][F] of dtype, rows lddy apart;   dW  fp32 [F][cols] out
+ *   dY   [rows][F] of dtype, rows lddy apart;   dW  fp32 [F][cols] out.  F, cols and lddy are below 2^22
  *   ws   dab_ckpt8_weight_gradient_workspace_bytes(...) bytes, 256-byte aligned
  */
 size_t dab_ckpt8_weight_gradient_workspace_bytes(int32_t rows, int32_t cols, int32_t F, int32_t dtype, int64_t lddy);
@@ -498,11 +501,12 @@ int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t lddy, const
  * The products run on the matrix cores a block of the vocabulary at a time; of a block only its rows'
  * maxima and sums and the targets' logits leave the compute unit.  Sums and logits are fp32.  fp32
  * inputs are multiplied as they are where tokens are few, else as sums of three bf16 numbers (six
- * products of pieces, what is left out is below 2^-24 of a term).
+ * products of pieces, what is left out is below 2^-24 of a term): the workspace then holds 6 bytes for every
+ * element of H and W, in the loss and in the gradient.
  *
  *   H        [T][D] of dtype (DAB_BF16 or DAB_F32; DAB_F16 -> DAB_ERR_UNSUPPORTED: softmax gradients leave its
  *            range), rows ldh apart
- *   W        [V][D] of the same dtype, rows ldw apart
+ *   W        [V][D] of the same dtype, rows ldw apart.  T and V are below 2^30, ldh and ldw below 2^22
  *   targets  [T] int64; ignore_index marks a token without a loss (its row of H may hold anything, infinities and NaN
  *            among it: loss 0, no part in any gradient).  A target that is neither that nor one of 0 .. V-1 gives a loss of
  *            NaN, and its token no part in any gradient.
@@ -520,9 +524,12 @@ int dab_head_loss(const void* H, int64_t ldh, const void* W, int64_t ldw, int32_
  * dab_head_loss_gradient - its gradient.  With g_t the gradient with respect to loss_t,
  *     P_tv = g_t (exp(L_tv - lse_t) - [v = target(t)]),   dH = P W,   dW = P^T H,
  * the logits recomputed a piece of the vocabulary at a time.  Where H and W are bf16 P is rounded to bf16 (as those
- * are: the products stay on the matrix cores, and dH and dW are rounded to bf16 themselves, so that their error is
- * about 1.4 times that of the rounding alone), of up to 128 tokens to 16 bits and of small heads not at all; for fp32 it is held
- * as the operands are.  Sums are fp32; no atomics: the same inputs give the same bits.
+ * are: the products stay on the matrix cores, and dH and dW are rounded to bf16 themselves), of up to 128 tokens to 16 bits and of
+ * small heads not at all; for fp32 it is held as the operands are.  An entry of P is then off by up to 2^-8 of itself, a weight that all
+ * tokens share aside (what is rounded is P over the significand of the first weight): the error of dH and dW is that of rounding them alone where
+ * the weights are the same, about 1.4 times that where they differ, and more where the terms of a sum cancel (words with a large part in
+ * common, which P's rows sum away; 16 times what sets them apart: dH 2.1 times).  A caller to whom that matters gives H and W
+ * in fp32.  Sums are fp32; no atomics: the same inputs give the same bits.
  *
  *   lse      [T] fp32 of dab_head_loss for the same H, W, targets
  *   g        [T] fp32, or NULL for 1
@@ -538,9 +545,9 @@ int dab_head_loss_gradient(const void* H, int64_t ldh, const void* W, int64_t ld
  * share a power of two, a weight is a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (codes 0 .. 7, the sign 8).
  * With a the largest magnitude of a group and f = floor(log2 a), the exponent is e = f - 2, or f - 1 where
  * a 2^-e would exceed 7 (further from 6 than half the step before it); values go to the nearest level, ties to the even
- * code, what lies above 6 to 6.  f - 2 is kept within -110 .. 120.
+ * code, what lies above 6 to 6.  f - 2 is kept within -110 .. 120: weights beyond 6 * 2^121 are cut to that.
  *
- *   W   [F][K] of dtype, rows ldw apart
+ *   W   [F][K] of dtype, rows ldw apart.  F is at most 16 * 65535, K 2^31 - 513
  *   Q   uint8 [ceil(F/16)][ceil(K/128)][64][16] out: piece l of a block of 16 rows and 128 weights holds
  *       row l % 16, weights 32 (l / 16) .. + 31 of the block, two to a byte, the lower weight in the lower four bits.
  *       (What one lane of a wavefront takes; a block is one contiguous kilobyte.)  Zeros past F and K.
@@ -552,7 +559,7 @@ int dab_w4_pack(const void* W, int32_t dtype, int32_t F, int32_t K, int64_t ldw,
 int dab_w4_unpack(const uint8_t* Q, const uint8_t* S, int32_t F, int32_t K, float* W, void* stream);
 
 /*
- * dab_w4_matvec - Y[b][f] = sum_k X[b][k] W[f][k] with packed weights, for one token or a few (any B is right; the
+ * dab_w4_matvec - Y[b][f] = sum_k X[b][k] W[f][k] with packed weights, for one token or a few (B up to 65535, K up to 2^26; the
  * weights are read once for every 48 bf16, 24 f16 or 16 fp32 tokens).  On the matrix cores in bf16, which hold a 4-bit weight times its
  * scale exactly; f16 inputs are sums of two bf16 numbers, fp32 ones of three: only the fp32 accumulation
  * rounds, and a 16-bit Y once more.  Infinities and NaN in X come out as in the sum itself.

@@ -115,7 +115,7 @@ static Route head_route(int32_t dtype, int64_t T, int64_t D, int64_t V) {
     return small <= wide && small <= planes ? Route::kSmall : wide <= planes ? Route::kWide : Route::kPlanes;
 }
 
-// Pieces of up to 256 MB of P (`bytes` an entry), which is about what the memory-side cache holds, of equal size; rows of P stay within
+// Pieces of up to 256 MB of P (`bytes` an entry), which is about what the memory-side cache holds, but no fewer than 1024 words, of equal size; rows of P stay within
 // the offsets of the product's copies.
 static void head_pieces(HeadPlan& p, int32_t T, int32_t D, int32_t V, int bytes) {
     int64_t words = (int64_t{256} << 20) / (static_cast<int64_t>(bytes) * T) / 1024 * 1024;

@@ -45,7 +45,7 @@ __device__ __forceinline__ v4f load4(const T* row, int c, int cols) {
     return v;
 }
 
-// (eight wavefronts on a SIMD, or else the compiler takes all rows at once, in 238 registers)
+// (six wavefronts on a SIMD asked for, or else the compiler takes all rows at once, in 238 registers)
 template <typename T>
 __global__ __launch_bounds__(64 * kW4PackWaves, 6) void w4_pack_kernel(const T* __restrict__ W, int F, int K, int64_t ldw, int Kt, int K4,
                                                                     uint8_t* __restrict__ Q, uint8_t* __restrict__ S) {
