@@ -488,7 +488,7 @@ int dab_ckpt8_restore(const int8_t* Q, const uint8_t* S, int32_t rows, int32_t c
  * three, so that every product is exact (pieces have steps of 2^-133) and only the fp32 accumulation rounds.  Infinities and NaN in dY come
  * out as in the sum itself.
  *
- *   dY   [rows][F] of dtype, rows lddy apart;   dW  fp32 [F][cols] out.  F, cols and lddy are below 2^22
+ *   dY   [rows][F] of dtype, rows lddy apart;   dW  fp32 [F][cols] out.  F, cols and lddy are below 2^22, rows below 2^31 - 63
  *   ws   dab_ckpt8_weight_gradient_workspace_bytes(...) bytes, 256-byte aligned
  */
 size_t dab_ckpt8_weight_gradient_workspace_bytes(int32_t rows, int32_t cols, int32_t F, int32_t dtype, int64_t lddy);
@@ -506,7 +506,8 @@ int dab_ckpt8_weight_gradient(const void* dY, int32_t dtype, int64_t lddy, const
  *
  *   H        [T][D] of dtype (DAB_BF16 or DAB_F32; DAB_F16 -> DAB_ERR_UNSUPPORTED: softmax gradients leave its
  *            range), rows ldh apart
- *   W        [V][D] of the same dtype, rows ldw apart.  T and V are below 2^30, ldh and ldw below 2^22
+ *   W        [V][D] of the same dtype, rows ldw apart.  T and V are below 2^30, ldh and ldw below 2^22, and T x V
+ *            is below 2^25 tiles of 128 x 128, T x D below 2^21
  *   targets  [T] int64; ignore_index marks a token without a loss (its row of H may hold anything, infinities and NaN
  *            among it: loss 0, no part in any gradient).  A target that is neither that nor one of 0 .. V-1 gives a loss of
  *            NaN, and its token no part in any gradient.

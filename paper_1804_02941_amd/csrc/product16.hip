@@ -850,7 +850,7 @@ static GradPlan grad_plan(int32_t rows, int32_t cols, int32_t F, int32_t dtype, 
     return p;
 }
 static bool grad_sizes(int32_t rows, int32_t cols, int32_t F, int32_t dtype, int64_t lddy) {
-    return real_dtype(dtype) && lddy < (1 << 22) && F < (1 << 22) && cols < (1 << 22) &&
+    return real_dtype(dtype) && rows <= INT32_MAX - (kStepK - 1) && lddy < (1 << 22) && F < (1 << 22) && cols < (1 << 22) &&
            ceil_div64(F, 128) * ceil_div64(cols, 128) < INT32_MAX / 64;
 }
 }  // namespace dab
