@@ -14,9 +14,9 @@ too), "norm_grad", "adamw" ("bits" of the states), "serve" (tokens through 4-bit
 forward beside a given product, then all gradients).
 
 Formats (include/dab.h).  Saved outputs and 4-bit weights are those of perf/operators.py.  A state in 8 bits: groups of 32 share
-a power of two, f = floor(log2(largest magnitude)) kept within -100 .. 120; a first moment is a sign, four bits of exponent and three of significand, the
-root of a second moment four bits of exponent and four of significand, both below 2^(f+1); they are rounded up or down by chance, with
-the probabilities that keep the mean, by a number that depends on (seed, step, place) alone.
+a power of two 2^f, the least that makes the last code no smaller than the largest magnitude, f within -100 .. 120; a first moment is a sign,
+four bits of exponent and three of significand, the root of a second moment four bits of exponent and four of significand, both below
+2^(f+1); they are rounded up or down by chance, with the probabilities that keep the mean, by a number that depends on (seed, step, place) alone.
 """
 import math
 
@@ -278,10 +278,10 @@ def _code(x, chance, bits):
     """(codes uint8, scale bytes) of values in groups of 32, rounded by 16 bits of chance; bits: of the significand (3: with a sign above it)."""
     v = x.reshape(-1, GROUP)
     big = v.abs().amax(dim=1, keepdim=True)
-    f = ((big.view(torch.int32) >> 23) - 127).clamp(-100, 120)
+    drop = 23 - bits
+    f = (((big.view(torch.int32) + ((1 << drop) - 1)) >> 23) - 127).clamp(-100, 120)
     y = v.abs() * _pow2(-f)
     whole = torch.where(y >= 2.0 ** -14, y.view(torch.int32) - (112 << 23), (y * 2.0 ** 37).to(torch.int32))
-    drop = 23 - bits
     code = ((whole + (chance.reshape(-1, GROUP).to(torch.int32) << (drop - 16))) >> drop).clamp(max=(16 << bits) - 1)
     if bits == 3:
         code = code + 128 * torch.signbit(v)
@@ -468,6 +468,7 @@ def _by_chance64(x, chance, bits):
     v = x.reshape(-1, GROUP)
     big = v.abs().amax(dim=1, keepdim=True).clamp(min=2.0 ** -100)
     top = torch.frexp(big)[1] - 1
+    top = torch.where(big > torch.ldexp(torch.full_like(big, 2.0 - 2.0 ** -bits), top), top + 1, top)
     own_binade = torch.frexp(v.abs().clamp(min=2.0 ** -300))[1] - 1
     step = torch.ldexp(torch.ones_like(v), torch.maximum(own_binade, top - 14) - bits)
     code = torch.floor(v.abs() / step + chance.reshape(-1, GROUP).double() / 65536.0)
