@@ -286,7 +286,7 @@ def _code(x, chance, bits):
     if bits == 3:
         code = code + 128 * torch.signbit(v)
     else:
-        code = torch.where(y > 0, code.clamp(min=1), code)
+        code = torch.where(v > 0, code.clamp(min=1), code)
     return code.to(torch.uint8).reshape(-1), (f + 127).to(torch.uint8).reshape(-1)
 
 
