@@ -573,6 +573,134 @@ size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t dt
 int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F,
                   void* Y, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * dab_rms_norm - the root-mean-square norm of a layer's input, with the residual's addition and, in the same pass, the output in 8 bits for
+ * dab_ckpt8_weight_gradient of the layer behind it:
+ *     h = x + r, rounded to dtype (x without a residual),   y_c = gain_c h_c rstd,  rstd = 1 / sqrt(mean_c(h_c^2) + eps).
+ * Sums are fp32 (a row whose squares pass fp32's range has an rstd of 0); y is rounded once, to dtype and, apart from that, to bytes.
+ *
+ *   X      [rows][cols] of dtype, rows ldx apart;  R  the same, rows ldr apart, or NULL.  cols is at most 2^26
+ *   gain   [cols] fp32
+ *   H      [rows][cols] of dtype out: h; written where R is given, else not touched and may be NULL.  May be X or R itself where their rows are cols apart
+ *   Y      [rows][cols] of dtype out, or NULL.  May be X itself where its rows are cols apart
+ *   Q, S   as dab_ckpt8_save writes them for y (in fp32), or both NULL.  One of Y and Q is given
+ *   rstd   [rows] fp32 out, what the gradient takes
+ * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE.
+ */
+int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const void* R, int64_t ldr, const float* gain, float eps, int32_t rows, int32_t cols,
+                 void* H, void* Y, int8_t* Q, uint8_t* S, float* rstd, void* stream);
+
+/*
+ * dab_rms_norm_gradient - its gradients.  With n = h rstd and w = gain dy:
+ *     dx_c = rstd (w_c - n_c mean(w n)) + dh_c   (the gradient of x and of r alike),   dgain_c = sum over rows of dy_c n_c.
+ * Sums are fp32, in an order that depends on the sizes alone: the same inputs give the same bits.
+ *
+ *   dY     [rows][cols] of dtype, rows lddy apart;  H  the h of dab_rms_norm (X without a residual), rows ldh apart;  rstd  its rstd
+ *   dH     [rows][cols] of dtype, rows lddh apart, what arrives at h beside the norm, or NULL
+ *   dX     [rows][cols] of dtype out.  May be dY or dH itself where their rows are cols apart;  dgain  [cols] fp32 out
+ *   ws     dab_rms_norm_gradient_workspace_bytes(rows, cols) bytes, 256-byte aligned
+ */
+size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t cols);
+int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t ldh, int32_t dtype, const float* gain, const float* rstd,
+                          const void* dH, int64_t lddh, int32_t rows, int32_t cols, void* dX, float* dgain, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dab_adamw - a step of Adam with decoupled weight decay over many tensors at once (thirty-two a launch).  With g the gradient
+ * times *grad_scale, every operation in fp32:
+ *     m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+ *     p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
+ * Everything is updated in place.  m and v are held in fp32 (bits 32), or in 8 bits (bits 8), m and sqrt(v), groups of 32 neighbouring elements
+ * sharing a scale 2^f, f = floor(log2(largest magnitude)), one more where that magnitude lies above the last code, kept within -100 .. 120
+ * (-100 for zeros):
+ *   m        a sign (128), four bits of exponent e, three of significand s: s 2^-17 2^f for e = 0, else (1 + s/8) 2^(e-15) 2^f
+ *   sqrt(v)  four bits of exponent, four of significand: s 2^-18 2^f for e = 0, else (1 + s/16) 2^(e-15) 2^f
+ * Both are rounded by chance, to the code above or below with the probabilities that keep the mean (with rounding to the nearest a
+ * second moment, which changes by one part in a thousand a step, would never fall): the 23 bits of a magnitude's significand plus 16 random
+ * bits at the top of those that go.  A sqrt(v) that is not zero keeps a code of at least 1.  The step itself takes m and v before they are rounded.
+ * The random bits of element i: mix(lower word of place + i, plus mix(its upper word + key)), key = mix(seed's lower word + mix(its upper one +
+ * mix(step))), the lower 16 bits for m, the upper for sqrt(v); mix(x): x ^= x >> 16, x *= 0x85A308D3, x ^= x >> 15, x *= 0x9E3779B1, x ^= x >> 16.
+ * A group with an infinity or a NaN has scale byte 255 and is restored as NaN throughout.
+ *
+ *   P       [n] fp32;  G  [n] of grad_dtype;  copy  [n] of copy_dtype (DAB_BF16 or DAB_F16): the new p rounded to it, or NULL
+ *   M, V    [n] fp32, MS and VS not used; or uint8 [32 ceil(n/32)] and MS, VS uint8 [ceil(n/32)]: f + 127
+ *   place   of the tensor's first element in the sequence of random numbers, a multiple of 32: tensors that round apart from one another
+ *           have places that lie their sizes apart
+ * P, G, M, V and copy are 16-byte aligned; n is at most 2^34.  No tensor may overlap another one of the call.
+ *   lr, step, grad_scale   in the structure, or in device memory (lr_dev, step_dev; grad_scale: NULL for 1), where a captured graph reads them anew at
+ *           every replay.  A *grad_scale that is infinite or a NaN leaves everything as it was; step counts from 1
+ * Errors: step < 1, a rate that is not finite, b1 or b2 outside 0 .. 1 (without 1), a negative eps, a place that is no multiple of 32 -> DAB_ERR_SHAPE.
+ */
+typedef struct dab_adamw_job {
+    float* P;
+    const void* G;
+    void *M, *V;
+    uint8_t *MS, *VS;
+    void* copy;
+    int64_t n;
+    uint64_t place;
+    int32_t grad_dtype, copy_dtype, bits;
+    float weight_decay;
+} dab_adamw_job;
+
+typedef struct dab_adamw_step {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    uint64_t seed;
+    const float* lr_dev;            /* device memory, or NULL: lr                        */
+    const int64_t* step_dev;        /* device memory, or NULL: step                      */
+    const float* grad_scale;        /* device memory, or NULL: 1                         */
+} dab_adamw_step;
+
+int dab_adamw(const dab_adamw_job* jobs /* host */, int32_t n_jobs, const dab_adamw_step* step /* host */, void* stream);
+
+/*
+ * dab_state8_restore / dab_state8_save - 8-bit states as numbers, and numbers as 8-bit states rounded to the nearest code (halves up): is_signed
+ * for m, else sqrt(v) (what is negative counts as 0).  X [n] of dtype (save: fp32), Q uint8 [32 ceil(n/32)], zeros behind the last
+ * element, S uint8 [ceil(n/32)].  X and Q are 16-byte aligned, n is at most 2^34.
+ */
+int dab_state8_restore(const uint8_t* Q, const uint8_t* S, int64_t n, int32_t is_signed, void* X, int32_t dtype, void* stream);
+int dab_state8_save(const float* X, int64_t n, int32_t is_signed, uint8_t* Q, uint8_t* S, void* stream);
+
+/*
+ * dab_adapters - products of low rank beside a shared projection.  A token t has adapter i = ids[t] (none where that is not one of 0 .. n-1):
+ *     U_t = A_i X_t,   Y_t = base_t + scale_i (U_t B_i),     Y_t = base_t and U_t = 0 without an adapter.
+ * Both matrices of an adapter are r long rows.  Products are exact and sums fp32; Y is rounded once.  What an adapter that a token does
+ * not have holds, infinities and NaN among it, does not reach the token.
+ *
+ *   X       [T][K] of dtype, rows ldx apart;  ids  int32 [T], in any order;  scale  fp32 [n], or NULL for 1
+ *   A       [n][r][K], B  [n][r][F] of dtype, contiguous.  r is at most 256, n 65535, T 2^25, K and F 2^24
+ *   base    [T][F] of dtype or fp32 (base_dtype), rows ldbase apart, or NULL for 0: any projection's output
+ *   Y       [T][F] of dtype out.  May be base itself where that is of dtype and its rows are F apart;  U  fp32 [T][r] out: what the gradient takes
+ */
+int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
+                 int32_t F, int32_t n, int32_t r, const void* base, int32_t base_dtype, int64_t ldbase, void* Y, float* U, void* stream);
+
+/*
+ * dab_adapters_gradient - its gradients.  With V_t = scale_i (B_i dY_t), 0 without an adapter:
+ *     dX_t = base_t + V_t A_i,   dA_i = sum over t with ids[t] = i of V_t^T X_t,   dB_i = scale_i sum over the same t of U_t^T dY_t.
+ * Sums are fp32, in an order that depends on the sizes and ids alone.  (base's gradient in dab_adapters is dY itself.)
+ *
+ *   dY      [T][F] of dtype, rows lddy apart;  X, ids, A, B, scale  as for dab_adapters, U  what it returned
+ *   base    [T][K] of dtype or fp32, rows ldbase apart, or NULL for 0: what the shared projection's gradient gives
+ *   dX      [T][K] of dtype out, or NULL where it is not needed (base is NULL then).  May be base itself where that is of dtype and its rows are K apart
+ *   dA      fp32 [n][r][K] out, dB  fp32 [n][r][F] out, zeros for an adapter without tokens
+ *   ws      dab_adapters_gradient_workspace_bytes(T, K, F, n, r) bytes, 256-byte aligned
+ */
+size_t dab_adapters_gradient_workspace_bytes(int32_t T, int32_t K, int32_t F, int32_t n, int32_t r);
+int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X, int32_t dtype, int64_t ldx, const float* U, const int32_t* ids, const void* A,
+                          const void* B, const float* scale, int32_t T, int32_t K, int32_t F, int32_t n, int32_t r, const void* base,
+                          int32_t base_dtype, int64_t ldbase, void* dX, float* dA, float* dB, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dab_w4_adapters - dab_w4_matvec and dab_adapters in one: Y_t = W X_t + scale_i (A_i X_t) B_i with the 4-bit weights Q, S that all tokens share, rounded
+ * once.  Arguments as for those two; Bt is dab_adapters' B.  B tokens, up to 65535.
+ *
+ *   ws      dab_w4_adapters_workspace_bytes(...) bytes, 256-byte aligned
+ */
+size_t dab_w4_adapters_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t r, int32_t dtype, int64_t ldx);
+int dab_w4_adapters(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, const int32_t* ids, const void* A, const void* Bt,
+                    const float* scale, int32_t B, int32_t K, int32_t F, int32_t n, int32_t r, void* Y, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
@@ -32,6 +32,16 @@ class DabError(RuntimeError):
     def __init__(self, name, status, text):
         super().__init__(f"{name} failed: status {status} ({text})")
         self.status = status
+
+
+class dab_adamw_job(ctypes.Structure):
+    _fields_ = [("P", c_void_p), ("G", c_void_p), ("M", c_void_p), ("V", c_void_p), ("MS", c_void_p), ("VS", c_void_p), ("copy", c_void_p),
+                ("n", c_int64), ("place", c_uint64), ("grad_dtype", c_int32), ("copy_dtype", c_int32), ("bits", c_int32), ("weight_decay", c_float)]
+
+
+class dab_adamw_step(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("step", c_int64), ("seed", c_uint64),
+                ("lr_dev", c_void_p), ("step_dev", c_void_p), ("grad_scale", c_void_p)]
 
 
 class dab_conv_desc(ctypes.Structure):
@@ -113,6 +123,23 @@ _SIGNATURES = {
     "dab_w4_matvec_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int64]),
     "dab_w4_matvec": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
                               c_size_t, c_void_p]),
+    "dab_rms_norm": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_int64, c_void_p, c_float, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
+                             c_void_p, c_void_p, c_void_p]),
+    "dab_rms_norm_gradient_workspace_bytes": (c_size_t, [c_int32, c_int32]),
+    "dab_rms_norm_gradient": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32,
+                                      c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "dab_adamw": (c_int, [ctypes.POINTER(dab_adamw_job), c_int32, ctypes.POINTER(dab_adamw_step), c_void_p]),
+    "dab_state8_restore": (c_int, [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p]),
+    "dab_state8_save": (c_int, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
+    "dab_adapters": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32,
+                             c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p]),
+    "dab_adapters_gradient_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "dab_adapters_gradient": (c_int, [c_void_p, c_int64, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
+                                      c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_size_t, c_void_p]),
+    "dab_w4_adapters_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int64]),
+    "dab_w4_adapters": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                c_int32, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
 }
 
 _lib = None
@@ -719,4 +746,282 @@ def dab_w4_matvec(X, Q, S, F, out=None, ws=None):
     Y = _result(out, (B, F), X.dtype, X.device, "out")
     ws, at, nbytes = _scratch(lib().dab_w4_matvec_workspace_bytes(B, K, F, dtype, ld), X.device, ws)
     _check("dab_w4_matvec", lib().dab_w4_matvec(ptr, dtype, ld, q, s, B, K, F, Y.data_ptr(), at, nbytes, _stream()))
+    return Y
+
+
+# ------------------------------------------------------------------ what stands around the layers: norms, steps, adapters
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, whose stream the calls take."""
+    now = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != now:
+            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{now}")
+
+
+def _beside(t, shape, dtypes, name):
+    """(address, element type, distance of the rows) of a matrix of this shape and one of these types, or of none."""
+    if t is None:
+        return None, DAB_F32, 0
+    ptr, code, ld = _matrix(t, name)
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    _shaped(t, shape, name)
+    return ptr, code, ld
+
+
+def dab_rms_norm(X, gain, residual=None, eps=1e-5, save=False, out=None):
+    """The root-mean-square norm of X + residual (fp32, bf16 or f16 [rows, cols]) times gain (fp32 [cols]) -> (Y, H, rstd, saved).
+
+    H is the sum (X itself without a residual), rstd fp32 [rows] what the gradient takes.  save: Y as dab_ckpt8_save() keeps it too, saved = (Q, S), or
+    only so (save="only": Y is None); else saved is None.  out: (Y, H, rstd, saved) to write into, None where a tensor is to be new; H may be
+    X or the residual, Y may be X."""
+    done = (_native or native()).rms_norm(X, gain, residual, eps, save, out)
+    if done is not None:
+        Y, H, rstd, Q, S = done
+        return Y, X if residual is None else H, rstd, None if Q is None else (Q, S)
+    ptr, dtype, ld = _matrix(X, "X")
+    rows, cols = X.shape
+    r, _, ldr = _beside(residual, X.shape, (X.dtype,), "residual")
+    g = _ptr(_shaped(gain, (cols,), "gain"), torch.float32, "gain")
+    Y, H, rstd, saved = out if out is not None else (None, None, None, None)
+    _here(X, residual, gain, Y, H, rstd, *(saved or ()))
+    H = _result(H, X.shape, X.dtype, X.device, "H") if residual is not None else X
+    Y = _result(Y, X.shape, X.dtype, X.device, "Y") if save != "only" else None
+    rstd = _result(rstd, (rows,), torch.float32, X.device, "rstd")
+    q = s = None
+    if save:
+        saved = saved if saved is not None else ckpt8_outputs(rows, cols, X.device)
+        q, s, n = _saved(*saved, cols)
+        if n != rows:
+            raise ValueError(f"Q: expected {rows} rows, got {n}")
+    _check("dab_rms_norm", lib().dab_rms_norm(ptr, dtype, ld, r, ldr, g, eps, rows, cols, H.data_ptr() if residual is not None else None,
+                                              Y.data_ptr() if Y is not None else None, q, s, rstd.data_ptr(), _stream()))
+    return Y, H, rstd, saved if save else None
+
+
+def dab_rms_norm_gradient(dY, H, gain, rstd, dH=None, out=None, ws=None):
+    """(dX [rows, cols] of H's type, dgain fp32 [cols]) from dY, dab_rms_norm()'s H and rstd, and what arrives at H beside the norm (dH)."""
+    done = (_native or native()).rms_norm_gradient(dY, H, gain, rstd, dH, out, ws)
+    if done is not None:
+        return done
+    h, dtype, ldh = _matrix(H, "H")
+    rows, cols = H.shape
+    dy, _, lddy = _beside(dY, H.shape, (H.dtype,), "dY")
+    if dy is None:
+        raise TypeError("dY: expected a tensor on the GPU")
+    d, _, ldd = _beside(dH, H.shape, (H.dtype,), "dH")
+    g, s = _ptr(_shaped(gain, (cols,), "gain"), torch.float32, "gain"), _ptr(_shaped(rstd, (rows,), "rstd"), torch.float32, "rstd")
+    dX, dgain = out if out is not None else (None, None)
+    _here(dY, H, gain, rstd, dH, dX, dgain)
+    dX, dgain = _result(dX, H.shape, H.dtype, H.device, "dX"), _result(dgain, (cols,), torch.float32, H.device, "dgain")
+    ws, at, nbytes = _scratch(lib().dab_rms_norm_gradient_workspace_bytes(rows, cols), H.device, ws)
+    _check("dab_rms_norm_gradient", lib().dab_rms_norm_gradient(dy, lddy, h, ldh, dtype, g, s, d, ldd, rows, cols, dX.data_ptr(), dgain.data_ptr(), at,
+                                                                nbytes, _stream()))
+    return dX, dgain
+
+
+def _flat(t, n, dtypes, name):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a tensor on the GPU")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: tensor must be contiguous")
+    if t.numel() != n:
+        raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def adamw_states(P, bits=32):
+    """The two states of a tensor before its first step: zeros, fp32 like P (bits=32) or pairs of codes and scale bytes (bits=8)."""
+    if bits == 32:
+        return torch.zeros_like(P, dtype=torch.float32), torch.zeros_like(P, dtype=torch.float32)
+    groups = (P.numel() + 31) // 32
+    return tuple((torch.zeros(32 * groups, dtype=torch.uint8, device=P.device), torch.full((groups,), 27, dtype=torch.uint8, device=P.device))
+                 for _ in range(2))
+
+
+class _AdamwJobs:
+    """What adamw_jobs() makes: the host array, and the tensors that it points into."""
+
+    def __init__(self, jobs, tensors, device):
+        self.jobs, self.tensors, self.device = jobs, tensors, device
+
+    def __len__(self):
+        return len(self.jobs)
+
+
+def adamw_jobs(items):
+    """A host array of dab_adamw_job from dicts(P, G, M, V, copy=None, weight_decay=0.0, place=None), built once and reused per step.
+
+    P: fp32; G: a gradient of as many elements (fp32, bf16 or f16); M, V: from adamw_states(); copy: a bf16 or f16 tensor that takes the new P
+    too; place: of the tensor in the sequence of random numbers (behind the tensor before it unless given).  The tensors are kept alive."""
+    if not items:
+        raise ValueError("expected one tensor at least")
+    arr, written, kept, place = (dab_adamw_job * len(items))(), [], [], 0
+    device = None
+    for k, it in enumerate(items):
+        P, G, M, V, copy = it["P"], it["G"], it["M"], it["V"], it.get("copy")
+        n = P.numel() if isinstance(P, torch.Tensor) else 0
+        p = _flat(P, n, (torch.float32,), "P")
+        device = P.device if device is None else device
+        g = _flat(G, n, tuple(_REAL), "G")
+        c = _flat(copy, n, (torch.bfloat16, torch.float16), "copy") if copy is not None else None
+        bits = 8 if isinstance(M, (tuple, list)) else 32
+        if bits == 8:
+            if not isinstance(V, (tuple, list)):
+                raise TypeError("V: expected codes and scale bytes, as for M")
+            groups = (n + 31) // 32
+            m, ms = _flat(M[0], 32 * groups, (torch.uint8,), "M"), _flat(M[1], groups, (torch.uint8,), "M's scales")
+            v, vs = _flat(V[0], 32 * groups, (torch.uint8,), "V"), _flat(V[1], groups, (torch.uint8,), "V's scales")
+            states = [*M, *V]
+        else:
+            m, v, ms, vs = _flat(M, n, (torch.float32,), "M"), _flat(V, n, (torch.float32,), "V"), None, None
+            states = [M, V]
+        tensors = [P, *states] + ([copy] if copy is not None else [])
+        for t in [G, *tensors]:
+            if t.device != device:
+                raise ValueError(f"all tensors are on one device: {t.device} and {device}")
+        if it.get("place") is not None:
+            place = it["place"]
+        arr[k] = dab_adamw_job(p, g, m, v, ms, vs, c, n, place, _REAL[G.dtype], _REAL[copy.dtype] if copy is not None else 0, bits,
+                               it.get("weight_decay", 0.0))
+        place += 32 * ((n + 31) // 32)
+        written += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), True) for t in tensors]
+        written.append((g, g + n * G.element_size(), False))
+        kept += [G, *tensors]
+    written.sort()
+    last_in = last_out = 0
+    for a, b, out in written:
+        if a < last_out or (out and a < last_in):
+            raise ValueError("two tensors of the step overlap")
+        if out:
+            last_out = max(last_out, b)
+        else:
+            last_in = max(last_in, b)
+    return _AdamwJobs(arr, kept, device)
+
+
+def dab_adamw(jobs, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0):
+    """A step of AdamW for every job of adamw_jobs(), in place.
+
+    lr, step (from 1 on): numbers, or tensors of one element on the GPU (fp32, int64) that a captured graph reads anew at every replay; grad_scale: an
+    fp32 tensor of one element that multiplies all gradients (infinite or a NaN: nothing is changed).  seed: of the random numbers that 8-bit states
+    are rounded by, with the step."""
+    lr_dev = _flat(lr, 1, (torch.float32,), "lr") if isinstance(lr, torch.Tensor) else None
+    step_dev = _flat(step, 1, (torch.int64,), "step") if isinstance(step, torch.Tensor) else None
+    scale = _flat(grad_scale, 1, (torch.float32,), "grad_scale") if grad_scale is not None else None
+    _here(jobs.tensors[0], grad_scale, *(t for t in (lr, step) if isinstance(t, torch.Tensor)))
+    s = dab_adamw_step(0.0 if lr_dev else lr, beta1, beta2, eps, 1 if step_dev else step, seed, lr_dev, step_dev, scale)
+    _check("dab_adamw", lib().dab_adamw(jobs.jobs, len(jobs.jobs), ctypes.byref(s), _stream()))
+
+
+def _state8(Q, S, name):
+    groups = S.numel() if isinstance(S, torch.Tensor) else 0
+    return _flat(Q, 32 * groups, (torch.uint8,), name), _flat(S, groups, (torch.uint8,), f"{name}'s scales"), 32 * groups
+
+
+def dab_state8_restore(Q, S, is_signed, dtype=torch.float32, n=None, out=None):
+    """What an 8-bit state stands for (is_signed: a first moment, else the root of a second one), of its first n elements (all unless given)."""
+    q, s, most = _state8(Q, S, "Q")
+    n = most if n is None else n
+    if not most - 32 < n <= most:
+        raise ValueError(f"n: expected {most - 31} .. {most}, got {n}")
+    if dtype not in _REAL:
+        raise TypeError(f"dtype: expected torch.float32, torch.bfloat16 or torch.float16, got {dtype}")
+    X = _result(out, (n,), dtype, Q.device, "out")
+    _here(Q, S, X)
+    _check("dab_state8_restore", lib().dab_state8_restore(q, s, n, int(bool(is_signed)), X.data_ptr(), _REAL[dtype], _stream()))
+    return X
+
+
+def dab_state8_save(X, is_signed, out=None):
+    """Numbers (fp32, any shape) as an 8-bit state, to the nearest code -> (Q uint8 [32 groups], S uint8 [groups])."""
+    n = X.numel()
+    x = _flat(X, n, (torch.float32,), "X")
+    groups = (n + 31) // 32
+    Q, S = out if out is not None else (None, None)
+    Q, S = _result(Q, (32 * groups,), torch.uint8, X.device, "Q"), _result(S, (groups,), torch.uint8, X.device, "S")
+    _here(X, Q, S)
+    _check("dab_state8_save", lib().dab_state8_save(x, n, int(bool(is_signed)), Q.data_ptr(), S.data_ptr(), _stream()))
+    return Q, S
+
+
+def _adapters(X, ids, A, B, scale, F):
+    """The arguments that the calls with adapters share, checked: (address, type, distance of X's rows), ids, A, B, scale, n, r."""
+    x, dtype, ld = _matrix(X, "X")
+    T, K = X.shape
+    if not isinstance(A, torch.Tensor) or A.dim() != 3:
+        raise ValueError("A: expected three dimensions")
+    n, r = A.shape[0], A.shape[1]
+    if F is None:
+        if not isinstance(B, torch.Tensor) or B.dim() != 3:
+            raise ValueError("B: expected three dimensions")
+        F = B.shape[2]
+    a, b = _ptr(_shaped(A, (n, r, K), "A"), X.dtype, "A"), _ptr(_shaped(B, (n, r, F), "B"), X.dtype, "B")
+    i = _ptr(_shaped(ids, (T,), "ids"), torch.int32, "ids")
+    s = None if scale is None else _ptr(_shaped(scale, (n,), "scale"), torch.float32, "scale")
+    if None in (a, b, i):
+        raise TypeError("A, B and ids: expected tensors on the GPU")
+    for t, name in ((A, "A"), (B, "B")):
+        _counted(t, name)
+    _here(X, ids, A, B, scale)
+    return (x, dtype, ld), i, a, b, s, T, K, F, n, r
+
+
+def dab_adapters(X, ids, A, B, scale=None, base=None, out=None):
+    """base + scale_i (X A_i^T) B_i for every token's adapter i = ids[t] (none unless 0 <= i < n) -> (Y [T, F] of X's type, U fp32 [T, r]).
+
+    X [T, K]; ids int32 [T]; A [n, r, K] and B [n, r, F] of X's type; scale fp32 [n] or None for ones; base [T, F] of X's type or fp32, or None for
+    zeros.  out: (Y, U) to write into, None where a tensor is to be new; Y may be base."""
+    done = (_native or native()).adapters(X, ids, A, B, scale, base, out)
+    if done is not None:
+        return done
+    (x, dtype, ld), i, a, b, s, T, K, F, n, r = _adapters(X, ids, A, B, scale, None)
+    p, base_dtype, ldb = _beside(base, (T, F), (X.dtype, torch.float32), "base")
+    Y, U = out if out is not None else (None, None)
+    _here(base, Y, U)
+    Y, U = _result(Y, (T, F), X.dtype, X.device, "Y"), _result(U, (T, r), torch.float32, X.device, "U")
+    _check("dab_adapters", lib().dab_adapters(x, dtype, ld, i, a, b, s, T, K, F, n, r, p, base_dtype, ldb, Y.data_ptr(), U.data_ptr(), _stream()))
+    return Y, U
+
+
+def dab_adapters_gradient(dY, X, U, ids, A, B, scale=None, base=None, want_dX=True, out=None, ws=None):
+    """(dX [T, K] of X's type, dA fp32 [n, r, K], dB fp32 [n, r, F]) of dab_adapters(), with U from it.
+
+    base [T, K] of X's type or fp32: what dX is added to (the shared projection's gradient), or None.  want_dX=False: dX is None.  out: (dX, dA, dB) to
+    write into, None where a tensor is to be new; dX may be base."""
+    done = (_native or native()).adapters_gradient(dY, X, U, ids, A, B, scale, base, want_dX, out, ws)
+    if done is not None:
+        return done
+    (x, dtype, ld), i, a, b, s, T, K, F, n, r = _adapters(X, ids, A, B, scale, None)
+    dy, _, lddy = _beside(dY, (T, F), (X.dtype,), "dY")
+    if dy is None:
+        raise TypeError("dY: expected a tensor on the GPU")
+    u = _ptr(_shaped(U, (T, r), "U"), torch.float32, "U")
+    p, base_dtype, ldb = _beside(base, (T, K), (X.dtype, torch.float32), "base")
+    if base is not None and not want_dX:
+        raise ValueError("base: there is no dX to add it to")
+    dX, dA, dB = out if out is not None else (None, None, None)
+    _here(dY, U, base, dX, dA, dB)
+    dX = _result(dX, (T, K), X.dtype, X.device, "dX") if want_dX else None
+    dA, dB = _result(dA, (n, r, K), torch.float32, X.device, "dA"), _result(dB, (n, r, F), torch.float32, X.device, "dB")
+    ws, at, nbytes = _scratch(lib().dab_adapters_gradient_workspace_bytes(T, K, F, n, r), X.device, ws)
+    _check("dab_adapters_gradient", lib().dab_adapters_gradient(dy, lddy, x, dtype, ld, u, i, a, b, s, T, K, F, n, r, p, base_dtype, ldb,
+                                                                dX.data_ptr() if want_dX else None, dA.data_ptr(), dB.data_ptr(), at, nbytes,
+                                                                _stream()))
+    return dX, dA, dB
+
+
+def dab_w4_adapters(X, Q, S, F, ids, A, B, scale=None, out=None, ws=None):
+    """X [T, K] times the F packed rows, plus every token's adapter (arguments as of dab_w4_matvec() and dab_adapters()) -> Y [T, F] of X's type."""
+    done = (_native or native()).w4_adapters(X, Q, S, F, ids, A, B, scale, out, ws)
+    if done is not None:
+        return done
+    (x, dtype, ld), i, a, b, s, T, K, F, n, r = _adapters(X, ids, A, B, scale, F)
+    q, sc = _packed(Q, S, F, K)
+    _here(Q, S, out)
+    Y = _result(out, (T, F), X.dtype, X.device, "out")
+    ws, at, nbytes = _scratch(lib().dab_w4_adapters_workspace_bytes(T, K, F, r, dtype, ld), X.device, ws)
+    _check("dab_w4_adapters", lib().dab_w4_adapters(x, dtype, ld, q, sc, i, a, b, s, T, K, F, n, r, Y.data_ptr(), at, nbytes, _stream()))
     return Y

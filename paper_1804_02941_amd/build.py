@@ -20,6 +20,7 @@ LIB = os.path.join(PKG, "libdab_hip.so")
 CALL = os.path.join(PKG, "_dab_call.so")
 SOURCES = ("api.hip", "binconv.hip", "direct.hip", "wbin.hip", "pack.hip", "estimate.hip", "training.hip",
            "ckpt.hip", "w4.hip", "product16.hip", "small32.hip", "head.hip",
+           "norm.hip", "adamw.hip", "adapters.hip",
            "probe.hip")
 
 FLAGS = [

@@ -418,12 +418,14 @@ void* packed(PyObject* o, at::ScalarType type, std::array<int64_t, N> shape) {
 }
 // Outputs and the workspace of a call.  item(): the i-th of the caller's outputs (a tuple of them where there are two).
 struct Outputs {
+    static constexpr int kMost = 5;
     c10::Device device;
-    PyObject* given[2] = {nullptr, nullptr};
-    at::Tensor made[2], scratch;
-    c10::SmallVector<int64_t, 4> shape[2];
-    at::ScalarType type[2];
-    void *out[2] = {nullptr, nullptr}, *ws = nullptr;
+    PyObject* given[kMost] = {};
+    at::Tensor made[kMost], scratch;
+    c10::SmallVector<int64_t, 4> shape[kMost];
+    at::ScalarType type[kMost];
+    bool wanted[kMost] = {};
+    void *out[kMost] = {}, *ws = nullptr;
     size_t ws_bytes = 0;
     int n = 0;
 
@@ -433,6 +435,11 @@ struct Outputs {
         for (const int64_t v : s) whole(v);
         type[n] = t, shape[n].assign(s.begin(), s.end());
         if (o != Py_None) given[n] = o, out[n] = packed(o, t, s);
+        wanted[n++] = true;
+        return *this;
+    }
+    // (an output of a call that this one has not: None among the results)
+    Outputs& none() {
         ++n;
         return *this;
     }
@@ -447,7 +454,7 @@ struct Outputs {
     }
     void allocate() {
         for (int i = 0; i < n; ++i)
-            if (out[i] == nullptr) {
+            if (wanted[i] && out[i] == nullptr) {
                 made[i] = at::empty(shape[i], at::TensorOptions().dtype(type[i]).device(device));
                 out[i] = made[i].data_ptr();
             }
@@ -457,20 +464,26 @@ struct Outputs {
         }
     }
     PyObject* item(int i) {
+        if (!wanted[i]) Py_RETURN_NONE;
         if (given[i] == nullptr) return THPVariable_Wrap(std::move(made[i]));
         Py_INCREF(given[i]);
         return given[i];
     }
     PyObject* result() {
         if (n == 1) return item(0);
-        PyObject *a = item(0), *b = item(1);
-        return a && b ? Py_BuildValue("NN", a, b) : nullptr;
+        PyObject* all = PyTuple_New(n);
+        for (int i = 0; all != nullptr && i < n; ++i) {
+            PyObject* one = item(i);
+            if (one == nullptr) Py_CLEAR(all);
+            else PyTuple_SET_ITEM(all, i, one);
+        }
+        return all;
     }
 };
-PyObject* item(PyObject* pair, int i) {
-    if (pair == Py_None) return Py_None;
-    if (!PyTuple_CheckExact(pair) || PyTuple_GET_SIZE(pair) != 2) throw Unusual{};
-    return PyTuple_GET_ITEM(pair, i);
+PyObject* item(PyObject* several, int i, int count = 2) {
+    if (several == Py_None) return Py_None;
+    if (!PyTuple_CheckExact(several) || PyTuple_GET_SIZE(several) != count) throw Unusual{};
+    return PyTuple_GET_ITEM(several, i);
 }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m; }
 int64_t whole_number(PyObject* o) {
@@ -605,6 +618,159 @@ PyObject* w4_matvec(PyObject*, PyObject* const* a, Py_ssize_t n) {
         });
     });
 }
+// ---------------------------------------------------------------- what stands around the layers
+// (tensors of another device than the current one are left to Python, which refuses them)
+const at::Tensor& here(const at::Tensor& t) {
+    if (t.device().index() != c10::hip::current_device()) throw Unusual{};
+    return t;
+}
+Matrix here(const Matrix& m) {
+    here(*m.t);
+    return m;
+}
+template <size_t N>
+void* here(PyObject* o, at::ScalarType type, std::array<int64_t, N> shape) {
+    here(plain(o, type));
+    return packed(o, type, shape);
+}
+// A matrix beside another one, of its shape and of this type (or of fp32), or none.
+Matrix beside(PyObject* o, int32_t rows, int32_t cols, int32_t dtype, bool or_f32 = false) {
+    if (o == Py_None) return {nullptr, nullptr, DAB_F32, rows, cols, 0};
+    const Matrix m = here(matrix(o));
+    if (m.rows != rows || m.cols != cols || (m.dtype != dtype && !(or_f32 && m.dtype == DAB_F32))) throw Unusual{};
+    return m;
+}
+void on_this_device(PyObject* out) {
+    if (out != Py_None && THPVariable_CheckExact(out)) here(THPVariable_Unpack(out));
+}
+bool truth(PyObject* o) {
+    if (o != Py_True && o != Py_False) throw Unusual{};
+    return o == Py_True;
+}
+// (X, gain, residual, eps, save, out)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<6>("dab_rms_norm", n, [&] {
+        const Matrix X = here(matrix(a[0])), R = beside(a[2], X.rows, X.cols, X.dtype);
+        const std::array shape{int64_t{X.rows}, int64_t{X.cols}};
+        const auto* gain = static_cast<const float*>(here(a[1], at::kFloat, std::array{int64_t{X.cols}}));
+        if (!PyFloat_CheckExact(a[3])) throw Unusual{};
+        const float eps = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
+        const bool save = truth(a[4]);
+        PyObject* saved = item(a[5], 3, 4);
+        for (int i = 0; i < 3; ++i) on_this_device(item(a[5], i, 4));
+        Outputs o(*X.t);
+        const auto type = X.t->scalar_type();
+        o.add(item(a[5], 0, 4), type, shape);
+        if (R.p) o.add(item(a[5], 1, 4), type, shape);
+        else o.none();
+        o.add(item(a[5], 2, 4), at::kFloat, std::array{int64_t{X.rows}});
+        if (save) {
+            on_this_device(item(saved, 0)), on_this_device(item(saved, 1));
+            o.add(item(saved, 0), at::kChar, std::array{int64_t{X.rows}, 32 * words(X.cols)}).add(item(saved, 1), at::kByte, std::array{int64_t{X.rows}, words(X.cols)});
+        } else {
+            o.none().none();
+        }
+        return std::pair(std::move(o), [=](const Outputs& b, void* st) {
+            return ::dab_rms_norm(X.p, X.dtype, X.ld, R.p, R.ld, gain, eps, X.rows, X.cols, b.out[1], b.out[0], static_cast<int8_t*>(b.out[3]),
+                                  static_cast<uint8_t*>(b.out[4]), static_cast<float*>(b.out[2]), st);
+        });
+    });
+}
+// (dY, H, gain, rstd, dH, out, ws)
+PyObject* rms_norm_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<7>("dab_rms_norm_gradient", n, [&] {
+        const Matrix H = here(matrix(a[1])), dH = beside(a[4], H.rows, H.cols, H.dtype);
+        if (a[0] == Py_None) throw Unusual{};
+        const Matrix dY = beside(a[0], H.rows, H.cols, H.dtype);
+        const auto* gain = static_cast<const float*>(here(a[2], at::kFloat, std::array{int64_t{H.cols}}));
+        const auto* rstd = static_cast<const float*>(here(a[3], at::kFloat, std::array{int64_t{H.rows}}));
+        Outputs o(*H.t);
+        on_this_device(item(a[5], 0)), on_this_device(item(a[5], 1));
+        o.add(item(a[5], 0), H.t->scalar_type(), std::array{int64_t{H.rows}, int64_t{H.cols}}).add(item(a[5], 1), at::kFloat, std::array{int64_t{H.cols}});
+        o.workspace(::dab_rms_norm_gradient_workspace_bytes(H.rows, H.cols), a[6]);
+        return std::pair(std::move(o), [=](const Outputs& b, void* st) {
+            return ::dab_rms_norm_gradient(dY.p, dY.ld, H.p, H.ld, H.dtype, gain, rstd, dH.p, dH.ld, H.rows, H.cols, b.out[0],
+                                           static_cast<float*>(b.out[1]), b.ws, b.ws_bytes, st);
+        });
+    });
+}
+struct WithAdapters {
+    Matrix X;
+    const int32_t* ids;
+    const void *A, *B;
+    const float* scale;
+    int32_t F, n, r;
+};
+WithAdapters with_adapters(PyObject* X, PyObject* ids, PyObject* A, PyObject* B, PyObject* scale) {
+    WithAdapters w{};
+    w.X = here(matrix(X));
+    const auto type = w.X.t->scalar_type();
+    const at::Tensor &a = here(plain(A, type)), &b = here(plain(B, type));
+    if (a.dim() != 3 || b.dim() != 3) throw Unusual{};
+    w.n = whole(a.size(0)), w.r = whole(a.size(1)), w.F = whole(b.size(2));
+    if (a.size(2) != w.X.cols || b.size(0) != w.n || b.size(1) != w.r) throw Unusual{};
+    w.A = a.data_ptr(), w.B = b.data_ptr();
+    w.ids = static_cast<const int32_t*>(here(ids, at::kInt, std::array{int64_t{w.X.rows}}));
+    w.scale = scale == Py_None ? nullptr : static_cast<const float*>(here(scale, at::kFloat, std::array{int64_t{w.n}}));
+    return w;
+}
+// (X, ids, A, B, scale, base, out)
+PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<7>("dab_adapters", n, [&] {
+        const WithAdapters w = with_adapters(a[0], a[1], a[2], a[3], a[4]);
+        const Matrix& X = w.X;
+        const Matrix base = beside(a[5], X.rows, w.F, X.dtype, true);
+        Outputs o(*X.t);
+        on_this_device(item(a[6], 0)), on_this_device(item(a[6], 1));
+        o.add(item(a[6], 0), X.t->scalar_type(), std::array{int64_t{X.rows}, int64_t{w.F}}).add(item(a[6], 1), at::kFloat, std::array{int64_t{X.rows}, int64_t{w.r}});
+        return std::pair(std::move(o), [w, base](const Outputs& b, void* st) {
+            return ::dab_adapters(w.X.p, w.X.dtype, w.X.ld, w.ids, w.A, w.B, w.scale, w.X.rows, w.X.cols, w.F, w.n, w.r, base.p, base.dtype, base.ld,
+                                  b.out[0], static_cast<float*>(b.out[1]), st);
+        });
+    });
+}
+// (dY, X, U, ids, A, B, scale, base, want_dX, out, ws)
+PyObject* adapters_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<11>("dab_adapters_gradient", n, [&] {
+        const WithAdapters w = with_adapters(a[1], a[3], a[4], a[5], a[6]);
+        const Matrix& X = w.X;
+        if (a[0] == Py_None) throw Unusual{};
+        const Matrix dY = beside(a[0], X.rows, w.F, X.dtype), base = beside(a[7], X.rows, X.cols, X.dtype, true);
+        const auto* U = static_cast<const float*>(here(a[2], at::kFloat, std::array{int64_t{X.rows}, int64_t{w.r}}));
+        const bool want = truth(a[8]);
+        if (base.p && !want) throw Unusual{};
+        Outputs o(*X.t);
+        for (int i = 0; i < 3; ++i) on_this_device(item(a[9], i, 3));
+        if (want) o.add(item(a[9], 0, 3), X.t->scalar_type(), std::array{int64_t{X.rows}, int64_t{X.cols}});
+        else o.none();
+        o.add(item(a[9], 1, 3), at::kFloat, std::array{int64_t{w.n}, int64_t{w.r}, int64_t{X.cols}});
+        o.add(item(a[9], 2, 3), at::kFloat, std::array{int64_t{w.n}, int64_t{w.r}, int64_t{w.F}});
+        o.workspace(::dab_adapters_gradient_workspace_bytes(X.rows, X.cols, w.F, w.n, w.r), a[10]);
+        return std::pair(std::move(o), [w, dY, U, base](const Outputs& b, void* st) {
+            return ::dab_adapters_gradient(dY.p, dY.ld, w.X.p, w.X.dtype, w.X.ld, U, w.ids, w.A, w.B, w.scale, w.X.rows, w.X.cols, w.F, w.n, w.r, base.p,
+                                           base.dtype, base.ld, b.out[0], static_cast<float*>(b.out[1]), static_cast<float*>(b.out[2]), b.ws,
+                                           b.ws_bytes, st);
+        });
+    });
+}
+// (X, Q, S, F, ids, A, B, scale, out, ws)
+PyObject* w4_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return whole_call<10>("dab_w4_adapters", n, [&] {
+        const WithAdapters w = with_adapters(a[0], a[4], a[5], a[6], a[7]);
+        const Matrix& X = w.X;
+        const int32_t F = whole(small_int(a[3]));
+        if (F != w.F) throw Unusual{};
+        const auto *Q = static_cast<const uint8_t*>(here(a[1], at::kByte, w4_codes(F, X.cols))), *S = static_cast<const uint8_t*>(here(a[2], at::kByte, w4_scales(F, X.cols)));
+        Outputs o(*X.t);
+        on_this_device(a[8]);
+        o.add(a[8], X.t->scalar_type(), std::array{int64_t{X.rows}, int64_t{F}});
+        o.workspace(::dab_w4_adapters_workspace_bytes(X.rows, X.cols, F, w.r, X.dtype, X.ld), a[9]);
+        return std::pair(std::move(o), [w, Q, S](const Outputs& b, void* st) {
+            return ::dab_w4_adapters(w.X.p, w.X.dtype, w.X.ld, Q, S, w.ids, w.A, w.B, w.scale, w.X.rows, w.X.cols, w.F, w.n, w.r, b.out[0], b.ws,
+                                     b.ws_bytes, st);
+        });
+    });
+}
 PyMethodDef whole_def(const char* name, PyObject* (*fn)(PyObject*, PyObject* const*, Py_ssize_t)) {
     return PyMethodDef{name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr};
 }
@@ -648,6 +814,8 @@ PyMethodDef* methods() {
         whole_def("ckpt8_save", ckpt8_save), whole_def("ckpt8_restore", ckpt8_restore), whole_def("ckpt8_weight_gradient", ckpt8_weight_gradient),
         whole_def("head_loss", head_loss), whole_def("head_loss_gradient", head_loss_gradient),
         whole_def("w4_pack", w4_pack), whole_def("w4_unpack", w4_unpack), whole_def("w4_matvec", w4_matvec),
+        whole_def("rms_norm", rms_norm), whole_def("rms_norm_gradient", rms_norm_gradient),
+        whole_def("adapters", adapters), whole_def("adapters_gradient", adapters_gradient), whole_def("w4_adapters", w4_adapters),
         {"setup", setup, METH_VARARGS, nullptr},
         {nullptr, nullptr, 0, nullptr},
     };

@@ -1,0 +1,412 @@
+// The root-mean-square norm: forward with the residual's addition and a copy of the output in 8 bits, and its gradients.
+//
+//     h = x + r (rounded to the tensors' type),  y = gain h / sqrt(mean(h^2) + eps)
+//     n = h rstd,  w = gain dy:   dx = rstd (w - n mean(w n)) + dh,   dgain = sum over rows of dy n
+//
+// One pass over memory each: 2^LOG lanes hold a row in registers, eight neighbouring values at a time, from the load to the store, so that
+// the sum over the row costs no second read.  Bound by memory.
+#include "lanes.h"
+#include "real16.h"
+
+namespace dab {
+
+constexpr int kNormThreads = 256;    // of a workgroup, unless a row takes more
+
+struct NormGeom {
+    int rows, cols, groups;          // groups of 32 of a row
+    int64_t ldx, ldr;                // of x and r, or of dy and h
+    int64_t ldd;                     // of dh
+    float eps;
+};
+
+// The sum over the 2^LOG lanes of a row; buffer: one of two, so that a barrier stands between a value's last reader and its next writer.
+template <int LOG>
+__device__ __forceinline__ float row_sum(float v, float (&part)[2][16], int buffer) {
+    v = lanes_sum<(LOG < 6 ? LOG : 6)>(v);
+    if constexpr (LOG > 6) {
+        constexpr int kWaves = 1 << (LOG - 6);
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) part[buffer][wave] = v;
+        __syncthreads();
+        const int first = wave & ~(kWaves - 1);
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) v += part[buffer][first + i];
+    }
+    return v;
+}
+
+// Eight values of y as bytes with their group's scale, as dab_ckpt8_save() writes them.
+__device__ __forceinline__ void save_eight(const float (&y)[8], int64_t row_groups, int c, int8_t* __restrict__ Q, uint8_t* __restrict__ S) {
+    const uint32_t m = group_max(y);
+    uint64_t word = 0;
+    int code = 255;
+    if (m < 0x7f800000u) {
+        const int e = group_exponent<6>(m);
+        const float inv = pow2f(-e);
+        code = e + 127;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int q = static_cast<int>(fminf(fmaxf(rintf(y[i] * inv), -127.f), 127.f));
+            word |= static_cast<uint64_t>(static_cast<uint8_t>(q)) << (8 * i);
+        }
+    }
+    *reinterpret_cast<uint64_t*>(Q + row_groups * 32 + c) = word;
+    if ((c & 31) == 0) S[row_groups + (c >> 5)] = static_cast<uint8_t>(code);
+}
+
+// Rows of at most 8 NV 2^LOG values.  Lane i of a row holds the eights i, i + 2^LOG, ..
+template <typename T, int LOG, int NV>
+__global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_kernel(const T* X, const T* R, const float* __restrict__ gain, NormGeom g,
+                                                                                T* H, T* Y, int8_t* Q, uint8_t* S, float* rstd) {
+    __shared__ float part[2][16];
+    DAB_RESERVE_VGPRS();
+    constexpr int kLanes = 1 << LOG, kRows = LOG > 8 ? 1 : kNormThreads >> LOG;
+    const int lane = threadIdx.x & (kLanes - 1);
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + (threadIdx.x >> LOG);
+    const bool live = row < g.rows;
+    float h[NV][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * kLanes + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[j][i] = 0.f;
+        if (live && c < g.cols) {
+            load8(X + row * g.ldx, c, g.cols, h[j]);
+            if (R) {
+                float r[8];
+                load8(R + row * g.ldr, c, g.cols, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[j][i] = static_cast<float>(static_cast<T>(h[j][i] + r[i]));
+                store8(H + row * g.cols, c, g.cols, h[j]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += h[j][i] * h[j][i];
+    }
+    sum = row_sum<LOG>(sum, part, 0);
+    const float scale = 1.f / sqrtf(sum / static_cast<float>(g.cols) + g.eps);
+    if (!live) return;
+    if (lane == 0) rstd[row] = scale;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * kLanes + lane) * 8;
+        float y[8] = {};
+        if (c < g.cols) {
+            load8(gain, c, g.cols, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = (h[j][i] * scale) * y[i];
+            if (Y) store8(Y + row * g.cols, c, g.cols, y);
+        }
+        // (the four lanes of a group are all here, those past the row's end with zeros)
+        if (Q && c < g.groups * 32) save_eight(y, row * g.groups, c, Q, S);
+    }
+}
+
+// Rows that no workgroup holds: read twice, the second time what the first has written where there is a residual.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const T* R, const float* __restrict__ gain, NormGeom g, T* H, T* Y, int8_t* Q,
+                                                         uint8_t* S, float* rstd) {
+    __shared__ float part[2][16];
+    const int64_t row = blockIdx.x;
+    const T* x = X + row * g.ldx;
+    T* hout = H + row * g.cols;                              // (not used without a residual)
+    float sum = 0.f;
+    for (int64_t c0 = threadIdx.x * 8; c0 < g.cols; c0 += 8192) {
+        const int c = static_cast<int>(c0);
+        float h[8];
+        load8(x, c, g.cols, h);
+        if (R) {
+            float r[8];
+            load8(R + row * g.ldr, c, g.cols, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = static_cast<float>(static_cast<T>(h[i] + r[i]));
+            store8(hout, c, g.cols, h);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += h[i] * h[i];
+    }
+    sum = row_sum<10>(sum, part, 0);
+    const float scale = 1.f / sqrtf(sum / static_cast<float>(g.cols) + g.eps);
+    if (threadIdx.x == 0) rstd[row] = scale;
+    for (int64_t c0 = threadIdx.x * 8; c0 < static_cast<int64_t>(g.groups) * 32; c0 += 8192) {
+        const int c = static_cast<int>(c0);
+        float h[8] = {}, y[8] = {};
+        if (c < g.cols) {
+            load8(R ? static_cast<const T*>(hout) : x, c, g.cols, h);
+            load8(gain, c, g.cols, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = (h[i] * scale) * y[i];
+            if (Y) store8(Y + row * g.cols, c, g.cols, y);
+        }
+        if (Q) save_eight(y, row * g.groups, c, Q, S);
+    }
+}
+
+// ---------------------------------------------------------------- gradients
+// A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it holds at once) and keeps its part of dgain in registers meanwhile;
+// norm_join_kernel adds the parts in a fixed order.
+template <typename T, int LOG, int NV>
+__global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_kernel(const T* dY, const T* H, const float* __restrict__ gain,
+                                                                                     const float* __restrict__ rstd, const T* dH, NormGeom g, T* dX,
+                                                                                     float* __restrict__ parts) {
+    __shared__ float part[2][16];
+    DAB_RESERVE_VGPRS();
+    constexpr int kLanes = 1 << LOG, kRows = LOG > 8 ? 1 : kNormThreads >> LOG;
+    const int lane = threadIdx.x & (kLanes - 1), slot = threadIdx.x >> LOG;
+    float dg[NV][8], gn[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * kLanes + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[j][i] = 0.f, gn[j][i] = 0.f;
+        if (c < g.cols) load8(gain, c, g.cols, gn[j]);
+    }
+    int buffer = 0;
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < g.rows; row0 += static_cast<int64_t>(gridDim.x) * kRows, buffer ^= 1) {
+        const int64_t row = row0 + slot;
+        const bool live = row < g.rows;
+        const float s = live ? rstd[row] : 0.f;
+        float n[NV][8], w[NV][8];
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * kLanes + lane) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n[j][i] = 0.f, w[j][i] = 0.f;
+            if (live && c < g.cols) {
+                load8(dY + row * g.ldx, c, g.cols, w[j]);
+                load8(H + row * g.ldr, c, g.cols, n[j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[j][i] *= s;
+                dg[j][i] += w[j][i] * n[j][i];
+                w[j][i] *= gn[j][i];
+                dot += w[j][i] * n[j][i];
+            }
+        }
+        dot = row_sum<LOG>(dot, part, buffer) / static_cast<float>(g.cols);
+        if (!live) continue;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * kLanes + lane) * 8;
+            if (c >= g.cols) continue;
+            float d[8] = {};
+            if (dH) load8(dH + row * g.ldd, c, g.cols, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] += (w[j][i] - n[j][i] * dot) * s;
+            store8(dX + row * g.cols, c, g.cols, d);
+        }
+    }
+    // [workgroup and slot][column]
+    float* to = parts + (static_cast<int64_t>(blockIdx.x) * kRows + slot) * g.cols;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * kLanes + lane) * 8;
+        if (c < g.cols) store8(to, c, g.cols, dg[j]);
+    }
+}
+
+// Rows that no workgroup holds: the workgroup's part of dgain lies in its row of `parts` meanwhile.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* dY, const T* H, const float* __restrict__ gain, const float* __restrict__ rstd,
+                                                              const T* dH, NormGeom g, T* dX, float* parts) {
+    __shared__ float part[2][16];
+    float* to = parts + static_cast<int64_t>(blockIdx.x) * g.cols;
+    int buffer = 0;
+    for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x, buffer ^= 1) {
+        const float s = rstd[row];
+        float dot = 0.f;
+        for (int64_t c0 = threadIdx.x * 8; c0 < g.cols; c0 += 8192) {
+            const int c = static_cast<int>(c0);
+            float w[8], n[8], gn[8], dg[8] = {};
+            load8(dY + row * g.ldx, c, g.cols, w), load8(H + row * g.ldr, c, g.cols, n), load8(gain, c, g.cols, gn);
+            if (row != blockIdx.x) load8(static_cast<const float*>(to), c, g.cols, dg);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[i] *= s;
+                dg[i] += w[i] * n[i];
+                dot += (w[i] * gn[i]) * n[i];
+            }
+            store8(to, c, g.cols, dg);
+        }
+        dot = row_sum<10>(dot, part, buffer) / static_cast<float>(g.cols);
+        for (int64_t c0 = threadIdx.x * 8; c0 < g.cols; c0 += 8192) {
+            const int c = static_cast<int>(c0);
+            float w[8], n[8], gn[8], d[8] = {};
+            load8(dY + row * g.ldx, c, g.cols, w), load8(H + row * g.ldr, c, g.cols, n), load8(gain, c, g.cols, gn);
+            if (dH) load8(dH + row * g.ldd, c, g.cols, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] += (w[i] * gn[i] - (n[i] * s) * dot) * s;
+            store8(dX + row * g.cols, c, g.cols, d);
+        }
+    }
+}
+
+// dgain[c] = sum over the parts: 64 columns a workgroup, 16 wavefronts that share the parts.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* __restrict__ parts, int n, int cols, float* __restrict__ dgain) {
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    float v = 0.f;
+    if (c < cols)
+        for (int i = wave; i < n; i += 16) v += parts[static_cast<int64_t>(i) * cols + c];
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || c >= cols) return;
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += sums[i][lane];
+    dgain[c] = v;
+}
+
+// ---------------------------------------------------------------- host side
+// Lanes of a row (their logarithm) and eights of a lane; log 0: the kernels for long rows.
+struct NormForm {
+    int log, nv;
+};
+static NormForm norm_form(int cols, int max_nv) {
+    const int eights = ceil_div(cols, 8);
+    NormForm f{2, 1};
+    while (f.log < 6 && (1 << f.log) < eights) ++f.log;
+    while (f.nv < max_nv && (f.nv << f.log) < eights) f.nv *= 2;
+    while (f.log < 10 && (f.nv << f.log) < eights) ++f.log;
+    if ((static_cast<int64_t>(f.nv) << f.log) < eights) f.log = 0;
+    return f;
+}
+static int norm_rows(NormForm f) { return f.log == 0 || f.log > 8 ? 1 : kNormThreads >> f.log; }
+static int norm_threads(NormForm f) { return f.log == 0 ? 1024 : f.log > 8 ? 1 << f.log : kNormThreads; }
+constexpr int kNormNV = 4, kNormGradNV = 2;
+
+template <typename T>
+struct NormArgs {
+    const T *X, *R;
+    const float* gain;
+    NormGeom g;
+    T *H, *Y;
+    int8_t* Q;
+    uint8_t* S;
+    float* rstd;
+};
+template <typename T, int LOG, int NV>
+static int norm_launch(const NormArgs<T>& a, NormForm f, hipStream_t st) {
+    const dim3 grid(static_cast<unsigned>(ceil_div64(a.g.rows, norm_rows(f)))), block(norm_threads(f));
+    return launch(norm_kernel<T, LOG, NV>, grid, block, 0, st, a.X, a.R, a.gain, a.g, a.H, a.Y, a.Q, a.S, a.rstd);
+}
+template <typename T>
+static int norm_launch(const NormArgs<T>& a, hipStream_t st) {
+    const NormForm f = norm_form(a.g.cols, kNormNV);
+    switch (f.log) {
+        case 0: return launch(norm_long_kernel<T>, dim3(a.g.rows), dim3(1024), 0, st, a.X, a.R, a.gain, a.g, a.H, a.Y, a.Q, a.S, a.rstd);
+        case 2: return norm_launch<T, 2, 1>(a, f, st);
+        case 3: return norm_launch<T, 3, 1>(a, f, st);
+        case 4: return norm_launch<T, 4, 1>(a, f, st);
+        case 5: return norm_launch<T, 5, 1>(a, f, st);
+        case 6: return f.nv == 1 ? norm_launch<T, 6, 1>(a, f, st) : f.nv == 2 ? norm_launch<T, 6, 2>(a, f, st) : norm_launch<T, 6, 4>(a, f, st);
+        case 7: return norm_launch<T, 7, 4>(a, f, st);
+        case 8: return norm_launch<T, 8, 4>(a, f, st);
+        case 9: return norm_launch<T, 9, 4>(a, f, st);
+        default: return norm_launch<T, 10, 4>(a, f, st);
+    }
+}
+
+template <typename T>
+struct NormGradArgs {
+    const T *dY, *H;
+    const float *gain, *rstd;
+    const T* dH;
+    NormGeom g;
+    T* dX;
+    float *dgain, *parts;
+    int blocks;
+};
+template <typename T, int LOG, int NV>
+static int norm_grad_launch(const NormGradArgs<T>& a, NormForm f, hipStream_t st) {
+    return launch(norm_grad_kernel<T, LOG, NV>, dim3(a.blocks), dim3(norm_threads(f)), 0, st, a.dY, a.H, a.gain, a.rstd, a.dH, a.g, a.dX, a.parts);
+}
+// Workgroups of the gradient's kernel: what the chip holds at once, fewer where there are fewer rows.
+static int norm_grad_blocks(int rows, NormForm f) {
+    const int64_t n = ceil_div64(rows, norm_rows(f)), most = 2048 / norm_threads(f) * int64_t{kNumCU};
+    return static_cast<int>(n < most ? n : most);
+}
+template <typename T>
+static int norm_grad_launch(const NormGradArgs<T>& a, hipStream_t st) {
+    const NormForm f = norm_form(a.g.cols, kNormGradNV);
+    int rc;
+    switch (f.log) {
+        case 0: rc = launch(norm_grad_long_kernel<T>, dim3(a.blocks), dim3(1024), 0, st, a.dY, a.H, a.gain, a.rstd, a.dH, a.g, a.dX, a.parts); break;
+        case 2: rc = norm_grad_launch<T, 2, 1>(a, f, st); break;
+        case 3: rc = norm_grad_launch<T, 3, 1>(a, f, st); break;
+        case 4: rc = norm_grad_launch<T, 4, 1>(a, f, st); break;
+        case 5: rc = norm_grad_launch<T, 5, 1>(a, f, st); break;
+        case 6: rc = f.nv == 1 ? norm_grad_launch<T, 6, 1>(a, f, st) : norm_grad_launch<T, 6, 2>(a, f, st); break;
+        case 7: rc = norm_grad_launch<T, 7, 2>(a, f, st); break;
+        case 8: rc = norm_grad_launch<T, 8, 2>(a, f, st); break;
+        case 9: rc = norm_grad_launch<T, 9, 2>(a, f, st); break;
+        default: rc = norm_grad_launch<T, 10, 2>(a, f, st);
+    }
+    if (rc) return rc;
+    return launch(norm_join_kernel, dim3(ceil_div(a.g.cols, 64)), dim3(1024), 0, st, static_cast<const float*>(a.parts), a.blocks * norm_rows(f),
+                  a.g.cols, a.dgain);
+}
+
+constexpr int kNormMaxCols = 1 << 26;
+
+}  // namespace dab
+
+extern "C" int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const void* R, int64_t ldr, const float* gain, float eps, int32_t rows,
+                            int32_t cols, void* H, void* Y, int8_t* Q, uint8_t* S, float* rstd, void* stream) {
+    using namespace dab;
+    if (!X || !gain || !rstd || (R && !H) || (!Y && !Q) || (Q == nullptr) != (S == nullptr)) return DAB_ERR_NULL;
+    if (rows < 1 || cols < 1 || ldx < cols || (R && ldr < cols) || !(eps >= 0.f)) return DAB_ERR_SHAPE;
+    if (!real_dtype(dtype) || cols > kNormMaxCols) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(X, 16) || misaligned(R, 16) || misaligned(H, 16) || misaligned(Y, 16) || misaligned(Q, 16) || misaligned(gain, 4) ||
+        misaligned(rstd, 4))
+        return DAB_ERR_ALIGN;
+    NormGeom g{};
+    g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ldx = ldx, g.ldr = ldr, g.eps = eps;
+    const auto st = static_cast<hipStream_t>(stream);
+    const auto go = [&](auto* t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        const NormArgs<T> a{static_cast<const T*>(X), static_cast<const T*>(R), gain, g, static_cast<T*>(H), static_cast<T*>(Y), Q, S, rstd};
+        return norm_launch(a, st);
+    };
+    if (dtype == DAB_F32) return go(static_cast<float*>(nullptr));
+    if (dtype == DAB_BF16) return go(static_cast<bf16*>(nullptr));
+    return go(static_cast<f16*>(nullptr));
+}
+
+extern "C" size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t cols) {
+    using namespace dab;
+    if (rows < 1 || cols < 1 || cols > kNormMaxCols) return 0;
+    const NormForm f = norm_form(cols, kNormGradNV);
+    return static_cast<size_t>(norm_grad_blocks(rows, f)) * norm_rows(f) * cols * 4;
+}
+
+extern "C" int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t ldh, int32_t dtype, const float* gain, const float* rstd,
+                                     const void* dH, int64_t lddh, int32_t rows, int32_t cols, void* dX, float* dgain, void* ws, size_t ws_bytes,
+                                     void* stream) {
+    using namespace dab;
+    if (!dY || !H || !gain || !rstd || !dX || !dgain) return DAB_ERR_NULL;
+    if (rows < 1 || cols < 1 || lddy < cols || ldh < cols || (dH && lddh < cols)) return DAB_ERR_SHAPE;
+    if (!real_dtype(dtype) || cols > kNormMaxCols) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(dY, 16) || misaligned(H, 16) || misaligned(dH, 16) || misaligned(dX, 16) || misaligned(gain, 4) || misaligned(rstd, 4) ||
+        misaligned(dgain, 4))
+        return DAB_ERR_ALIGN;
+    const size_t need = dab_rms_norm_gradient_workspace_bytes(rows, cols);
+    if (!ws || ws_bytes < need || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    NormGeom g{};
+    g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ldx = lddy, g.ldr = ldh, g.ldd = lddh;
+    const int blocks = norm_grad_blocks(rows, norm_form(cols, kNormGradNV));
+    const auto st = static_cast<hipStream_t>(stream);
+    const auto go = [&](auto* t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        const NormGradArgs<T> a{static_cast<const T*>(dY), static_cast<const T*>(H), gain, rstd, static_cast<const T*>(dH), g,
+                                static_cast<T*>(dX), dgain, static_cast<float*>(ws), blocks};
+        return norm_grad_launch(a, st);
+    };
+    if (dtype == DAB_F32) return go(static_cast<float*>(nullptr));
+    if (dtype == DAB_BF16) return go(static_cast<bf16*>(nullptr));
+    return go(static_cast<f16*>(nullptr));
+}

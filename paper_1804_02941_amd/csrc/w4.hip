@@ -347,9 +347,8 @@ extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F,
     return static_cast<size_t>(ceil_div(B, nb)) * ceil_div(K, 128) * 4 * ceil_div(nb * P, 16) * 1024;
 }
 
-extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K,
-                             int32_t F, void* Y, void* ws, size_t ws_bytes, void* stream) {
-    using namespace dab;
+int dab::w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y,
+                    int32_t y_dtype, void* ws, size_t ws_bytes, void* stream) {
     if (!X || !Q || !S || !Y) return DAB_ERR_NULL;
     if (B < 1 || K < 1 || F < 1 || ldx < K) return DAB_ERR_SHAPE;
     if (!real_dtype(dtype) || K > (1 << 26) || B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
@@ -378,7 +377,7 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
     // groups of a workgroup: eight wavefronts, fewer where that leaves compute units without one (30 tokens, 1024 x 1024: 11.8 -> 7.1)
     g.groups = 8 / g.ks;
     while (g.groups > 1 && ceil_div(g.Ft, g.groups * TB) < kNumCU) g.groups /= 2;
-    g.dtype = dtype;
+    g.dtype = y_dtype;
     const bf16* x = static_cast<const bf16*>(X);
     g.ldx = ldx;
     if (need) {
@@ -393,4 +392,9 @@ extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const ui
         x = out;
     }
     return launch_matvec(g, columns, TB, !need, st, x, Q, S, Y);
+}
+
+extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K,
+                             int32_t F, void* Y, void* ws, size_t ws_bytes, void* stream) {
+    return dab::w4_product(X, dtype, ldx, Q, S, B, K, F, Y, dtype, ws, ws_bytes, stream);
 }
