@@ -605,7 +605,7 @@ int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t l
                           const void* dH, int64_t lddh, int32_t rows, int32_t cols, void* dX, float* dgain, void* ws, size_t ws_bytes, void* stream);
 
 /*
- * dab_adamw - a step of Adam with decoupled weight decay over many tensors at once (thirty-two a launch).  With g the gradient
+ * dab_adamw - a step of Adam with decoupled weight decay over many tensors at once, in one launch.  With g the gradient
  * times *grad_scale, every operation in fp32:
  *     m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
  *     p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
@@ -651,7 +651,20 @@ typedef struct dab_adamw_step {
     const float* grad_scale;        /* device memory, or NULL: 1                         */
 } dab_adamw_step;
 
-int dab_adamw(const dab_adamw_job* jobs /* host */, int32_t n_jobs, const dab_adamw_step* step /* host */, void* stream);
+/*
+ * The tensors of a step are laid out once, in a table of the caller's device memory: dab_adamw_plan_of checks the jobs and says how large it is,
+ * dab_adamw_table writes it (on `stream`, without reading host memory after it returns), and any number of dab_adamw calls take it as
+ * long as the tensors stay where they are.  The plan is the caller's too; what another call than these wrote into plan or table is not supported.
+ *   table   plan.table_bytes bytes, 256-byte aligned.  More than 2^23 workgroups (2^36 elements) -> DAB_ERR_UNSUPPORTED
+ */
+typedef struct dab_adamw_plan {
+    int32_t n_jobs, turns, workgroups;
+    int64_t table_bytes;
+} dab_adamw_plan;
+
+int dab_adamw_plan_of(const dab_adamw_job* jobs /* host */, int32_t n_jobs, dab_adamw_plan* plan /* host, out */);
+int dab_adamw_table(const dab_adamw_job* jobs /* host */, const dab_adamw_plan* plan /* host */, void* table, size_t table_bytes, void* stream);
+int dab_adamw(const void* table, size_t table_bytes, const dab_adamw_plan* plan /* host */, const dab_adamw_step* step /* host */, void* stream);
 
 /*
  * dab_state8_restore / dab_state8_save - 8-bit states as numbers, and numbers as 8-bit states rounded to the nearest code (halves up): is_signed

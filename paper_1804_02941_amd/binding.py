@@ -39,6 +39,10 @@ class dab_adamw_job(ctypes.Structure):
                 ("n", c_int64), ("place", c_uint64), ("grad_dtype", c_int32), ("copy_dtype", c_int32), ("bits", c_int32), ("weight_decay", c_float)]
 
 
+class dab_adamw_plan(ctypes.Structure):
+    _fields_ = [("n_jobs", c_int32), ("turns", c_int32), ("workgroups", c_int32), ("table_bytes", c_int64)]
+
+
 class dab_adamw_step(ctypes.Structure):
     _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("step", c_int64), ("seed", c_uint64),
                 ("lr_dev", c_void_p), ("step_dev", c_void_p), ("grad_scale", c_void_p)]
@@ -128,7 +132,9 @@ _SIGNATURES = {
     "dab_rms_norm_gradient_workspace_bytes": (c_size_t, [c_int32, c_int32]),
     "dab_rms_norm_gradient": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32,
                                       c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
-    "dab_adamw": (c_int, [ctypes.POINTER(dab_adamw_job), c_int32, ctypes.POINTER(dab_adamw_step), c_void_p]),
+    "dab_adamw_plan_of": (c_int, [ctypes.POINTER(dab_adamw_job), c_int32, ctypes.POINTER(dab_adamw_plan)]),
+    "dab_adamw_table": (c_int, [ctypes.POINTER(dab_adamw_job), ctypes.POINTER(dab_adamw_plan), c_void_p, c_size_t, c_void_p]),
+    "dab_adamw": (c_int, [c_void_p, c_size_t, ctypes.POINTER(dab_adamw_plan), ctypes.POINTER(dab_adamw_step), c_void_p]),
     "dab_state8_restore": (c_int, [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p]),
     "dab_state8_save": (c_int, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
     "dab_adapters": (c_int, [c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32,
@@ -842,20 +848,21 @@ def adamw_states(P, bits=32):
 
 
 class _AdamwJobs:
-    """What adamw_jobs() makes: the host array, and the tensors that it points into."""
+    """What adamw_jobs() makes: the table in device memory, and the tensors that it points into."""
 
-    def __init__(self, jobs, tensors, device):
-        self.jobs, self.tensors, self.device = jobs, tensors, device
+    def __init__(self, table, plan, tensors):
+        self.table, self.plan, self.tensors = table, plan, tensors
 
     def __len__(self):
-        return len(self.jobs)
+        return self.plan.n_jobs
 
 
 def adamw_jobs(items):
-    """A host array of dab_adamw_job from dicts(P, G, M, V, copy=None, weight_decay=0.0, place=None), built once and reused per step.
+    """The table of a step's tensors from dicts(P, G, M, V, copy=None, weight_decay=0.0, place=None), built once and reused per step.
 
     P: fp32; G: a gradient of as many elements (fp32, bf16 or f16); M, V: from adamw_states(); copy: a bf16 or f16 tensor that takes the new P
-    too; place: of the tensor in the sequence of random numbers (behind the tensor before it unless given).  The tensors are kept alive."""
+    too; place: of the tensor in the sequence of random numbers (behind the tensor before it unless given).  The tensors are kept alive.  The
+    table is written on the current stream and waited for (in a graph that is being captured, it is written at every replay)."""
     if not items:
         raise ValueError("expected one tensor at least")
     arr, written, kept, place = (dab_adamw_job * len(items))(), [], [], 0
@@ -899,7 +906,14 @@ def adamw_jobs(items):
             last_out = max(last_out, b)
         else:
             last_in = max(last_in, b)
-    return _AdamwJobs(arr, kept, device)
+    _here(*kept)
+    plan = dab_adamw_plan()
+    _check("dab_adamw_plan_of", lib().dab_adamw_plan_of(arr, len(arr), ctypes.byref(plan)))
+    table = torch.empty(plan.table_bytes, dtype=torch.uint8, device=device)
+    _check("dab_adamw_table", lib().dab_adamw_table(arr, ctypes.byref(plan), table.data_ptr(), table.numel(), _stream()))
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream().synchronize()
+    return _AdamwJobs(table, plan, kept)
 
 
 def dab_adamw(jobs, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, seed=0):
@@ -911,9 +925,9 @@ def dab_adamw(jobs, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None,
     lr_dev = _flat(lr, 1, (torch.float32,), "lr") if isinstance(lr, torch.Tensor) else None
     step_dev = _flat(step, 1, (torch.int64,), "step") if isinstance(step, torch.Tensor) else None
     scale = _flat(grad_scale, 1, (torch.float32,), "grad_scale") if grad_scale is not None else None
-    _here(jobs.tensors[0], grad_scale, *(t for t in (lr, step) if isinstance(t, torch.Tensor)))
+    _here(jobs.table, grad_scale, *(t for t in (lr, step) if isinstance(t, torch.Tensor)))
     s = dab_adamw_step(0.0 if lr_dev else lr, beta1, beta2, eps, 1 if step_dev else step, seed, lr_dev, step_dev, scale)
-    _check("dab_adamw", lib().dab_adamw(jobs.jobs, len(jobs.jobs), ctypes.byref(s), _stream()))
+    _check("dab_adamw", lib().dab_adamw(jobs.table.data_ptr(), jobs.table.numel(), ctypes.byref(jobs.plan), ctypes.byref(s), _stream()))
 
 
 def _state8(Q, S, name):

@@ -2,9 +2,10 @@
 //
 //     m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// One pass over memory: a lane holds eight neighbouring elements of everything, four lanes a group of 32 that shares a scale.  The tensors' addresses
-// come with the launch, so that a captured graph keeps them and nothing is copied to the device.  Bound by memory: 28 bytes an element with
-// fp32 gradients and states, 14 with bf16 gradients, 8-bit states and a bf16 copy.
+// One pass over memory: a lane holds eight neighbouring elements of everything, four lanes a group of 32 that shares a scale.  One launch
+// for all tensors: a table in device memory, written once by kernels that get the addresses with their launch (nothing is copied to the device, so
+// that it may be made in a captured graph too), says which stretch of which tensor a workgroup takes.  Bound by memory: 28 bytes an element with
+// fp32 gradients and states, 16.1 with bf16 gradients, 8-bit states and a bf16 copy.
 #include <cmath>
 
 #include "real16.h"
@@ -12,7 +13,7 @@
 namespace dab {
 
 constexpr int kAdamThreads = 256;
-constexpr int kAdamJobs = 32;                    // tensors of a launch: what its arguments hold
+constexpr int kAdamFill = 32;                    // tensors that a launch writes into the table: what its arguments hold
 
 struct AdamTensor {
     float* P;
@@ -22,23 +23,35 @@ struct AdamTensor {
     void* copy;
     int64_t n;
     uint64_t place;
-    float keep_rate;                             // weight decay
+    float decay;
     int16_t kind;                                // 3 * (8-bit states) + type of the gradient
     int16_t copy_dtype;
-    uint32_t first;                              // first workgroup
+    uint32_t first, blocks;                      // workgroups
 };
-struct AdamLaunch {
+// The table: the tensors, then for every workgroup its tensor's number.
+struct AdamFill {
+    int first, count;
+    AdamTensor t[kAdamFill];
+};
+static_assert(sizeof(AdamFill) <= 4000, "arguments of a launch");
+struct AdamStep {
     double lr, b1, b2;
-    int64_t step;
+    double rise1, rise2;                         // 1 - b1^t, 1 - b2^t, where the step is known
     const float* lr_dev;
     const int64_t* step_dev;
     const float* grad_scale;
     uint64_t seed;
+    int64_t step;
     float c_b1, c_g1, c_b2, c_g2, eps;           // b1, 1 - b1, b2, 1 - b2 as they multiply
-    int count, turns;                            // tensors; eights of a lane
-    AdamTensor t[kAdamJobs];
+    int turns;                                   // eights of a lane
 };
-static_assert(sizeof(AdamLaunch) <= 4096, "arguments of a launch");
+
+__global__ __launch_bounds__(256) void adamw_table_kernel(const AdamFill f, AdamTensor* __restrict__ tensors, uint32_t* __restrict__ of) {
+    const AdamTensor& t = f.t[blockIdx.x];
+    const uint32_t which = f.first + blockIdx.x;
+    if (threadIdx.x == 0) tensors[which] = t;
+    for (uint32_t i = threadIdx.x; i < t.blocks; i += 256) of[t.first + i] = which;
+}
 
 // 32 bits, mixed: two multiplications by odd numbers (digits of pi and of the golden ratio), each after the upper half is brought down.
 __device__ __host__ __forceinline__ uint32_t mix32(uint32_t x) {
@@ -171,25 +184,20 @@ __device__ __forceinline__ void adam_eight(const AdamTensor& t, const AdamRates&
     }
 }
 
-__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamLaunch a) {
+__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamTensor* __restrict__ tensors, const uint32_t* __restrict__ of, const AdamStep a) {
     DAB_RESERVE_VGPRS();
-    // the tensor of this workgroup
-    int lo = 0, hi = a.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.t[mid].first <= blockIdx.x) lo = mid;
-        else hi = mid - 1;
-    }
-    const AdamTensor t = a.t[lo];
+    const AdamTensor t = tensors[__builtin_amdgcn_readfirstlane(of[blockIdx.x])];
     AdamRates r;
     r.c_b1 = a.c_b1, r.c_g1 = a.c_g1, r.c_b2 = a.c_b2, r.c_g2 = a.c_g2, r.eps = a.eps;
     r.scale = a.grad_scale ? *a.grad_scale : 1.f;
     if (!(fabsf(r.scale) < __builtin_inff())) return;                   // a scale that is no number: no step
     const double lr = a.lr_dev ? static_cast<double>(*a.lr_dev) : a.lr;
-    const int64_t step = a.step_dev ? *a.step_dev : a.step;
-    r.keep = static_cast<float>(1.0 - lr * static_cast<double>(t.keep_rate));
-    r.first = static_cast<float>(lr / (1.0 - whole_power(a.b1, step)));
-    r.root = static_cast<float>(1.0 / sqrt(1.0 - whole_power(a.b2, step)));
+    int64_t step = a.step;
+    double rise1 = a.rise1, rise2 = a.rise2;
+    if (a.step_dev) step = *a.step_dev, rise1 = 1.0 - whole_power(a.b1, step), rise2 = 1.0 - whole_power(a.b2, step);
+    r.keep = static_cast<float>(1.0 - lr * static_cast<double>(t.decay));
+    r.first = static_cast<float>(lr / rise1);
+    r.root = static_cast<float>(1.0 / sqrt(rise2));
     r.key = mix32(static_cast<uint32_t>(a.seed) + mix32(static_cast<uint32_t>(a.seed >> 32) + mix32(static_cast<uint32_t>(step))));
     const int64_t end = t.kind < 3 ? t.n : (t.n + 31) & ~int64_t{31};
     int64_t at = static_cast<int64_t>(blockIdx.x - t.first) * a.turns * (kAdamThreads * 8) + threadIdx.x * 8;
@@ -258,41 +266,76 @@ static int check_job(const dab_adamw_job& j) {
     return DAB_OK;
 }
 
+// Eights of a lane: four once the chip is full of workgroups several times over.
+static int adam_turns(const dab_adamw_job* jobs, int32_t n) {
+    int64_t all = 0;
+    for (int32_t i = 0; i < n; ++i) all += ceil_div64(jobs[i].n, kAdamThreads * 8);
+    return all > 8 * 8 * kNumCU ? 4 : 1;
+}
+static int64_t adam_blocks(int64_t n, int turns) { return ceil_div64(n, static_cast<int64_t>(kAdamThreads) * 8 * turns); }
+static int64_t adam_table_bytes(int32_t n_jobs, int64_t workgroups) { return round_up(n_jobs * static_cast<int64_t>(sizeof(AdamTensor)) + 4 * workgroups, 256); }
+constexpr int64_t kAdamMost = int64_t{1} << 23;  // workgroups
+
 }  // namespace dab
 
-extern "C" int dab_adamw(const dab_adamw_job* jobs, int32_t n_jobs, const dab_adamw_step* s, void* stream) {
+extern "C" int dab_adamw_plan_of(const dab_adamw_job* jobs, int32_t n_jobs, dab_adamw_plan* plan) {
     using namespace dab;
-    if (!jobs || !s) return DAB_ERR_NULL;
+    if (!jobs || !plan) return DAB_ERR_NULL;
     if (n_jobs < 1) return DAB_ERR_SHAPE;
+    for (int32_t i = 0; i < n_jobs; ++i)
+        if (int rc = check_job(jobs[i])) return rc;
+    const int turns = adam_turns(jobs, n_jobs);
+    int64_t blocks = 0;
+    for (int32_t i = 0; i < n_jobs; ++i) blocks += adam_blocks(jobs[i].n, turns);
+    if (blocks > kAdamMost) return DAB_ERR_UNSUPPORTED;
+    plan->n_jobs = n_jobs, plan->turns = turns, plan->workgroups = static_cast<int32_t>(blocks);
+    plan->table_bytes = adam_table_bytes(n_jobs, blocks);
+    return DAB_OK;
+}
+
+extern "C" int dab_adamw_table(const dab_adamw_job* jobs, const dab_adamw_plan* plan, void* table, size_t table_bytes, void* stream) {
+    using namespace dab;
+    if (!jobs || !plan || !table) return DAB_ERR_NULL;
+    dab_adamw_plan now;
+    if (int rc = dab_adamw_plan_of(jobs, plan->n_jobs, &now)) return rc;
+    if (now.turns != plan->turns || now.workgroups != plan->workgroups) return DAB_ERR_SHAPE;
+    if (static_cast<int64_t>(table_bytes) < now.table_bytes || misaligned(table, 256)) return DAB_ERR_WORKSPACE;
+    AdamTensor* tensors = static_cast<AdamTensor*>(table);
+    uint32_t* of = reinterpret_cast<uint32_t*>(tensors + now.n_jobs);
+    int64_t blocks = 0;
+    for (int32_t i0 = 0; i0 < now.n_jobs; i0 += kAdamFill) {
+        AdamFill f{};
+        f.first = i0, f.count = now.n_jobs - i0 < kAdamFill ? now.n_jobs - i0 : kAdamFill;
+        for (int k = 0; k < f.count; ++k) {
+            const dab_adamw_job& j = jobs[i0 + k];
+            AdamTensor& t = f.t[k];
+            t.P = j.P, t.G = j.G, t.M = j.M, t.V = j.V, t.MS = j.MS, t.VS = j.VS, t.copy = j.copy, t.n = j.n, t.place = j.place;
+            t.decay = j.weight_decay, t.kind = static_cast<int16_t>((j.bits == 8 ? 3 : 0) + j.grad_dtype), t.copy_dtype = static_cast<int16_t>(j.copy_dtype);
+            t.first = static_cast<uint32_t>(blocks), t.blocks = static_cast<uint32_t>(adam_blocks(j.n, now.turns));
+            blocks += t.blocks;
+        }
+        if (int rc = launch(adamw_table_kernel, dim3(f.count), dim3(256), 0, static_cast<hipStream_t>(stream), f, tensors, of)) return rc;
+    }
+    return DAB_OK;
+}
+
+extern "C" int dab_adamw(const void* table, size_t table_bytes, const dab_adamw_plan* plan, const dab_adamw_step* s, void* stream) {
+    using namespace dab;
+    if (!table || !plan || !s) return DAB_ERR_NULL;
+    if (plan->n_jobs < 1 || plan->workgroups < plan->n_jobs || plan->workgroups > kAdamMost || (plan->turns != 1 && plan->turns != 4)) return DAB_ERR_SHAPE;
+    if (static_cast<int64_t>(table_bytes) < adam_table_bytes(plan->n_jobs, plan->workgroups) || misaligned(table, 256)) return DAB_ERR_WORKSPACE;
     const bool rates = s->beta1 >= 0. && s->beta1 < 1. && s->beta2 >= 0. && s->beta2 < 1. && s->eps >= 0. && std::isfinite(s->eps);
     if (!rates || (!s->lr_dev && !std::isfinite(s->lr)) || (!s->step_dev && s->step < 1)) return DAB_ERR_SHAPE;
     if (misaligned(s->lr_dev, 4) || misaligned(s->step_dev, 8) || misaligned(s->grad_scale, 4)) return DAB_ERR_ALIGN;
-    for (int32_t i = 0; i < n_jobs; ++i)
-        if (int rc = check_job(jobs[i])) return rc;
-    const auto st = static_cast<hipStream_t>(stream);
-    for (int32_t i0 = 0; i0 < n_jobs; i0 += kAdamJobs) {
-        AdamLaunch a{};
-        a.lr = s->lr, a.b1 = s->beta1, a.b2 = s->beta2, a.step = s->step, a.lr_dev = s->lr_dev, a.step_dev = s->step_dev;
-        a.grad_scale = s->grad_scale, a.seed = s->seed;
-        a.c_b1 = static_cast<float>(s->beta1), a.c_g1 = static_cast<float>(1.0 - s->beta1);
-        a.c_b2 = static_cast<float>(s->beta2), a.c_g2 = static_cast<float>(1.0 - s->beta2), a.eps = static_cast<float>(s->eps);
-        a.count = n_jobs - i0 < kAdamJobs ? n_jobs - i0 : kAdamJobs;
-        int64_t all = 0;
-        for (int k = 0; k < a.count; ++k) all += ceil_div64(jobs[i0 + k].n, kAdamThreads * 8);
-        a.turns = all > 8 * 8 * kNumCU ? 4 : 1;
-        int64_t blocks = 0;
-        for (int k = 0; k < a.count; ++k) {
-            const dab_adamw_job& j = jobs[i0 + k];
-            AdamTensor& t = a.t[k];
-            t.P = j.P, t.G = j.G, t.M = j.M, t.V = j.V, t.MS = j.MS, t.VS = j.VS, t.copy = j.copy, t.n = j.n, t.place = j.place;
-            t.keep_rate = j.weight_decay, t.kind = static_cast<int16_t>((j.bits == 8 ? 3 : 0) + j.grad_dtype), t.copy_dtype = static_cast<int16_t>(j.copy_dtype);
-            t.first = static_cast<uint32_t>(blocks);
-            blocks += ceil_div64(j.n, static_cast<int64_t>(kAdamThreads) * 8 * a.turns);
-        }
-        if (blocks * kAdamThreads >> 32) return DAB_ERR_UNSUPPORTED;
-        if (int rc = launch(adamw_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kAdamThreads), 0, st, a)) return rc;
-    }
-    return DAB_OK;
+    AdamStep a{};
+    a.lr = s->lr, a.b1 = s->beta1, a.b2 = s->beta2, a.step = s->step, a.lr_dev = s->lr_dev, a.step_dev = s->step_dev;
+    a.rise1 = 1.0 - whole_power(s->beta1, s->step), a.rise2 = 1.0 - whole_power(s->beta2, s->step);
+    a.grad_scale = s->grad_scale, a.seed = s->seed, a.turns = plan->turns;
+    a.c_b1 = static_cast<float>(s->beta1), a.c_g1 = static_cast<float>(1.0 - s->beta1);
+    a.c_b2 = static_cast<float>(s->beta2), a.c_g2 = static_cast<float>(1.0 - s->beta2), a.eps = static_cast<float>(s->eps);
+    const AdamTensor* tensors = static_cast<const AdamTensor*>(table);
+    return launch(adamw_kernel, dim3(plan->workgroups), dim3(kAdamThreads), 0, static_cast<hipStream_t>(stream), tensors,
+                  reinterpret_cast<const uint32_t*>(tensors + plan->n_jobs), a);
 }
 
 extern "C" int dab_state8_restore(const uint8_t* Q, const uint8_t* S, int64_t n, int32_t is_signed, void* X, int32_t dtype, void* stream) {

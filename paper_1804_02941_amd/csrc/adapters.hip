@@ -9,24 +9,11 @@
 // reach another's tokens.
 #include <algorithm>
 
-#include "lanes.h"
-#include "real16.h"
+#include "adapters.h"
 
 namespace dab {
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-
-struct Adapters {
-    const int32_t* ids;
-    const float* scale;              // or null: 1
-    int T, n, r;
-};
-
-__device__ __forceinline__ int adapter_of(const Adapters& a, int64_t t) {
-    const int id = t < a.T ? a.ids[t] : -1;
-    return static_cast<uint32_t>(id) < static_cast<uint32_t>(a.n) ? id : -1;
-}
-__device__ __forceinline__ float scale_of(const Adapters& a, int id) { return a.scale ? a.scale[id] : 1.f; }
 
 // ---------------------------------------------------------------- shrink
 // Eight k as the matrix cores take them: 16-bit numbers as they are, fp32 ones for eight products of four k.
@@ -36,6 +23,12 @@ template <>
 struct Long<float> {
     float v[8];
     __device__ __forceinline__ void load(const float* row, int k, int K) { load8(row, k, K, v); }
+    __device__ __forceinline__ void load(const float* row, int k) {
+        Eight<float> e;
+        e.load(row, k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e.v[i];
+    }
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
@@ -55,16 +48,19 @@ template <>
 struct Long<bf16> {
     v8bf v;
     __device__ __forceinline__ void load(const bf16* row, int k, int K) { load_raw(row, k, K, &v); }
+    __device__ __forceinline__ void load(const bf16* row, int k) { v = *reinterpret_cast<const Unaligned<bf16, 8>::type*>(row + k); }
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }
 };
 template <>
 struct Long<f16> {
     v8h v;
     __device__ __forceinline__ void load(const f16* row, int k, int K) { load_raw(row, k, K, &v); }
+    __device__ __forceinline__ void load(const f16* row, int k) { v = *reinterpret_cast<const Unaligned<f16, 8>::type*>(row + k); }
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
 };
 
-// Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth step of 32 k.
+// Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth step of 32 k; the loads of several steps are in
+// flight at once.
 constexpr int kShrinkWaves = 8;
 template <typename T, int RT>
 __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a,
@@ -85,14 +81,33 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(const T* __re
         v4f acc[RT];
 #pragma unroll
         for (int j = 0; j < RT; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
-        for (int64_t k0 = wave * 32; k0 < K; k0 += kShrinkWaves * 32) {
+        const T* mine[RT];
+#pragma unroll
+        for (int j = 0; j < RT; ++j) mine[j] = rows + static_cast<int64_t>(min(r0 + j * 16 + m, a.r - 1)) * K;
+        constexpr int kStep = kShrinkWaves * 32, kAhead = sizeof(T) == 4 && RT == 4 ? 2 : 4;
+        int64_t k0 = wave * 32;
+        for (; k0 + (kAhead - 1) * kStep + 32 <= K; k0 += kAhead * kStep) {
+            Long<T> xv[kAhead], av[kAhead][RT];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int k = static_cast<int>(k0) + u * kStep + g * 8;
+                xv[u].load(x, k);
+#pragma unroll
+                for (int j = 0; j < RT; ++j) av[u][j].load(mine[j], k);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int j = 0; j < RT; ++j) acc[j] = Long<T>::mul(av[u][j], xv[u], acc[j]);
+        }
+        for (; k0 < K; k0 += kStep) {
             const int k = static_cast<int>(k0) + g * 8;
             Long<T> xv;
             xv.load(x, k, K);
 #pragma unroll
             for (int j = 0; j < RT; ++j) {
                 Long<T> av;
-                av.load(rows + static_cast<int64_t>(min(r0 + j * 16 + m, a.r - 1)) * K, k, K);
+                av.load(mine[j], k, K);
                 acc[j] = Long<T>::mul(av, xv, acc[j]);
             }
         }
@@ -121,114 +136,145 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(const T* __re
     }
 }
 
-// Few tokens: a wavefront takes one row of a token's adapter.
 template <typename T>
 __global__ __launch_bounds__(256) void shrink_few_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a, int scaled,
                                                          float* __restrict__ U) {
-    const int lane = threadIdx.x & 63;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (at >= static_cast<int64_t>(a.T) * a.r) return;
-    const int64_t t = at / a.r;
-    const int row = static_cast<int>(at - t * a.r), id = adapter_of(a, t);
-    float sum = 0.f;
-    if (id >= 0) {
-        const T *x = X + t * ldx, *w = A + (static_cast<int64_t>(id) * a.r + row) * K;
-        for (int64_t k0 = lane * 8; k0 < K; k0 += 512) {
-            float p[8], q[8];
-            load8(x, static_cast<int>(k0), K, p), load8(w, static_cast<int>(k0), K, q);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += p[i] * q[i];
-        }
-        if (scaled) sum *= scale_of(a, id);
-    }
-    sum = lanes_sum<6>(sum);
-    if (lane == 0) U[at] = sum;
+    if (at < static_cast<int64_t>(a.T) * a.r) shrink_few(X, ldx, A, K, a, scaled != 0, at, U);
 }
 
 // ---------------------------------------------------------------- expand
 struct Base {
     const void* p;                   // or null
     int64_t ld;
-    int dtype;
+    int dtype;                       // fp32, or the tokens'
 };
-__device__ __forceinline__ void load_base(const Base& b, int64_t t, int f, int F, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    if (!b.p) return;
-    if (b.dtype == DAB_F32) load8(static_cast<const float*>(b.p) + t * b.ld, f, F, v);
-    else if (b.dtype == DAB_BF16) load8(static_cast<const bf16*>(b.p) + t * b.ld, f, F, v);
-    else load8(static_cast<const f16*>(b.p) + t * b.ld, f, F, v);
-}
 
-// Many tokens: a wavefront takes sixteen of them and 128 columns, lane l the eight columns 8 (l % 16) .. of tokens 4 (l / 16) .. + 3.  In
-// fp32 on the matrix cores, whatever the type: U is fp32, and the products are few.
-constexpr int kExpandWaves = 4;
-template <typename T>
+// Many tokens: a wavefront takes two tiles of sixteen and 128 columns, lane l the eight columns 8 (l % 16) .. of tokens 4 (l / 16) .. + 3 of each.
+// In fp32 on the matrix cores, whatever the type: U is fp32, and the products are few.  Where the tiles share an adapter, which sequences of
+// tokens do, everything that sixteen of the r rows need is in flight at once, base ahead of it.
+constexpr int kExpandWaves = 4, kExpandTiles = 2;
+template <typename T, typename TB>
 __global__ __launch_bounds__(64 * kExpandWaves) void expand_kernel(const float* __restrict__ U, const T* __restrict__ B, int F, Adapters a, int scaled,
-                                                                   Base base, T* Y) {
+                                                                   const TB* base, int64_t ldbase, T* Y) {
     DAB_RESERVE_VGPRS();
+    constexpr int N = kExpandTiles;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16 * N;
     const int64_t f64 = (static_cast<int64_t>(blockIdx.y) * kExpandWaves + wave) * 128 + m * 8;
     if (f64 - m * 8 >= F) return;
     const int f = static_cast<int>(f64);
-    const int id = adapter_of(a, t0 + m);
-    const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
-    v4f out[8];
+    const bool whole = f64 - m * 8 + 128 <= F && t0 + 16 * N <= a.T;
+    // (lanes from 16 N on repeat the ids)
+    const int all = adapter_of(a, t0 + (lane & (16 * N - 1))), first = __builtin_amdgcn_readfirstlane(all);
+    v4f out[N][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) out[j] = v4f{0.f, 0.f, 0.f, 0.f};
-    bool waiting = id >= 0;
-    while (__any(waiting)) {
-        const int now = __shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1);
-        const T* rows = B + static_cast<int64_t>(now) * a.r * F;
-        v4f acc[8];
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
-        for (int q = 0; q < a.r; q += 4) {
-            const int row = q + g;
-            float b[8] = {};
-            float u = 0.f;
-            if (row < a.r) {
-                load8(rows + static_cast<int64_t>(row) * F, f, F, b);
-                if (id == now) u = U[(t0 + m) * a.r + row] * s;
+        for (int j = 0; j < 8; ++j) out[n][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    if (whole && __all(all == first)) {
+        Eight<TB> y[N][4];
+        if (base)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) y[n][v].load(base + (t0 + 16 * n + 4 * g + v) * ldbase, f);
+        if (first >= 0) {
+            const T* rows = B + static_cast<int64_t>(first) * a.r * F;
+            const float s = scaled ? scale_of(a, first) : 1.f;
+            for (int q0 = 0; q0 < a.r; q0 += 16) {
+                Eight<T> b[4];
+                float u[N][4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int row = q0 + 4 * q + g;
+                    // (a row past the last is read from the last, its numbers replaced: an infinity there times 0 would be undefined)
+                    b[q].load(rows + static_cast<int64_t>(min(row, a.r - 1)) * F, f);
+#pragma unroll
+                    for (int n = 0; n < N; ++n) u[n][q] = row < a.r ? U[(t0 + 16 * n + m) * a.r + row] * s : 0.f;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bool in = q0 + 4 * q + g < a.r;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float w = in ? b[q][j] : 0.f;
+#pragma unroll
+                        for (int n = 0; n < N; ++n) out[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[n][q], w, out[n][j], 0, 0, 0);
+                    }
+                }
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u, b[j], acc[j], 0, 0, 0);
         }
-        // (of the tokens in this lane's results)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = out[n][j][v] + (base ? y[n][v][j] : 0.f);
+                store8(Y + (t0 + 16 * n + 4 * g + v) * F, f, F, w);
+            }
+        return;
+    }
+    // tiles of several adapters, the last columns and the last tokens: one adapter after the other
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int id = __shfl(all, 16 * n + m);
+        const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
+        bool waiting = id >= 0;
+        while (__any(waiting)) {
+            const int now = __shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1);
+            const T* rows = B + static_cast<int64_t>(now) * a.r * F;
+            v4f acc[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int q = 0; q < a.r; q += 4) {
+                const int row = q + g;
+                float b[8] = {};
+                float u = 0.f;
+                if (row < a.r) {
+                    load8(rows + static_cast<int64_t>(row) * F, f, F, b);
+                    if (id == now) u = U[(t0 + 16 * n + m) * a.r + row] * s;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u, b[j], acc[j], 0, 0, 0);
+            }
+            // (of the tokens in this lane's results)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const bool mine = __shfl(id, 4 * g + v) == now;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) out[n][j][v] = mine ? acc[j][v] : out[n][j][v];
+            }
+            waiting = waiting && id != now;
+        }
+        if (f >= F) continue;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const bool mine = __shfl(id, 4 * g + v) == now;
+            const int64_t t = t0 + 16 * n + 4 * g + v;
+            if (t >= a.T) break;
+            float w[8] = {};
+            if (base) load8(base + t * ldbase, f, F, w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) out[j][v] = mine ? acc[j][v] : out[j][v];
+            for (int j = 0; j < 8; ++j) w[j] += out[n][j][v];
+            store8(Y + t * F, f, F, w);
         }
-        waiting = waiting && id != now;
-    }
-    if (f >= F) return;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const int64_t t = t0 + 4 * g + v;
-        if (t >= a.T) break;
-        float y[8];
-        load_base(base, t, f, F, y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] += out[j][v];
-        store8(Y + t * F, f, F, y);
     }
 }
 
 // Few tokens: a lane takes eight columns of one.
-template <typename T>
-__global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict__ U, const T* __restrict__ B, int F, Adapters a, int scaled, Base base,
-                                                        T* Y) {
+template <typename T, typename TB>
+__global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict__ U, const T* __restrict__ B, int F, Adapters a, int scaled,
+                                                        const TB* base, int64_t ldbase, T* Y) {
     const int64_t t = blockIdx.y, f64 = (static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x) * 8;
     if (f64 >= F) return;
     const int f = static_cast<int>(f64), id = adapter_of(a, t);
-    float y[8], v[8] = {};
-    load_base(base, t, f, F, y);
+    float y[8] = {}, v[8] = {};
+    if (base) load8(base + t * ldbase, f, F, y);
     if (id >= 0) {
         const T* rows = B + static_cast<int64_t>(id) * a.r * F;
         const float s = scaled ? scale_of(a, id) : 1.f;
+#pragma unroll 4
         for (int row = 0; row < a.r; ++row) {
             float b[8];
             load8(rows + static_cast<int64_t>(row) * F, f, F, b);
@@ -243,64 +289,109 @@ __global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict_
 }
 
 // ---------------------------------------------------------------- outer
-// A workgroup takes 128 columns, 16 RT of the r rows, a share of the tokens and every slices-th adapter; of each adapter that has tokens in its share
-// its wavefronts take every eighth four of them, and add up in LDS.  parts: [share][adapter][r][columns], have: [share][adapter], 1
-// where the share has tokens of the adapter (other parts are not written).
-constexpr int kOuterWaves = 8, kOuterMaxAdapters = 65536;
-struct Outer {
-    int cols, tokens, slices;        // columns, tokens of a share (a multiple of 32), slices of the adapters
+// Both gradients of the adapters in one launch: a workgroup takes 128 columns of one, 16 RT of the r rows, a share of the tokens and every slices-th
+// adapter; of each adapter that has tokens in its share its wavefronts take every eighth four of them (four such fours in flight) and add up
+// in LDS.  With one share that is the gradient; else it goes to parts: [share][adapter][r][columns], and have: [share][adapter] is 1 where
+// the share has tokens of the adapter (other parts are not written).
+constexpr int kOuterWaves = 8, kOuterIds = 2048;
+template <typename T>
+struct OuterSide {
+    const float* V;                  // [tokens][r]
+    const T* X;
     int64_t ldx;
+    int cols, scaled;
+    float* out;                      // the gradient, or parts
+};
+template <typename T>
+struct Outer {
+    OuterSide<T> side[2];
+    int tiles0, tiles;               // column tiles of the first side, of both
+    int tokens, shares, slices;      // tokens of a share (a multiple of 32); slices of the adapters
     int32_t* have;
 };
 template <typename T, int RT>
-__global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const float* __restrict__ V, const T* __restrict__ X, Adapters a, int scaled, Outer o,
-                                                                 float* __restrict__ parts) {
+__global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters a, const Outer<T> o) {
     extern __shared__ uint32_t present[];                    // a bit for every adapter
     __shared__ float sums[kOuterWaves / 2][16][132];
+    __shared__ int ids[kOuterIds];
     DAB_RESERVE_VGPRS();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-    const int tiles = (o.cols + 127) >> 7, tile = blockIdx.x % tiles, rb = blockIdx.x / tiles;
-    const int share = blockIdx.y, slice = blockIdx.z, r0 = rb * 16 * RT;
-    const int64_t first = static_cast<int64_t>(share) * o.tokens, last = min(first + o.tokens, static_cast<int64_t>(a.T));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+    const int rb = blockIdx.x / o.tiles, tile2 = blockIdx.x - rb * o.tiles;
+    const bool second = tile2 >= o.tiles0;
+    const OuterSide<T> side = o.side[second];
+    const int tile = second ? tile2 - o.tiles0 : tile2, share = blockIdx.y, slice = blockIdx.z, r0 = rb * 16 * RT, cols = side.cols;
+    const int64_t first = static_cast<int64_t>(share) * o.tokens;
+    const int count = static_cast<int>(min(static_cast<int64_t>(o.tokens), a.T - first));
     const int words = (a.n + 31) >> 5;
+    const bool kept = count <= kOuterIds;                    // the share's ids in LDS
     for (int i = threadIdx.x; i < words; i += 64 * kOuterWaves) present[i] = 0;
     __syncthreads();
-    for (int64_t t = first + threadIdx.x; t < last; t += 64 * kOuterWaves) {
-        const int id = adapter_of(a, t);
+    for (int t = threadIdx.x; t < count; t += 64 * kOuterWaves) {
+        const int id = adapter_of(a, first + t);
+        if (kept) ids[t] = id;
         if (id >= 0) atomicOr(&present[id >> 5], 1u << (id & 31));
     }
     __syncthreads();
-    if (tile == 0 && rb == 0)
+    if (o.shares > 1 && tile2 == 0 && rb == 0)
         for (int i = slice + threadIdx.x * o.slices; i < a.n; i += 64 * kOuterWaves * o.slices)
             o.have[static_cast<int64_t>(share) * a.n + i] = (present[i >> 5] >> (i & 31)) & 1u;
     const int c = tile * 128 + m * 8;
+    const bool whole = tile * 128 + 128 <= cols;
+    const T* x0 = side.X + first * side.ldx;
+    const float* v0 = side.V + first * a.r;
     for (int id = slice; id < a.n; id += o.slices) {
-        if (!((present[id >> 5] >> (id & 31)) & 1u)) continue;              // (the same for the whole workgroup)
-        const float s = scaled ? scale_of(a, id) : 1.f;
+        const bool none = !((present[id >> 5] >> (id & 31)) & 1u);          // (the same for the whole workgroup)
+        if (none && o.shares > 1) continue;
+        const float s = side.scaled && !none ? scale_of(a, id) : 1.f;       // (zeros stay zeros)
         v4f acc[RT][8];
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
-        for (int64_t t1 = first + wave * 4; t1 < last; t1 += kOuterWaves * 4) {
-            const int64_t t = t1 + g;
-            const bool mine = t < last && a.ids[t] == id;
-            if (!__any(mine)) continue;
-            float x[8] = {}, v[RT];
+        constexpr int kAhead = RT == 4 ? 2 : 4;
+        for (int t1 = none ? count : wave * 4; t1 < count; t1 += kOuterWaves * 4 * kAhead) {
+            bool mine[kAhead], some[kAhead], any = false;
 #pragma unroll
-            for (int j = 0; j < RT; ++j) v[j] = 0.f;
-            if (mine) {
-                if (c < o.cols) load8(X + t * o.ldx, c, o.cols, x);
+            for (int u = 0; u < kAhead; ++u) {
+                const int t = t1 + u * kOuterWaves * 4 + g;
+                mine[u] = t < count && (kept ? ids[t] : a.ids[first + t]) == id;
+                some[u] = __any(mine[u]);
+                any = any || some[u];
+            }
+            if (!any) continue;
+            Eight<T> x[kAhead];
+            float v[kAhead][RT];
 #pragma unroll
-                for (int j = 0; j < RT; ++j)
-                    if (r0 + j * 16 + m < a.r) v[j] = V[t * a.r + r0 + j * 16 + m] * s;
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t t = t1 + u * kOuterWaves * 4 + g;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u].v[i] = static_cast<T>(0.f);
+#pragma unroll
+                for (int j = 0; j < RT; ++j) v[u][j] = 0.f;
+                if (mine[u]) {
+                    const T* from = x0 + t * side.ldx;
+                    if (whole) {
+                        x[u].load(from, c);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (c + i < cols) x[u].v[i] = from[c + i];
+                    }
+#pragma unroll
+                    for (int j = 0; j < RT; ++j)
+                        if (r0 + j * 16 + m < a.r) v[u][j] = v0[t * a.r + r0 + j * 16 + m];
+                }
             }
 #pragma unroll
-            for (int j = 0; j < RT; ++j)
+            for (int u = 0; u < kAhead; ++u)
+                if (some[u])
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], x[i], acc[j][i], 0, 0, 0);
+                    for (int j = 0; j < RT; ++j)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][j], x[u][i], acc[j][i], 0, 0, 0);
         }
         // rows 4 g + v of 16, columns 8 m + i of 128: added up in a fixed order, the upper wavefronts' onto the lower ones'
+        float* out = side.out + (static_cast<int64_t>(o.shares > 1 ? share : 0) * a.n + id) * a.r * cols;
 #pragma unroll
         for (int j = 0; j < RT; ++j) {
 #pragma unroll
@@ -318,32 +409,41 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const float* __
                         for (int v = 0; v < 4; ++v) acc[j][i][v] += sums[wave][4 * g + v][m * 8 + i];
                 __syncthreads();
             }
-            if (wave == 0 && c < o.cols)
+            if (wave == 0 && c < cols)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     const int row = r0 + j * 16 + 4 * g + v;
                     if (row >= a.r) break;
                     float w[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = acc[j][i][v];
-                    store8(parts + ((static_cast<int64_t>(share) * a.n + id) * a.r + row) * o.cols, c, o.cols, w);
+                    for (int i = 0; i < 8; ++i) w[i] = acc[j][i][v] * s;
+                    store8(out + static_cast<int64_t>(row) * cols, c, cols, w);
                 }
         }
     }
 }
 
-// The shares' parts added in a fixed order; zeros for an adapter without tokens.
-__global__ __launch_bounds__(256) void outer_join_kernel(const float* __restrict__ parts, const int32_t* __restrict__ have, int shares, int n,
-                                                         int64_t size, float* __restrict__ out) {
-    const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+// The shares' parts of both gradients added in a fixed order; zeros for an adapter without tokens.
+struct Join {
+    const float* parts[2];
+    float* out[2];
+    int64_t size[2];                 // of an adapter
+    unsigned blocks0;                // workgroups of the first
+    const int32_t* have;
+    int shares, n;
+};
+__global__ __launch_bounds__(256) void outer_join_kernel(const Join j) {
+    const bool second = blockIdx.x >= j.blocks0;
+    const int64_t at = (static_cast<int64_t>(second ? blockIdx.x - j.blocks0 : blockIdx.x) * 256 + threadIdx.x) * 4, size = j.size[second];
     const int id = blockIdx.y;
     if (at >= size) return;
     const int left = static_cast<int>(min(size - at, int64_t{4}));
     float v[4] = {};
-    for (int s = 0; s < shares; ++s) {
-        const int64_t who = static_cast<int64_t>(s) * n + id;
-        if (!have[who]) continue;
-        const float* from = parts + who * size + at;
+#pragma unroll 4
+    for (int s = 0; s < j.shares; ++s) {
+        const int64_t who = static_cast<int64_t>(s) * j.n + id;
+        if (!j.have[who]) continue;
+        const float* from = j.parts[second] + who * size + at;
         if (left == 4) {
             const auto got = *reinterpret_cast<const Unaligned<float, 4>::type*>(from);
 #pragma unroll
@@ -352,16 +452,15 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const float* __restrict
             for (int i = 0; i < left; ++i) v[i] += from[i];
         }
     }
-    float* to = out + static_cast<int64_t>(id) * size + at;
+    float* to = j.out[second] + static_cast<int64_t>(id) * size + at;
     for (int i = 0; i < left; ++i) to[i] = v[i];
 }
 
 // ---------------------------------------------------------------- host side
-constexpr int kFewTokens = 64;       // up to these, a wavefront or a lane per token and row
 constexpr int kMaxRank = 256;
 
 template <typename T>
-static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
+int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
     if (a.T <= kFewTokens)
         return launch(shrink_few_kernel<T>, dim3(static_cast<unsigned>(ceil_div64(static_cast<int64_t>(a.T) * a.r, 4))), dim3(256), 0, st, X, ldx, A, K, a,
                       static_cast<int>(scaled), U);
@@ -373,55 +472,72 @@ static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a,
     return launch(shrink_kernel<T, 4>, dim3(tiles, ceil_div(a.r, 64)), block, 0, st, X, ldx, A, K, a, s, U);
 }
 
+template int shrink(const float*, int64_t, const float*, int, const Adapters&, bool, float*, hipStream_t);
+template int shrink(const bf16*, int64_t, const bf16*, int, const Adapters&, bool, float*, hipStream_t);
+template int shrink(const f16*, int64_t, const f16*, int, const Adapters&, bool, float*, hipStream_t);
+
+template <typename T, typename TB>
+static int expand_from(const float* U, const T* B, int F, const Adapters& a, bool scaled, const Base& base, T* Y, hipStream_t st) {
+    const TB* p = static_cast<const TB*>(base.p);
+    const int s = scaled;
+    if (a.T <= kFewTokens)
+        return launch(expand_few_kernel<T, TB>, dim3(static_cast<unsigned>(ceil_div64(F, 512)), a.T), dim3(64), 0, st, U, B, F, a, s, p, base.ld, Y);
+    return launch(expand_kernel<T, TB>, dim3(static_cast<unsigned>(ceil_div64(a.T, 16 * kExpandTiles)), static_cast<unsigned>(ceil_div64(F, 128 * kExpandWaves))),
+                  dim3(64 * kExpandWaves), 0, st, U, B, F, a, s, p, base.ld, Y);
+}
 template <typename T>
 static int expand(const float* U, const T* B, int F, const Adapters& a, bool scaled, const Base& base, T* Y, hipStream_t st) {
-    if (a.T <= kFewTokens)
-        return launch(expand_few_kernel<T>, dim3(static_cast<unsigned>(ceil_div64(F, 512)), a.T), dim3(64), 0, st, U, B, F, a, static_cast<int>(scaled),
-                      base, Y);
-    return launch(expand_kernel<T>, dim3(static_cast<unsigned>(ceil_div64(a.T, 16)), static_cast<unsigned>(ceil_div64(F, 128 * kExpandWaves))),
-                  dim3(64 * kExpandWaves), 0, st, U, B, F, a, static_cast<int>(scaled), base, Y);
+    return base.p && base.dtype == DAB_F32 ? expand_from<T, float>(U, B, F, a, scaled, base, Y, st) : expand_from<T, T>(U, B, F, a, scaled, base, Y, st);
 }
 
 struct OuterPlan {
-    int shares, tokens, slices, rt;
-    size_t parts, have;              // bytes, multiples of 256
+    int shares, tokens, slices, rt, tiles0, tiles, row_blocks;
+    size_t parts0, parts1, have;     // bytes, multiples of 256
+    size_t bytes() const { return parts0 + parts1 + have; }
 };
-static OuterPlan outer_plan(int T, int n, int r, int cols) {
+static OuterPlan outer_plan(int T, int n, int r, int cols0, int cols1) {
     OuterPlan p{};
     p.rt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
-    const int64_t tiles = static_cast<int64_t>(ceil_div(cols, 128)) * ceil_div(r, 16 * p.rt), part = static_cast<int64_t>(n) * r * cols * 4;
+    p.row_blocks = ceil_div(r, 16 * p.rt), p.tiles0 = ceil_div(cols0, 128), p.tiles = p.tiles0 + ceil_div(cols1, 128);
+    const int64_t blocks = static_cast<int64_t>(p.tiles) * p.row_blocks, row = static_cast<int64_t>(n) * r * 4;
     // about two workgroups for every compute unit, shares of at least 128 tokens, parts of at most 256 MB
-    int64_t shares = ceil_div64(2 * kNumCU, tiles);
+    int64_t shares = ceil_div64(2 * kNumCU, blocks);
     shares = std::min<int64_t>(shares, ceil_div64(T, 128));
-    shares = std::max<int64_t>(1, std::min<int64_t>(shares, (int64_t{256} << 20) / part));
+    shares = std::max<int64_t>(1, std::min<int64_t>(shares, (int64_t{256} << 20) / (row * (static_cast<int64_t>(cols0) + cols1))));
     p.tokens = static_cast<int>(round_up(ceil_div64(T, shares), 32));
     p.shares = static_cast<int>(ceil_div64(T, p.tokens));
-    p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min(n, 1024), 2 * kNumCU / (tiles * p.shares))));
-    p.parts = round_up(part * p.shares, 256), p.have = round_up(static_cast<int64_t>(p.shares) * n * 4, 256);
+    p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min(n, 1024), 2 * kNumCU / (blocks * p.shares))));
+    if (p.shares > 1)
+        p.parts0 = round_up(row * cols0 * p.shares, 256), p.parts1 = round_up(row * cols1 * p.shares, 256), p.have = round_up(static_cast<int64_t>(p.shares) * n * 4, 256);
     return p;
 }
+// One side of the gradients: out[i] = sum over adapter i's tokens of V^T X, times scale[i] where `scaled`.
 template <typename T>
-static int outer(const float* V, const T* X, int64_t ldx, int cols, const Adapters& a, bool scaled, float* out, char* ws, hipStream_t st) {
-    const OuterPlan p = outer_plan(a.T, a.n, a.r, cols);
-    Outer o{};
-    o.cols = cols, o.tokens = p.tokens, o.slices = p.slices, o.ldx = ldx, o.have = reinterpret_cast<int32_t*>(ws + p.parts);
-    float* parts = reinterpret_cast<float*>(ws);
-    const int64_t x = static_cast<int64_t>(ceil_div(cols, 128)) * ceil_div(a.r, 16 * p.rt);
-    const dim3 grid(static_cast<unsigned>(x), p.shares, p.slices), block(64 * kOuterWaves);
+static int outer(OuterSide<T> first, OuterSide<T> second, const Adapters& a, char* ws, hipStream_t st) {
+    const OuterPlan p = outer_plan(a.T, a.n, a.r, first.cols, second.cols);
+    Outer<T> o{};
+    Join j{};
+    j.out[0] = first.out, j.out[1] = second.out;
+    if (p.shares > 1) {
+        first.out = reinterpret_cast<float*>(ws), second.out = reinterpret_cast<float*>(ws + p.parts0);
+        o.have = reinterpret_cast<int32_t*>(ws + p.parts0 + p.parts1);
+    }
+    o.side[0] = first, o.side[1] = second, o.tiles0 = p.tiles0, o.tiles = p.tiles, o.tokens = p.tokens, o.shares = p.shares, o.slices = p.slices;
+    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.tiles) * p.row_blocks), p.shares, p.slices), block(64 * kOuterWaves);
     const size_t lds = static_cast<size_t>(ceil_div(a.n, 32)) * 4;
-    const int s = scaled;
     int rc;
-    if (p.rt == 1) rc = launch(outer_kernel<T, 1>, grid, block, lds, st, V, X, a, s, o, parts);
-    else if (p.rt == 2) rc = launch(outer_kernel<T, 2>, grid, block, lds, st, V, X, a, s, o, parts);
-    else rc = launch(outer_kernel<T, 4>, grid, block, lds, st, V, X, a, s, o, parts);
-    if (rc) return rc;
-    const int64_t size = static_cast<int64_t>(a.r) * cols;
-    return launch(outer_join_kernel, dim3(static_cast<unsigned>(ceil_div64(size, 1024)), a.n), dim3(256), 0, st, static_cast<const float*>(parts),
-                  static_cast<const int32_t*>(o.have), p.shares, a.n, size, out);
+    if (p.rt == 1) rc = launch(outer_kernel<T, 1>, grid, block, lds, st, a, o);
+    else if (p.rt == 2) rc = launch(outer_kernel<T, 2>, grid, block, lds, st, a, o);
+    else rc = launch(outer_kernel<T, 4>, grid, block, lds, st, a, o);
+    if (rc || p.shares == 1) return rc;
+    j.parts[0] = first.out, j.parts[1] = second.out, j.have = o.have, j.shares = p.shares, j.n = a.n;
+    j.size[0] = static_cast<int64_t>(a.r) * first.cols, j.size[1] = static_cast<int64_t>(a.r) * second.cols;
+    j.blocks0 = static_cast<unsigned>(ceil_div64(j.size[0], 1024));
+    return launch(outer_join_kernel, dim3(j.blocks0 + static_cast<unsigned>(ceil_div64(j.size[1], 1024)), a.n), dim3(256), 0, st, j);
 }
 
-static int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T,
-                          int32_t K, int32_t F, int32_t n, int32_t r) {
+int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
+                   int32_t F, int32_t n, int32_t r) {
     if (!X || !ids || !A || !B) return DAB_ERR_NULL;
     if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || ldx < K) return DAB_ERR_SHAPE;
     if (!real_dtype(dtype) || K > (1 << 24) || F > (1 << 24) || n > 65535 || r > kMaxRank || T > (1 << 25)) return DAB_ERR_UNSUPPORTED;
@@ -460,8 +576,7 @@ extern "C" int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int
 extern "C" size_t dab_adapters_gradient_workspace_bytes(int32_t T, int32_t K, int32_t F, int32_t n, int32_t r) {
     using namespace dab;
     if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || K > (1 << 24) || F > (1 << 24) || n > 65535 || r > kMaxRank || T > (1 << 25)) return 0;
-    const OuterPlan p = outer_plan(T, n, r, K), q = outer_plan(T, n, r, F);
-    return static_cast<size_t>(round_up(static_cast<int64_t>(T) * r * 4, 256)) + std::max(p.parts + p.have, q.parts + q.have);
+    return static_cast<size_t>(round_up(static_cast<int64_t>(T) * r * 4, 256)) + outer_plan(T, n, r, F, K).bytes();
 }
 
 extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X, int32_t dtype, int64_t ldx, const float* U, const int32_t* ids,
@@ -484,46 +599,11 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
         typedef std::remove_pointer_t<decltype(t)> E;
         const E *x = static_cast<const E*>(X), *dy = static_cast<const E*>(dY), *up = static_cast<const E*>(B), *down = static_cast<const E*>(A);
         if (int rc = shrink(dy, lddy, up, F, a, true, V, st)) return rc;
-        if (int rc = outer(U, dy, lddy, F, a, true, dB, rest, st)) return rc;
-        if (int rc = outer(static_cast<const float*>(V), x, ldx, K, a, false, dA, rest, st)) return rc;
+        if (int rc = outer(OuterSide<E>{U, dy, lddy, F, 1, dB}, OuterSide<E>{V, x, ldx, K, 0, dA}, a, rest, st)) return rc;
         if (!dX) return DAB_OK;
         return expand(static_cast<const float*>(V), down, K, a, false, Base{base, ldbase, base_dtype}, static_cast<E*>(dX), st);
     };
     if (dtype == DAB_F32) return go(static_cast<float*>(nullptr));
     if (dtype == DAB_BF16) return go(static_cast<bf16*>(nullptr));
     return go(static_cast<f16*>(nullptr));
-}
-
-namespace dab {
-// Workspace of the served call: the projection's own, its sums in fp32, and U.
-struct ServeSpace {
-    size_t product, base, u;
-};
-static ServeSpace serve_space(int32_t B, int32_t K, int32_t F, int32_t r, int32_t dtype, int64_t ldx) {
-    return {static_cast<size_t>(round_up(static_cast<int64_t>(dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx)), 256)),
-            static_cast<size_t>(round_up(static_cast<int64_t>(B) * F * 4, 256)), static_cast<size_t>(round_up(static_cast<int64_t>(B) * r * 4, 256))};
-}
-}  // namespace dab
-
-extern "C" size_t dab_w4_adapters_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t r, int32_t dtype, int64_t ldx) {
-    using namespace dab;
-    if (B < 1 || K < 1 || F < 1 || r < 1 || !real_dtype(dtype)) return 0;
-    const ServeSpace s = serve_space(B, K, F, r, dtype, ldx);
-    return s.product + s.base + s.u;
-}
-
-extern "C" int dab_w4_adapters(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, const int32_t* ids, const void* A,
-                               const void* Bt, const float* scale, int32_t B, int32_t K, int32_t F, int32_t n, int32_t r, void* Y, void* ws,
-                               size_t ws_bytes, void* stream) {
-    using namespace dab;
-    if (int rc = check_adapters(X, dtype, ldx, ids, A, Bt, scale, B, K, F, n, r)) return rc;
-    if (!Q || !S || !Y) return DAB_ERR_NULL;
-    if (B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
-    if (misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
-    const ServeSpace s = serve_space(B, K, F, r, dtype, ldx);
-    if (!ws || ws_bytes < s.product + s.base + s.u || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
-    char* at = static_cast<char*>(ws);
-    float *base = reinterpret_cast<float*>(at + s.product), *U = reinterpret_cast<float*>(at + s.product + s.base);
-    if (int rc = w4_product(X, dtype, ldx, Q, S, B, K, F, base, DAB_F32, ws, s.product, stream)) return rc;
-    return dab_adapters(X, dtype, ldx, ids, A, Bt, scale, B, K, F, n, r, base, DAB_F32, F, Y, U, stream);
 }

@@ -145,8 +145,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const T* R,
 }
 
 // ---------------------------------------------------------------- gradients
-// A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it holds at once) and keeps its part of dgain in registers meanwhile;
-// norm_join_kernel adds the parts in a fixed order.
+// A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it holds at once) and keeps its part of dgain in registers meanwhile, that of
+// its rows' lanes together in LDS at the end; norm_join_kernel adds the workgroups' parts in a fixed order.
 template <typename T, int LOG, int NV>
 __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_kernel(const T* dY, const T* H, const float* __restrict__ gain,
                                                                                      const float* __restrict__ rstd, const T* dH, NormGeom g, T* dX,
@@ -200,12 +200,27 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_k
             store8(dX + row * g.cols, c, g.cols, d);
         }
     }
-    // [workgroup and slot][column]
-    float* to = parts + (static_cast<int64_t>(blockIdx.x) * kRows + slot) * g.cols;
+    float* to = parts + static_cast<int64_t>(blockIdx.x) * g.cols;
+    if constexpr (kRows == 1) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * kLanes + lane) * 8;
-        if (c < g.cols) store8(to, c, g.cols, dg[j]);
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * kLanes + lane) * 8;
+            if (c < g.cols) store8(to, c, g.cols, dg[j]);
+        }
+    } else {
+        constexpr int kCols = kLanes * NV * 8;
+        __shared__ float all[kRows][kCols];
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) all[slot][(j * kLanes + lane) * 8 + i] = dg[j][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < g.cols; c += kNormThreads) {
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) v += all[i][c];
+            to[c] = v;
+        }
     }
 }
 
@@ -245,20 +260,42 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* dY, const
     }
 }
 
-// dgain[c] = sum over the parts: 64 columns a workgroup, 16 wavefronts that share the parts.
+// dgain[c] = sum over the parts: 32 columns a workgroup, 128 threads that share the parts of four columns.
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float* __restrict__ parts, int n, int cols, float* __restrict__ dgain) {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-    float v = 0.f;
-    if (c < cols)
-        for (int i = wave; i < n; i += 16) v += parts[static_cast<int64_t>(i) * cols + c];
-    sums[wave][lane] = v;
-    __syncthreads();
-    if (wave != 0 || c >= cols) return;
-    v = 0.f;
+    __shared__ float sums[128][33];
+    DAB_RESERVE_VGPRS();
+    const int slice = threadIdx.x >> 3, c = blockIdx.x * 32 + (threadIdx.x & 7) * 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c + 4 <= cols) {
+#pragma unroll 8
+        for (int i = slice; i < n; i += 128) {
+            const auto got = *reinterpret_cast<const Unaligned<float, 4>::type*>(parts + static_cast<int64_t>(i) * cols + c);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v += sums[i][lane];
-    dgain[c] = v;
+            for (int k = 0; k < 4; ++k) v[k] += got[k];
+        }
+    } else {
+        for (int i = slice; i < n; i += 128)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < cols) v[k] += parts[static_cast<int64_t>(i) * cols + c + k];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[slice][(threadIdx.x & 7) * 4 + k] = v[k];
+    __syncthreads();
+    // eight slices by each wavefront half, then the sixteen that are left
+    const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
+    float w = 0.f;
+    if (part < 16)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w += sums[part * 8 + i][col];
+    __syncthreads();
+    if (part < 16) sums[part][col] = w;
+    __syncthreads();
+    if (part != 0 || blockIdx.x * 32 + col >= cols) return;
+    w = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w += sums[i][col];
+    dgain[blockIdx.x * 32 + col] = w;
 }
 
 // ---------------------------------------------------------------- host side
@@ -278,6 +315,7 @@ static NormForm norm_form(int cols, int max_nv) {
 static int norm_rows(NormForm f) { return f.log == 0 || f.log > 8 ? 1 : kNormThreads >> f.log; }
 static int norm_threads(NormForm f) { return f.log == 0 ? 1024 : f.log > 8 ? 1 << f.log : kNormThreads; }
 constexpr int kNormNV = 4, kNormGradNV = 2;
+constexpr int64_t kNormFew = 256 * 4096;
 
 template <typename T>
 struct NormArgs {
@@ -296,7 +334,9 @@ static int norm_launch(const NormArgs<T>& a, NormForm f, hipStream_t st) {
 }
 template <typename T>
 static int norm_launch(const NormArgs<T>& a, hipStream_t st) {
-    const NormForm f = norm_form(a.g.cols, kNormNV);
+    // (rows that do not fill the chip: as many lanes as a row has eights)
+    const bool few = static_cast<int64_t>(a.g.rows) * a.g.cols <= kNormFew;
+    const NormForm f = few ? norm_form(a.g.cols, a.g.cols <= 8192 ? 1 : kNormNV) : norm_form(a.g.cols, kNormNV);
     switch (f.log) {
         case 0: return launch(norm_long_kernel<T>, dim3(a.g.rows), dim3(1024), 0, st, a.X, a.R, a.gain, a.g, a.H, a.Y, a.Q, a.S, a.rstd);
         case 2: return norm_launch<T, 2, 1>(a, f, st);
@@ -304,10 +344,10 @@ static int norm_launch(const NormArgs<T>& a, hipStream_t st) {
         case 4: return norm_launch<T, 4, 1>(a, f, st);
         case 5: return norm_launch<T, 5, 1>(a, f, st);
         case 6: return f.nv == 1 ? norm_launch<T, 6, 1>(a, f, st) : f.nv == 2 ? norm_launch<T, 6, 2>(a, f, st) : norm_launch<T, 6, 4>(a, f, st);
-        case 7: return norm_launch<T, 7, 4>(a, f, st);
-        case 8: return norm_launch<T, 8, 4>(a, f, st);
-        case 9: return norm_launch<T, 9, 4>(a, f, st);
-        default: return norm_launch<T, 10, 4>(a, f, st);
+        case 7: return f.nv == 1 ? norm_launch<T, 7, 1>(a, f, st) : norm_launch<T, 7, 4>(a, f, st);
+        case 8: return f.nv == 1 ? norm_launch<T, 8, 1>(a, f, st) : norm_launch<T, 8, 4>(a, f, st);
+        case 9: return f.nv == 1 ? norm_launch<T, 9, 1>(a, f, st) : norm_launch<T, 9, 4>(a, f, st);
+        default: return f.nv == 1 ? norm_launch<T, 10, 1>(a, f, st) : norm_launch<T, 10, 4>(a, f, st);
     }
 }
 
@@ -327,7 +367,7 @@ static int norm_grad_launch(const NormGradArgs<T>& a, NormForm f, hipStream_t st
 }
 // Workgroups of the gradient's kernel: what the chip holds at once, fewer where there are fewer rows.
 static int norm_grad_blocks(int rows, NormForm f) {
-    const int64_t n = ceil_div64(rows, norm_rows(f)), most = 2048 / norm_threads(f) * int64_t{kNumCU};
+    const int64_t n = ceil_div64(rows, norm_rows(f)), most = 1024 / norm_threads(f) * int64_t{kNumCU};
     return static_cast<int>(n < most ? n : most);
 }
 template <typename T>
@@ -347,8 +387,7 @@ static int norm_grad_launch(const NormGradArgs<T>& a, hipStream_t st) {
         default: rc = norm_grad_launch<T, 10, 2>(a, f, st);
     }
     if (rc) return rc;
-    return launch(norm_join_kernel, dim3(ceil_div(a.g.cols, 64)), dim3(1024), 0, st, static_cast<const float*>(a.parts), a.blocks * norm_rows(f),
-                  a.g.cols, a.dgain);
+    return launch(norm_join_kernel, dim3(ceil_div(a.g.cols, 32)), dim3(1024), 0, st, static_cast<const float*>(a.parts), a.blocks, a.g.cols, a.dgain);
 }
 
 constexpr int kNormMaxCols = 1 << 26;
@@ -381,7 +420,7 @@ extern "C" size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t co
     using namespace dab;
     if (rows < 1 || cols < 1 || cols > kNormMaxCols) return 0;
     const NormForm f = norm_form(cols, kNormGradNV);
-    return static_cast<size_t>(norm_grad_blocks(rows, f)) * norm_rows(f) * cols * 4;
+    return static_cast<size_t>(norm_grad_blocks(rows, f)) * cols * 4;
 }
 
 extern "C" int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t ldh, int32_t dtype, const float* gain, const float* rstd,

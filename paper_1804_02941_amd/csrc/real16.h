@@ -21,10 +21,6 @@ inline int dtype_pieces(int32_t t) { return t == DAB_F32 ? 3 : t == DAB_F16 ? 2 
 inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// dab_w4_matvec() with outputs of another type than the tokens' (w4.hip).
-int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y, int32_t y_dtype,
-               void* ws, size_t ws_bytes, void* stream);
-
 // 2^e as fp32 for -126 <= e <= 127.
 __device__ __forceinline__ float pow2f(int e) { return __builtin_bit_cast(float, static_cast<uint32_t>(e + 127) << 23); }
 

@@ -8,7 +8,7 @@
 // the columns of a token are added up at the end.  The layout (include/dab.h) gives every lane the 32 weights of one group,
 // so that a load is 16 bytes a lane and a kilobyte a wavefront, and a lane has one scale for them; the order of the weights within
 // the sum is then that of the lanes, which the tokens' loads follow.
-#include "real16.h"
+#include "adapters.h"
 
 namespace dab {
 
@@ -150,20 +150,40 @@ __global__ __launch_bounds__(64 * kW4PackWaves) void w4_unpack_kernel(const uint
 // [pass][block of 128 k][i][column tile][lane] pieces of 16 bytes: column c = 16 tile + lane % 16 is piece c / nb of token c % nb of the pass, and
 // the piece holds its k = 128 block + 32 (lane / 16) + 8 i .. + 7; zeros past the last column and the last k.  A wavefront's load of them is a
 // kilobyte in a row; from the tokens' own rows it would touch 16 rows in four places each.  Little more than a launch: 7 x 9111 fp32 2.7 us.
+struct W4Tokens {
+    int B, K;
+    int64_t ldx;
+    int Kt, nb, P, tiles;            // blocks of 128 k; tokens of a pass, pieces, column tiles
+};
 template <typename T>
-__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int Kt, int nb, int P,
-                                                        int tiles, bf16* __restrict__ out) {
-    const int at = blockIdx.x * 256 + threadIdx.x, lane = at & 63, frag = at >> 6;
-    const int i4 = frag / tiles, t = frag - i4 * tiles, kt = i4 >> 2, i = i4 & 3;
-    if (kt >= Kt) return;
-    const int b0 = blockIdx.y * nb, n = min(nb, B - b0), c = t * 16 + (lane & 15), p = c / n, b = c - p * n;
+__device__ __forceinline__ void w4_tokens(const T* __restrict__ X, const W4Tokens& g, int block, int pass, bf16* __restrict__ out) {
+    const int at = block * 256 + threadIdx.x, lane = at & 63, frag = at >> 6;
+    const int i4 = frag / g.tiles, t = frag - i4 * g.tiles, kt = i4 >> 2, i = i4 & 3;
+    if (kt >= g.Kt) return;
+    const int b0 = pass * g.nb, n = min(g.nb, g.B - b0), c = t * 16 + (lane & 15), p = c / n, b = c - p * n;
     float v[8] = {};
     const int k = kt * 128 + (lane >> 4) * 32 + 8 * i;
-    if (p < P && k < K) load8(X + (b0 + b) * ldx, k, K, v);
+    if (p < g.P && k < g.K) load8(X + (b0 + b) * g.ldx, k, g.K, v);
     v8bf o;
 #pragma unroll
     for (int u = 0; u < 8; ++u) o[u] = piece_of(v[u], p);
-    *reinterpret_cast<v8bf*>(out + ((static_cast<int64_t>(blockIdx.y) * Kt * 4 * tiles + frag) * 64 + lane) * 8) = o;
+    *reinterpret_cast<v8bf*>(out + ((static_cast<int64_t>(pass) * g.Kt * 4 * g.tiles + frag) * 64 + lane) * 8) = o;
+}
+template <typename T>
+__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, W4Tokens g, bf16* __restrict__ out) {
+    w4_tokens(X, g, blockIdx.x, blockIdx.y, out);
+}
+// The same beside U of the few tokens' adapters (shrink_few), in workgroups behind the layout's.
+template <typename T>
+__global__ __launch_bounds__(256) void w4_tokens_shrink_kernel(const T* __restrict__ X, W4Tokens g, int blocks, bf16* __restrict__ out, const T* __restrict__ A,
+                                                               Adapters a, float* __restrict__ U) {
+    const int pass = blockIdx.x / max(blocks, 1), passes = (g.B + g.nb - 1) / g.nb;
+    if (blocks > 0 && pass < passes) {
+        w4_tokens(X, g, blockIdx.x - pass * blocks, pass, out);
+        return;
+    }
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) - blocks * passes) * 4 + (threadIdx.x >> 6);
+    if (at < static_cast<int64_t>(a.T) * a.r) shrink_few(X, g.ldx, A, g.K, a, true, at, U);
 }
 
 // ---------------------------------------------------------------- product
@@ -204,10 +224,46 @@ struct Step4 {
     }
 };
 
-// ROWS: bf16 tokens in rows of their own, X; else as w4_tokens_kernel lays them out.
-template <int NCT, int TB, bool ROWS>
+// The adapters of the tokens, behind the product.
+struct W4Adapters {
+    Adapters a;
+    const float* U;                  // times the adapters' scales
+    const void* B;
+};
+// y += U_t B_i of eight columns.
+template <typename T>
+__device__ __forceinline__ void add_adapter(const W4Adapters& w, int id, int64_t t, int f, int F, float (&y)[8]) {
+    const T* rows = static_cast<const T*>(w.B) + static_cast<int64_t>(id) * w.a.r * F;
+    const float* u = w.U + t * w.a.r;
+    float v[8] = {};
+    int row = 0;
+    if (f + 8 <= F) {
+        // (eight rows in flight)
+        for (; row + 8 <= w.a.r; row += 8) {
+            Eight<T> b[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) b[q].load(rows + static_cast<int64_t>(row + q) * F, f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += u[row + q] * b[q][i];
+        }
+    }
+    for (; row < w.a.r; ++row) {
+        float b[8];
+        load8(rows + static_cast<int64_t>(row) * F, f, F, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += u[row] * b[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] += v[i];
+}
+
+// ROWS: bf16 tokens in rows of their own, X; else as w4_tokens_kernel lays them out.  ADAPT: each token's adapter is added to its sums.
+template <int NCT, int TB, bool ROWS, bool ADAPT>
 __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16* __restrict__ X, const uint8_t* __restrict__ Q,
-                                                                     const uint8_t* __restrict__ S, W4Geom g, void* __restrict__ Y) {
+                                                                     const uint8_t* __restrict__ S, W4Geom g, void* __restrict__ Y,
+                                                                     const W4Adapters w) {
     extern __shared__ float sums[];                          // [wavefront][tile][column][16 rows]
     DAB_RESERVE_VGPRS();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -277,6 +333,34 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
     __syncthreads();
     // the shares of a tile and the pieces of a token, added in a fixed order
     const int rows = g.groups * TB * 16;
+    if constexpr (ADAPT) {
+        // eight rows of a token a thread, so that the adapter's rows are read in vectors
+        const int eights = rows >> 3;
+        for (int i = threadIdx.x; i < eights * nb; i += blockDim.x) {
+            const int b = i / eights, row = (i - b * eights) * 8, tl = row >> 4, grp = tl / TB, u = tl - grp * TB, f = tile0 * 16 + row;
+            if (f >= g.F) continue;
+            float y[8] = {};
+            for (int p = g.P - 1; p >= 0; --p)
+                for (int k = 0; k < g.ks; ++k) {
+                    const v4f* at = reinterpret_cast<const v4f*>(sums + (((grp * g.ks + k) * TB + u) * NCT * 16 + p * nb + b) * 16 + (row & 15));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] += at[0][e], y[4 + e] += at[1][e];
+                }
+            const int64_t t = b0 + b;
+            const int id = adapter_of(w.a, t);
+            if (g.dtype == DAB_F32) {
+                if (id >= 0) add_adapter<float>(w, id, t, f, g.F, y);
+                store8(static_cast<float*>(Y) + t * g.F, f, g.F, y);
+            } else if (g.dtype == DAB_BF16) {
+                if (id >= 0) add_adapter<bf16>(w, id, t, f, g.F, y);
+                store8(static_cast<bf16*>(Y) + t * g.F, f, g.F, y);
+            } else {
+                if (id >= 0) add_adapter<f16>(w, id, t, f, g.F, y);
+                store8(static_cast<f16*>(Y) + t * g.F, f, g.F, y);
+            }
+        }
+        return;
+    }
     for (int i = threadIdx.x; i < rows * nb; i += blockDim.x) {
         const int b = i / rows, row = i - b * rows, r = row & 15, tl = row >> 4, grp = tl / TB, u = tl - grp * TB;
         const int f = tile0 * 16 + row;
@@ -298,20 +382,22 @@ static int w4_tokens(int B, int P) { return ceil_div(B, ceil_div(B, kW4Columns /
 static bool w4_rows(int32_t B, int32_t K, int32_t dtype, int64_t ldx) { return dtype == DAB_BF16 && B <= 16 && K % 8 == 0 && ldx % 8 == 0; }
 
 template <int NCT, int TB, bool ROWS>
-static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y) {
+static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S, void* Y, const W4Adapters* w) {
     const int waves = g.ks * g.groups;
-    const dim3 grid(ceil_div(g.Ft, g.groups * TB), ceil_div(g.B, g.nb));
-    return launch(w4_matvec_kernel<NCT, TB, ROWS>, grid, dim3(64 * waves), static_cast<size_t>(waves) * TB * NCT * 1024, st, X, Q, S, g, Y);
+    const dim3 grid(ceil_div(g.Ft, g.groups * TB), ceil_div(g.B, g.nb)), block(64 * waves);
+    const size_t lds = static_cast<size_t>(waves) * TB * NCT * 1024;
+    if (w) return launch(w4_matvec_kernel<NCT, TB, ROWS, true>, grid, block, lds, st, X, Q, S, g, Y, *w);
+    return launch(w4_matvec_kernel<NCT, TB, ROWS, false>, grid, block, lds, st, X, Q, S, g, Y, W4Adapters{});
 }
 static int launch_matvec(const W4Geom& g, int columns, int TB, bool rows, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S,
-                         void* Y) {
-    if (rows) return TB == 2 ? launch_matvec<1, 2, true>(g, st, X, Q, S, Y) : launch_matvec<1, 1, true>(g, st, X, Q, S, Y);
-    if (columns == 1) return TB == 2 ? launch_matvec<1, 2, false>(g, st, X, Q, S, Y) : launch_matvec<1, 1, false>(g, st, X, Q, S, Y);
+                         void* Y, const W4Adapters* w) {
+    if (rows) return TB == 2 ? launch_matvec<1, 2, true>(g, st, X, Q, S, Y, w) : launch_matvec<1, 1, true>(g, st, X, Q, S, Y, w);
+    if (columns == 1) return TB == 2 ? launch_matvec<1, 2, false>(g, st, X, Q, S, Y, w) : launch_matvec<1, 1, false>(g, st, X, Q, S, Y, w);
     if (columns == 2)
-        return TB == 4   ? launch_matvec<2, 4, false>(g, st, X, Q, S, Y)
-               : TB == 2 ? launch_matvec<2, 2, false>(g, st, X, Q, S, Y)
-                         : launch_matvec<2, 1, false>(g, st, X, Q, S, Y);
-    return TB == 2 ? launch_matvec<3, 2, false>(g, st, X, Q, S, Y) : launch_matvec<3, 1, false>(g, st, X, Q, S, Y);
+        return TB == 4   ? launch_matvec<2, 4, false>(g, st, X, Q, S, Y, w)
+               : TB == 2 ? launch_matvec<2, 2, false>(g, st, X, Q, S, Y, w)
+                         : launch_matvec<2, 1, false>(g, st, X, Q, S, Y, w);
+    return TB == 2 ? launch_matvec<3, 2, false>(g, st, X, Q, S, Y, w) : launch_matvec<3, 1, false>(g, st, X, Q, S, Y, w);
 }
 
 }  // namespace dab
@@ -347,15 +433,17 @@ extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F,
     return static_cast<size_t>(ceil_div(B, nb)) * ceil_div(K, 128) * 4 * ceil_div(nb * P, 16) * 1024;
 }
 
-int dab::w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y,
-                    int32_t y_dtype, void* ws, size_t ws_bytes, void* stream) {
+namespace dab {
+
+// The product alone, or with the tokens' adapters behind it (A, w; U goes to `u`).
+static int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y, void* ws,
+                      size_t ws_bytes, hipStream_t st, const void* A = nullptr, const W4Adapters* w = nullptr, float* u = nullptr) {
     if (!X || !Q || !S || !Y) return DAB_ERR_NULL;
     if (B < 1 || K < 1 || F < 1 || ldx < K) return DAB_ERR_SHAPE;
     if (!real_dtype(dtype) || K > (1 << 26) || B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
     const size_t need = dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx);
     if (need && (!ws || ws_bytes < need || misaligned(ws, 256))) return DAB_ERR_WORKSPACE;
-    const auto st = static_cast<hipStream_t>(stream);
 
     W4Geom g{};
     g.F = F, g.K = K, g.Kt = ceil_div(K, 128), g.K4 = ceil_div(g.Kt, 4);
@@ -377,24 +465,60 @@ int dab::w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q,
     // groups of a workgroup: eight wavefronts, fewer where that leaves compute units without one (30 tokens, 1024 x 1024: 11.8 -> 7.1)
     g.groups = 8 / g.ks;
     while (g.groups > 1 && ceil_div(g.Ft, g.groups * TB) < kNumCU) g.groups /= 2;
-    g.dtype = y_dtype;
+    g.dtype = dtype;
     const bf16* x = static_cast<const bf16*>(X);
     g.ldx = ldx;
-    if (need) {
-        bf16* out = static_cast<bf16*>(ws);
-        const int64_t frags = static_cast<int64_t>(g.Kt) * 4 * columns;
-        const dim3 grid(static_cast<unsigned>(ceil_div64(frags, 4)), ceil_div(B, g.nb)), block(256);
-        int rc;
-        if (dtype == DAB_F32) rc = launch(w4_tokens_kernel<float>, grid, block, 0, st, static_cast<const float*>(X), B, K, ldx, g.Kt, g.nb, g.P, columns, out);
-        else if (dtype == DAB_F16) rc = launch(w4_tokens_kernel<f16>, grid, block, 0, st, static_cast<const f16*>(X), B, K, ldx, g.Kt, g.nb, g.P, columns, out);
-        else rc = launch(w4_tokens_kernel<bf16>, grid, block, 0, st, static_cast<const bf16*>(X), B, K, ldx, g.Kt, g.nb, g.P, columns, out);
-        if (rc) return rc;
-        x = out;
-    }
-    return launch_matvec(g, columns, TB, !need, st, x, Q, S, Y);
+    const int blocks = need ? static_cast<int>(ceil_div64(static_cast<int64_t>(g.Kt) * 4 * columns, 4)) : 0, passes = ceil_div(B, g.nb);
+    const W4Tokens to{B, K, ldx, g.Kt, g.nb, g.P, columns};
+    bf16* out = static_cast<bf16*>(ws);
+    const auto prepare = [&](auto* t) -> int {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        const T *from = static_cast<const T*>(X), *down = static_cast<const T*>(A);
+        const bool few = w && B <= kFewTokens;
+        if (w && !few)
+            if (int rc = shrink(from, ldx, down, K, w->a, true, u, st)) return rc;
+        if (few) {
+            const int64_t rows = ceil_div64(static_cast<int64_t>(B) * w->a.r, 4);
+            return launch(w4_tokens_shrink_kernel<T>, dim3(static_cast<unsigned>(static_cast<int64_t>(blocks) * passes + rows)), dim3(256), 0, st, from, to,
+                          blocks, out, down, w->a, u);
+        }
+        return need ? launch(w4_tokens_kernel<T>, dim3(blocks, passes), dim3(256), 0, st, from, to, out) : static_cast<int>(DAB_OK);
+    };
+    if (need || w)
+        if (int rc = dtype == DAB_F32   ? prepare(static_cast<float*>(nullptr))
+                     : dtype == DAB_F16 ? prepare(static_cast<f16*>(nullptr))
+                                        : prepare(static_cast<bf16*>(nullptr)))
+            return rc;
+    return launch_matvec(g, columns, TB, !need, st, need ? out : x, Q, S, Y, w);
 }
+
+}  // namespace dab
 
 extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K,
                              int32_t F, void* Y, void* ws, size_t ws_bytes, void* stream) {
-    return dab::w4_product(X, dtype, ldx, Q, S, B, K, F, Y, dtype, ws, ws_bytes, stream);
+    return dab::w4_product(X, dtype, ldx, Q, S, B, K, F, Y, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+// Workspace of the product with adapters: the product's own, then U.
+static size_t w4_own_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
+    return static_cast<size_t>(dab::round_up(static_cast<int64_t>(dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx)), 256));
+}
+extern "C" size_t dab_w4_adapters_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t r, int32_t dtype, int64_t ldx) {
+    if (B < 1 || K < 1 || F < 1 || r < 1 || !dab::real_dtype(dtype)) return 0;
+    return w4_own_bytes(B, K, F, dtype, ldx) + static_cast<size_t>(dab::round_up(static_cast<int64_t>(B) * r * 4, 256));
+}
+
+extern "C" int dab_w4_adapters(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, const int32_t* ids, const void* A,
+                               const void* Bt, const float* scale, int32_t B, int32_t K, int32_t F, int32_t n, int32_t r, void* Y, void* ws,
+                               size_t ws_bytes, void* stream) {
+    using namespace dab;
+    if (int rc = check_adapters(X, dtype, ldx, ids, A, Bt, scale, B, K, F, n, r)) return rc;
+    if (!Q || !S || !Y) return DAB_ERR_NULL;
+    if (B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
+    if (!ws || ws_bytes < dab_w4_adapters_workspace_bytes(B, K, F, r, dtype, ldx) || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    const size_t product = w4_own_bytes(B, K, F, dtype, ldx);
+    float* U = reinterpret_cast<float*>(static_cast<char*>(ws) + product);
+    const W4Adapters w{Adapters{ids, scale, B, n, r}, U, Bt};
+    return w4_product(X, dtype, ldx, Q, S, B, K, F, Y, ws, product, static_cast<hipStream_t>(stream), A, &w, U);
 }

@@ -50,25 +50,44 @@ def test_norm_gradient(lib):
     assert call(ws=None) == WORKSPACE and call(n=need - 1) == WORKSPACE and call(ws=ctypes.c_void_p(4096 + 16)) == WORKSPACE
 
 
-def test_adamw(lib):
-    def call(count=1, step=None, **k):
+def test_adamw_jobs(lib):
+    def call(count=1, **k):
         job = binding.dab_adamw_job(4096, 4096, 4096, 4096, 4096, 4096, 4096, 100, 64, F32, BF16, 8, 0.1)
         for name, v in k.items():
             setattr(job, name, v)
-        s = binding.dab_adamw_step(1e-3, 0.9, 0.999, 1e-8, 1, 0, None, None, None)
-        for name, v in (step or {}).items():
-            setattr(s, name, v)
-        return lib.dab_adamw((binding.dab_adamw_job * 1)(job), count, ctypes.byref(s), None)
-    assert lib.dab_adamw(None, 1, None, None) == NULL and call(count=0) == SHAPE
+        plan = binding.dab_adamw_plan()
+        rc = lib.dab_adamw_plan_of((binding.dab_adamw_job * 1)(job), count, ctypes.byref(plan))
+        return rc if rc else plan
+    assert lib.dab_adamw_plan_of(None, 1, ctypes.byref(binding.dab_adamw_plan())) == NULL and call(count=0) == SHAPE
     for k in ("P", "G", "M", "V", "MS", "VS"):
         assert call(**{k: None}) == NULL
     assert call(n=0) == SHAPE and call(place=33) == SHAPE and call(weight_decay=float("inf")) == SHAPE
     assert call(grad_dtype=3) == UNSUPPORTED and call(copy_dtype=F32) == UNSUPPORTED and call(bits=16) == UNSUPPORTED and call(n=(1 << 34) + 1) == UNSUPPORTED
     for k in ("P", "G", "M", "V", "copy"):
         assert call(**{k: 4098}) == ALIGN
+    plan = call()
+    assert plan.n_jobs == 1 and plan.workgroups == 1 and plan.table_bytes >= 100
+    job = (binding.dab_adamw_job * 1)(binding.dab_adamw_job(4096, 4096, 4096, 4096, 4096, 4096, 4096, 100, 64, F32, BF16, 8, 0.1))
+    table = lib.dab_adamw_table
+    assert table(None, ctypes.byref(plan), p, 4096, None) == NULL and table(job, ctypes.byref(plan), None, 4096, None) == NULL
+    assert table(job, ctypes.byref(plan), p, plan.table_bytes - 1, None) == WORKSPACE and table(job, ctypes.byref(plan), odd, 4096, None) == WORKSPACE
+    other = call(n=100000)
+    assert table(job, ctypes.byref(other), p, 1 << 20, None) == SHAPE
+
+
+def test_adamw(lib):
+    plan = binding.dab_adamw_plan(1, 1, 1, 256)
+
+    def call(table=p, size=4096, plan=plan, **k):
+        s = binding.dab_adamw_step(1e-3, 0.9, 0.999, 1e-8, 1, 0, None, None, None)
+        for name, v in k.items():
+            setattr(s, name, v)
+        return lib.dab_adamw(table, size, ctypes.byref(plan), ctypes.byref(s), None)
+    assert lib.dab_adamw(p, 4096, ctypes.byref(plan), None, None) == NULL and call(table=None) == NULL and call(table=odd) == WORKSPACE
+    assert call(size=100) == WORKSPACE and call(plan=binding.dab_adamw_plan(0, 1, 1, 256)) == SHAPE and call(plan=binding.dab_adamw_plan(2, 1, 1, 256)) == SHAPE
     for bad in (dict(lr=float("nan")), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("inf")), dict(step=0)):
-        assert call(step=bad) == SHAPE
-    assert call(step=dict(lr_dev=4097)) == ALIGN and call(step=dict(step_dev=4100)) == ALIGN and call(step=dict(grad_scale=4097)) == ALIGN
+        assert call(**bad) == SHAPE
+    assert call(lr_dev=4097) == ALIGN and call(step_dev=4100) == ALIGN and call(grad_scale=4097) == ALIGN
 
 
 def test_states(lib):
