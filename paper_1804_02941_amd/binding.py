@@ -922,6 +922,8 @@ def dab_adamw(jobs, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None,
     lr, step (from 1 on): numbers, or tensors of one element on the GPU (fp32, int64) that a captured graph reads anew at every replay; grad_scale: an
     fp32 tensor of one element that multiplies all gradients (infinite or a NaN: nothing is changed).  seed: of the random numbers that 8-bit states
     are rounded by, with the step."""
+    if (_native or native()).adamw(jobs.table, jobs.plan, lr, step, beta1, beta2, eps, grad_scale, seed):
+        return
     lr_dev = _flat(lr, 1, (torch.float32,), "lr") if isinstance(lr, torch.Tensor) else None
     step_dev = _flat(step, 1, (torch.int64,), "step") if isinstance(step, torch.Tensor) else None
     scale = _flat(grad_scale, 1, (torch.float32,), "grad_scale") if grad_scale is not None else None
@@ -937,6 +939,10 @@ def _state8(Q, S, name):
 
 def dab_state8_restore(Q, S, is_signed, dtype=torch.float32, n=None, out=None):
     """What an 8-bit state stands for (is_signed: a first moment, else the root of a second one), of its first n elements (all unless given)."""
+    if n is None and out is None:
+        done = (_native or native()).state8_restore(Q, S, is_signed, dtype)
+        if done is not None:
+            return done
     q, s, most = _state8(Q, S, "Q")
     n = most if n is None else n
     if not most - 32 < n <= most:

@@ -93,7 +93,7 @@ def build_call() -> str:
            "-isystem", os.path.join(tdir, "include"), "-isystem", sysconfig.get_paths()["include"],
            "-isystem", "/opt/rocm/include", "-I", os.path.join(ROOT, "include"), os.path.join(CSRC, "binding_call.cpp"),
            "-o", CALL + ".tmp", "-L", PKG, "-l:libdab_hip.so", "-L", os.path.join(tdir, "lib"),
-           "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+           "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if proc.returncode != 0:
         raise RuntimeError("compiling the binding failed:\n" + proc.stdout)

@@ -19,48 +19,64 @@ __device__ __forceinline__ int adapter_of(const Adapters& a, int64_t t) {
 }
 __device__ __forceinline__ float scale_of(const Adapters& a, int id) { return a.scale ? a.scale[id] : 1.f; }
 
-// Eight neighbouring elements as they are, all of them in the row.
-template <typename T>
-struct Eight {
-    typename Unaligned<T, 8>::type v;
-    __device__ __forceinline__ void load(const T* row, int c) { v = *reinterpret_cast<const typename Unaligned<T, 8>::type*>(row + c); }
+// N neighbouring elements as they are: all of them in the row, or zeros past its end.
+template <typename T, int N>
+struct Some {
+    typedef typename Unaligned<T, N>::type V;
+    V v;
+    __device__ __forceinline__ void load(const T* row, int c) { v = *reinterpret_cast<const V*>(row + c); }
+    // (past the caches: what nobody reads again soon)
+    __device__ __forceinline__ void load_once(const T* row, int c) { v = __builtin_nontemporal_load(reinterpret_cast<const V*>(row + c)); }
+    __device__ __forceinline__ void load(const T* row, int c, int cols) {
+        if (c + N <= cols) {
+            load(row, c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = c + i < cols ? row[c + i] : static_cast<T>(0.f);
+        }
+    }
     __device__ __forceinline__ float operator[](int i) const { return static_cast<float>(v[i]); }
 };
+template <typename T>
+using Eight = Some<T, 8>;
 
-// Few tokens: a wavefront takes one row of a token's adapter, its lanes eight k of 512, four of those turns in flight.
-constexpr int kFewTokens = 64;
+// Rows of kNarrow columns and more are read eight at a time throughout: the last eight of a row, some of them a second time, where fewer are left.
+constexpr int kNarrow = 8;
+
+// Few tokens: a workgroup of four wavefronts takes one row of a token's adapter, a lane eight k of 2048 at a time, four of those turns in flight.  (A
+// wavefront a row: seven fp32 tokens, 8 rows of 9111, 6.8 us.)
+constexpr int kFewTokens = 64, kFewWaves = 4;
 template <typename T>
 __device__ __forceinline__ void shrink_few(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, const Adapters& a, bool scaled,
                                            int64_t at, float* __restrict__ U) {
-    const int lane = threadIdx.x & 63;
+    __shared__ float part[kFewWaves];
     const int64_t t = at / a.r;
     const int row = static_cast<int>(at - t * a.r), id = adapter_of(a, t);
+    if (id < 0) {
+        if (threadIdx.x == 0) U[at] = 0.f;
+        return;
+    }
+    const T *x = X + t * ldx, *w = A + (static_cast<int64_t>(id) * a.r + row) * K;
     float sum = 0.f;
-    if (id >= 0) {
-        const T *x = X + t * ldx, *w = A + (static_cast<int64_t>(id) * a.r + row) * K;
-        int64_t k0 = 0;
-        for (; k0 + 2048 <= K; k0 += 2048) {
-            Eight<T> p[4], q[4];
+    for (int64_t k0 = threadIdx.x * 8; k0 < K; k0 += 8192) {
+        Eight<T> p[4], q[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int k = static_cast<int>(k0) + u * 512 + lane * 8;
-                p[u].load(x, k), q[u].load(w, k);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum += p[u][i] * q[u][i];
+        for (int u = 0; u < 4; ++u) {
+            const int64_t k = k0 + u * 2048;
+            p[u].v = {}, q[u].v = {};
+            if (k < K) p[u].load(x, static_cast<int>(k), K), q[u].load(w, static_cast<int>(k), K);
         }
-        for (k0 += lane * 8; k0 < K; k0 += 512) {
-            float p[8], q[8];
-            load8(x, static_cast<int>(k0), K, p), load8(w, static_cast<int>(k0), K, q);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += p[i] * q[i];
-        }
-        if (scaled) sum *= scale_of(a, id);
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += p[u][i] * q[u][i];
     }
     sum = lanes_sum<6>(sum);
-    if (lane == 0) U[at] = sum;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    U[at] = scaled ? sum * scale_of(a, id) : sum;
 }
 
 // U of any number of tokens (adapters.hip).

@@ -21,56 +21,41 @@ template <typename T>
 struct Long;
 template <>
 struct Long<float> {
-    float v[8];
-    __device__ __forceinline__ void load(const float* row, int k, int K) { load8(row, k, K, v); }
-    __device__ __forceinline__ void load(const float* row, int k) {
-        Eight<float> e;
-        e.load(row, k);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = e.v[i];
-    }
+    typedef float v8f __attribute__((ext_vector_type(8)));
+    v8f v;
+    __device__ __forceinline__ void load(const float* row, int k) { v = *reinterpret_cast<const Unaligned<float, 8>::type*>(row + k); }
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
         return c;
     }
 };
-template <typename T, typename V>
-__device__ __forceinline__ void load_raw(const T* row, int k, int K, V* v) {
-    if (k + 8 <= K) {
-        *v = *reinterpret_cast<const typename Unaligned<T, 8>::type*>(row + k);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) (*v)[i] = k + i < K ? row[k + i] : static_cast<T>(0.f);
-    }
-}
 template <>
 struct Long<bf16> {
     v8bf v;
-    __device__ __forceinline__ void load(const bf16* row, int k, int K) { load_raw(row, k, K, &v); }
     __device__ __forceinline__ void load(const bf16* row, int k) { v = *reinterpret_cast<const Unaligned<bf16, 8>::type*>(row + k); }
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }
 };
 template <>
 struct Long<f16> {
     v8h v;
-    __device__ __forceinline__ void load(const f16* row, int k, int K) { load_raw(row, k, K, &v); }
     __device__ __forceinline__ void load(const f16* row, int k) { v = *reinterpret_cast<const Unaligned<f16, 8>::type*>(row + k); }
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
 };
 
-// Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth step of 32 k; the loads of several steps are in
-// flight at once.
+// Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth stretch of 128 k, whose loads are in flight
+// at once.
 constexpr int kShrinkWaves = 8;
 template <typename T, int RT>
-__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a,
+__global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && sizeof(T) == 4 ? 2 : 4) void shrink_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a,
                                                                    int scaled, float* __restrict__ U) {
     __shared__ float sums[kShrinkWaves][RT][16][17];
     DAB_RESERVE_VGPRS();
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16, t = t0 + m;
-    const int r0 = blockIdx.y * 16 * RT, id = adapter_of(a, t);
+    const int r0 = blockIdx.y * 16 * RT;
     const T* x = X + (t < a.T ? t : a.T - 1) * ldx;
+    const int id = adapter_of(a, t);
     v4f out[RT];
 #pragma unroll
     for (int j = 0; j < RT; ++j) out[j] = v4f{0.f, 0.f, 0.f, 0.f};
@@ -84,30 +69,52 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(const T* __re
         const T* mine[RT];
 #pragma unroll
         for (int j = 0; j < RT; ++j) mine[j] = rows + static_cast<int64_t>(min(r0 + j * 16 + m, a.r - 1)) * K;
-        constexpr int kStep = kShrinkWaves * 32, kAhead = sizeof(T) == 4 && RT == 4 ? 2 : 4;
-        int64_t k0 = wave * 32;
-        for (; k0 + (kAhead - 1) * kStep + 32 <= K; k0 += kAhead * kStep) {
-            Long<T> xv[kAhead], av[kAhead][RT];
+        // a stretch of k: its loads, then, with those of the next one on their way, its products
+        constexpr int kAhead = RT == 1 ? 8 / static_cast<int>(sizeof(T)) : RT == 2 && sizeof(T) == 2 ? 2 : 1, kStep = kShrinkWaves * 32 * kAhead;
+        struct Stretch {
+            Long<T> x[kAhead], a[kAhead][RT];
+            // (eights that the row does not hold whole are zeros here)
+            __device__ __forceinline__ void load(const T* from, const T* const (&rows)[RT], int64_t k0, int g, int K) {
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int k = static_cast<int>(k0) + u * kStep + g * 8;
-                xv[u].load(x, k);
+                for (int u = 0; u < kAhead; ++u) {
+                    const int64_t k = k0 + u * 32 + g * 8;
+                    x[u].v = {};
 #pragma unroll
-                for (int j = 0; j < RT; ++j) av[u][j].load(mine[j], k);
+                    for (int j = 0; j < RT; ++j) a[u][j].v = {};
+                    if (k + 8 <= K) {
+                        x[u].load(from, static_cast<int>(k));
+#pragma unroll
+                        for (int j = 0; j < RT; ++j) a[u][j].load(rows[j], static_cast<int>(k));
+                    }
+                }
             }
+        };
+        int64_t k0 = wave * 32 * kAhead;
+        if (k0 < K) {
+            Stretch cur, next;
+            cur.load(x, mine, k0, g, K);
+            for (; k0 < K; k0 += kStep) {
+                const bool more = k0 + kStep < K;
+                if (more) next.load(x, mine, k0 + kStep, g, K);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
+                for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int j = 0; j < RT; ++j) acc[j] = Long<T>::mul(av[u][j], xv[u], acc[j]);
+                    for (int j = 0; j < RT; ++j) acc[j] = Long<T>::mul(cur.a[u][j], cur.x[u], acc[j]);
+                if (more) cur = next;
+            }
         }
-        for (; k0 < K; k0 += kStep) {
-            const int k = static_cast<int>(k0) + g * 8;
-            Long<T> xv;
-            xv.load(x, k, K);
+        if ((K & 7) != 0 && wave == kShrinkWaves - 1) {
+            // the last few of a row: those of its last eight that no eight before holds
+            const int again = g == 0 ? 8 - (K & 7) : 8;
+            Long<T> xv, av;
+            xv.load(x, K - 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xv.v[i] = i < again ? static_cast<T>(0.f) : xv.v[i];
 #pragma unroll
             for (int j = 0; j < RT; ++j) {
-                Long<T> av;
-                av.load(mine[j], k, K);
+                av.load(mine[j], K - 8);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) av.v[i] = i < again ? static_cast<T>(0.f) : av.v[i];
                 acc[j] = Long<T>::mul(av, xv, acc[j]);
             }
         }
@@ -136,11 +143,27 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(const T* __re
     }
 }
 
+// Rows of fewer than eight k: a thread takes a token and a row.
+template <typename T>
+__global__ __launch_bounds__(256) void shrink_narrow_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a, int scaled,
+                                                            float* __restrict__ U) {
+    const int64_t all = static_cast<int64_t>(a.T) * a.r;
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < all; at += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t t = at / a.r, row = at - t * a.r;
+        const int id = adapter_of(a, t);
+        float u = 0.f;
+        if (id >= 0) {
+            for (int k = 0; k < K; ++k) u += static_cast<float>(X[t * ldx + k]) * static_cast<float>(A[(static_cast<int64_t>(id) * a.r + row) * K + k]);
+            if (scaled) u *= scale_of(a, id);
+        }
+        U[at] = u;
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void shrink_few_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a, int scaled,
                                                          float* __restrict__ U) {
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (at < static_cast<int64_t>(a.T) * a.r) shrink_few(X, ldx, A, K, a, scaled != 0, at, U);
+    shrink_few(X, ldx, A, K, a, scaled != 0, blockIdx.x, U);
 }
 
 // ---------------------------------------------------------------- expand
@@ -150,115 +173,100 @@ struct Base {
     int dtype;                       // fp32, or the tokens'
 };
 
-// Many tokens: a wavefront takes two tiles of sixteen and 128 columns, lane l the eight columns 8 (l % 16) .. of tokens 4 (l / 16) .. + 3 of each.
-// In fp32 on the matrix cores, whatever the type: U is fp32, and the products are few.  Where the tiles share an adapter, which sequences of
-// tokens do, everything that sixteen of the r rows need is in flight at once, base ahead of it.
-constexpr int kExpandWaves = 4, kExpandTiles = 2;
+// Values of N columns, without the first `again` of them.
+template <typename T, int N>
+__device__ __forceinline__ void store_own(T* to, int again, const float (&w)[N]) {
+    if (again == 0) {
+        typename Unaligned<T, N>::type v;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = static_cast<T>(w[i]);
+        *reinterpret_cast<typename Unaligned<T, N>::type*>(to) = v;
+    } else {
+#pragma unroll
+        for (int i = 1; i < N; ++i)
+            if (i >= again) to[i] = static_cast<T>(w[i]);
+    }
+}
+
+// Many tokens: a wavefront takes sixteen and 128 columns, lane l the columns 8 (l % 16) .. of tokens 4 (l / 16) .. + 3.  In fp32 on the
+// matrix cores, whatever the type: U is fp32, and the products are few.  All that sixteen of the r rows need is in flight at once, base ahead of it.
+// 8192 x 4096 bf16, r = 16, base added: 34.3 us, 3.9 TB/s.  Measured and left: tiles of 16 x 64 40.6 us, base and U on their way before the ids 39 (registers),
+// several tiles a wavefront with the next one's loads ahead 74 (registers), products in bf16 pieces of U 42 (registers).
+constexpr int kExpandWaves = 4;
 template <typename T, typename TB>
-__global__ __launch_bounds__(64 * kExpandWaves) void expand_kernel(const float* __restrict__ U, const T* __restrict__ B, int F, Adapters a, int scaled,
-                                                                   const TB* base, int64_t ldbase, T* Y) {
+__global__ __launch_bounds__(64 * kExpandWaves, sizeof(TB) == 4 ? 3 : 4) void expand_kernel(const float* __restrict__ U, const T* __restrict__ B, int F,
+                                                                                        Adapters a, int scaled, const TB* base, int64_t ldbase, T* Y) {
     DAB_RESERVE_VGPRS();
-    constexpr int N = kExpandTiles;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16 * N;
-    const int64_t f64 = (static_cast<int64_t>(blockIdx.y) * kExpandWaves + wave) * 128 + m * 8;
-    if (f64 - m * 8 >= F) return;
-    const int f = static_cast<int>(f64);
-    const bool whole = f64 - m * 8 + 128 <= F && t0 + 16 * N <= a.T;
-    // (lanes from 16 N on repeat the ids)
-    const int all = adapter_of(a, t0 + (lane & (16 * N - 1))), first = __builtin_amdgcn_readfirstlane(all);
-    v4f out[N][8];
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y) * 16;
+    const int64_t f0 = (static_cast<int64_t>(blockIdx.x) * kExpandWaves + wave) * 128;
+    if (f0 >= F || t0 >= a.T) return;
+    // (a lane whose eight columns pass the row's end takes the last eight, and stores those that are its own)
+    const int64_t f64 = f0 + m * 8;
+    const int f = static_cast<int>(min(f64, static_cast<int64_t>(F) - 8)), again = static_cast<int>(f64 - f);
+    const int id = adapter_of(a, t0 + m);
+    const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
+    // one adapter after the other, -1 among them; of sequences' tokens there is one
+    bool waiting = true;
+    while (__any(waiting)) {
+        const int now = __shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1);
+        waiting = waiting && id != now;
+        Eight<TB> y[4];
+        bool mine[4];
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+        for (int v = 0; v < 4; ++v) {
+            const int64_t t = t0 + 4 * g + v;
+            mine[v] = __shfl(id, 4 * g + v) == now && t < a.T && f64 < F;
+            y[v].v = {};
+            if (base && mine[v]) y[v].load_once(base + t * ldbase, f);
+        }
+        v4f out[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) out[n][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    if (whole && __all(all == first)) {
-        Eight<TB> y[N][4];
-        if (base)
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) y[n][v].load(base + (t0 + 16 * n + 4 * g + v) * ldbase, f);
-        if (first >= 0) {
-            const T* rows = B + static_cast<int64_t>(first) * a.r * F;
-            const float s = scaled ? scale_of(a, first) : 1.f;
+        for (int j = 0; j < 8; ++j) out[j] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (now >= 0) {
+            const T* rows = B + static_cast<int64_t>(now) * a.r * F;
             for (int q0 = 0; q0 < a.r; q0 += 16) {
                 Eight<T> b[4];
-                float u[N][4];
+                float u[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int row = q0 + 4 * q + g;
-                    // (a row past the last is read from the last, its numbers replaced: an infinity there times 0 would be undefined)
-                    b[q].load(rows + static_cast<int64_t>(min(row, a.r - 1)) * F, f);
-#pragma unroll
-                    for (int n = 0; n < N; ++n) u[n][q] = row < a.r ? U[(t0 + 16 * n + m) * a.r + row] * s : 0.f;
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const bool in = q0 + 4 * q + g < a.r;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float w = in ? b[q][j] : 0.f;
-#pragma unroll
-                        for (int n = 0; n < N; ++n) out[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[n][q], w, out[n][j], 0, 0, 0);
+                    b[q].v = {}, u[q] = 0.f;
+                    if (row < a.r) {
+                        b[q].load(rows + static_cast<int64_t>(row) * F, f);
+                        if (id == now) u[q] = U[(t0 + m) * a.r + row] * s;
                     }
                 }
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) out[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], b[q][j], out[j], 0, 0, 0);
             }
         }
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                float w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = out[n][j][v] + (base ? y[n][v][j] : 0.f);
-                store8(Y + (t0 + 16 * n + 4 * g + v) * F, f, F, w);
-            }
-        return;
-    }
-    // tiles of several adapters, the last columns and the last tokens: one adapter after the other
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int id = __shfl(all, 16 * n + m);
-        const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
-        bool waiting = id >= 0;
-        while (__any(waiting)) {
-            const int now = __shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1);
-            const T* rows = B + static_cast<int64_t>(now) * a.r * F;
-            v4f acc[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
-            for (int q = 0; q < a.r; q += 4) {
-                const int row = q + g;
-                float b[8] = {};
-                float u = 0.f;
-                if (row < a.r) {
-                    load8(rows + static_cast<int64_t>(row) * F, f, F, b);
-                    if (id == now) u = U[(t0 + 16 * n + m) * a.r + row] * s;
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u, b[j], acc[j], 0, 0, 0);
-            }
-            // (of the tokens in this lane's results)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const bool mine = __shfl(id, 4 * g + v) == now;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) out[n][j][v] = mine ? acc[j][v] : out[n][j][v];
-            }
-            waiting = waiting && id != now;
-        }
-        if (f >= F) continue;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int64_t t = t0 + 16 * n + 4 * g + v;
-            if (t >= a.T) break;
-            float w[8] = {};
-            if (base) load8(base + t * ldbase, f, F, w);
+            if (!mine[v]) continue;
+            float w[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] += out[n][j][v];
-            store8(Y + t * F, f, F, w);
+            for (int j = 0; j < 8; ++j) w[j] = y[v][j] + out[j][v];
+            store_own(Y + (t0 + 4 * g + v) * F + f, again, w);
         }
+    }
+}
+
+// Rows of fewer than eight columns: a thread takes a token.
+template <typename T, typename TB>
+__global__ __launch_bounds__(256) void expand_narrow_kernel(const float* __restrict__ U, const T* __restrict__ B, int F, Adapters a, int scaled,
+                                                            const TB* base, int64_t ldbase, T* Y) {
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (t >= a.T) return;
+    const int id = adapter_of(a, t);
+    const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
+    for (int f = 0; f < F; ++f) {
+        float v = 0.f;
+        if (id >= 0)
+            for (int row = 0; row < a.r; ++row) v += (U[t * a.r + row] * s) * static_cast<float>(B[(static_cast<int64_t>(id) * a.r + row) * F + f]);
+        Y[t * F + f] = static_cast<T>((base ? static_cast<float>(base[t * ldbase + f]) : 0.f) + v);
     }
 }
 
@@ -290,8 +298,7 @@ __global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict_
 
 // ---------------------------------------------------------------- outer
 // Both gradients of the adapters in one launch: a workgroup takes 128 columns of one, 16 RT of the r rows, a share of the tokens and every slices-th
-// adapter; of each adapter that has tokens in its share its wavefronts take every eighth four of them (four such fours in flight) and add up
-// in LDS.  With one share that is the gradient; else it goes to parts: [share][adapter][r][columns], and have: [share][adapter] is 1 where
+// adapter; of each adapter that has tokens in its share its wavefronts take every eighth four of them (bf16: 32) and add up in LDS.  With one share that is the gradient; else it goes to parts: [share][adapter][r][columns], and have: [share][adapter] is 1 where
 // the share has tokens of the adapter (other parts are not written).
 constexpr int kOuterWaves = 8, kOuterIds = 2048;
 template <typename T>
@@ -309,10 +316,21 @@ struct Outer {
     int tokens, shares, slices;      // tokens of a share (a multiple of 32); slices of the adapters
     int32_t* have;
 };
+// Columns 2 d and 2 d + 1 of eight rows' eight columns, as the matrix cores take the rows: eight numbers of a column a lane.
+__device__ __forceinline__ void columns(const v4u32 (&x)[8], int d, v8bf* even, v8bf* odd) {
+    v4u32 p, q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p[i] = __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], 0x05040100u);
+        q[i] = __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], 0x07060302u);
+    }
+    *even = __builtin_bit_cast(v8bf, p), *odd = __builtin_bit_cast(v8bf, q);
+}
+
 template <typename T, int RT>
 __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters a, const Outer<T> o) {
     extern __shared__ uint32_t present[];                    // a bit for every adapter
-    __shared__ float sums[kOuterWaves / 2][16][132];
+    __shared__ float sums[kOuterWaves][8][132];
     __shared__ int ids[kOuterIds];
     DAB_RESERVE_VGPRS();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -335,8 +353,8 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters 
     if (o.shares > 1 && tile2 == 0 && rb == 0)
         for (int i = slice + threadIdx.x * o.slices; i < a.n; i += 64 * kOuterWaves * o.slices)
             o.have[static_cast<int64_t>(share) * a.n + i] = (present[i >> 5] >> (i & 31)) & 1u;
-    const int c = tile * 128 + m * 8;
     const bool whole = tile * 128 + 128 <= cols;
+    const int c = min(tile * 128 + m * 8, cols - 8), again = tile * 128 + m * 8 - c;         // (as in expand)
     const T* x0 = side.X + first * side.ldx;
     const float* v0 = side.V + first * a.r;
     for (int id = slice; id < a.n; id += o.slices) {
@@ -348,78 +366,147 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters 
         for (int j = 0; j < RT; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
-        constexpr int kAhead = RT == 4 ? 2 : 4;
-        for (int t1 = none ? count : wave * 4; t1 < count; t1 += kOuterWaves * 4 * kAhead) {
-            bool mine[kAhead], some[kAhead], any = false;
+        if constexpr (std::is_same_v<T, bf16>) {
+            // 32 tokens a step, eight of them a lane: V as the sum of three bf16 numbers, eight rows of eight columns transposed in the lane's registers
+            for (int t1 = none ? count : wave * 32; t1 < count; t1 += kOuterWaves * 32) {
+                bool mine[8], any = false;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int t = t1 + u * kOuterWaves * 4 + g;
-                mine[u] = t < count && (kept ? ids[t] : a.ids[first + t]) == id;
-                some[u] = __any(mine[u]);
-                any = any || some[u];
-            }
-            if (!any) continue;
-            Eight<T> x[kAhead];
-            float v[kAhead][RT];
+                for (int e = 0; e < 8; ++e) {
+                    const int t = t1 + 8 * g + e;
+                    mine[e] = t < count && (kept ? ids[t] : a.ids[first + t]) == id;
+                    any = any || mine[e];
+                }
+                if (!__any(any)) continue;
+                v4u32 x[8];
+                float v[RT][8];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int64_t t = t1 + u * kOuterWaves * 4 + g;
+                for (int e = 0; e < 8; ++e) {
+                    const int64_t t = t1 + 8 * g + e;
+                    Eight<bf16> w;
+                    w.v = {};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[u].v[i] = static_cast<T>(0.f);
+                    for (int j = 0; j < RT; ++j) v[j][e] = 0.f;
+                    if (mine[e]) {
+                        w.load(x0 + t * side.ldx, c);
 #pragma unroll
-                for (int j = 0; j < RT; ++j) v[u][j] = 0.f;
-                if (mine[u]) {
-                    const T* from = x0 + t * side.ldx;
-                    if (whole) {
-                        x[u].load(from, c);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (c + i < cols) x[u].v[i] = from[c + i];
+                        for (int j = 0; j < RT; ++j)
+                            if (r0 + j * 16 + m < a.r) v[j][e] = v0[t * a.r + r0 + j * 16 + m];
                     }
+                    x[e] = __builtin_bit_cast(v4u32, w.v);
+                }
+                v8bf p[RT][3];
 #pragma unroll
-                    for (int j = 0; j < RT; ++j)
-                        if (r0 + j * 16 + m < a.r) v[u][j] = v0[t * a.r + r0 + j * 16 + m];
+                for (int j = 0; j < RT; ++j)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[j][k][e] = piece_of(v[j][e], k);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    v8bf even, odd;
+                    columns(x, d, &even, &odd);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+#pragma unroll
+                        for (int j = 0; j < RT; ++j) {
+                            acc[j][2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[j][k], even, acc[j][2 * d], 0, 0, 0);
+                            acc[j][2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[j][k], odd, acc[j][2 * d + 1], 0, 0, 0);
+                        }
                 }
             }
+        } else {
+            constexpr int kAhead = RT == 4 ? 2 : 4;
+            for (int t1 = none ? count : wave * 4; t1 < count; t1 += kOuterWaves * 4 * kAhead) {
+                bool mine[kAhead], some[kAhead], any = false;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (some[u])
+                for (int u = 0; u < kAhead; ++u) {
+                    const int t = t1 + u * kOuterWaves * 4 + g;
+                    mine[u] = t < count && (kept ? ids[t] : a.ids[first + t]) == id;
+                    some[u] = __any(mine[u]);
+                    any = any || some[u];
+                }
+                if (!any) continue;
+                Eight<T> x[kAhead];
+                float v[kAhead][RT];
 #pragma unroll
-                    for (int j = 0; j < RT; ++j)
+                for (int u = 0; u < kAhead; ++u) {
+                    const int64_t t = t1 + u * kOuterWaves * 4 + g;
+                    x[u].v = {};
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][j], x[u][i], acc[j][i], 0, 0, 0);
+                    for (int j = 0; j < RT; ++j) v[u][j] = 0.f;
+                    if (mine[u]) {
+                        x[u].load(x0 + t * side.ldx, c);
+#pragma unroll
+                        for (int j = 0; j < RT; ++j)
+                            if (r0 + j * 16 + m < a.r) v[u][j] = v0[t * a.r + r0 + j * 16 + m];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (some[u])
+#pragma unroll
+                        for (int j = 0; j < RT; ++j)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][j], x[u][i], acc[j][i], 0, 0, 0);
+            }
         }
-        // rows 4 g + v of 16, columns 8 m + i of 128: added up in a fixed order, the upper wavefronts' onto the lower ones'
+        // rows 4 g + v of 16, columns 8 m + i of 128: every wavefront's into LDS, then a thread adds up four columns
         float* out = side.out + (static_cast<int64_t>(o.shares > 1 ? share : 0) * a.n + id) * a.r * cols;
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
+        for (int j = 0; j < 2 * RT; ++j) {                   // (eight of the rows at a time: those of v = 0 and 1, then of 2 and 3)
+            if (!none)
 #pragma unroll
-            for (int half = kOuterWaves / 2; half >= 1; half /= 2) {
-                if (wave >= half && wave < 2 * half)
+                for (int i = 0; i < 8; i += 4)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int h = 0; h < 2; ++h) {
+                        const int v = 2 * (j & 1) + h;
+                        if (again == 0) {
+                            *reinterpret_cast<v4f*>(&sums[wave][2 * g + h][m * 8 + i]) =
+                                v4f{acc[j / 2][i][v], acc[j / 2][i + 1][v], acc[j / 2][i + 2][v], acc[j / 2][i + 3][v]};
+                        } else if (again < 8) {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) sums[wave - half][4 * g + v][m * 8 + i] = acc[j][i][v];
-                __syncthreads();
-                if (wave < half)
+                            for (int k = 0; k < 4; ++k)
+                                if (i + k >= again) sums[wave][2 * g + h][m * 8 + i + k - again] = acc[j / 2][i + k][v];
+                        }
+                    }
+            __syncthreads();
+            const int at = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4, row = r0 + (j / 2) * 16 + 4 * (at >> 1) + 2 * (j & 1) + (at & 1);
+            if (at < 8 && row < a.r) {
+                v4f w = v4f{0.f, 0.f, 0.f, 0.f};
+                if (!none)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int k = 0; k < kOuterWaves; ++k) w += *reinterpret_cast<const v4f*>(&sums[k][at][col]);
+                float* to = out + static_cast<int64_t>(row) * cols + tile * 128 + col;
+                if (whole) {
+                    *reinterpret_cast<Unaligned<float, 4>::type*>(to) = w * s;
+                } else {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[j][i][v] += sums[wave][4 * g + v][m * 8 + i];
-                __syncthreads();
-            }
-            if (wave == 0 && c < cols)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int row = r0 + j * 16 + 4 * g + v;
-                    if (row >= a.r) break;
-                    float w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = acc[j][i][v] * s;
-                    store8(out + static_cast<int64_t>(row) * cols, c, cols, w);
+                    for (int i = 0; i < 4; ++i)
+                        if (tile * 128 + col + i < cols) to[i] = w[i] * s;
                 }
+            }
+            __syncthreads();
         }
+    }
+}
+
+// Rows of fewer than eight columns: a workgroup takes a row of an adapter.
+template <typename T>
+__global__ __launch_bounds__(256) void outer_narrow_kernel(const Adapters a, const OuterSide<T> side) {
+    __shared__ float sums[4];
+    const int row = blockIdx.x, id = blockIdx.y;
+    for (int c = 0; c < side.cols; ++c) {
+        float v = 0.f;
+        bool any = false;
+        for (int64_t t = threadIdx.x; t < a.T; t += 256)
+            if (a.ids[t] == id) v += side.V[t * a.r + row] * static_cast<float>(side.X[t * side.ldx + c]), any = true;
+        v = lanes_sum<6>(v);
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+        any = __syncthreads_or(any);
+        if (threadIdx.x == 0)
+            side.out[(static_cast<int64_t>(id) * a.r + row) * side.cols + c] =
+                any ? ((sums[0] + sums[1]) + (sums[2] + sums[3])) * (side.scaled ? scale_of(a, id) : 1.f) : 0.f;
+        __syncthreads();
     }
 }
 
@@ -462,11 +549,13 @@ constexpr int kMaxRank = 256;
 template <typename T>
 int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
     if (a.T <= kFewTokens)
-        return launch(shrink_few_kernel<T>, dim3(static_cast<unsigned>(ceil_div64(static_cast<int64_t>(a.T) * a.r, 4))), dim3(256), 0, st, X, ldx, A, K, a,
-                      static_cast<int>(scaled), U);
+        return launch(shrink_few_kernel<T>, dim3(a.T * a.r), dim3(64 * kFewWaves), 0, st, X, ldx, A, K, a, static_cast<int>(scaled), U);
     const unsigned tiles = static_cast<unsigned>(ceil_div64(a.T, 16));
     const dim3 block(64 * kShrinkWaves);
     const int s = scaled;
+    if (K < kNarrow)
+        return launch(shrink_narrow_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(ceil_div64(static_cast<int64_t>(a.T) * a.r, 256), 1 << 20))), dim3(256),
+                      0, st, X, ldx, A, K, a, s, U);
     if (a.r <= 16) return launch(shrink_kernel<T, 1>, dim3(tiles), block, 0, st, X, ldx, A, K, a, s, U);
     if (a.r <= 32) return launch(shrink_kernel<T, 2>, dim3(tiles), block, 0, st, X, ldx, A, K, a, s, U);
     return launch(shrink_kernel<T, 4>, dim3(tiles, ceil_div(a.r, 64)), block, 0, st, X, ldx, A, K, a, s, U);
@@ -482,8 +571,13 @@ static int expand_from(const float* U, const T* B, int F, const Adapters& a, boo
     const int s = scaled;
     if (a.T <= kFewTokens)
         return launch(expand_few_kernel<T, TB>, dim3(static_cast<unsigned>(ceil_div64(F, 512)), a.T), dim3(64), 0, st, U, B, F, a, s, p, base.ld, Y);
-    return launch(expand_kernel<T, TB>, dim3(static_cast<unsigned>(ceil_div64(a.T, 16 * kExpandTiles)), static_cast<unsigned>(ceil_div64(F, 128 * kExpandWaves))),
-                  dim3(64 * kExpandWaves), 0, st, U, B, F, a, s, p, base.ld, Y);
+    if (F < kNarrow)
+        return launch(expand_narrow_kernel<T, TB>, dim3(static_cast<unsigned>(ceil_div64(a.T, 256))), dim3(256), 0, st, U, B, F, a, s, p, base.ld, Y);
+    // (token tiles along y and z: more than 65535 of them)
+    const int64_t tiles = ceil_div64(a.T, 16);
+    const dim3 grid(static_cast<unsigned>(ceil_div64(F, 128 * kExpandWaves)), static_cast<unsigned>(std::min<int64_t>(tiles, 32768)),
+                    static_cast<unsigned>(ceil_div64(tiles, 32768))), block(64 * kExpandWaves);
+    return launch(expand_kernel<T, TB>, grid, block, 0, st, U, B, F, a, s, p, base.ld, Y);
 }
 template <typename T>
 static int expand(const float* U, const T* B, int F, const Adapters& a, bool scaled, const Base& base, T* Y, hipStream_t st) {
@@ -511,18 +605,26 @@ static OuterPlan outer_plan(int T, int n, int r, int cols0, int cols1) {
         p.parts0 = round_up(row * cols0 * p.shares, 256), p.parts1 = round_up(row * cols1 * p.shares, 256), p.have = round_up(static_cast<int64_t>(p.shares) * n * 4, 256);
     return p;
 }
-// One side of the gradients: out[i] = sum over adapter i's tokens of V^T X, times scale[i] where `scaled`.
+// Both sides of the gradients: out[i] = sum over adapter i's tokens of V^T X, times scale[i] where `scaled`.
 template <typename T>
-static int outer(OuterSide<T> first, OuterSide<T> second, const Adapters& a, char* ws, hipStream_t st) {
-    const OuterPlan p = outer_plan(a.T, a.n, a.r, first.cols, second.cols);
+static int outer(const OuterSide<T> (&sides)[2], const Adapters& a, char* ws, hipStream_t st) {
+    OuterSide<T> wide[2];
+    int n = 0;
+    for (const OuterSide<T>& s : sides) {
+        if (s.cols >= kNarrow) wide[n++] = s;
+        else if (int rc = launch(outer_narrow_kernel<T>, dim3(a.r, a.n), dim3(256), 0, st, a, s)) return rc;
+    }
+    if (n == 0) return DAB_OK;
+    if (n == 1) wide[1] = wide[0], wide[1].cols = 0;
+    const OuterPlan p = outer_plan(a.T, a.n, a.r, wide[0].cols, wide[1].cols);
     Outer<T> o{};
     Join j{};
-    j.out[0] = first.out, j.out[1] = second.out;
+    j.out[0] = wide[0].out, j.out[1] = wide[1].out;
     if (p.shares > 1) {
-        first.out = reinterpret_cast<float*>(ws), second.out = reinterpret_cast<float*>(ws + p.parts0);
+        wide[0].out = reinterpret_cast<float*>(ws), wide[1].out = reinterpret_cast<float*>(ws + p.parts0);
         o.have = reinterpret_cast<int32_t*>(ws + p.parts0 + p.parts1);
     }
-    o.side[0] = first, o.side[1] = second, o.tiles0 = p.tiles0, o.tiles = p.tiles, o.tokens = p.tokens, o.shares = p.shares, o.slices = p.slices;
+    o.side[0] = wide[0], o.side[1] = wide[1], o.tiles0 = p.tiles0, o.tiles = p.tiles, o.tokens = p.tokens, o.shares = p.shares, o.slices = p.slices;
     const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.tiles) * p.row_blocks), p.shares, p.slices), block(64 * kOuterWaves);
     const size_t lds = static_cast<size_t>(ceil_div(a.n, 32)) * 4;
     int rc;
@@ -530,10 +632,15 @@ static int outer(OuterSide<T> first, OuterSide<T> second, const Adapters& a, cha
     else if (p.rt == 2) rc = launch(outer_kernel<T, 2>, grid, block, lds, st, a, o);
     else rc = launch(outer_kernel<T, 4>, grid, block, lds, st, a, o);
     if (rc || p.shares == 1) return rc;
-    j.parts[0] = first.out, j.parts[1] = second.out, j.have = o.have, j.shares = p.shares, j.n = a.n;
-    j.size[0] = static_cast<int64_t>(a.r) * first.cols, j.size[1] = static_cast<int64_t>(a.r) * second.cols;
+    j.parts[0] = wide[0].out, j.parts[1] = wide[1].out, j.have = o.have, j.shares = p.shares, j.n = a.n;
+    j.size[0] = static_cast<int64_t>(a.r) * wide[0].cols, j.size[1] = static_cast<int64_t>(a.r) * wide[1].cols;
     j.blocks0 = static_cast<unsigned>(ceil_div64(j.size[0], 1024));
     return launch(outer_join_kernel, dim3(j.blocks0 + static_cast<unsigned>(ceil_div64(j.size[1], 1024)), a.n), dim3(256), 0, st, j);
+}
+// (rows that the narrow kernels take are no part of the plan)
+static size_t outer_bytes(int T, int n, int r, int F, int K) {
+    if (F < kNarrow && K < kNarrow) return 0;
+    return F < kNarrow ? outer_plan(T, n, r, K, 0).bytes() : outer_plan(T, n, r, F, K < kNarrow ? 0 : K).bytes();
 }
 
 int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
@@ -576,7 +683,7 @@ extern "C" int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int
 extern "C" size_t dab_adapters_gradient_workspace_bytes(int32_t T, int32_t K, int32_t F, int32_t n, int32_t r) {
     using namespace dab;
     if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || K > (1 << 24) || F > (1 << 24) || n > 65535 || r > kMaxRank || T > (1 << 25)) return 0;
-    return static_cast<size_t>(round_up(static_cast<int64_t>(T) * r * 4, 256)) + outer_plan(T, n, r, F, K).bytes();
+    return static_cast<size_t>(round_up(static_cast<int64_t>(T) * r * 4, 256)) + outer_bytes(T, n, r, F, K);
 }
 
 extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X, int32_t dtype, int64_t ldx, const float* U, const int32_t* ids,
@@ -599,7 +706,7 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
         typedef std::remove_pointer_t<decltype(t)> E;
         const E *x = static_cast<const E*>(X), *dy = static_cast<const E*>(dY), *up = static_cast<const E*>(B), *down = static_cast<const E*>(A);
         if (int rc = shrink(dy, lddy, up, F, a, true, V, st)) return rc;
-        if (int rc = outer(OuterSide<E>{U, dy, lddy, F, 1, dB}, OuterSide<E>{V, x, ldx, K, 0, dA}, a, rest, st)) return rc;
+        if (int rc = outer<E>({{U, dy, lddy, F, 1, dB}, {V, x, ldx, K, 0, dA}}, a, rest, st)) return rc;
         if (!dX) return DAB_OK;
         return expand(static_cast<const float*>(V), down, K, a, false, Base{base, ldbase, base_dtype}, static_cast<E*>(dX), st);
     };

@@ -182,8 +182,7 @@ __global__ __launch_bounds__(256) void w4_tokens_shrink_kernel(const T* __restri
         w4_tokens(X, g, blockIdx.x - pass * blocks, pass, out);
         return;
     }
-    const int64_t at = (static_cast<int64_t>(blockIdx.x) - blocks * passes) * 4 + (threadIdx.x >> 6);
-    if (at < static_cast<int64_t>(a.T) * a.r) shrink_few(X, g.ldx, A, g.K, a, true, at, U);
+    shrink_few(X, g.ldx, A, g.K, a, true, static_cast<int64_t>(blockIdx.x) - blocks * passes, U);
 }
 
 // ---------------------------------------------------------------- product
@@ -230,37 +229,48 @@ struct W4Adapters {
     const float* U;                  // times the adapters' scales
     const void* B;
 };
-// y += U_t B_i of eight columns.
-template <typename T>
-__device__ __forceinline__ void add_adapter(const W4Adapters& w, int id, int64_t t, int f, int F, float (&y)[8]) {
-    const T* rows = static_cast<const T*>(w.B) + static_cast<int64_t>(id) * w.a.r * F;
-    const float* u = w.U + t * w.a.r;
-    float v[8] = {};
-    int row = 0;
-    if (f + 8 <= F) {
-        // (eight rows in flight)
-        for (; row + 8 <= w.a.r; row += 8) {
-            Eight<T> b[8];
+// LANES lanes share a token's eight columns: the shares of the sums, the pieces of the token and the adapter's rows are dealt out to them, ROWS
+// rows a lane read at once.
+template <typename T, int LANES, int ROWS>
+struct W4Rows {
+    Eight<T> b[ROWS];
+    float u[ROWS];
+    int id;
+    __device__ __forceinline__ void load(const W4Adapters& w, int64_t t, int f, int F, int lane) {
+        id = adapter_of(w.a, t);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) b[q].load(rows + static_cast<int64_t>(row + q) * F, f);
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += u[row + q] * b[q][i];
+        for (int q = 0; q < ROWS; ++q) {
+            const int row = q * LANES + lane;
+            b[q].v = {}, u[q] = 0.f;
+            if (id >= 0 && row < w.a.r) {
+                b[q].load(static_cast<const T*>(w.B) + (static_cast<int64_t>(id) * w.a.r + row) * F, f, F);
+                u[q] = w.U[t * w.a.r + row];
+            }
         }
     }
-    for (; row < w.a.r; ++row) {
-        float b[8];
-        load8(rows + static_cast<int64_t>(row) * F, f, F, b);
+    // y += the lane's part of U_t B_i
+    __device__ __forceinline__ void add(const W4Adapters& w, int64_t t, int f, int F, int lane, float (&y)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += u[row] * b[i];
+        for (int q = 0; q < ROWS; ++q)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] += u[q] * b[q][i];
+        if (id < 0) return;
+        const T* rows = static_cast<const T*>(w.B) + static_cast<int64_t>(id) * w.a.r * F;
+#pragma unroll 4
+        for (int row = ROWS * LANES + lane; row < w.a.r; row += LANES) {
+            Eight<T> c;
+            c.load(rows + static_cast<int64_t>(row) * F, f, F);
+            const float by = w.U[t * w.a.r + row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] += by * c[i];
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] += v[i];
-}
+};
+struct NoAdapters {};
 
-// ROWS: bf16 tokens in rows of their own, X; else as w4_tokens_kernel lays them out.  ADAPT: each token's adapter is added to its sums.
-template <int NCT, int TB, bool ROWS, bool ADAPT>
+// ROWS: bf16 tokens in rows of their own, X; else as w4_tokens_kernel lays them out.  TA: the type of the
+// adapters that are added to the tokens' sums, and of Y then; or NoAdapters.
+template <int NCT, int TB, bool ROWS, typename TA>
 __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16* __restrict__ X, const uint8_t* __restrict__ Q,
                                                                      const uint8_t* __restrict__ S, W4Geom g, void* __restrict__ Y,
                                                                      const W4Adapters w) {
@@ -270,6 +280,13 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
     const int group = __builtin_amdgcn_readfirstlane(wave / g.ks), part = wave - group * g.ks;
     const int tile0 = blockIdx.x * g.groups * TB, tile = tile0 + group * TB;
     const int b0 = blockIdx.y * g.nb, nb = min(g.nb, g.B - b0), cols = nb * g.P;
+    constexpr bool kAdapt = !std::is_same_v<TA, NoAdapters>;
+    // Where registers are left the adapter's number and first rows are read before the product, by eight lanes each (one token, 4096 x 4096: 4.6 us, 4.4
+    // without an adapter; read behind the product 6.3 to 7.3); else behind it, by two (32 tokens, 16384 x 4096: 14.4 us, 13.8 without).
+    constexpr bool kEarly = NCT * TB <= 4;
+    constexpr int kLanes = kEarly ? 8 : 2;
+    std::conditional_t<kAdapt, W4Rows<std::conditional_t<kAdapt, TA, float>, kLanes, kEarly ? 2 : 4>, NoAdapters> early;
+    const int eights = g.groups * TB * 2, units = eights * nb * kLanes;        // eight rows of a token a unit
 
     v4f acc[TB][NCT];
 #pragma unroll
@@ -279,9 +296,14 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
     // (columns past the last read the first one's token; their results are not used)
     const bf16* x0 = ROWS ? X + (b0 + ((lane & 15) < cols ? lane & 15 : 0)) * g.ldx
                           : X + static_cast<int64_t>(blockIdx.y) * g.Kt * (4 * NCT * 512) + lane * 8;
-    if (tile < g.Ft && part < g.K4) {
-        Step4<TB> now, next;
-        now.load(Q, S, g, tile, part, lane);
+    const bool some = tile < g.Ft && part < g.K4;
+    Step4<TB> now, next;
+    if (some) now.load(Q, S, g, tile, part, lane);
+    if constexpr (kAdapt && kEarly) {
+        const int unit = threadIdx.x / kLanes, f = tile0 * 16 + unit % eights * 8;
+        if (static_cast<int>(threadIdx.x) < units && f < g.F) early.load(w, b0 + unit / eights, f, g.F, threadIdx.x % kLanes);
+    }
+    if (some) {
         for (int s = part; s < g.K4; s += g.ks) {
             const bool more = s + g.ks < g.K4;
             if (more) next.load(Q, S, g, tile, s + g.ks, lane);
@@ -333,31 +355,24 @@ __global__ __launch_bounds__(64 * kW4MaxWaves) void w4_matvec_kernel(const bf16*
     __syncthreads();
     // the shares of a tile and the pieces of a token, added in a fixed order
     const int rows = g.groups * TB * 16;
-    if constexpr (ADAPT) {
-        // eight rows of a token a thread, so that the adapter's rows are read in vectors
-        const int eights = rows >> 3;
-        for (int i = threadIdx.x; i < eights * nb; i += blockDim.x) {
-            const int b = i / eights, row = (i - b * eights) * 8, tl = row >> 4, grp = tl / TB, u = tl - grp * TB, f = tile0 * 16 + row;
+    if constexpr (kAdapt) {
+        for (int i = threadIdx.x; i < units; i += blockDim.x) {
+            const int unit = i / kLanes, l = i % kLanes, b = unit / eights, row = (unit - b * eights) * 8, tl = row >> 4, grp = tl / TB, u = tl - grp * TB;
+            const int f = tile0 * 16 + row;
             if (f >= g.F) continue;
-            float y[8] = {};
-            for (int p = g.P - 1; p >= 0; --p)
-                for (int k = 0; k < g.ks; ++k) {
-                    const v4f* at = reinterpret_cast<const v4f*>(sums + (((grp * g.ks + k) * TB + u) * NCT * 16 + p * nb + b) * 16 + (row & 15));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] += at[0][e], y[4 + e] += at[1][e];
-                }
             const int64_t t = b0 + b;
-            const int id = adapter_of(w.a, t);
-            if (g.dtype == DAB_F32) {
-                if (id >= 0) add_adapter<float>(w, id, t, f, g.F, y);
-                store8(static_cast<float*>(Y) + t * g.F, f, g.F, y);
-            } else if (g.dtype == DAB_BF16) {
-                if (id >= 0) add_adapter<bf16>(w, id, t, f, g.F, y);
-                store8(static_cast<bf16*>(Y) + t * g.F, f, g.F, y);
-            } else {
-                if (id >= 0) add_adapter<f16>(w, id, t, f, g.F, y);
-                store8(static_cast<f16*>(Y) + t * g.F, f, g.F, y);
+            if (!kEarly || i != static_cast<int>(threadIdx.x)) early.load(w, t, f, g.F, l);
+            float y[8] = {};
+            for (int k = l; k < g.ks * g.P; k += kLanes) {
+                const int p = k / g.ks;
+                const v4f* at = reinterpret_cast<const v4f*>(sums + (((grp * g.ks + k - p * g.ks) * TB + u) * NCT * 16 + p * nb + b) * 16 + (row & 15));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] += at[0][e], y[4 + e] += at[1][e];
             }
+            early.add(w, t, f, g.F, l, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = lanes_sum<kEarly ? 3 : 1>(y[e]);
+            if (l == 0) store8(static_cast<TA*>(Y) + t * g.F, f, g.F, y);
         }
         return;
     }
@@ -386,8 +401,12 @@ static int launch_matvec(const W4Geom& g, hipStream_t st, const bf16* X, const u
     const int waves = g.ks * g.groups;
     const dim3 grid(ceil_div(g.Ft, g.groups * TB), ceil_div(g.B, g.nb)), block(64 * waves);
     const size_t lds = static_cast<size_t>(waves) * TB * NCT * 1024;
-    if (w) return launch(w4_matvec_kernel<NCT, TB, ROWS, true>, grid, block, lds, st, X, Q, S, g, Y, *w);
-    return launch(w4_matvec_kernel<NCT, TB, ROWS, false>, grid, block, lds, st, X, Q, S, g, Y, W4Adapters{});
+    if (!w) return launch(w4_matvec_kernel<NCT, TB, ROWS, NoAdapters>, grid, block, lds, st, X, Q, S, g, Y, W4Adapters{});
+    if constexpr (!ROWS) {
+        if (g.dtype == DAB_F32) return launch(w4_matvec_kernel<NCT, TB, ROWS, float>, grid, block, lds, st, X, Q, S, g, Y, *w);
+        if (g.dtype == DAB_F16) return launch(w4_matvec_kernel<NCT, TB, ROWS, f16>, grid, block, lds, st, X, Q, S, g, Y, *w);
+    }
+    return launch(w4_matvec_kernel<NCT, TB, ROWS, bf16>, grid, block, lds, st, X, Q, S, g, Y, *w);
 }
 static int launch_matvec(const W4Geom& g, int columns, int TB, bool rows, hipStream_t st, const bf16* X, const uint8_t* Q, const uint8_t* S,
                          void* Y, const W4Adapters* w) {
@@ -478,7 +497,7 @@ static int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* 
         if (w && !few)
             if (int rc = shrink(from, ldx, down, K, w->a, true, u, st)) return rc;
         if (few) {
-            const int64_t rows = ceil_div64(static_cast<int64_t>(B) * w->a.r, 4);
+            const int64_t rows = static_cast<int64_t>(B) * w->a.r;
             return launch(w4_tokens_shrink_kernel<T>, dim3(static_cast<unsigned>(static_cast<int64_t>(blocks) * passes + rows)), dim3(256), 0, st, from, to,
                           blocks, out, down, w->a, u);
         }

@@ -256,7 +256,9 @@ def test_served_tokens_keep_to_themselves():
     Y = dab.dab_w4_adapters(X, Q, S, F, ids, A, B, scale)
     for t in range(T):
         assert torch.equal(Y[t], clean[t]) if t != 2 else bool(Y[t].isnan().all())
-    assert torch.equal(Y[3], dab.dab_w4_matvec(X[3:4], Q, S, F)[0])
+    # without an adapter it is the product alone, its sums in another order: a step of bf16 apart at most
+    alone = dab.dab_w4_matvec(X[3:4], Q, S, F)[0]
+    assert bool(((Y[3].float() - alone.float()).abs() <= 2.0 ** -7 * alone.float().abs() + (3 * K + 8) * U * f64(X[3:4].abs()).sum() * 6).all())
 
 
 # ------------------------------------------------------------------ graphs, streams, refusals
