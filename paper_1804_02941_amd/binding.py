@@ -783,8 +783,7 @@ def dab_rms_norm(X, gain, residual=None, eps=1e-5, save=False, out=None):
     X or the residual, Y may be X."""
     done = (_native or native()).rms_norm(X, gain, residual, eps, save, out)
     if done is not None:
-        Y, H, rstd, Q, S = done
-        return Y, X if residual is None else H, rstd, None if Q is None else (Q, S)
+        return done
     ptr, dtype, ld = _matrix(X, "X")
     rows, cols = X.shape
     r, _, ldr = _beside(residual, X.shape, (X.dtype,), "residual")

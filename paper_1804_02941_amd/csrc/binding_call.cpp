@@ -658,7 +658,7 @@ bool truth(PyObject* o) {
 }
 // (X, gain, residual, eps, save, out)
 PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return whole_call<6>("dab_rms_norm", n, [&] {
+    PyObject* all = whole_call<6>("dab_rms_norm", n, [&] {
         const Matrix X = here(matrix(a[0])), R = beside(a[2], X.rows, X.cols, X.dtype);
         const std::array shape{int64_t{X.rows}, int64_t{X.cols}};
         const auto* gain = static_cast<const float*>(here(a[1], at::kFloat, std::array{int64_t{X.cols}}));
@@ -684,6 +684,14 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                   static_cast<uint8_t*>(b.out[4]), static_cast<float*>(b.out[2]), st);
         });
     });
+    if (all == nullptr || all == Py_None) return all;
+    // (Y, H or X itself, rstd, (Q, S) or None)
+    const auto of = [&](int i) { return PyTuple_GET_ITEM(all, i); };
+    PyObject* saved = of(3) == Py_None ? Py_None : PyTuple_Pack(2, of(3), of(4));
+    PyObject* four = saved ? PyTuple_Pack(4, of(0), of(1) == Py_None ? a[0] : of(1), of(2), saved) : nullptr;
+    if (saved != Py_None) Py_XDECREF(saved);
+    Py_DECREF(all);
+    return four;
 }
 // (dY, H, gain, rstd, dH, out, ws)
 PyObject* rms_norm_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {

@@ -368,12 +368,15 @@ static int norm_grad_launch(const NormGradArgs<T>& a, NormForm f, hipStream_t st
 // Workgroups of the gradient's kernel: what the chip holds at once, fewer where there are fewer rows.
 static int norm_grad_blocks(int rows, NormForm f) {
     const int64_t n = ceil_div64(rows, norm_rows(f)), most = 1024 / norm_threads(f) * int64_t{kNumCU};
+    if (n <= 2) return 1;
     return static_cast<int>(n < most ? n : most);
 }
 template <typename T>
-static int norm_grad_launch(const NormGradArgs<T>& a, hipStream_t st) {
+static int norm_grad_launch(NormGradArgs<T> a, hipStream_t st) {
     const NormForm f = norm_form(a.g.cols, kNormGradNV);
     int rc;
+    // (the part of a workgroup that has all rows is the gradient)
+    if (a.blocks == 1) a.parts = a.dgain;
     switch (f.log) {
         case 0: rc = launch(norm_grad_long_kernel<T>, dim3(a.blocks), dim3(1024), 0, st, a.dY, a.H, a.gain, a.rstd, a.dH, a.g, a.dX, a.parts); break;
         case 2: rc = norm_grad_launch<T, 2, 1>(a, f, st); break;
@@ -386,7 +389,7 @@ static int norm_grad_launch(const NormGradArgs<T>& a, hipStream_t st) {
         case 9: rc = norm_grad_launch<T, 9, 2>(a, f, st); break;
         default: rc = norm_grad_launch<T, 10, 2>(a, f, st);
     }
-    if (rc) return rc;
+    if (rc || a.blocks == 1) return rc;
     return launch(norm_join_kernel, dim3(ceil_div(a.g.cols, 32)), dim3(1024), 0, st, static_cast<const float*>(a.parts), a.blocks, a.g.cols, a.dgain);
 }
 
@@ -420,7 +423,8 @@ extern "C" size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t co
     using namespace dab;
     if (rows < 1 || cols < 1 || cols > kNormMaxCols) return 0;
     const NormForm f = norm_form(cols, kNormGradNV);
-    return static_cast<size_t>(norm_grad_blocks(rows, f)) * cols * 4;
+    const int blocks = norm_grad_blocks(rows, f);
+    return blocks == 1 ? 0 : static_cast<size_t>(blocks) * cols * 4;
 }
 
 extern "C" int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t ldh, int32_t dtype, const float* gain, const float* rstd,
@@ -434,7 +438,7 @@ extern "C" int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H
         misaligned(dgain, 4))
         return DAB_ERR_ALIGN;
     const size_t need = dab_rms_norm_gradient_workspace_bytes(rows, cols);
-    if (!ws || ws_bytes < need || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    if (need && (!ws || ws_bytes < need || misaligned(ws, 256))) return DAB_ERR_WORKSPACE;
     NormGeom g{};
     g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ldx = lddy, g.ldr = ldh, g.ldd = lddh;
     const int blocks = norm_grad_blocks(rows, norm_form(cols, kNormGradNV));

@@ -19,7 +19,9 @@ HALF = {torch.float32: U, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 # tokens, K, F, adapters, rank: few and many tokens, every width of the rank, sizes that fit nothing
 SIZES = [(1, 1, 1, 1, 1), (1, 40, 24, 3, 4), (3, 100, 130, 2, 16), (17, 64, 129, 5, 3), (33, 301, 70, 4, 8), (64, 129, 257, 7, 20), (65, 128, 128, 1, 16),
-         (70, 33, 1000, 3, 17), (100, 257, 120, 2, 33), (130, 96, 260, 70, 5), (200, 520, 64, 4, 64), (257, 90, 40, 3, 70), (300, 40, 136, 2, 130), (1100, 64, 72, 3, 12)]
+         (70, 33, 1000, 3, 17), (100, 257, 120, 2, 33), (130, 96, 260, 70, 5), (200, 520, 64, 4, 64), (257, 90, 40, 3, 70), (300, 40, 136, 2, 130), (1100, 64, 72, 3, 12),
+         # rows of fewer than eight
+         (100, 5, 40, 2, 3), (150, 40, 7, 3, 20), (90, 3, 2, 2, 4), (500, 8, 9, 2, 6)]
 
 
 def f64(t):
@@ -130,6 +132,25 @@ def test_many_tokens(dtype):
         dX, dA, dB = dab.dab_adapters_gradient(dy, x, Ug, i, a, b, s)
         dXo, dAo, dBo = oa.adapters_gradient(dY, X, Uo, ids, A, B, scale, None)
         assert np.array_equal(f64(dA), dAo) and np.array_equal(f64(dB), dBo) and torch.equal(dX, on_gpu(dXo, dtype)) and not dA[3].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_share_of_more_tokens_than_lds_holds(dtype):
+    """So many columns that the tokens are not shared out: 2500 of them a workgroup."""
+    T, K, F, n, r = 2500, 16, 65600, 2, 3
+    g = torch.Generator(device=DEV).manual_seed(4)
+    X, dY, A, B = (torch.randint(-2, 3, s, generator=g, device=DEV).to(dtype) for s in ((T, K), (T, F), (n, r, K), (n, r, F)))
+    ids = torch.randint(-1, n, (T,), generator=g, device=DEV).int()
+    Y, Ug = dab.dab_adapters(X, ids, A, B)
+    dX, dA, dB = dab.dab_adapters_gradient(dY, X, Ug, ids, A, B)
+    for i in range(n):
+        at = torch.nonzero(ids == i).squeeze(1)
+        x, y, b = X[at].float(), dY[at].float(), B[i].float()
+        u = x @ A[i].float().t()
+        v = (y.double() @ b.double().t()).float()                  # whole numbers below 2^24: exact
+        assert torch.equal(Ug[at], u) and torch.equal(dB[i], u.t().contiguous() @ y) and torch.equal(dA[i].double(), v.double().t().contiguous() @ x.double())
+        assert torch.equal(dX[at], (v @ A[i].float()).to(dtype)) and torch.equal(Y[at], (u @ b).to(dtype))
+    assert not dX[ids < 0].any()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
