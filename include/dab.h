@@ -681,7 +681,8 @@ int dab_state8_save(const float* X, int64_t n, int32_t is_signed, uint8_t* Q, ui
  * not have holds, infinities and NaN among it, does not reach the token.
  *
  *   X       [T][K] of dtype, rows ldx apart;  ids  int32 [T], in any order;  scale  fp32 [n], or NULL for 1
- *   A       [n][r][K], B  [n][r][F] of dtype, contiguous.  r is at most 256, n 65535, T 2^25, K and F 2^24
+ *   A       [n][r][K], B  [n][r][F] of dtype, contiguous.  r is at most 256, n 65535, T 2^25, K and F 2^21,
+ *           the rows' distances (of dY and base too) 2^25
  *   base    [T][F] of dtype or fp32 (base_dtype), rows ldbase apart, or NULL for 0: any projection's output
  *   Y       [T][F] of dtype out.  May be base itself where that is of dtype and its rows are F apart;  U  fp32 [T][r] out: what the gradient takes
  */

@@ -43,20 +43,13 @@ struct Long<f16> {
     static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
 };
 
-// Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth stretch of 128 k, whose loads are in flight
-// at once.
+// Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth stretch of 128 k (RT = 1, 16-bit types), whose
+// loads are in flight at once, those of the next one behind them.  This lane's sums over its wavefront's k: rows 4 (lane / 16) .. + 3 of
+// each sixteen from r0 on, of token lane % 16.
 constexpr int kShrinkWaves = 8;
 template <typename T, int RT>
-__global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && sizeof(T) == 4 ? 2 : 4) void shrink_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a,
-                                                                   int scaled, float* __restrict__ U) {
-    __shared__ float sums[kShrinkWaves][RT][16][17];
-    DAB_RESERVE_VGPRS();
+__device__ __forceinline__ void shrink_tile(const T* __restrict__ x, const T* __restrict__ A, int K, const Adapters& a, int id, int r0, v4f (&out)[RT]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16, t = t0 + m;
-    const int r0 = blockIdx.y * 16 * RT;
-    const T* x = X + (t < a.T ? t : a.T - 1) * ldx;
-    const int id = adapter_of(a, t);
-    v4f out[RT];
 #pragma unroll
     for (int j = 0; j < RT; ++j) out[j] = v4f{0.f, 0.f, 0.f, 0.f};
     bool waiting = id >= 0;
@@ -124,23 +117,39 @@ __global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && sizeof(T) == 4 ? 2 : 
             waiting = false;
         }
     }
+}
+// The wavefronts' sums added up in LDS: put(token, row, sum) for each of the tile's.
+template <int RT, typename Put>
+__device__ __forceinline__ void shrink_join(const v4f (&out)[RT], float (&sums)[kShrinkWaves][RT][16][17], Put put) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int j = 0; j < RT; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) sums[wave][j][m][g * 4 + v] = out[j][v];       // [token][row]
     __syncthreads();
     for (int i = threadIdx.x; i < RT * 256; i += 64 * kShrinkWaves) {
-        const int j = i >> 8, token = (i >> 4) & 15, row = r0 + j * 16 + (i & 15);
-        if (t0 + token >= a.T || row >= a.r) continue;
+        const int j = i >> 8, token = (i >> 4) & 15;
         float u = 0.f;
 #pragma unroll
         for (int w = 0; w < kShrinkWaves; ++w) u += sums[w][j][token][i & 15];
-        if (scaled) {
-            const int who = adapter_of(a, t0 + token);
-            u = who >= 0 ? u * scale_of(a, who) : 0.f;
-        }
-        U[(t0 + token) * a.r + row] = u;
+        put(token, j * 16 + (i & 15), u);
     }
+}
+template <typename T, int RT>
+__global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && sizeof(T) == 4 ? 2 : 4) void shrink_kernel(const T* __restrict__ X, int64_t ldx,
+                                                                                                  const T* __restrict__ A, int K, Adapters a, int scaled,
+                                                                                                  float* __restrict__ U) {
+    __shared__ float sums[kShrinkWaves][RT][16][17];
+    DAB_RESERVE_VGPRS();
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16, t = t0 + (threadIdx.x & 15);
+    const int r0 = blockIdx.y * 16 * RT;
+    v4f out[RT];
+    shrink_tile<T, RT>(X + min(t, static_cast<int64_t>(a.T) - 1) * ldx, A, K, a, adapter_of(a, t), r0, out);
+    shrink_join<RT>(out, sums, [&](int token, int row, float u) {
+        if (t0 + token >= a.T || r0 + row >= a.r) return;
+        const int who = adapter_of(a, t0 + token);
+        U[(t0 + token) * a.r + r0 + row] = who < 0 ? 0.f : scaled ? u * scale_of(a, who) : u;
+    });
 }
 
 // Rows of fewer than eight k: a thread takes a token and a row.
@@ -173,6 +182,12 @@ struct Base {
     int dtype;                       // fp32, or the tokens'
 };
 
+// An element behind a place that all lanes share, by less than 2^32 bytes: the address is that place's scalar registers and 32 bits a lane.
+template <typename T>
+__device__ __forceinline__ T* past(T* shared, uint32_t elements) {
+    typedef std::conditional_t<std::is_const_v<T>, const char, char> Byte;
+    return reinterpret_cast<T*>(reinterpret_cast<Byte*>(shared) + static_cast<uint32_t>(elements * static_cast<uint32_t>(sizeof(T))));
+}
 // Values of N columns, without the first `again` of them.
 template <typename T, int N>
 __device__ __forceinline__ void store_own(T* to, int again, const float (&w)[N]) {
@@ -190,35 +205,25 @@ __device__ __forceinline__ void store_own(T* to, int again, const float (&w)[N])
 
 // Many tokens: a wavefront takes sixteen and 128 columns, lane l the columns 8 (l % 16) .. of tokens 4 (l / 16) .. + 3.  In fp32 on the
 // matrix cores, whatever the type: U is fp32, and the products are few.  All that sixteen of the r rows need is in flight at once, base ahead of it.
-// 8192 x 4096 bf16, r = 16, base added: 34.3 us, 3.9 TB/s.  Measured and left: tiles of 16 x 64 40.6 us, base and U on their way before the ids 39 (registers),
-// several tiles a wavefront with the next one's loads ahead 74 (registers), products in bf16 pieces of U 42 (registers).
-constexpr int kExpandWaves = 4;
-template <typename T, typename TB>
-__global__ __launch_bounds__(64 * kExpandWaves, sizeof(TB) == 4 ? 3 : 4) void expand_kernel(const float* __restrict__ U, const T* __restrict__ B, int F,
-                                                                                        Adapters a, int scaled, const TB* base, int64_t ldbase, T* Y) {
-    DAB_RESERVE_VGPRS();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-    const int64_t t0 = (static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y) * 16;
-    const int64_t f0 = (static_cast<int64_t>(blockIdx.x) * kExpandWaves + wave) * 128;
-    if (f0 >= F || t0 >= a.T) return;
+// id: the adapter of token lane % 16; u_of(row): its U, times its scale.
+template <typename T, typename TB, typename UOf>
+__device__ __forceinline__ void expand_tile(const T* __restrict__ B, int F, const Adapters& a, const TB* base, int64_t ldbase, T* Y, int64_t t0, int64_t f0,
+                                            int id, UOf u_of) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     // (a lane whose eight columns pass the row's end takes the last eight, and stores those that are its own)
-    const int64_t f64 = f0 + m * 8;
-    const int f = static_cast<int>(min(f64, static_cast<int64_t>(F) - 8)), again = static_cast<int>(f64 - f);
-    const int id = adapter_of(a, t0 + m);
-    const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
+    const int f = min(static_cast<int>(f0) + m * 8, F - 8), again = static_cast<int>(f0) + m * 8 - f;
     // one adapter after the other, -1 among them; of sequences' tokens there is one
     bool waiting = true;
     while (__any(waiting)) {
-        const int now = __shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1);
+        const int now = __builtin_amdgcn_readfirstlane(__shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1));
         waiting = waiting && id != now;
         Eight<TB> y[4];
         bool mine[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int64_t t = t0 + 4 * g + v;
-            mine[v] = __shfl(id, 4 * g + v) == now && t < a.T && f64 < F;
+            mine[v] = __shfl(id, 4 * g + v) == now && t0 + 4 * g + v < a.T && again < 8;
             y[v].v = {};
-            if (base && mine[v]) y[v].load_once(base + t * ldbase, f);
+            if (base && mine[v]) y[v].load_once(past(base + t0 * ldbase, (4 * g + v) * static_cast<uint32_t>(ldbase) + f), 0);
         }
         v4f out[8];
 #pragma unroll
@@ -233,8 +238,8 @@ __global__ __launch_bounds__(64 * kExpandWaves, sizeof(TB) == 4 ? 3 : 4) void ex
                     const int row = q0 + 4 * q + g;
                     b[q].v = {}, u[q] = 0.f;
                     if (row < a.r) {
-                        b[q].load(rows + static_cast<int64_t>(row) * F, f);
-                        if (id == now) u[q] = U[(t0 + m) * a.r + row] * s;
+                        b[q].load(past(rows, static_cast<uint32_t>(row) * F + f), 0);
+                        if (id == now) u[q] = u_of(row);
                     }
                 }
 #pragma unroll
@@ -249,9 +254,50 @@ __global__ __launch_bounds__(64 * kExpandWaves, sizeof(TB) == 4 ? 3 : 4) void ex
             float w[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = y[v][j] + out[j][v];
-            store_own(Y + (t0 + 4 * g + v) * F + f, again, w);
+            store_own(past(Y + t0 * F, (4 * g + v) * static_cast<uint32_t>(F) + f), again, w);
         }
     }
+}
+
+// 8192 x 4096 bf16, r = 16, base added: 34.3 us, 3.9 TB/s.  Measured and left: tiles of 16 x 64 40.6 us, base and U on their way before the ids 39 (registers),
+// several tiles a wavefront with the next one's loads ahead 74 (registers), products in bf16 pieces of U 42 (registers).
+constexpr int kExpandWaves = 4;
+template <typename T, typename TB>
+__global__ __launch_bounds__(64 * kExpandWaves, sizeof(TB) == 4 ? 3 : 4) void expand_kernel(const float* __restrict__ U, const T* __restrict__ B, int F,
+                                                                                        Adapters a, int scaled, const TB* base, int64_t ldbase, T* Y) {
+    DAB_RESERVE_VGPRS();
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y) * 16;
+    const int64_t f0 = (static_cast<int64_t>(blockIdx.x) * kExpandWaves + (threadIdx.x >> 6)) * 128;
+    if (f0 >= F || t0 >= a.T) return;
+    const int64_t t = t0 + (threadIdx.x & 15);
+    const int id = adapter_of(a, t);
+    const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
+    expand_tile<T, TB>(B, F, a, base, ldbase, Y, t0, f0, id, [&](int row) { return U[t * a.r + row] * s; });
+}
+
+// Both in one launch, for tiles that fill the chip: a workgroup's eight wavefronts share the tile's k, then its columns, with U in LDS between.  U goes out
+// as well (times the scale where `scaled`, which the columns then are not multiplied by again).
+template <typename T, typename TB, int RT>
+__global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 || sizeof(TB) == 4 ? 2 : 4) void shrink_expand_kernel(
+    const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, const T* __restrict__ B, int F, Adapters a, int scaled, float* __restrict__ U,
+    const TB* base, int64_t ldbase, T* Y) {
+    __shared__ float sums[kShrinkWaves][RT][16][17];
+    __shared__ float kept[16][16 * RT + 1];
+    DAB_RESERVE_VGPRS();
+    const int m = threadIdx.x & 15;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16;
+    const int id = adapter_of(a, t0 + m);
+    v4f out[RT];
+    shrink_tile<T, RT>(X + min(t0 + m, static_cast<int64_t>(a.T) - 1) * ldx, A, K, a, id, 0, out);
+    shrink_join<RT>(out, sums, [&](int token, int row, float u) {
+        const int who = adapter_of(a, t0 + token);
+        const float by = who < 0 ? 0.f : u * scale_of(a, who);
+        kept[token][row] = by;
+        if (t0 + token < a.T && row < a.r) U[(t0 + token) * a.r + row] = scaled ? by : who < 0 ? 0.f : u;
+    });
+    __syncthreads();
+    for (int64_t f0 = static_cast<int64_t>(threadIdx.x >> 6) * 128; f0 < F; f0 += 128 * kShrinkWaves)
+        expand_tile<T, TB>(B, F, a, base, ldbase, Y, t0, f0, id, [&](int row) { return kept[m][row]; });
 }
 
 // Rows of fewer than eight columns: a thread takes a token.
@@ -544,7 +590,8 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const Join j) {
 }
 
 // ---------------------------------------------------------------- host side
-constexpr int kMaxRank = 256;
+constexpr int kMaxRank = 256, kAdapterCols = 1 << 21;         // (a row block of an adapter and sixteen tokens stay below 2^32 bytes)
+constexpr int64_t kAdapterLd = 1 << 25;
 
 template <typename T>
 int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
@@ -582,6 +629,32 @@ static int expand_from(const float* U, const T* B, int F, const Adapters& a, boo
 template <typename T>
 static int expand(const float* U, const T* B, int F, const Adapters& a, bool scaled, const Base& base, T* Y, hipStream_t st) {
     return base.p && base.dtype == DAB_F32 ? expand_from<T, float>(U, B, F, a, scaled, base, Y, st) : expand_from<T, T>(U, B, F, a, scaled, base, Y, st);
+}
+
+// U and Y (or V and dX): one launch where a row of rows is short enough and the tiles fill the chip, or their columns are one round of a workgroup's.
+template <typename T, typename TB, int RT>
+static int shrink_expand_from(const T* X, int64_t ldx, const T* A, int K, const T* B, int F, const Adapters& a, bool scaled, float* U, const Base& base, T* Y,
+                              hipStream_t st) {
+    return launch(shrink_expand_kernel<T, TB, RT>, dim3(static_cast<unsigned>(ceil_div64(a.T, 16))), dim3(64 * kShrinkWaves), 0, st, X, ldx, A, K, B, F, a,
+                  static_cast<int>(scaled), U, static_cast<const TB*>(base.p), base.ld, Y);
+}
+template <typename T>
+static int shrink_expand(const T* X, int64_t ldx, const T* A, int K, const T* B, int F, const Adapters& a, bool scaled, float* U, const Base& base, T* Y,
+                         hipStream_t st) {
+    const int64_t tiles = ceil_div64(a.T, 16);
+    if (a.T > kFewTokens && a.r <= 64 && K >= kNarrow && F >= kNarrow && (tiles >= kNumCU || F <= 128 * kShrinkWaves)) {
+        const bool wide = base.p && base.dtype == DAB_F32 && sizeof(T) == 2;
+        if (wide) {
+            if (a.r <= 16) return shrink_expand_from<T, float, 1>(X, ldx, A, K, B, F, a, scaled, U, base, Y, st);
+            if (a.r <= 32) return shrink_expand_from<T, float, 2>(X, ldx, A, K, B, F, a, scaled, U, base, Y, st);
+            return shrink_expand_from<T, float, 4>(X, ldx, A, K, B, F, a, scaled, U, base, Y, st);
+        }
+        if (a.r <= 16) return shrink_expand_from<T, T, 1>(X, ldx, A, K, B, F, a, scaled, U, base, Y, st);
+        if (a.r <= 32) return shrink_expand_from<T, T, 2>(X, ldx, A, K, B, F, a, scaled, U, base, Y, st);
+        return shrink_expand_from<T, T, 4>(X, ldx, A, K, B, F, a, scaled, U, base, Y, st);
+    }
+    if (int rc = shrink(X, ldx, A, K, a, scaled, U, st)) return rc;
+    return expand(static_cast<const float*>(U), B, F, a, !scaled, base, Y, st);
 }
 
 struct OuterPlan {
@@ -647,14 +720,15 @@ int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids
                    int32_t F, int32_t n, int32_t r) {
     if (!X || !ids || !A || !B) return DAB_ERR_NULL;
     if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || ldx < K) return DAB_ERR_SHAPE;
-    if (!real_dtype(dtype) || K > (1 << 24) || F > (1 << 24) || n > 65535 || r > kMaxRank || T > (1 << 25)) return DAB_ERR_UNSUPPORTED;
+    if (!real_dtype(dtype) || K > kAdapterCols || F > kAdapterCols || n > 65535 || r > kMaxRank || T > (1 << 25) || ldx > kAdapterLd)
+        return DAB_ERR_UNSUPPORTED;
     if (misaligned(X, 16) || misaligned(A, 16) || misaligned(B, 16) || misaligned(ids, 4) || misaligned(scale, 4)) return DAB_ERR_ALIGN;
     return DAB_OK;
 }
 static int check_base(const void* base, int32_t dtype, int64_t ld, int32_t cols, int32_t own_dtype) {
     if (!base) return DAB_OK;
     if (ld < cols) return DAB_ERR_SHAPE;
-    if (dtype != DAB_F32 && dtype != own_dtype) return DAB_ERR_UNSUPPORTED;
+    if ((dtype != DAB_F32 && dtype != own_dtype) || ld > kAdapterLd) return DAB_ERR_UNSUPPORTED;
     return misaligned(base, 16) ? DAB_ERR_ALIGN : DAB_OK;
 }
 
@@ -672,8 +746,8 @@ extern "C" int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int
     const auto st = static_cast<hipStream_t>(stream);
     const auto go = [&](auto* t) -> int {
         typedef std::remove_pointer_t<decltype(t)> E;
-        if (int rc = shrink(static_cast<const E*>(X), ldx, static_cast<const E*>(A), K, a, false, U, st)) return rc;
-        return expand(static_cast<const float*>(U), static_cast<const E*>(B), F, a, true, Base{base, ldbase, base_dtype}, static_cast<E*>(Y), st);
+        return shrink_expand(static_cast<const E*>(X), ldx, static_cast<const E*>(A), K, static_cast<const E*>(B), F, a, false, U,
+                             Base{base, ldbase, base_dtype}, static_cast<E*>(Y), st);
     };
     if (dtype == DAB_F32) return go(static_cast<float*>(nullptr));
     if (dtype == DAB_BF16) return go(static_cast<bf16*>(nullptr));
@@ -682,7 +756,7 @@ extern "C" int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int
 
 extern "C" size_t dab_adapters_gradient_workspace_bytes(int32_t T, int32_t K, int32_t F, int32_t n, int32_t r) {
     using namespace dab;
-    if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || K > (1 << 24) || F > (1 << 24) || n > 65535 || r > kMaxRank || T > (1 << 25)) return 0;
+    if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || K > kAdapterCols || F > kAdapterCols || n > 65535 || r > kMaxRank || T > (1 << 25)) return 0;
     return static_cast<size_t>(round_up(static_cast<int64_t>(T) * r * 4, 256)) + outer_bytes(T, n, r, F, K);
 }
 
@@ -694,6 +768,7 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
     if (int rc = check_adapters(X, dtype, ldx, ids, A, B, scale, T, K, F, n, r)) return rc;
     if (!dY || !U || !dA || !dB || (base && !dX)) return DAB_ERR_NULL;
     if (lddy < F) return DAB_ERR_SHAPE;
+    if (lddy > kAdapterLd) return DAB_ERR_UNSUPPORTED;
     if (int rc = check_base(base, base_dtype, ldbase, K, dtype)) return rc;
     if (misaligned(dY, 16) || misaligned(dX, 16) || misaligned(U, 4) || misaligned(dA, 4) || misaligned(dB, 4)) return DAB_ERR_ALIGN;
     const size_t need = dab_adapters_gradient_workspace_bytes(T, K, F, n, r);
@@ -705,10 +780,10 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
     const auto go = [&](auto* t) -> int {
         typedef std::remove_pointer_t<decltype(t)> E;
         const E *x = static_cast<const E*>(X), *dy = static_cast<const E*>(dY), *up = static_cast<const E*>(B), *down = static_cast<const E*>(A);
-        if (int rc = shrink(dy, lddy, up, F, a, true, V, st)) return rc;
-        if (int rc = outer<E>({{U, dy, lddy, F, 1, dB}, {V, x, ldx, K, 0, dA}}, a, rest, st)) return rc;
-        if (!dX) return DAB_OK;
-        return expand(static_cast<const float*>(V), down, K, a, false, Base{base, ldbase, base_dtype}, static_cast<E*>(dX), st);
+        if (int rc = dX ? shrink_expand(dy, lddy, up, F, down, K, a, true, V, Base{base, ldbase, base_dtype}, static_cast<E*>(dX), st)
+                        : shrink(dy, lddy, up, F, a, true, V, st))
+            return rc;
+        return outer<E>({{U, dy, lddy, F, 1, dB}, {V, x, ldx, K, 0, dA}}, a, rest, st);
     };
     if (dtype == DAB_F32) return go(static_cast<float*>(nullptr));
     if (dtype == DAB_BF16) return go(static_cast<bf16*>(nullptr));
