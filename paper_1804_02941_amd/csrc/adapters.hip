@@ -343,8 +343,8 @@ __global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict_
 }
 
 // ---------------------------------------------------------------- outer
-// Both gradients of the adapters in one launch: a workgroup takes 128 columns of one, 16 RT of the r rows, a share of the tokens and every slices-th
-// adapter; of each adapter that has tokens in its share its wavefronts take every eighth four of them (bf16: 32) and add up in LDS.  With one share that is the gradient; else it goes to parts: [share][adapter][r][columns], and have: [share][adapter] is 1 where
+// Both gradients of the adapters in one launch: a workgroup takes 128 columns of one, sixteen of the r rows, a share of the tokens and every slices-th
+// adapter; of each adapter that has tokens in its share they are listed, dealt out to the wavefronts and the sums added up in LDS.  With one share that is the gradient; else it goes to parts: [share][adapter][r][columns], and have: [share][adapter] is 1 where
 // the share has tokens of the adapter (other parts are not written).
 constexpr int kOuterWaves = 8, kOuterIds = 2048;
 template <typename T>
@@ -373,17 +373,19 @@ __device__ __forceinline__ void columns(const v4u32 (&x)[8], int d, v8bf* even, 
     *even = __builtin_bit_cast(v8bf, p), *odd = __builtin_bit_cast(v8bf, q);
 }
 
-template <typename T, int RT>
+template <typename T>
 __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters a, const Outer<T> o) {
     extern __shared__ uint32_t present[];                    // a bit for every adapter
     __shared__ float sums[kOuterWaves][8][132];
     __shared__ int ids[kOuterIds];
+    __shared__ __attribute__((aligned(16))) uint16_t list[kOuterIds];
+    __shared__ int counts[kOuterWaves];
     DAB_RESERVE_VGPRS();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
     const int rb = blockIdx.x / o.tiles, tile2 = blockIdx.x - rb * o.tiles;
     const bool second = tile2 >= o.tiles0;
     const OuterSide<T> side = o.side[second];
-    const int tile = second ? tile2 - o.tiles0 : tile2, share = blockIdx.y, slice = blockIdx.z, r0 = rb * 16 * RT, cols = side.cols;
+    const int tile = second ? tile2 - o.tiles0 : tile2, share = blockIdx.y, slice = blockIdx.z, r0 = rb * 16, cols = side.cols;
     const int64_t first = static_cast<int64_t>(share) * o.tokens;
     const int count = static_cast<int>(min(static_cast<int64_t>(o.tokens), a.T - first));
     const int words = (a.n + 31) >> 5;
@@ -407,116 +409,116 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters 
         const bool none = !((present[id >> 5] >> (id & 31)) & 1u);          // (the same for the whole workgroup)
         if (none && o.shares > 1) continue;
         const float s = side.scaled && !none ? scale_of(a, id) : 1.f;       // (zeros stay zeros)
-        v4f acc[RT][8];
+        v4f acc[8];
 #pragma unroll
-        for (int j = 0; j < RT; ++j)
+        for (int i = 0; i < 8; ++i) acc[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int w0 = none ? count : 0; w0 < count; w0 += kOuterIds) {
+            // the adapter's tokens among the next ones, in their order
+            uint64_t hits[kOuterIds / 64 / kOuterWaves];
+            int found = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
-        if constexpr (std::is_same_v<T, bf16>) {
-            // 32 tokens a step, eight of them a lane: V as the sum of three bf16 numbers, eight rows of eight columns transposed in the lane's registers
-            for (int t1 = none ? count : wave * 32; t1 < count; t1 += kOuterWaves * 32) {
-                bool mine[8], any = false;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int t = t1 + 8 * g + e;
-                    mine[e] = t < count && (kept ? ids[t] : a.ids[first + t]) == id;
-                    any = any || mine[e];
-                }
-                if (!__any(any)) continue;
-                v4u32 x[8];
-                float v[RT][8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t t = t1 + 8 * g + e;
-                    Eight<bf16> w;
-                    w.v = {};
-#pragma unroll
-                    for (int j = 0; j < RT; ++j) v[j][e] = 0.f;
-                    if (mine[e]) {
-                        w.load(x0 + t * side.ldx, c);
-#pragma unroll
-                        for (int j = 0; j < RT; ++j)
-                            if (r0 + j * 16 + m < a.r) v[j][e] = v0[t * a.r + r0 + j * 16 + m];
-                    }
-                    x[e] = __builtin_bit_cast(v4u32, w.v);
-                }
-                v8bf p[RT][3];
-#pragma unroll
-                for (int j = 0; j < RT; ++j)
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p[j][k][e] = piece_of(v[j][e], k);
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    v8bf even, odd;
-                    columns(x, d, &even, &odd);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-#pragma unroll
-                        for (int j = 0; j < RT; ++j) {
-                            acc[j][2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[j][k], even, acc[j][2 * d], 0, 0, 0);
-                            acc[j][2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[j][k], odd, acc[j][2 * d + 1], 0, 0, 0);
-                        }
-                }
+            for (int k = 0; k < kOuterIds / 64 / kOuterWaves; ++k) {
+                const int t = w0 + (wave * (kOuterIds / 64 / kOuterWaves) + k) * 64 + lane;
+                hits[k] = __ballot(t < count && (kept ? ids[t] : a.ids[first + t]) == id);
+                found += __popcll(hits[k]);
             }
-        } else {
-            constexpr int kAhead = RT == 4 ? 2 : 4;
-            for (int t1 = none ? count : wave * 4; t1 < count; t1 += kOuterWaves * 4 * kAhead) {
-                bool mine[kAhead], some[kAhead], any = false;
+            if (lane == 0) counts[wave] = found;
+            __syncthreads();
+            int before = 0, c_tokens = 0;
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int t = t1 + u * kOuterWaves * 4 + g;
-                    mine[u] = t < count && (kept ? ids[t] : a.ids[first + t]) == id;
-                    some[u] = __any(mine[u]);
-                    any = any || some[u];
-                }
-                if (!any) continue;
-                Eight<T> x[kAhead];
-                float v[kAhead][RT];
+            for (int k = 0; k < kOuterWaves; ++k) {
+                if (k == wave) before = c_tokens;
+                c_tokens += counts[k];
+            }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int64_t t = t1 + u * kOuterWaves * 4 + g;
-                    x[u].v = {};
+            for (int k = 0; k < kOuterIds / 64 / kOuterWaves; ++k) {
+                if ((hits[k] >> lane) & 1)
+                    list[before + __popcll(hits[k] & ((uint64_t{1} << lane) - 1))] =
+                        static_cast<uint16_t>((wave * (kOuterIds / 64 / kOuterWaves) + k) * 64 + lane);
+                before += __popcll(hits[k]);
+            }
+            __syncthreads();
+            if constexpr (std::is_same_v<T, bf16>) {
+                // 32 tokens a step and wavefront, eight of them a lane: V as the sum of three bf16 numbers, eight rows of eight columns transposed in
+                // the lane's registers
+                for (int i0 = 0; i0 < c_tokens; i0 += 32 * kOuterWaves) {
+                    const int p0 = i0 + (g * kOuterWaves + wave) * 8;
+                    if (!__any(p0 < c_tokens)) continue;
+                    const v4u32 eight = *reinterpret_cast<const v4u32*>(&list[min(p0, kOuterIds - 8)]);
+                    v4u32 x[8];
+                    float v[8];
 #pragma unroll
-                    for (int j = 0; j < RT; ++j) v[u][j] = 0.f;
-                    if (mine[u]) {
-                        x[u].load(x0 + t * side.ldx, c);
+                    for (int e = 0; e < 8; ++e) {
+                        const int64_t t = w0 + ((eight[e / 2] >> (16 * (e & 1))) & 0xffffu);
+                        Eight<bf16> w;
+                        w.v = {}, v[e] = 0.f;
+                        if (p0 + e < c_tokens) {
+                            w.load(x0 + t * side.ldx, c);
+                            if (r0 + m < a.r) v[e] = v0[t * a.r + r0 + m];
+                        }
+                        x[e] = __builtin_bit_cast(v4u32, w.v);
+                    }
+                    v8bf p[3];
 #pragma unroll
-                        for (int j = 0; j < RT; ++j)
-                            if (r0 + j * 16 + m < a.r) v[u][j] = v0[t * a.r + r0 + j * 16 + m];
+                    for (int k = 0; k < 3; ++k)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[k][e] = piece_of(v[e], k);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        v8bf even, odd;
+                        columns(x, d, &even, &odd);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) {
+                            acc[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[k], even, acc[2 * d], 0, 0, 0);
+                            acc[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[k], odd, acc[2 * d + 1], 0, 0, 0);
+                        }
                     }
                 }
+            } else {
+                // four tokens a step and wavefront, one a lane, several steps in flight
+                constexpr int kAhead = 4;
+                for (int i0 = 0; i0 < c_tokens; i0 += 4 * kOuterWaves * kAhead) {
+                    Eight<T> x[kAhead];
+                    float v[kAhead];
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u)
-                    if (some[u])
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int p0 = i0 + (u * kOuterWaves + wave) * 4 + g;
+                        x[u].v = {}, v[u] = 0.f;
+                        if (p0 < c_tokens) {
+                            const int64_t t = w0 + list[p0];
+                            x[u].load(x0 + t * side.ldx, c);
+                            if (r0 + m < a.r) v[u] = v0[t * a.r + r0 + m];
+                        }
+                    }
 #pragma unroll
-                        for (int j = 0; j < RT; ++j)
+                    for (int u = 0; u < kAhead; ++u)
+                        if (i0 + (u * kOuterWaves + wave) * 4 < c_tokens)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u][j], x[u][i], acc[j][i], 0, 0, 0);
+                            for (int i = 0; i < 8; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[u], x[u][i], acc[i], 0, 0, 0);
+                }
             }
         }
         // rows 4 g + v of 16, columns 8 m + i of 128: every wavefront's into LDS, then a thread adds up four columns
         float* out = side.out + (static_cast<int64_t>(o.shares > 1 ? share : 0) * a.n + id) * a.r * cols;
 #pragma unroll
-        for (int j = 0; j < 2 * RT; ++j) {                   // (eight of the rows at a time: those of v = 0 and 1, then of 2 and 3)
+        for (int j = 0; j < 2; ++j) {                        // (eight of the rows at a time: those of v = 0 and 1, then of 2 and 3)
             if (!none)
 #pragma unroll
                 for (int i = 0; i < 8; i += 4)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int v = 2 * (j & 1) + h;
+                        const int v = 2 * j + h;
                         if (again == 0) {
                             *reinterpret_cast<v4f*>(&sums[wave][2 * g + h][m * 8 + i]) =
-                                v4f{acc[j / 2][i][v], acc[j / 2][i + 1][v], acc[j / 2][i + 2][v], acc[j / 2][i + 3][v]};
+                                v4f{acc[i][v], acc[i + 1][v], acc[i + 2][v], acc[i + 3][v]};
                         } else if (again < 8) {
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
-                                if (i + k >= again) sums[wave][2 * g + h][m * 8 + i + k - again] = acc[j / 2][i + k][v];
+                                if (i + k >= again) sums[wave][2 * g + h][m * 8 + i + k - again] = acc[i + k][v];
                         }
                     }
             __syncthreads();
-            const int at = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4, row = r0 + (j / 2) * 16 + 4 * (at >> 1) + 2 * (j & 1) + (at & 1);
+            const int at = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4, row = r0 + 4 * (at >> 1) + 2 * j + (at & 1);
             if (at < 8 && row < a.r) {
                 v4f w = v4f{0.f, 0.f, 0.f, 0.f};
                 if (!none)
@@ -658,14 +660,13 @@ static int shrink_expand(const T* X, int64_t ldx, const T* A, int K, const T* B,
 }
 
 struct OuterPlan {
-    int shares, tokens, slices, rt, tiles0, tiles, row_blocks;
+    int shares, tokens, slices, tiles0, tiles, row_blocks;
     size_t parts0, parts1, have;     // bytes, multiples of 256
     size_t bytes() const { return parts0 + parts1 + have; }
 };
 static OuterPlan outer_plan(int T, int n, int r, int cols0, int cols1) {
     OuterPlan p{};
-    p.rt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
-    p.row_blocks = ceil_div(r, 16 * p.rt), p.tiles0 = ceil_div(cols0, 128), p.tiles = p.tiles0 + ceil_div(cols1, 128);
+    p.row_blocks = ceil_div(r, 16), p.tiles0 = ceil_div(cols0, 128), p.tiles = p.tiles0 + ceil_div(cols1, 128);
     const int64_t blocks = static_cast<int64_t>(p.tiles) * p.row_blocks, row = static_cast<int64_t>(n) * r * 4;
     // about two workgroups for every compute unit, shares of at least 128 tokens, parts of at most 256 MB
     int64_t shares = ceil_div64(2 * kNumCU, blocks);
@@ -700,10 +701,7 @@ static int outer(const OuterSide<T> (&sides)[2], const Adapters& a, char* ws, hi
     o.side[0] = wide[0], o.side[1] = wide[1], o.tiles0 = p.tiles0, o.tiles = p.tiles, o.tokens = p.tokens, o.shares = p.shares, o.slices = p.slices;
     const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.tiles) * p.row_blocks), p.shares, p.slices), block(64 * kOuterWaves);
     const size_t lds = static_cast<size_t>(ceil_div(a.n, 32)) * 4;
-    int rc;
-    if (p.rt == 1) rc = launch(outer_kernel<T, 1>, grid, block, lds, st, a, o);
-    else if (p.rt == 2) rc = launch(outer_kernel<T, 2>, grid, block, lds, st, a, o);
-    else rc = launch(outer_kernel<T, 4>, grid, block, lds, st, a, o);
+    const int rc = launch(outer_kernel<T>, grid, block, lds, st, a, o);
     if (rc || p.shares == 1) return rc;
     j.parts[0] = wide[0].out, j.parts[1] = wide[1].out, j.have = o.have, j.shares = p.shares, j.n = a.n;
     j.size[0] = static_cast<int64_t>(a.r) * wide[0].cols, j.size[1] = static_cast<int64_t>(a.r) * wide[1].cols;
