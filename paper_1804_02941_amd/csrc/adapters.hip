@@ -275,14 +275,101 @@ __global__ __launch_bounds__(64 * kExpandWaves, sizeof(TB) == 4 ? 3 : 4) void ex
     expand_tile<T, TB>(B, F, a, base, ldbase, Y, t0, f0, id, [&](int row) { return U[t * a.r + row] * s; });
 }
 
+// Columns 2 d and 2 d + 1 of eight rows' eight columns, as the matrix cores take the rows: eight numbers of a column a lane.
+__device__ __forceinline__ void columns(const v4u32 (&x)[8], int d, v8bf* even, v8bf* odd) {
+    v4u32 p, q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p[i] = __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], 0x05040100u);
+        q[i] = __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], 0x07060302u);
+    }
+    *even = __builtin_bit_cast(v8bf, p), *odd = __builtin_bit_cast(v8bf, q);
+}
+
+// The same tile on the bf16 matrix instruction, with U as three bf16 numbers in LDS, [piece][token][row], whose sum it is, so that products stay exact.  Of
+// the 32 numbers that an instruction adds up the first sixteen are one piece times sixteen rows, the others another piece times the
+// same rows; eight rows of eight columns are transposed in a lane's registers.
+template <int RT>
+struct Pieces {
+    static constexpr int kRow = 16 * RT + 8;
+    __attribute__((aligned(16))) bf16 v[3][16][kRow];
+};
+template <typename TB, int RT>
+__device__ __forceinline__ void expand_tile16(const bf16* __restrict__ B, int F, const Adapters& a, const TB* base, int64_t ldbase, bf16* Y, int64_t t0,
+                                              int64_t f0, int id, const Pieces<RT>& u) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int f = min(static_cast<int>(f0) + m * 8, F - 8), again = static_cast<int>(f0) + m * 8 - f;
+    bool waiting = true;
+    while (__any(waiting)) {
+        // (offsets are made anew where they are used: kept over the columns they take the registers of the loads)
+        uint32_t step_base = static_cast<uint32_t>(ldbase), step_y = F;
+        asm volatile("" : "+s"(step_base), "+s"(step_y));
+        const int now = __builtin_amdgcn_readfirstlane(__shfl(id, __ffsll(static_cast<unsigned long long>(__ballot(waiting))) - 1));
+        waiting = waiting && id != now;
+        Eight<TB> y[4];
+        bool mine[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            mine[v] = __shfl(id, 4 * g + v) == now && t0 + 4 * g + v < a.T && again < 8;
+            y[v].v = {};
+            if (base && mine[v]) y[v].load_once(past(base + t0 * ldbase, (4 * g + v) * step_base + f), 0);
+        }
+        v4f out[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[j] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (now >= 0) {
+            const bf16* rows = B + static_cast<int64_t>(now) * a.r * F;
+            for (int q0 = 0; q0 < a.r; q0 += 16) {
+                const int row0 = q0 + 8 * (g & 1);
+                uint32_t step = F;
+                asm volatile("" : "+s"(step));
+                v4u32 b[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    b[e] = v4u32{0, 0, 0, 0};
+                    if (row0 + e < a.r) {
+                        Eight<bf16> w;
+                        w.load(past(rows, static_cast<uint32_t>(row0 + e) * step + f), 0);
+                        b[e] = __builtin_bit_cast(v4u32, w.v);
+                    }
+                }
+                v8bf p = *reinterpret_cast<const v8bf*>(&u.v[g < 2 ? 0 : 1][m][row0]), q = *reinterpret_cast<const v8bf*>(&u.v[2][m][row0]);
+                if (id != now) p = v8bf{}, q = v8bf{};
+                if (g >= 2) q = v8bf{};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    v8bf even, odd;
+                    columns(b, d, &even, &odd);
+                    out[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, even, out[2 * d], 0, 0, 0);
+                    out[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, odd, out[2 * d + 1], 0, 0, 0);
+                    out[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, even, out[2 * d], 0, 0, 0);
+                    out[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, odd, out[2 * d + 1], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (!mine[v]) continue;
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = y[v][j] + out[j][v];
+            store_own(past(Y + t0 * F, (4 * g + v) * step_y + f), again, w);
+        }
+    }
+}
+
 // Both in one launch, for tiles that fill the chip: a workgroup's eight wavefronts share the tile's k, then its columns, with U in LDS between.  U goes out
 // as well (times the scale where `scaled`, which the columns then are not multiplied by again).
 template <typename T, typename TB, int RT>
-__global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 || sizeof(TB) == 4 ? 2 : 4) void shrink_expand_kernel(
+__global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 ? 2 : 4) void shrink_expand_kernel(
     const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, const T* __restrict__ B, int F, Adapters a, int scaled, float* __restrict__ U,
     const TB* base, int64_t ldbase, T* Y) {
+    constexpr bool k16 = std::is_same_v<T, bf16> && sizeof(TB) == 2;          // (with an fp32 base its registers are not left)
+    struct Floats {
+        float v[16][16 * RT + 1];
+    };
     __shared__ float sums[kShrinkWaves][RT][16][17];
-    __shared__ float kept[16][16 * RT + 1];
+    __shared__ std::conditional_t<k16, Pieces<RT>, Floats> kept;
     DAB_RESERVE_VGPRS();
     const int m = threadIdx.x & 15;
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16;
@@ -292,12 +379,19 @@ __global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 || sizeof(TB) == 
     shrink_join<RT>(out, sums, [&](int token, int row, float u) {
         const int who = adapter_of(a, t0 + token);
         const float by = who < 0 ? 0.f : u * scale_of(a, who);
-        kept[token][row] = by;
+        if constexpr (k16) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) kept.v[p][token][row] = piece_of(row < a.r ? by : 0.f, p);
+        } else {
+            kept.v[token][row] = by;
+        }
         if (t0 + token < a.T && row < a.r) U[(t0 + token) * a.r + row] = scaled ? by : who < 0 ? 0.f : u;
     });
     __syncthreads();
-    for (int64_t f0 = static_cast<int64_t>(threadIdx.x >> 6) * 128; f0 < F; f0 += 128 * kShrinkWaves)
-        expand_tile<T, TB>(B, F, a, base, ldbase, Y, t0, f0, id, [&](int row) { return kept[m][row]; });
+    for (int64_t f0 = static_cast<int64_t>(threadIdx.x >> 6) * 128; f0 < F; f0 += 128 * kShrinkWaves) {
+        if constexpr (k16) expand_tile16<TB, RT>(B, F, a, base, ldbase, Y, t0, f0, id, kept);
+        else expand_tile<T, TB>(B, F, a, base, ldbase, Y, t0, f0, id, [&](int row) { return kept.v[m][row]; });
+    }
 }
 
 // Rows of fewer than eight columns: a thread takes a token.
@@ -362,17 +456,6 @@ struct Outer {
     int tokens, shares, slices;      // tokens of a share (a multiple of 32); slices of the adapters
     int32_t* have;
 };
-// Columns 2 d and 2 d + 1 of eight rows' eight columns, as the matrix cores take the rows: eight numbers of a column a lane.
-__device__ __forceinline__ void columns(const v4u32 (&x)[8], int d, v8bf* even, v8bf* odd) {
-    v4u32 p, q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        p[i] = __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], 0x05040100u);
-        q[i] = __builtin_amdgcn_perm(x[2 * i + 1][d], x[2 * i][d], 0x07060302u);
-    }
-    *even = __builtin_bit_cast(v8bf, p), *odd = __builtin_bit_cast(v8bf, q);
-}
-
 template <typename T>
 __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const Adapters a, const Outer<T> o) {
     extern __shared__ uint32_t present[];                    // a bit for every adapter
