@@ -153,6 +153,21 @@ def test_a_share_of_more_tokens_than_lds_holds(dtype):
     assert not dX[ids < 0].any()
 
 
+def test_more_tiles_of_tokens_than_a_grid_has_along_one_dimension():
+    T, K, F, n, r = 600001, 16, 8, 2, 65                           # (a rank of two row blocks: U and Y in launches of their own)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    X, A, B = (torch.randint(-2, 3, s, generator=g, device=DEV).bfloat16() for s in ((T, K), (n, r, K), (n, r, F)))
+    ids = torch.randint(-1, n, (T // 37 + 1,), generator=g, device=DEV).repeat_interleave(37)[:T].int()
+    base = torch.randint(-9, 10, (T, F), generator=g, device=DEV).bfloat16()
+    Y, Ug = dab.dab_adapters(X, ids, A, B, base=base)
+    for i in range(n):
+        at = torch.nonzero(ids == i).squeeze(1)
+        u = X[at].float() @ A[i].float().t()
+        assert torch.equal(Ug[at], u) and torch.equal(Y[at], (base[at].float() + u @ B[i].float()).bfloat16())
+    none = ids < 0
+    assert torch.equal(Y[none], base[none]) and not Ug[none].any()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T", [5, 100])
 def test_infinities_stay_with_their_tokens(dtype, T):
