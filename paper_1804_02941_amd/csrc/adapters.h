@@ -79,12 +79,15 @@ __device__ __forceinline__ void shrink_few(const T* __restrict__ X, int64_t ldx,
     U[at] = scaled ? sum * scale_of(a, id) : sum;
 }
 
-// U of any number of tokens (adapters.hip).
-template <typename T>
-int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st);
-
-// What all calls with adapters refuse alike.
-int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
-                   int32_t F, int32_t n, int32_t r);
+// The adapters of the tokens behind a 4-bit product (w4.hip).
+struct W4Adapters {
+    Adapters a;
+    float* U;                        // times the adapters' scales
+    const void *A, *B;
+};
+// The product alone (w null), or with the tokens' adapters behind it.  Of up to kFewTokens tokens it makes U itself, in the launch that lays
+// the tokens out; of more U is there already.
+int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y, void* ws,
+               size_t ws_bytes, hipStream_t st, const W4Adapters* w = nullptr);
 
 }  // namespace dab

@@ -679,7 +679,7 @@ constexpr int kMaxRank = 256, kAdapterCols = 1 << 21;         // (a row block of
 constexpr int64_t kAdapterLd = 1 << 25;
 
 template <typename T>
-int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
+static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
     if (a.T <= kFewTokens)
         return launch(shrink_few_kernel<T>, dim3(a.T * a.r), dim3(64 * kFewWaves), 0, st, X, ldx, A, K, a, static_cast<int>(scaled), U);
     const unsigned tiles = static_cast<unsigned>(ceil_div64(a.T, 16));
@@ -693,9 +693,6 @@ int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool s
     return launch(shrink_kernel<T, 4>, dim3(tiles, ceil_div(a.r, 64)), block, 0, st, X, ldx, A, K, a, s, U);
 }
 
-template int shrink(const float*, int64_t, const float*, int, const Adapters&, bool, float*, hipStream_t);
-template int shrink(const bf16*, int64_t, const bf16*, int, const Adapters&, bool, float*, hipStream_t);
-template int shrink(const f16*, int64_t, const f16*, int, const Adapters&, bool, float*, hipStream_t);
 
 template <typename T, typename TB>
 static int expand_from(const float* U, const T* B, int F, const Adapters& a, bool scaled, const Base& base, T* Y, hipStream_t st) {
@@ -797,7 +794,7 @@ static size_t outer_bytes(int T, int n, int r, int F, int K) {
     return F < kNarrow ? outer_plan(T, n, r, K, 0).bytes() : outer_plan(T, n, r, F, K < kNarrow ? 0 : K).bytes();
 }
 
-int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
+static int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
                    int32_t F, int32_t n, int32_t r) {
     if (!X || !ids || !A || !B) return DAB_ERR_NULL;
     if (T < 1 || K < 1 || F < 1 || n < 1 || r < 1 || ldx < K) return DAB_ERR_SHAPE;
@@ -869,4 +866,36 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
     if (dtype == DAB_F32) return go(static_cast<float*>(nullptr));
     if (dtype == DAB_BF16) return go(static_cast<bf16*>(nullptr));
     return go(static_cast<f16*>(nullptr));
+}
+
+// Workspace of the product with adapters: the product's own, then U.
+static size_t w4_own_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
+    return static_cast<size_t>(dab::round_up(static_cast<int64_t>(dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx)), 256));
+}
+extern "C" size_t dab_w4_adapters_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t r, int32_t dtype, int64_t ldx) {
+    if (B < 1 || K < 1 || F < 1 || r < 1 || !dab::real_dtype(dtype)) return 0;
+    return w4_own_bytes(B, K, F, dtype, ldx) + static_cast<size_t>(dab::round_up(static_cast<int64_t>(B) * r * 4, 256));
+}
+
+extern "C" int dab_w4_adapters(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, const int32_t* ids, const void* A,
+                               const void* Bt, const float* scale, int32_t B, int32_t K, int32_t F, int32_t n, int32_t r, void* Y, void* ws,
+                               size_t ws_bytes, void* stream) {
+    using namespace dab;
+    if (int rc = check_adapters(X, dtype, ldx, ids, A, Bt, scale, B, K, F, n, r)) return rc;
+    if (!Q || !S || !Y) return DAB_ERR_NULL;
+    if (B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
+    if (misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
+    if (!ws || ws_bytes < dab_w4_adapters_workspace_bytes(B, K, F, r, dtype, ldx) || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    const size_t product = w4_own_bytes(B, K, F, dtype, ldx);
+    float* U = reinterpret_cast<float*>(static_cast<char*>(ws) + product);
+    const W4Adapters w{Adapters{ids, scale, B, n, r}, U, A, Bt};
+    const auto st = static_cast<hipStream_t>(stream);
+    if (B > kFewTokens) {
+        int rc;
+        if (dtype == DAB_F32) rc = shrink(static_cast<const float*>(X), ldx, static_cast<const float*>(A), K, w.a, true, U, st);
+        else if (dtype == DAB_BF16) rc = shrink(static_cast<const bf16*>(X), ldx, static_cast<const bf16*>(A), K, w.a, true, U, st);
+        else rc = shrink(static_cast<const f16*>(X), ldx, static_cast<const f16*>(A), K, w.a, true, U, st);
+        if (rc) return rc;
+    }
+    return w4_product(X, dtype, ldx, Q, S, B, K, F, Y, ws, product, st, &w);
 }

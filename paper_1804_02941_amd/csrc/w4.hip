@@ -170,8 +170,9 @@ __device__ __forceinline__ void w4_tokens(const T* __restrict__ X, const W4Token
     *reinterpret_cast<v8bf*>(out + ((static_cast<int64_t>(pass) * g.Kt * 4 * g.tiles + frag) * 64 + lane) * 8) = o;
 }
 template <typename T>
-__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, W4Tokens g, bf16* __restrict__ out) {
-    w4_tokens(X, g, blockIdx.x, blockIdx.y, out);
+__global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X, int B, int K, int64_t ldx, int Kt, int nb, int P,
+                                                        int tiles, bf16* __restrict__ out) {
+    w4_tokens(X, W4Tokens{B, K, ldx, Kt, nb, P, tiles}, blockIdx.x, blockIdx.y, out);
 }
 // The same beside U of the few tokens' adapters (shrink_few), in workgroups behind the layout's.
 template <typename T>
@@ -223,12 +224,6 @@ struct Step4 {
     }
 };
 
-// The adapters of the tokens, behind the product.
-struct W4Adapters {
-    Adapters a;
-    const float* U;                  // times the adapters' scales
-    const void* B;
-};
 // LANES lanes share a token's eight columns: the shares of the sums, the pieces of the token and the adapter's rows are dealt out to them, ROWS
 // rows a lane read at once.
 template <typename T, int LANES, int ROWS>
@@ -454,9 +449,8 @@ extern "C" size_t dab_w4_matvec_workspace_bytes(int32_t B, int32_t K, int32_t F,
 
 namespace dab {
 
-// The product alone, or with the tokens' adapters behind it (A, w; U goes to `u`).
-static int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y, void* ws,
-                      size_t ws_bytes, hipStream_t st, const void* A = nullptr, const W4Adapters* w = nullptr, float* u = nullptr) {
+int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K, int32_t F, void* Y, void* ws,
+               size_t ws_bytes, hipStream_t st, const W4Adapters* w) {
     if (!X || !Q || !S || !Y) return DAB_ERR_NULL;
     if (B < 1 || K < 1 || F < 1 || ldx < K) return DAB_ERR_SHAPE;
     if (!real_dtype(dtype) || K > (1 << 26) || B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
@@ -492,18 +486,17 @@ static int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* 
     bf16* out = static_cast<bf16*>(ws);
     const auto prepare = [&](auto* t) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;
-        const T *from = static_cast<const T*>(X), *down = static_cast<const T*>(A);
-        const bool few = w && B <= kFewTokens;
-        if (w && !few)
-            if (int rc = shrink(from, ldx, down, K, w->a, true, u, st)) return rc;
-        if (few) {
+        const T* from = static_cast<const T*>(X);
+        if (w && B <= kFewTokens) {
             const int64_t rows = static_cast<int64_t>(B) * w->a.r;
             return launch(w4_tokens_shrink_kernel<T>, dim3(static_cast<unsigned>(static_cast<int64_t>(blocks) * passes + rows)), dim3(256), 0, st, from, to,
-                          blocks, out, down, w->a, u);
+                          blocks, out, static_cast<const T*>(w->A), w->a, w->U);
         }
-        return need ? launch(w4_tokens_kernel<T>, dim3(blocks, passes), dim3(256), 0, st, from, to, out) : static_cast<int>(DAB_OK);
+        return need ? launch(w4_tokens_kernel<T>, dim3(blocks, passes), dim3(256), 0, st, from, B, K, ldx, g.Kt, g.nb, g.P, columns, out)
+                    : static_cast<int>(DAB_OK);
     };
-    if (need || w)
+    // (U of many tokens is the caller's work)
+    if (need || (w && B <= kFewTokens))
         if (int rc = dtype == DAB_F32   ? prepare(static_cast<float*>(nullptr))
                      : dtype == DAB_F16 ? prepare(static_cast<f16*>(nullptr))
                                         : prepare(static_cast<bf16*>(nullptr)))
@@ -516,28 +509,4 @@ static int w4_product(const void* X, int32_t dtype, int64_t ldx, const uint8_t* 
 extern "C" int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, int32_t B, int32_t K,
                              int32_t F, void* Y, void* ws, size_t ws_bytes, void* stream) {
     return dab::w4_product(X, dtype, ldx, Q, S, B, K, F, Y, ws, ws_bytes, static_cast<hipStream_t>(stream));
-}
-
-// Workspace of the product with adapters: the product's own, then U.
-static size_t w4_own_bytes(int32_t B, int32_t K, int32_t F, int32_t dtype, int64_t ldx) {
-    return static_cast<size_t>(dab::round_up(static_cast<int64_t>(dab_w4_matvec_workspace_bytes(B, K, F, dtype, ldx)), 256));
-}
-extern "C" size_t dab_w4_adapters_workspace_bytes(int32_t B, int32_t K, int32_t F, int32_t r, int32_t dtype, int64_t ldx) {
-    if (B < 1 || K < 1 || F < 1 || r < 1 || !dab::real_dtype(dtype)) return 0;
-    return w4_own_bytes(B, K, F, dtype, ldx) + static_cast<size_t>(dab::round_up(static_cast<int64_t>(B) * r * 4, 256));
-}
-
-extern "C" int dab_w4_adapters(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, const uint8_t* S, const int32_t* ids, const void* A,
-                               const void* Bt, const float* scale, int32_t B, int32_t K, int32_t F, int32_t n, int32_t r, void* Y, void* ws,
-                               size_t ws_bytes, void* stream) {
-    using namespace dab;
-    if (int rc = check_adapters(X, dtype, ldx, ids, A, Bt, scale, B, K, F, n, r)) return rc;
-    if (!Q || !S || !Y) return DAB_ERR_NULL;
-    if (B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
-    if (misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
-    if (!ws || ws_bytes < dab_w4_adapters_workspace_bytes(B, K, F, r, dtype, ldx) || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
-    const size_t product = w4_own_bytes(B, K, F, dtype, ldx);
-    float* U = reinterpret_cast<float*>(static_cast<char*>(ws) + product);
-    const W4Adapters w{Adapters{ids, scale, B, n, r}, U, Bt};
-    return w4_product(X, dtype, ldx, Q, S, B, K, F, Y, ws, product, static_cast<hipStream_t>(stream), A, &w, U);
 }
