@@ -650,26 +650,29 @@ struct Join {
     const int32_t* have;
     int shares, n;
 };
+// (a lane four neighbouring elements, the workgroup's four wavefronts every fourth share)
 __global__ __launch_bounds__(256) void outer_join_kernel(const Join j) {
+    __shared__ v4f sums[3][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool second = blockIdx.x >= j.blocks0;
-    const int64_t at = (static_cast<int64_t>(second ? blockIdx.x - j.blocks0 : blockIdx.x) * 256 + threadIdx.x) * 4, size = j.size[second];
-    const int id = blockIdx.y;
-    if (at >= size) return;
-    const int left = static_cast<int>(min(size - at, int64_t{4}));
-    float v[4] = {};
+    const int64_t at = (static_cast<int64_t>(second ? blockIdx.x - j.blocks0 : blockIdx.x) * 64 + lane) * 4, size = j.size[second];
+    const int id = blockIdx.y, left = static_cast<int>(max(min(size - at, int64_t{4}), int64_t{0}));
+    v4f v = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = 0; s < j.shares; ++s) {
+    for (int s = wave; s < j.shares; s += 4) {
         const int64_t who = static_cast<int64_t>(s) * j.n + id;
         if (!j.have[who]) continue;
         const float* from = j.parts[second] + who * size + at;
         if (left == 4) {
-            const auto got = *reinterpret_cast<const Unaligned<float, 4>::type*>(from);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += got[i];
+            v += static_cast<v4f>(*reinterpret_cast<const Unaligned<float, 4>::type*>(from));
         } else {
             for (int i = 0; i < left; ++i) v[i] += from[i];
         }
     }
+    if (wave) sums[wave - 1][lane] = v;
+    __syncthreads();
+    if (wave) return;
+    v = (v + sums[0][lane]) + (sums[1][lane] + sums[2][lane]);
     float* to = j.out[second] + static_cast<int64_t>(id) * size + at;
     for (int i = 0; i < left; ++i) to[i] = v[i];
 }
@@ -680,7 +683,9 @@ constexpr int64_t kAdapterLd = 1 << 25;
 
 template <typename T>
 static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
-    if (a.T <= kFewTokens)
+    // A workgroup for every token and row, or for sixteen tokens: the one's time grows with both, the other's with k alone until its workgroups fill the
+    // chip.  bf16, r = 16, rows of 4096: 128 tokens 5.2 us and 10.8, 256 8.7 and 10.8, 512 14.1 and 11.0; of 1024, 256 tokens 6.0 and 4.9.
+    if (static_cast<int64_t>(a.T) * a.r <= 1024 + K)
         return launch(shrink_few_kernel<T>, dim3(a.T * a.r), dim3(64 * kFewWaves), 0, st, X, ldx, A, K, a, static_cast<int>(scaled), U);
     const unsigned tiles = static_cast<unsigned>(ceil_div64(a.T, 16));
     const dim3 block(64 * kShrinkWaves);
@@ -785,8 +790,8 @@ static int outer(const OuterSide<T> (&sides)[2], const Adapters& a, char* ws, hi
     if (rc || p.shares == 1) return rc;
     j.parts[0] = wide[0].out, j.parts[1] = wide[1].out, j.have = o.have, j.shares = p.shares, j.n = a.n;
     j.size[0] = static_cast<int64_t>(a.r) * wide[0].cols, j.size[1] = static_cast<int64_t>(a.r) * wide[1].cols;
-    j.blocks0 = static_cast<unsigned>(ceil_div64(j.size[0], 1024));
-    return launch(outer_join_kernel, dim3(j.blocks0 + static_cast<unsigned>(ceil_div64(j.size[1], 1024)), a.n), dim3(256), 0, st, j);
+    j.blocks0 = static_cast<unsigned>(ceil_div64(j.size[0], 256));
+    return launch(outer_join_kernel, dim3(j.blocks0 + static_cast<unsigned>(ceil_div64(j.size[1], 256)), a.n), dim3(256), 0, st, j);
 }
 // (rows that the narrow kernels take are no part of the plan)
 static size_t outer_bytes(int T, int n, int r, int F, int K) {
