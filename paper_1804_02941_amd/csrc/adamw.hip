@@ -5,7 +5,8 @@
 // One pass over memory: a lane holds eight neighbouring elements of everything, four lanes a group of 32 that shares a scale.  One launch
 // for all tensors: a table in device memory, written once by kernels that get the addresses with their launch (nothing is copied to the device, so
 // that it may be made in a captured graph too), says which stretch of which tensor a workgroup takes.  Bound by memory: 28 bytes an element with
-// fp32 gradients and states, 16.1 with bf16 gradients, 8-bit states and a bf16 copy.
+// fp32 gradients and states (8.5 M of them 50 us, 4.8 TB/s), 16.1 with bf16 gradients, 8-bit states and a bf16 copy (75.5 M 237 to 263 us, 4.6 to 5.1).
+// 96 tensors of a few thousand elements: 5.8 us, a chain of three reads behind a launch; with the tensors among the arguments, 32 a launch, 21.6.
 #include <cmath>
 
 #include "real16.h"

@@ -4,7 +4,8 @@
 //     n = h rstd,  w = gain dy:   dx = rstd (w - n mean(w n)) + dh,   dgain = sum over rows of dy n
 //
 // One pass over memory each: 2^LOG lanes hold a row in registers, eight neighbouring values at a time, from the load to the store, so that
-// the sum over the row costs no second read.  Bound by memory.
+// the sum over the row costs no second read.  Bound by memory: 16384 x 4096 bf16 with residual and bytes 121 us, 5.0 TB/s, its gradients 102 + 5, 5.1
+// (a copy of 2 GB reaches 4.92); counters: 269 MB read and 338 written, what the formulas need.
 #include "lanes.h"
 #include "real16.h"
 
@@ -55,7 +56,8 @@ __device__ __forceinline__ void save_eight(const float (&y)[8], int64_t row_grou
     if ((c & 31) == 0) S[row_groups + (c >> 5)] = static_cast<uint8_t>(code);
 }
 
-// Rows of at most 8 NV 2^LOG values.  Lane i of a row holds the eights i, i + 2^LOG, ..
+// Rows of at most 8 NV 2^LOG values.  Lane i of a row holds the eights i, i + 2^LOG, ..  Four eights a lane where rows fill the chip; fewer of them are
+// spread over as many lanes as a row has eights (one row of 4096: 2.4 us, with four eights a lane 4.4).
 template <typename T, int LOG, int NV>
 __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_kernel(const T* X, const T* R, const float* __restrict__ gain, NormGeom g,
                                                                                 T* H, T* Y, int8_t* Q, uint8_t* S, float* rstd) {
@@ -146,7 +148,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const T* R,
 
 // ---------------------------------------------------------------- gradients
 // A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it holds at once) and keeps its part of dgain in registers meanwhile, that of
-// its rows' lanes together in LDS at the end; norm_join_kernel adds the workgroups' parts in a fixed order.
+// its rows' lanes together in LDS at the end; norm_join_kernel adds the workgroups' parts in a fixed order.  (Every row's lanes with a part of their
+// own: 1999 x 1003 fp32 11.8 us and 37 for joining 2000 parts, now 9.5 and 5.7.)  Two eights a lane: gain and the part of dgain stay in registers too.
 template <typename T, int LOG, int NV>
 __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_kernel(const T* dY, const T* H, const float* __restrict__ gain,
                                                                                      const float* __restrict__ rstd, const T* dH, NormGeom g, T* dX,
@@ -260,7 +263,8 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* dY, const
     }
 }
 
-// dgain[c] = sum over the parts: 32 columns a workgroup, 128 threads that share the parts of four columns.
+// dgain[c] = sum over the parts: 32 columns a workgroup, 128 threads that share the parts of four columns, so that a thread's few loads are in flight
+// together (1024 parts of 4096: 5.1 us).
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float* __restrict__ parts, int n, int cols, float* __restrict__ dgain) {
     __shared__ float sums[128][33];
     DAB_RESERVE_VGPRS();
