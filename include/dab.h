@@ -577,7 +577,7 @@ int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, c
  * dab_rms_norm - the root-mean-square norm of a layer's input, with the residual's addition and, in the same pass, the output in 8 bits for
  * dab_ckpt8_weight_gradient of the layer behind it:
  *     h = x + r, rounded to dtype (x without a residual),   y_c = gain_c h_c rstd,  rstd = 1 / sqrt(mean_c(h_c^2) + eps).
- * Sums are fp32 (a row whose squares pass fp32's range has an rstd of 0); y is rounded once, to dtype and, apart from that, to bytes.
+ * Sums are fp32 (a row whose squares pass fp32's range has an rstd of 0, a row of zeros with an eps of 0 an infinite one); y is rounded once, to dtype and, apart from that, to bytes.
  *
  *   X      [rows][cols] of dtype, rows ldx apart;  R  the same, rows ldr apart, or NULL.  cols is at most 2^26
  *   gain   [cols] fp32
@@ -678,7 +678,7 @@ int dab_state8_save(const float* X, int64_t n, int32_t is_signed, uint8_t* Q, ui
  * dab_adapters - products of low rank beside a shared projection.  A token t has adapter i = ids[t] (none where that is not one of 0 .. n-1):
  *     U_t = A_i X_t,   Y_t = base_t + scale_i (U_t B_i),     Y_t = base_t and U_t = 0 without an adapter.
  * Both matrices of an adapter are r long rows.  Products are exact and sums fp32; Y is rounded once.  What an adapter that a token does
- * not have holds, infinities and NaN among it, does not reach the token.
+ * not have holds, infinities and NaN among it, does not reach the token; an infinity among a token's own numbers may come out as a NaN.
  *
  *   X       [T][K] of dtype, rows ldx apart;  ids  int32 [T], in any order;  scale  fp32 [n], or NULL for 1
  *   A       [n][r][K], B  [n][r][F] of dtype, contiguous.  r is at most 256, n 65535, T 2^25, K and F 2^21,
@@ -696,7 +696,8 @@ int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, 
  *
  *   dY      [T][F] of dtype, rows lddy apart;  X, ids, A, B, scale  as for dab_adapters, U  what it returned
  *   base    [T][K] of dtype or fp32, rows ldbase apart, or NULL for 0: what the shared projection's gradient gives
- *   dX      [T][K] of dtype out, or NULL where it is not needed (base is NULL then).  May be base itself where that is of dtype and its rows are K apart
+ *   dX      [T][K] of dtype out, or NULL where it is not needed (base is NULL then).  May be base itself where that is of dtype and its rows are K
+ *           apart; must not overlap X or dY (DAB_ERR_UNSUPPORTED)
  *   dA      fp32 [n][r][K] out, dB  fp32 [n][r][F] out, zeros for an adapter without tokens
  *   ws      dab_adapters_gradient_workspace_bytes(T, K, F, n, r) bytes, 256-byte aligned
  */

@@ -702,7 +702,6 @@ static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a,
     return launch(shrink_kernel<T, 4>, dim3(tiles, ceil_div(a.r, 64)), block, 0, st, X, ldx, A, K, a, s, U);
 }
 
-
 template <typename T, typename TB>
 static int expand_from(const float* U, const T* B, int F, const Adapters& a, bool scaled, const Base& base, T* Y, hipStream_t st) {
     const TB* p = static_cast<const TB*>(base.p);
@@ -813,6 +812,11 @@ static int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32
     if (misaligned(X, 16) || misaligned(A, 16) || misaligned(B, 16) || misaligned(ids, 4) || misaligned(scale, 4)) return DAB_ERR_ALIGN;
     return DAB_OK;
 }
+// Whether a matrix's bytes, first to last, meet another one's.
+static bool meet(const void* p, int64_t rows, int64_t cols, int64_t ld, const void* q, int64_t q_rows, int64_t q_cols, int64_t q_ld, int64_t size) {
+    const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + static_cast<uintptr_t>(((q_rows - 1) * q_ld + q_cols) * size) && b < a + static_cast<uintptr_t>(((rows - 1) * ld + cols) * size);
+}
 static int check_base(const void* base, int32_t dtype, int64_t ld, int32_t cols, int32_t own_dtype) {
     if (!base) return DAB_OK;
     if (ld < cols) return DAB_ERR_SHAPE;
@@ -859,6 +863,8 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
     if (lddy > kAdapterLd) return DAB_ERR_UNSUPPORTED;
     if (int rc = check_base(base, base_dtype, ldbase, K, dtype)) return rc;
     if (misaligned(dY, 16) || misaligned(dX, 16) || misaligned(U, 4) || misaligned(dA, 4) || misaligned(dB, 4)) return DAB_ERR_ALIGN;
+    // (X and dY are read again behind dX)
+    if (dX && (meet(dX, T, K, K, X, T, K, ldx, dtype_bytes(dtype)) || meet(dX, T, K, K, dY, T, F, lddy, dtype_bytes(dtype)))) return DAB_ERR_UNSUPPORTED;
     const size_t need = dab_adapters_gradient_workspace_bytes(T, K, F, n, r);
     if (!ws || ws_bytes < need || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
     const Adapters a{ids, scale, T, n, r};

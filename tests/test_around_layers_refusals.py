@@ -118,12 +118,16 @@ def test_adapters_gradient(lib):
     need = size(5, 40, 24, 2, 3)
     assert need > 0 and size(0, 40, 24, 2, 3) == 0 and size(5, 40, 24, 2, 257) == 0
     assert size(8192, 4096, 4096, 4, 16) < 1 << 27
-    ok = dict(dY=p, lddy=24, X=p, t=BF16, ldx=40, U=p, ids=p, A=p, B=p, s=p, T=5, K=40, F=24, n=2, r=3, base=p, bt=F32, ldb=40, dX=p, dA=p, dB=p, ws=p, nb=need)
+    q = ctypes.c_void_p(1 << 20)
+    ok = dict(dY=p, lddy=24, X=p, t=BF16, ldx=40, U=p, ids=p, A=p, B=p, s=p, T=5, K=40, F=24, n=2, r=3, base=p, bt=F32, ldb=40, dX=q, dA=p, dB=p, ws=p, nb=need)
 
     def call(**k):
         return lib.dab_adapters_gradient(*{**ok, **k}.values(), None)
     for k in ("dY", "X", "U", "ids", "A", "B", "dX", "dA", "dB"):
         assert call(**{k: None}) == NULL
+    # X and dY are read again behind dX
+    assert call(dX=p) == UNSUPPORTED and call(dX=ctypes.c_void_p(4096 + 4 * 24 * 2 + 16)) == UNSUPPORTED and call(X=q) == UNSUPPORTED
+    assert call(X=q, dX=ctypes.c_void_p((1 << 20) + 400), ws=None) == WORKSPACE              # right behind X
     assert call(lddy=23) == SHAPE and call(ldb=39) == SHAPE and call(bt=F16) == UNSUPPORTED and call(dY=odd) == ALIGN and call(dA=odd) == ALIGN
     assert call(ws=None) == WORKSPACE and call(nb=need - 1) == WORKSPACE and call(ws=ctypes.c_void_p(4096 + 16)) == WORKSPACE
 

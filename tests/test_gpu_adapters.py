@@ -153,6 +153,22 @@ def test_a_share_of_more_tokens_than_lds_holds(dtype):
     assert not dX[ids < 0].any()
 
 
+@pytest.mark.parametrize("T", [3, 100, 400])
+def test_the_smallest_f16_numbers_count(T):
+    """Subnormal inputs, 2^-24 and its multiples, are not taken for zeros."""
+    rng = np.random.default_rng(12)
+    K, F, n, r = 96, 64, 2, 8
+    X, A, B, dY, _, _, _ = whole_numbers(rng, T, K, F, n, r)
+    ids = who(rng, T, n, "runs")
+    x, a, b, dy, i = on_gpu(X * 2.0 ** -24, torch.float16), on_gpu(A, torch.float16), on_gpu(B, torch.float16), on_gpu(dY * 2.0 ** -24, torch.float16), on_gpu(ids, torch.int32)
+    Y, Ug = dab.dab_adapters(x, i, a, b)
+    Yo, Uo = oa.adapters(X, ids, A, B, np.ones(n), None)
+    assert np.array_equal(f64(Ug), Uo * 2.0 ** -24) and torch.equal(Y, on_gpu(Yo * 2.0 ** -24, torch.float16))
+    dX, dA, dB = dab.dab_adapters_gradient(dy, x, Ug, i, a, b)
+    dXo, dAo, dBo = oa.adapters_gradient(dY, X, Uo, ids, A, B, np.ones(n), None)
+    assert torch.equal(dX, on_gpu(dXo * 2.0 ** -24, torch.float16)) and np.array_equal(f64(dA), dAo * 2.0 ** -48) and np.array_equal(f64(dB), dBo * 2.0 ** -48)
+
+
 def test_more_tiles_of_tokens_than_a_grid_has_along_one_dimension():
     T, K, F, n, r = 600001, 16, 8, 2, 65                           # (a rank of two row blocks: U and Y in launches of their own)
     g = torch.Generator(device=DEV).manual_seed(5)
@@ -347,6 +363,8 @@ def test_refusals():
             dab.dab_adapters(**{**good, **bad})
     _, Ug = dab.dab_adapters(**good)
     grads = dict(dY=dY, X=X, U=Ug, ids=ids, A=A, B=B, scale=scale, base=dbase)
+    with pytest.raises(dab.DabError):
+        dab.dab_adapters_gradient(**grads, out=(X, None, None))     # X is read again behind dX
     for bad, error in ((dict(dY=None), TypeError), (dict(dY=dY.half()), TypeError), (dict(U=Ug[:, :2]), ValueError), (dict(base=base), ValueError),
                        (dict(want_dX=False), ValueError)):
         with pytest.raises(error):
