@@ -577,15 +577,16 @@ int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, c
  * dab_rms_norm - the root-mean-square norm of a layer's input, with the residual's addition and, in the same pass, the output in 8 bits for
  * dab_ckpt8_weight_gradient of the layer behind it:
  *     h = x + r, rounded to dtype (x without a residual),   y_c = gain_c h_c rstd,  rstd = 1 / sqrt(mean_c(h_c^2) + eps).
- * Sums are fp32 (a row whose squares pass fp32's range has an rstd of 0, a row of zeros with an eps of 0 an infinite one); y is rounded once, to dtype and, apart from that, to bytes.
+ * Sums are fp32 (a row whose squares pass fp32's range has an rstd of 0, a row of zeros with an eps of 0 an infinite one); y is rounded once, to
+ * dtype and, apart from that, to bytes.
  *
  *   X      [rows][cols] of dtype, rows ldx apart;  R  the same, rows ldr apart, or NULL.  cols is at most 2^26
  *   gain   [cols] fp32
  *   H      [rows][cols] of dtype out: h; written where R is given, else not touched and may be NULL.  May be X or R itself where their rows are cols apart
- *   Y      [rows][cols] of dtype out, or NULL.  May be X itself where its rows are cols apart
+ *   Y      [rows][cols] of dtype out, or NULL.  May be X or R itself where their rows are cols apart
  *   Q, S   as dab_ckpt8_save writes them for y (in fp32), or both NULL.  One of Y and Q is given
  *   rstd   [rows] fp32 out, what the gradient takes
- * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE.
+ * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE; Y or H over X or R in any other way -> DAB_ERR_UNSUPPORTED.
  */
 int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const void* R, int64_t ldr, const float* gain, float eps, int32_t rows, int32_t cols,
                  void* H, void* Y, int8_t* Q, uint8_t* S, float* rstd, void* stream);
@@ -597,7 +598,8 @@ int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const void* R, int64
  *
  *   dY     [rows][cols] of dtype, rows lddy apart;  H  the h of dab_rms_norm (X without a residual), rows ldh apart;  rstd  its rstd
  *   dH     [rows][cols] of dtype, rows lddh apart, what arrives at h beside the norm, or NULL
- *   dX     [rows][cols] of dtype out.  May be dY or dH itself where their rows are cols apart;  dgain  [cols] fp32 out
+ *   dX     [rows][cols] of dtype out.  May be dY, H or dH itself where their rows are cols apart (over them in another way:
+ *          DAB_ERR_UNSUPPORTED);  dgain  [cols] fp32 out
  *   ws     dab_rms_norm_gradient_workspace_bytes(rows, cols) bytes, 256-byte aligned
  */
 size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t cols);
@@ -628,6 +630,7 @@ int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t l
  * P, G, M, V and copy are 16-byte aligned; n is at most 2^34.  No tensor may overlap another one of the call.
  *   lr, step, grad_scale   in the structure, or in device memory (lr_dev, step_dev; grad_scale: NULL for 1), where a captured graph reads them anew at
  *           every replay.  A *grad_scale that is infinite or a NaN leaves everything as it was; step counts from 1
+ * With an eps of 0 (in fp32) an element whose gradients were all 0 becomes 0/0, a NaN.
  * Errors: step < 1, a rate that is not finite, b1 or b2 outside 0 .. 1 (without 1), a negative eps, a place that is no multiple of 32 -> DAB_ERR_SHAPE.
  */
 typedef struct dab_adamw_job {
@@ -684,7 +687,8 @@ int dab_state8_save(const float* X, int64_t n, int32_t is_signed, uint8_t* Q, ui
  *   A       [n][r][K], B  [n][r][F] of dtype, contiguous.  r is at most 256, n 65535, T 2^25, K and F 2^21,
  *           the rows' distances (of dY and base too) 2^25
  *   base    [T][F] of dtype or fp32 (base_dtype), rows ldbase apart, or NULL for 0: any projection's output
- *   Y       [T][F] of dtype out.  May be base itself where that is of dtype and its rows are F apart;  U  fp32 [T][r] out: what the gradient takes
+ *   Y       [T][F] of dtype out.  May be base itself where that is of dtype and its rows are F apart; must not overlap X (DAB_ERR_UNSUPPORTED)
+ *   U       fp32 [T][r] out: what the gradient takes
  */
 int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
                  int32_t F, int32_t n, int32_t r, const void* base, int32_t base_dtype, int64_t ldbase, void* Y, float* U, void* stream);
@@ -708,7 +712,7 @@ int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X, int32_t d
 
 /*
  * dab_w4_adapters - dab_w4_matvec and dab_adapters in one: Y_t = W X_t + scale_i (A_i X_t) B_i with the 4-bit weights Q, S that all tokens share, rounded
- * once.  Arguments as for those two; Bt is dab_adapters' B.  B tokens, up to 65535.
+ * once.  Arguments as for those two; Bt is dab_adapters' B.  B tokens, up to 65535; Y must not overlap X (DAB_ERR_UNSUPPORTED).
  *
  *   ws      dab_w4_adapters_workspace_bytes(...) bytes, 256-byte aligned
  */

@@ -812,11 +812,6 @@ static int check_adapters(const void* X, int32_t dtype, int64_t ldx, const int32
     if (misaligned(X, 16) || misaligned(A, 16) || misaligned(B, 16) || misaligned(ids, 4) || misaligned(scale, 4)) return DAB_ERR_ALIGN;
     return DAB_OK;
 }
-// Whether a matrix's bytes, first to last, meet another one's.
-static bool meet(const void* p, int64_t rows, int64_t cols, int64_t ld, const void* q, int64_t q_rows, int64_t q_cols, int64_t q_ld, int64_t size) {
-    const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return a < b + static_cast<uintptr_t>(((q_rows - 1) * q_ld + q_cols) * size) && b < a + static_cast<uintptr_t>(((rows - 1) * ld + cols) * size);
-}
 static int check_base(const void* base, int32_t dtype, int64_t ld, int32_t cols, int32_t own_dtype) {
     if (!base) return DAB_OK;
     if (ld < cols) return DAB_ERR_SHAPE;
@@ -834,6 +829,8 @@ extern "C" int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int
     if (!Y || !U) return DAB_ERR_NULL;
     if (int rc = check_base(base, base_dtype, ldbase, F, dtype)) return rc;
     if (misaligned(Y, 16) || misaligned(U, 4)) return DAB_ERR_ALIGN;
+    // (X is read for other columns of Y)
+    if (meet({Y, T, F, F, dtype_bytes(dtype)}, {X, T, K, ldx, dtype_bytes(dtype)})) return DAB_ERR_UNSUPPORTED;
     const Adapters a{ids, scale, T, n, r};
     const auto st = static_cast<hipStream_t>(stream);
     const auto go = [&](auto* t) -> int {
@@ -864,7 +861,8 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
     if (int rc = check_base(base, base_dtype, ldbase, K, dtype)) return rc;
     if (misaligned(dY, 16) || misaligned(dX, 16) || misaligned(U, 4) || misaligned(dA, 4) || misaligned(dB, 4)) return DAB_ERR_ALIGN;
     // (X and dY are read again behind dX)
-    if (dX && (meet(dX, T, K, K, X, T, K, ldx, dtype_bytes(dtype)) || meet(dX, T, K, K, dY, T, F, lddy, dtype_bytes(dtype)))) return DAB_ERR_UNSUPPORTED;
+    const int64_t size = dtype_bytes(dtype);
+    if (dX && (meet({dX, T, K, K, size}, {X, T, K, ldx, size}) || meet({dX, T, K, K, size}, {dY, T, F, lddy, size}))) return DAB_ERR_UNSUPPORTED;
     const size_t need = dab_adapters_gradient_workspace_bytes(T, K, F, n, r);
     if (!ws || ws_bytes < need || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
     const Adapters a{ids, scale, T, n, r};
@@ -902,6 +900,7 @@ extern "C" int dab_w4_adapters(const void* X, int32_t dtype, int64_t ldx, const 
     if (B > 65535 || F > 65535 * 16) return DAB_ERR_UNSUPPORTED;
     if (misaligned(Q, 16) || misaligned(S, 16) || misaligned(Y, 16)) return DAB_ERR_ALIGN;
     if (!ws || ws_bytes < dab_w4_adapters_workspace_bytes(B, K, F, r, dtype, ldx) || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
+    if (meet({Y, B, F, F, dtype_bytes(dtype)}, {X, B, K, ldx, dtype_bytes(dtype)})) return DAB_ERR_UNSUPPORTED;
     const size_t product = w4_own_bytes(B, K, F, dtype, ldx);
     float* U = reinterpret_cast<float*>(static_cast<char*>(ws) + product);
     const W4Adapters w{Adapters{ids, scale, B, n, r}, U, A, Bt};

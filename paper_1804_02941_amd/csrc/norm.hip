@@ -398,6 +398,10 @@ static int norm_grad_launch(NormGradArgs<T> a, hipStream_t st) {
 }
 
 constexpr int kNormMaxCols = 1 << 26;
+// An output over an input: only element by element, which the same lane reads before it writes.
+static bool crosses(const void* out, const void* in, int rows, int cols, int64_t ld, int64_t size) {
+    return out && in && !(out == in && (ld == cols || rows == 1)) && meet({out, rows, cols, cols, size}, {in, rows, cols, ld, size});
+}
 
 }  // namespace dab
 
@@ -410,6 +414,9 @@ extern "C" int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const voi
     if (misaligned(X, 16) || misaligned(R, 16) || misaligned(H, 16) || misaligned(Y, 16) || misaligned(Q, 16) || misaligned(gain, 4) ||
         misaligned(rstd, 4))
         return DAB_ERR_ALIGN;
+    const int64_t size = dtype_bytes(dtype);
+    if (R && (crosses(H, X, rows, cols, ldx, size) || crosses(H, R, rows, cols, ldr, size))) return DAB_ERR_UNSUPPORTED;
+    if (crosses(Y, X, rows, cols, ldx, size) || crosses(Y, R, rows, cols, ldr, size)) return DAB_ERR_UNSUPPORTED;
     NormGeom g{};
     g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ldx = ldx, g.ldr = ldr, g.eps = eps;
     const auto st = static_cast<hipStream_t>(stream);
@@ -441,6 +448,8 @@ extern "C" int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H
     if (misaligned(dY, 16) || misaligned(H, 16) || misaligned(dH, 16) || misaligned(dX, 16) || misaligned(gain, 4) || misaligned(rstd, 4) ||
         misaligned(dgain, 4))
         return DAB_ERR_ALIGN;
+    const int64_t size = dtype_bytes(dtype);
+    if (crosses(dX, dY, rows, cols, lddy, size) || crosses(dX, H, rows, cols, ldh, size) || crosses(dX, dH, rows, cols, lddh, size)) return DAB_ERR_UNSUPPORTED;
     const size_t need = dab_rms_norm_gradient_workspace_bytes(rows, cols);
     if (need && (!ws || ws_bytes < need || misaligned(ws, 256))) return DAB_ERR_WORKSPACE;
     NormGeom g{};

@@ -20,6 +20,14 @@ inline int64_t dtype_bytes(int32_t t) { return t == DAB_F32 ? 4 : 2; }
 inline int dtype_pieces(int32_t t) { return t == DAB_F32 ? 3 : t == DAB_F16 ? 2 : 1; }
 inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Whether the bytes of two matrices, first to last, meet.
+struct Extent {
+    const void* p;
+    int64_t rows, cols, ld, size;
+    uintptr_t first() const { return reinterpret_cast<uintptr_t>(p); }
+    uintptr_t end() const { return first() + static_cast<uintptr_t>(((rows - 1) * ld + cols) * size); }
+};
+inline bool meet(const Extent& a, const Extent& b) { return a.first() < b.end() && b.first() < a.end(); }
 
 // 2^e as fp32 for -126 <= e <= 127.
 __device__ __forceinline__ float pow2f(int e) { return __builtin_bit_cast(float, static_cast<uint32_t>(e + 127) << 23); }

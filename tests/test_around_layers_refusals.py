@@ -31,6 +31,13 @@ def test_norm(lib):
     assert call(eps=float("nan")) == SHAPE and call(t=9) == UNSUPPORTED and call(cols=(1 << 26) + 1, ldx=1 << 27, ldr=1 << 27) == UNSUPPORTED
     for k in ("X", "R", "H", "Y", "Q", "g", "rstd"):
         assert call(**{k: odd}) == ALIGN
+    # an output over an input: only element by element
+    for k, ld in (("X", "ldx"), ("R", "ldr")):
+        for out in ("H", "Y"):
+            apart = {"X": 1 << 20, "R": 1 << 21, "H": 1 << 22, "Y": 1 << 23}
+            for shift in (-16, 16, 3 * 40 * 2 + 64):
+                assert call(**{**apart, out: apart[k] + shift}) == UNSUPPORTED
+            assert call(**{**apart, out: apart[k], ld: 48}) == UNSUPPORTED
 
 
 def test_norm_gradient(lib):
@@ -48,6 +55,10 @@ def test_norm_gradient(lib):
     for k in ("lddy", "ldh", "lddh"):
         assert call(**{k: 39}) == SHAPE
     assert call(t=-1) == UNSUPPORTED and call(dX=odd) == ALIGN and call(dH=odd) == ALIGN
+    for k, ld in (("dY", "lddy"), ("H", "ldh"), ("dH", "lddh")):
+        apart = {"dY": 1 << 20, "H": 1 << 21, "dH": 1 << 22, "dX": 1 << 23, "ws": None}
+        assert call(**{**apart, "dX": apart[k]}) == WORKSPACE and call(**{**apart, "dX": apart[k], ld: 41}) == UNSUPPORTED
+        assert call(**{**apart, "dX": apart[k] + 16}) == UNSUPPORTED and call(**{**apart, "dX": apart[k] - 16}) == UNSUPPORTED
     assert call(ws=None) == WORKSPACE and call(n=need - 1) == WORKSPACE and call(ws=ctypes.c_void_p(4096 + 16)) == WORKSPACE
 
 
@@ -111,6 +122,8 @@ def test_adapters(lib):
     assert call(r=257) == UNSUPPORTED and call(n=65536) == UNSUPPORTED and call(T=(1 << 25) + 1) == UNSUPPORTED
     for k in ("X", "A", "B", "base", "Y", "U", "ids", "s"):
         assert call(**{k: odd}) == ALIGN
+    # X is read for other columns of Y
+    assert call() == UNSUPPORTED and call(Y=ctypes.c_void_p(4096 + 4 * 40 * 2 + 64)) == UNSUPPORTED
 
 
 def test_adapters_gradient(lib):
@@ -144,3 +157,4 @@ def test_served(lib):
         assert call(**{k: None}) == NULL
     assert call(F=0) == SHAPE and call(r=257) == UNSUPPORTED and call(T=65536) == UNSUPPORTED and call(F=65536 * 16) == UNSUPPORTED
     assert call(Q=odd) == ALIGN and call(Y=odd) == ALIGN and call(ws=None) == WORKSPACE and call(nb=need - 1) == WORKSPACE
+    assert call() == UNSUPPORTED                                   # Y over X
