@@ -149,7 +149,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const T* R,
 // ---------------------------------------------------------------- gradients
 // A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it holds at once) and keeps its part of dgain in registers meanwhile, that of
 // its rows' lanes together in LDS at the end; norm_join_kernel adds the workgroups' parts in a fixed order.  (Every row's lanes with a part of their
-// own: 1999 x 1003 fp32 11.8 us and 37 for joining 2000 parts, now 9.5 and 5.7.)  Two eights a lane: gain and the part of dgain stay in registers too.
+// own: 1999 x 1003 fp32 11.8 us and 37 for joining 2000 parts, now 9.7 and 3.8.)  Two eights a lane: gain and the part of dgain stay in registers too.
 template <typename T, int LOG, int NV>
 __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_kernel(const T* dY, const T* H, const float* __restrict__ gain,
                                                                                      const float* __restrict__ rstd, const T* dH, NormGeom g, T* dX,
@@ -369,11 +369,14 @@ template <typename T, int LOG, int NV>
 static int norm_grad_launch(const NormGradArgs<T>& a, NormForm f, hipStream_t st) {
     return launch(norm_grad_kernel<T, LOG, NV>, dim3(a.blocks), dim3(norm_threads(f)), 0, st, a.dY, a.H, a.gain, a.rstd, a.dH, a.g, a.dX, a.parts);
 }
-// Workgroups of the gradient's kernel: what the chip holds at once, fewer where there are fewer rows.
+// Workgroups of the gradient's kernel: what the chip holds at once, fewer where there are fewer rows: half as many as these would fill, once that leaves
+// one for every other compute unit, so that half the parts are joined (both kernels, us: 1999 x 1003 fp32 15.0 and 13.9, 512 x 4096 bf16 12.9 and
+// 12.4, 1000 x 2000 11.4 and 11.8; below, 100 x 16384 12.6 and 13.4; a quarter as many is slower throughout).
 static int norm_grad_blocks(int rows, NormForm f) {
     const int64_t n = ceil_div64(rows, norm_rows(f)), most = 1024 / norm_threads(f) * int64_t{kNumCU};
     if (n <= 2) return 1;
-    return static_cast<int>(n < most ? n : most);
+    if (n >= most) return static_cast<int>(most);
+    return static_cast<int>(n <= kNumCU ? n : (n + 1) / 2);
 }
 template <typename T>
 static int norm_grad_launch(NormGradArgs<T> a, hipStream_t st) {
