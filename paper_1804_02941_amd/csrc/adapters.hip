@@ -6,7 +6,7 @@
 // results a token), `expand` (r numbers a token times long rows) and `outer` (the sum over an adapter's tokens of r numbers times a long row).  Each is
 // bound by its long rows in memory: 2 r operations an element.  Tokens come in any order; a tile of sixteen takes its adapters one after the other,
 // and what a token is not to take is left out by selection, not by a product with zero, so that no adapter's infinities and NaN
-// reach another's tokens.  8192 tokens of four adapters, 4096 -> 4096, r = 16, bf16: U and Y 47 us (207 MB, 4.4 TB/s), V and dX the same, dA and dB 37
+// reach another's tokens.  8192 tokens of four adapters, 4096 -> 4096, r = 16, bf16: U and Y 46 us (207 MB, 4.5 TB/s), V and dX the same, dA and dB 34
 // (132 MB, 3.6) and 6 for joining shares.
 #include <algorithm>
 
@@ -189,14 +189,15 @@ __device__ __forceinline__ T* past(T* shared, uint32_t elements) {
     typedef std::conditional_t<std::is_const_v<T>, const char, char> Byte;
     return reinterpret_cast<T*>(reinterpret_cast<Byte*>(shared) + static_cast<uint32_t>(elements * static_cast<uint32_t>(sizeof(T))));
 }
-// Values of N columns, without the first `again` of them.
+// Values of N columns, without the first `again` of them.  Past the caches, which keep what the sums over tokens read next instead (8192 x 4096 bf16: 34
+// us for those, 36.7 with ordinary stores, and 46.4 for the tile's own launch, 47.3).
 template <typename T, int N>
 __device__ __forceinline__ void store_own(T* to, int again, const float (&w)[N]) {
     if (again == 0) {
         typename Unaligned<T, N>::type v;
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = static_cast<T>(w[i]);
-        *reinterpret_cast<typename Unaligned<T, N>::type*>(to) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<typename Unaligned<T, N>::type*>(to));
     } else {
 #pragma unroll
         for (int i = 1; i < N; ++i)
@@ -722,7 +723,7 @@ static int expand(const float* U, const T* B, int F, const Adapters& a, bool sca
 }
 
 // U and Y (or V and dX): one launch of up to 64 rows where the tiles fill the chip, or the columns are one round of a workgroup's wavefronts.  8192 tokens,
-// 4096 -> 4096, r = 16, bf16: 47 us, in two launches 22 + 34; 1999 tokens, 777 -> 301, r = 5, f16: 8.7, 4.8 + 5.5.
+// 4096 -> 4096, r = 16, bf16: 46 us, in two launches 22 + 34; 1999 tokens, 777 -> 301, r = 5, f16: 8.7, 4.8 + 5.5.
 template <typename T, typename TB, int RT>
 static int shrink_expand_from(const T* X, int64_t ldx, const T* A, int K, const T* B, int F, const Adapters& a, bool scaled, float* U, const Base& base, T* Y,
                               hipStream_t st) {
