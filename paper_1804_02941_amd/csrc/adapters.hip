@@ -17,38 +17,62 @@ namespace dab {
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------- shrink
-// Eight k as the matrix cores take them: 16-bit numbers as they are, fp32 ones for eight products of four k.
-template <typename T>
+// Eight k as the matrix cores take them: 16-bit numbers as they are, fp32 ones for eight products of four k.  ODD: 16-bit rows at odd distances, every
+// other one of which lies two bytes behind a multiple of four, where 16 bytes a lane from sixteen rows are slow: there the four words that hold an eight's
+// first seven are read, and the eighth alone, nothing outside the matrix.  1024 tokens, 4095 k, bf16: r = 16 13.7 us (27.2 from the rows as they are, 4094
+// k 11.9), r = 32 17.0 (39.3), r = 64 27.2 (63.5); 8192 tokens with 4095 columns of Y, r = 16: 67.5 (85).
+template <typename T, bool ODD>
 struct Long;
 template <>
-struct Long<float> {
+struct Long<float, false> {
     typedef float v8f __attribute__((ext_vector_type(8)));
     v8f v;
+    __device__ __forceinline__ void clear() { v = {}; }
     __device__ __forceinline__ void load(const float* row, int k) { v = *reinterpret_cast<const Unaligned<float, 8>::type*>(row + k); }
-    static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) {
+    static __device__ __forceinline__ v4f mul(const Long& a, const float*, const Long& b, const float*, v4f c) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
         return c;
     }
 };
-template <>
-struct Long<bf16> {
-    v8bf v;
-    __device__ __forceinline__ void load(const bf16* row, int k) { v = *reinterpret_cast<const Unaligned<bf16, 8>::type*>(row + k); }
-    static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }
+__device__ __forceinline__ v4f mul_eights(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v4f mul_eights(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+template <typename T>
+struct Long<T, false> {
+    typedef T v8 __attribute__((ext_vector_type(8)));
+    v8 v;
+    __device__ __forceinline__ void clear() { v = {}; }
+    __device__ __forceinline__ void load(const T* row, int k) { v = *reinterpret_cast<const typename Unaligned<T, 8>::type*>(row + k); }
+    static __device__ __forceinline__ v4f mul(const Long& a, const T*, const Long& b, const T*, v4f c) { return mul_eights(a.v, b.v, c); }
 };
-template <>
-struct Long<f16> {
-    v8h v;
-    __device__ __forceinline__ void load(const f16* row, int k) { v = *reinterpret_cast<const Unaligned<f16, 8>::type*>(row + k); }
-    static __device__ __forceinline__ v4f mul(const Long& a, const Long& b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
+template <typename T>
+struct Long<T, true> {
+    typedef T v8 __attribute__((ext_vector_type(8)));
+    v4u32 words;
+    uint32_t last;
+    __device__ __forceinline__ void clear() { words = v4u32{0, 0, 0, 0}, last = 0; }
+    // (only rows behind the first lie so: there is an element before theirs)
+    __device__ __forceinline__ void load(const T* row, int k) {
+        words = *reinterpret_cast<const Unaligned<uint32_t, 4>::type*>(row - (reinterpret_cast<uintptr_t>(row) >> 1 & 1) + k);
+        last = __builtin_bit_cast(uint16_t, row[k + 7]);
+    }
+    __device__ __forceinline__ v8 eight(const T* row) const {
+        const uint32_t by = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 2u;
+        v4u32 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(i < 3 ? words[(i + 1) & 3] : last, words[i], by);
+        return __builtin_bit_cast(v8, v);
+    }
+    static __device__ __forceinline__ v4f mul(const Long& a, const T* row_a, const Long& b, const T* row_b, v4f c) {
+        return mul_eights(a.eight(row_a), b.eight(row_b), c);
+    }
 };
 
 // Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth stretch of 128 k (RT = 1, 16-bit types), whose
 // loads are in flight at once, those of the next one behind them.  This lane's sums over its wavefront's k: rows 4 (lane / 16) .. + 3 of
 // each sixteen from r0 on, of token lane % 16.
 constexpr int kShrinkWaves = 8;
-template <typename T, int RT>
+template <typename T, int RT, bool ODD>
 __device__ __forceinline__ void shrink_tile(const T* __restrict__ x, const T* __restrict__ A, int K, const Adapters& a, int id, int r0, v4f (&out)[RT]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -64,17 +88,17 @@ __device__ __forceinline__ void shrink_tile(const T* __restrict__ x, const T* __
 #pragma unroll
         for (int j = 0; j < RT; ++j) mine[j] = rows + static_cast<int64_t>(min(r0 + j * 16 + m, a.r - 1)) * K;
         // a stretch of k: its loads, then, with those of the next one on their way, its products
-        constexpr int kAhead = RT == 1 ? 8 / static_cast<int>(sizeof(T)) : RT == 2 && sizeof(T) == 2 ? 2 : 1, kStep = kShrinkWaves * 32 * kAhead;
+        constexpr int kAhead = RT == 1 ? 8 / static_cast<int>(sizeof(T)) - ODD : RT == 2 && sizeof(T) == 2 && !ODD ? 2 : 1, kStep = kShrinkWaves * 32 * kAhead;
         struct Stretch {
-            Long<T> x[kAhead], a[kAhead][RT];
+            Long<T, ODD> x[kAhead], a[kAhead][RT];
             // (eights that the row does not hold whole are zeros here)
             __device__ __forceinline__ void load(const T* from, const T* const (&rows)[RT], int64_t k0, int g, int K) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
                     const int64_t k = k0 + u * 32 + g * 8;
-                    x[u].v = {};
+                    x[u].clear();
 #pragma unroll
-                    for (int j = 0; j < RT; ++j) a[u][j].v = {};
+                    for (int j = 0; j < RT; ++j) a[u][j].clear();
                     if (k + 8 <= K) {
                         x[u].load(from, static_cast<int>(k));
 #pragma unroll
@@ -93,14 +117,14 @@ __device__ __forceinline__ void shrink_tile(const T* __restrict__ x, const T* __
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                    for (int j = 0; j < RT; ++j) acc[j] = Long<T>::mul(cur.a[u][j], cur.x[u], acc[j]);
+                    for (int j = 0; j < RT; ++j) acc[j] = Long<T, ODD>::mul(cur.a[u][j], mine[j], cur.x[u], x, acc[j]);
                 if (more) cur = next;
             }
         }
         if ((K & 7) != 0 && wave == kShrinkWaves - 1) {
             // the last few of a row: those of its last eight that no eight before holds
             const int again = g == 0 ? 8 - (K & 7) : 8;
-            Long<T> xv, av;
+            Long<T, false> xv, av;
             xv.load(x, K - 8);
 #pragma unroll
             for (int i = 0; i < 8; ++i) xv.v[i] = i < again ? static_cast<T>(0.f) : xv.v[i];
@@ -109,7 +133,7 @@ __device__ __forceinline__ void shrink_tile(const T* __restrict__ x, const T* __
                 av.load(mine[j], K - 8);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) av.v[i] = i < again ? static_cast<T>(0.f) : av.v[i];
-                acc[j] = Long<T>::mul(av, xv, acc[j]);
+                acc[j] = Long<T, false>::mul(av, mine[j], xv, x, acc[j]);
             }
         }
         if (id == now) {
@@ -136,8 +160,8 @@ __device__ __forceinline__ void shrink_join(const v4f (&out)[RT], float (&sums)[
         put(token, j * 16 + (i & 15), u);
     }
 }
-template <typename T, int RT>
-__global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && sizeof(T) == 4 ? 2 : 4) void shrink_kernel(const T* __restrict__ X, int64_t ldx,
+template <typename T, int RT, bool ODD>
+__global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && (ODD || sizeof(T) == 4) ? 2 : 4) void shrink_kernel(const T* __restrict__ X, int64_t ldx,
                                                                                                   const T* __restrict__ A, int K, Adapters a, int scaled,
                                                                                                   float* __restrict__ U) {
     __shared__ float sums[kShrinkWaves][RT][16][17];
@@ -145,7 +169,7 @@ __global__ __launch_bounds__(64 * kShrinkWaves, RT == 4 && sizeof(T) == 4 ? 2 : 
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16, t = t0 + (threadIdx.x & 15);
     const int r0 = blockIdx.y * 16 * RT;
     v4f out[RT];
-    shrink_tile<T, RT>(X + min(t, static_cast<int64_t>(a.T) - 1) * ldx, A, K, a, adapter_of(a, t), r0, out);
+    shrink_tile<T, RT, ODD>(X + min(t, static_cast<int64_t>(a.T) - 1) * ldx, A, K, a, adapter_of(a, t), r0, out);
     shrink_join<RT>(out, sums, [&](int token, int row, float u) {
         if (t0 + token >= a.T || r0 + row >= a.r) return;
         const int who = adapter_of(a, t0 + token);
@@ -362,8 +386,8 @@ __device__ __forceinline__ void expand_tile16(const bf16* __restrict__ B, int F,
 
 // Both in one launch, for tiles that fill the chip: a workgroup's eight wavefronts share the tile's k, then its columns, with U in LDS between.  U goes out
 // as well (times the scale where `scaled`).  What is left above the time of its bytes: all workgroups are resident at once and read, then write, in step.
-template <typename T, typename TB, int RT>
-__global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 ? 2 : 4) void shrink_expand_kernel(
+template <typename T, typename TB, int RT, bool ODD>
+__global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 || (RT == 4 && ODD) ? 2 : 4) void shrink_expand_kernel(
     const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, const T* __restrict__ B, int F, Adapters a, int scaled, float* __restrict__ U,
     const TB* base, int64_t ldbase, T* Y) {
     constexpr bool k16 = std::is_same_v<T, bf16> && sizeof(TB) == 2;          // (with an fp32 base its registers are not left)
@@ -377,7 +401,7 @@ __global__ __launch_bounds__(64 * kShrinkWaves, sizeof(T) == 4 ? 2 : 4) void shr
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * 16;
     const int id = adapter_of(a, t0 + m);
     v4f out[RT];
-    shrink_tile<T, RT>(X + min(t0 + m, static_cast<int64_t>(a.T) - 1) * ldx, A, K, a, id, 0, out);
+    shrink_tile<T, RT, ODD>(X + min(t0 + m, static_cast<int64_t>(a.T) - 1) * ldx, A, K, a, id, 0, out);
     shrink_join<RT>(out, sums, [&](int token, int row, float u) {
         const int who = adapter_of(a, t0 + token);
         const float by = who < 0 ? 0.f : u * scale_of(a, who);
@@ -412,30 +436,43 @@ __global__ __launch_bounds__(256) void expand_narrow_kernel(const float* __restr
     }
 }
 
-// Few tokens: a lane takes eight columns of one.
+// Few tokens: a lane takes eight columns of one, the last eight of a row, and stores those that are its own, where fewer are left (read one by one there,
+// r = 24, rows of 8005 and 2672, bf16: 10.4 us on average, now 6.5).
 template <typename T, typename TB>
 __global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict__ U, const T* __restrict__ B, int F, Adapters a, int scaled,
                                                         const TB* base, int64_t ldbase, T* Y) {
+    DAB_RESERVE_VGPRS();
     const int64_t t = blockIdx.y, f64 = (static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x) * 8;
     if (f64 >= F) return;
-    const int f = static_cast<int>(f64), id = adapter_of(a, t);
-    float y[8] = {}, v[8] = {};
-    if (base) load8(base + t * ldbase, f, F, y);
-    if (id >= 0) {
-        const T* rows = B + static_cast<int64_t>(id) * a.r * F;
-        const float s = scaled ? scale_of(a, id) : 1.f;
-#pragma unroll 4
-        for (int row = 0; row < a.r; ++row) {
-            float b[8];
-            load8(rows + static_cast<int64_t>(row) * F, f, F, b);
-            const float u = U[t * a.r + row] * s;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += u * b[i];
+    const int id = adapter_of(a, t);
+    const T* rows = B + static_cast<int64_t>(max(id, 0)) * a.r * F;
+    const float s = id >= 0 && scaled ? scale_of(a, id) : 1.f;
+    const float* u = U + t * a.r;
+    const int r = id >= 0 ? a.r : 0;
+    if (F < kNarrow) {
+        for (int c = 0; c < F; ++c) {
+            float v = 0.f;
+            for (int row = 0; row < r; ++row) v += (u[row] * s) * static_cast<float>(rows[static_cast<int64_t>(row) * F + c]);
+            Y[t * F + c] = static_cast<T>((base ? static_cast<float>(base[t * ldbase + c]) : 0.f) + v);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] += v[i];
+        return;
     }
-    store8(Y + t * F, f, F, y);
+    const int f = static_cast<int>(min(f64, static_cast<int64_t>(F) - 8)), again = static_cast<int>(f64) - f;
+    Eight<TB> y;
+    y.v = {};
+    if (base) y.load(base + t * ldbase, f);
+    float v[8] = {};
+#pragma unroll 8
+    for (int row = 0; row < r; ++row) {
+        Eight<T> b;
+        b.load(rows + static_cast<int64_t>(row) * F, f);
+        const float by = u[row] * s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += by * b[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += y[i];
+    store_own(Y + t * F + f, again, v);
 }
 
 // ---------------------------------------------------------------- outer
@@ -686,6 +723,8 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const Join j) {
 constexpr int kMaxRank = 256, kAdapterCols = 1 << 21;         // (a row block of an adapter and sixteen tokens stay below 2^32 bytes)
 constexpr int64_t kAdapterLd = 1 << 25;
 
+static bool odd_rows(int64_t ldx, int K) { return ((ldx | K) & 1) != 0; }
+
 template <typename T>
 static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
     // A workgroup for every token and row, or for sixteen tokens: the one's time grows with both, the other's with k alone until its workgroups fill the
@@ -698,9 +737,13 @@ static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a,
     if (K < kNarrow)
         return launch(shrink_narrow_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(ceil_div64(static_cast<int64_t>(a.T) * a.r, 256), 1 << 20))), dim3(256),
                       0, st, X, ldx, A, K, a, s, U);
-    if (a.r <= 16) return launch(shrink_kernel<T, 1>, dim3(tiles), block, 0, st, X, ldx, A, K, a, s, U);
-    if (a.r <= 32) return launch(shrink_kernel<T, 2>, dim3(tiles), block, 0, st, X, ldx, A, K, a, s, U);
-    return launch(shrink_kernel<T, 4>, dim3(tiles, ceil_div(a.r, 64)), block, 0, st, X, ldx, A, K, a, s, U);
+    const auto go = [&](auto odd) {
+        constexpr bool ODD = sizeof(T) == 2 && decltype(odd)::value;
+        if (a.r <= 16) return launch(shrink_kernel<T, 1, ODD>, dim3(tiles), block, 0, st, X, ldx, A, K, a, s, U);
+        if (a.r <= 32) return launch(shrink_kernel<T, 2, ODD>, dim3(tiles), block, 0, st, X, ldx, A, K, a, s, U);
+        return launch(shrink_kernel<T, 4, ODD>, dim3(tiles, ceil_div(a.r, 64)), block, 0, st, X, ldx, A, K, a, s, U);
+    };
+    return odd_rows(ldx, K) ? go(std::true_type{}) : go(std::false_type{});
 }
 
 template <typename T, typename TB>
@@ -727,8 +770,12 @@ static int expand(const float* U, const T* B, int F, const Adapters& a, bool sca
 template <typename T, typename TB, int RT>
 static int shrink_expand_from(const T* X, int64_t ldx, const T* A, int K, const T* B, int F, const Adapters& a, bool scaled, float* U, const Base& base, T* Y,
                               hipStream_t st) {
-    return launch(shrink_expand_kernel<T, TB, RT>, dim3(static_cast<unsigned>(ceil_div64(a.T, 16))), dim3(64 * kShrinkWaves), 0, st, X, ldx, A, K, B, F, a,
-                  static_cast<int>(scaled), U, static_cast<const TB*>(base.p), base.ld, Y);
+    const auto go = [&](auto odd) {
+        constexpr bool ODD = sizeof(T) == 2 && decltype(odd)::value;
+        return launch(shrink_expand_kernel<T, TB, RT, ODD>, dim3(static_cast<unsigned>(ceil_div64(a.T, 16))), dim3(64 * kShrinkWaves), 0, st, X, ldx, A, K, B, F,
+                      a, static_cast<int>(scaled), U, static_cast<const TB*>(base.p), base.ld, Y);
+    };
+    return odd_rows(ldx, K) ? go(std::true_type{}) : go(std::false_type{});
 }
 template <typename T>
 static int shrink_expand(const T* X, int64_t ldx, const T* A, int K, const T* B, int F, const Adapters& a, bool scaled, float* U, const Base& base, T* Y,

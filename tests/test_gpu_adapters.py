@@ -169,6 +169,31 @@ def test_the_smallest_f16_numbers_count(T):
     assert torch.equal(dX, on_gpu(dXo * 2.0 ** -24, torch.float16)) and np.array_equal(f64(dA), dAo * 2.0 ** -48) and np.array_equal(f64(dB), dBo * 2.0 ** -48)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("r", [5, 24, 64, 70])
+@pytest.mark.parametrize("T,K,F,gap", [(200, 1337, 4099, 0), (200, 1337, 301, 6), (300, 600, 264, 1), (4200, 9, 1031, 4), (41, 771, 8, 1), (41, 7, 15, 2)])
+def test_rows_at_odd_distances(dtype, r, T, K, F, gap):
+    """16-bit rows every other one of which lies between two words; what is between the rows, NaN, does not get in."""
+    rng = np.random.default_rng(T + K + F + r)
+    n = 3
+    X, A, B, dY, scale, base, dbase = whole_numbers(rng, T, K, F, n, r)
+    a, b, s = on_gpu(A, dtype), on_gpu(B, dtype), on_gpu(scale, torch.float32)
+
+    def apart(m):
+        wide = torch.full((T, m.shape[1] + gap), float("nan"), dtype=dtype, device=DEV)
+        wide[:, :m.shape[1]] = on_gpu(m, dtype)
+        return wide[:, :m.shape[1]]
+    for form in ("runs", "any"):
+        ids = who(rng, T, n, form)
+        i = on_gpu(ids, torch.int32)
+        Y, Ug = dab.dab_adapters(apart(X), i, a, b, s, base=apart(base))
+        Yo, Uo = oa.adapters(X, ids, A, B, scale, base)
+        assert np.array_equal(f64(Ug), Uo) and torch.equal(Y, on_gpu(Yo, dtype))
+        dX, dA, dB = dab.dab_adapters_gradient(apart(dY), apart(X), Ug, i, a, b, s, base=apart(dbase))
+        dXo, dAo, dBo = oa.adapters_gradient(dY, X, Uo, ids, A, B, scale, dbase)
+        assert torch.equal(dX, on_gpu(dXo, dtype)) and np.array_equal(f64(dA), dAo) and np.array_equal(f64(dB), dBo)
+
+
 def test_more_tiles_of_tokens_than_a_grid_has_along_one_dimension():
     T, K, F, n, r = 600001, 16, 8, 2, 65                           # (a rank of two row blocks: U and Y in launches of their own)
     g = torch.Generator(device=DEV).manual_seed(5)
