@@ -20,6 +20,39 @@ struct NormGeom {
     float eps;
 };
 
+// Eight values of a row from column c on.  Where fewer are left they are the row's last eight, the first again_of() of which another lane has: loads
+// without a branch for each value (one by one, every row of 8192 x 4095 waited for them: its gradients 93 us and 12 for joining, now 59 and 5; 8192 x 4096 54 and
+// 5).  Shorter rows: zeros behind them.
+__device__ __forceinline__ int place_of(int c, int cols) { return cols < 8 ? c : min(c, cols - 8); }
+__device__ __forceinline__ int again_of(int c, int cols) { return c - place_of(c, cols); }
+template <typename T>
+__device__ __forceinline__ void row8(const T* row, int c, int cols, float (&v)[8]) {
+    if (cols < 8) {
+        load8(row, c, cols, v);
+    } else {
+        const auto eight = *reinterpret_cast<const typename Unaligned<T, 8>::type*>(row + place_of(c, cols));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(eight[i]);
+    }
+}
+// Zeros in place of another lane's.
+__device__ __forceinline__ void drop(int again, float (&v)[8]) {
+    if (again > 0)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < again ? 0.f : v[i];
+}
+template <typename T>
+__device__ __forceinline__ void put8(T* row, int c, int cols, const float (&v)[8]) {
+    const int again = again_of(c, cols);
+    if (again == 0) {
+        store8(row, c, cols, v);
+    } else {
+#pragma unroll
+        for (int i = 1; i < 8; ++i)
+            if (i >= again) row[c - again + i] = static_cast<T>(v[i]);
+    }
+}
+
 // The sum over the 2^LOG lanes of a row; buffer: one of two, so that a barrier stands between a value's last reader and its next writer.
 template <int LOG>
 __device__ __forceinline__ float row_sum(float v, float (&part)[2][16], int buffer) {
@@ -37,6 +70,15 @@ __device__ __forceinline__ float row_sum(float v, float (&part)[2][16], int buff
     return v;
 }
 
+// The lane's own values, those behind the first `again`, moved to the front, zeros behind them.
+__device__ __forceinline__ void own_first(int again, float (&y)[8]) {
+    if (again == 0) return;
+#pragma unroll
+    for (int by = 4; by > 0; by >>= 1)
+        if (again & by)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = i + by < 8 ? y[(i + by) & 7] : 0.f;
+}
 // Eight values of y as bytes with their group's scale, as dab_ckpt8_save() writes them.
 __device__ __forceinline__ void save_eight(const float (&y)[8], int64_t row_groups, int c, int8_t* __restrict__ Q, uint8_t* __restrict__ S) {
     const uint32_t m = group_max(y);
@@ -75,14 +117,15 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_kernel
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[j][i] = 0.f;
         if (live && c < g.cols) {
-            load8(X + row * g.ldx, c, g.cols, h[j]);
+            row8(X + row * g.ldx, c, g.cols, h[j]);
             if (R) {
                 float r[8];
-                load8(R + row * g.ldr, c, g.cols, r);
+                row8(R + row * g.ldr, c, g.cols, r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[j][i] = static_cast<float>(static_cast<T>(h[j][i] + r[i]));
-                store8(H + row * g.cols, c, g.cols, h[j]);
+                put8(H + row * g.cols, c, g.cols, h[j]);
             }
+            drop(again_of(c, g.cols), h[j]);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += h[j][i] * h[j][i];
@@ -96,13 +139,16 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_kernel
         const int c = (j * kLanes + lane) * 8;
         float y[8] = {};
         if (c < g.cols) {
-            load8(gain, c, g.cols, y);
+            row8(gain, c, g.cols, y);
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = (h[j][i] * scale) * y[i];
-            if (Y) store8(Y + row * g.cols, c, g.cols, y);
+            if (Y) put8(Y + row * g.cols, c, g.cols, y);
         }
         // (the four lanes of a group are all here, those past the row's end with zeros)
-        if (Q && c < g.groups * 32) save_eight(y, row * g.groups, c, Q, S);
+        if (Q && c < g.groups * 32) {
+            if (c < g.cols) own_first(again_of(c, g.cols), y);
+            save_eight(y, row * g.groups, c, Q, S);
+        }
     }
 }
 
@@ -118,14 +164,15 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const T* R,
     for (int64_t c0 = threadIdx.x * 8; c0 < g.cols; c0 += 8192) {
         const int c = static_cast<int>(c0);
         float h[8];
-        load8(x, c, g.cols, h);
+        row8(x, c, g.cols, h);
         if (R) {
             float r[8];
-            load8(R + row * g.ldr, c, g.cols, r);
+            row8(R + row * g.ldr, c, g.cols, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = static_cast<float>(static_cast<T>(h[i] + r[i]));
-            store8(hout, c, g.cols, h);
+            put8(hout, c, g.cols, h);
         }
+        drop(again_of(c, g.cols), h);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += h[i] * h[i];
     }
@@ -136,20 +183,24 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const T* R,
         const int c = static_cast<int>(c0);
         float h[8] = {}, y[8] = {};
         if (c < g.cols) {
-            load8(R ? static_cast<const T*>(hout) : x, c, g.cols, h);
-            load8(gain, c, g.cols, y);
+            row8(R ? static_cast<const T*>(hout) : x, c, g.cols, h);
+            row8(gain, c, g.cols, y);
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = (h[i] * scale) * y[i];
-            if (Y) store8(Y + row * g.cols, c, g.cols, y);
+            if (Y) put8(Y + row * g.cols, c, g.cols, y);
+            own_first(again_of(c, g.cols), y);
         }
         if (Q) save_eight(y, row * g.groups, c, Q, S);
     }
 }
 
 // ---------------------------------------------------------------- gradients
+// Columns of a part of dgain, with up to three behind the row's, so that every part is read in fours.
+__host__ __device__ __forceinline__ int64_t part_ld(int cols) { return (static_cast<int64_t>(cols) + 3) & ~int64_t{3}; }
+
 // A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it holds at once) and keeps its part of dgain in registers meanwhile, that of
 // its rows' lanes together in LDS at the end; norm_join_kernel adds the workgroups' parts in a fixed order.  (Every row's lanes with a part of their
-// own: 1999 x 1003 fp32 11.8 us and 37 for joining 2000 parts, now 9.7 and 3.8.)  Two eights a lane: gain and the part of dgain stay in registers too.
+// own: 1999 x 1003 fp32 11.8 us and 37 for joining 2000 parts, now 9.5 and 2.9.)  Two eights a lane: gain and the part of dgain stay in registers too.
 template <typename T, int LOG, int NV>
 __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_kernel(const T* dY, const T* H, const float* __restrict__ gain,
                                                                                      const float* __restrict__ rstd, const T* dH, NormGeom g, T* dX,
@@ -164,7 +215,7 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_k
         const int c = (j * kLanes + lane) * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i) dg[j][i] = 0.f, gn[j][i] = 0.f;
-        if (c < g.cols) load8(gain, c, g.cols, gn[j]);
+        if (c < g.cols) row8(gain, c, g.cols, gn[j]), drop(again_of(c, g.cols), gn[j]);
     }
     int buffer = 0;
     for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < g.rows; row0 += static_cast<int64_t>(gridDim.x) * kRows, buffer ^= 1) {
@@ -179,8 +230,9 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_k
 #pragma unroll
             for (int i = 0; i < 8; ++i) n[j][i] = 0.f, w[j][i] = 0.f;
             if (live && c < g.cols) {
-                load8(dY + row * g.ldx, c, g.cols, w[j]);
-                load8(H + row * g.ldr, c, g.cols, n[j]);
+                row8(dY + row * g.ldx, c, g.cols, w[j]);
+                row8(H + row * g.ldr, c, g.cols, n[j]);
+                drop(again_of(c, g.cols), w[j]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -197,26 +249,27 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_k
             const int c = (j * kLanes + lane) * 8;
             if (c >= g.cols) continue;
             float d[8] = {};
-            if (dH) load8(dH + row * g.ldd, c, g.cols, d);
+            if (dH) row8(dH + row * g.ldd, c, g.cols, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] += (w[j][i] - n[j][i] * dot) * s;
-            store8(dX + row * g.cols, c, g.cols, d);
+            put8(dX + row * g.cols, c, g.cols, d);
         }
     }
-    float* to = parts + static_cast<int64_t>(blockIdx.x) * g.cols;
+    float* to = parts + static_cast<int64_t>(blockIdx.x) * part_ld(g.cols);
     if constexpr (kRows == 1) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * kLanes + lane) * 8;
-            if (c < g.cols) store8(to, c, g.cols, dg[j]);
+            if (c < g.cols) put8(to, c, g.cols, dg[j]);
         }
     } else {
         constexpr int kCols = kLanes * NV * 8;
         __shared__ float all[kRows][kCols];
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) all[slot][(j * kLanes + lane) * 8 + i] = dg[j][i];
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * kLanes + lane) * 8;
+            if (c < g.cols) put8(all[slot], c, g.cols, dg[j]);
+        }
         __syncthreads();
         for (int c = threadIdx.x; c < g.cols; c += kNormThreads) {
             float v = 0.f;
@@ -232,7 +285,8 @@ template <typename T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* dY, const T* H, const float* __restrict__ gain, const float* __restrict__ rstd,
                                                               const T* dH, NormGeom g, T* dX, float* parts) {
     __shared__ float part[2][16];
-    float* to = parts + static_cast<int64_t>(blockIdx.x) * g.cols;
+    DAB_RESERVE_VGPRS();
+    float* to = parts + static_cast<int64_t>(blockIdx.x) * part_ld(g.cols);
     int buffer = 0;
     for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x, buffer ^= 1) {
         const float s = rstd[row];
@@ -240,25 +294,26 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* dY, const
         for (int64_t c0 = threadIdx.x * 8; c0 < g.cols; c0 += 8192) {
             const int c = static_cast<int>(c0);
             float w[8], n[8], gn[8], dg[8] = {};
-            load8(dY + row * g.ldx, c, g.cols, w), load8(H + row * g.ldr, c, g.cols, n), load8(gain, c, g.cols, gn);
-            if (row != blockIdx.x) load8(static_cast<const float*>(to), c, g.cols, dg);
+            row8(dY + row * g.ldx, c, g.cols, w), row8(H + row * g.ldr, c, g.cols, n), row8(gain, c, g.cols, gn);
+            if (row != blockIdx.x) row8(static_cast<const float*>(to), c, g.cols, dg);
+            drop(again_of(c, g.cols), w), drop(again_of(c, g.cols), gn);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 n[i] *= s;
                 dg[i] += w[i] * n[i];
                 dot += (w[i] * gn[i]) * n[i];
             }
-            store8(to, c, g.cols, dg);
+            put8(to, c, g.cols, dg);
         }
         dot = row_sum<10>(dot, part, buffer) / static_cast<float>(g.cols);
         for (int64_t c0 = threadIdx.x * 8; c0 < g.cols; c0 += 8192) {
             const int c = static_cast<int>(c0);
             float w[8], n[8], gn[8], d[8] = {};
-            load8(dY + row * g.ldx, c, g.cols, w), load8(H + row * g.ldr, c, g.cols, n), load8(gain, c, g.cols, gn);
-            if (dH) load8(dH + row * g.ldd, c, g.cols, d);
+            row8(dY + row * g.ldx, c, g.cols, w), row8(H + row * g.ldr, c, g.cols, n), row8(gain, c, g.cols, gn);
+            if (dH) row8(dH + row * g.ldd, c, g.cols, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] += (w[i] * gn[i] - (n[i] * s) * dot) * s;
-            store8(dX + row * g.cols, c, g.cols, d);
+            put8(dX + row * g.cols, c, g.cols, d);
         }
     }
 }
@@ -270,18 +325,15 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* __restrict
     DAB_RESERVE_VGPRS();
     const int slice = threadIdx.x >> 3, c = blockIdx.x * 32 + (threadIdx.x & 7) * 4;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c + 4 <= cols) {
+    if (c < cols) {
+        const float* from = parts + c;
+        const int64_t ld = part_ld(cols);
 #pragma unroll 8
         for (int i = slice; i < n; i += 128) {
-            const auto got = *reinterpret_cast<const Unaligned<float, 4>::type*>(parts + static_cast<int64_t>(i) * cols + c);
+            const v4f got = *reinterpret_cast<const v4f*>(from + i * ld);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] += got[k];
         }
-    } else {
-        for (int i = slice; i < n; i += 128)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < cols) v[k] += parts[static_cast<int64_t>(i) * cols + c + k];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) sums[slice][(threadIdx.x & 7) * 4 + k] = v[k];
@@ -438,7 +490,7 @@ extern "C" size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t co
     if (rows < 1 || cols < 1 || cols > kNormMaxCols) return 0;
     const NormForm f = norm_form(cols, kNormGradNV);
     const int blocks = norm_grad_blocks(rows, f);
-    return blocks == 1 ? 0 : static_cast<size_t>(blocks) * cols * 4;
+    return blocks == 1 ? 0 : static_cast<size_t>(blocks) * part_ld(cols) * 4;
 }
 
 extern "C" int dab_rms_norm_gradient(const void* dY, int64_t lddy, const void* H, int64_t ldh, int32_t dtype, const float* gain, const float* rstd,

@@ -153,6 +153,34 @@ def test_values_at_the_edges():
     assert bool(zero[2].isinf().all()) and bool(zero[0].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [9, 37, 131, 515, 4097, 33003])
+def test_what_the_last_columns_neighbours_hold(dtype, cols):
+    """A row's last few columns are read with those before them, whose infinities and NaN stay where they are."""
+    x, r, gain, dy, dh = inputs(5, cols, dtype, 3)
+    at, own = cols - 8, cols % 8                                    # read again; columns of the last lane
+    Y, H, rstd, (q, s) = dab.dab_rms_norm(x, gain, r, save=True)
+    dX, dgain = dab.dab_rms_norm_gradient(dy, H, gain, rstd, dh)
+    group = at // 32
+    for bad in (float("inf"), float("nan")):
+        wrong = gain.clone()
+        wrong[at] = bad
+        Yb, Hb, rb, (qb, sb) = dab.dab_rms_norm(x, wrong, r, save=True)
+        rest = [c for c in range(cols) if c != at]
+        assert torch.equal(Hb, H) and torch.equal(rb, rstd) and torch.equal(Yb[:, rest], Y[:, rest]) and not torch.isfinite(Yb[:, at].float()).any()
+        groups = [g for g in range(s.shape[1]) if g != group]
+        assert torch.all(sb[:, group] == 255) and torch.equal(sb[:, groups], s[:, groups])
+        for g in groups:
+            assert torch.equal(qb[:, 32 * g:32 * g + 32], q[:, 32 * g:32 * g + 32])
+        far = dy.clone()
+        far[2, at] = bad                                            # the whole row's dX, but one column's dgain
+        dXb, dgb = dab.dab_rms_norm_gradient(far, H, gain, rstd, dh)
+        others = [0, 1, 3, 4]
+        assert torch.equal(dXb[others], dX[others]) and torch.isnan(dXb[2].float()).any()
+        assert torch.equal(dgb[rest], dgain[rest]) and not torch.isfinite(dgb[at])
+    assert own != 0
+
+
 def test_nothing_behind_the_outputs_is_written():
     rows, cols = 3, 45
     x, r, gain, dy, dh = inputs(rows, cols, torch.bfloat16)
