@@ -35,6 +35,11 @@ struct Some {
             for (int i = 0; i < N; ++i) v[i] = c + i < cols ? row[c + i] : static_cast<T>(0.f);
         }
     }
+    // those from column c on, or the row's last N where fewer are left (of rows of N columns at least)
+    __device__ __forceinline__ void load_last(const T* row, int c, int cols) {
+        if (cols < N) load(row, c, cols);
+        else load(row, min(c, cols - N));
+    }
     __device__ __forceinline__ float operator[](int i) const { return static_cast<float>(v[i]); }
 };
 template <typename T>
@@ -64,7 +69,17 @@ __device__ __forceinline__ void shrink_few(const T* __restrict__ X, int64_t ldx,
         for (int u = 0; u < 4; ++u) {
             const int64_t k = k0 + u * 2048;
             p[u].v = {}, q[u].v = {};
-            if (k < K) p[u].load(x, static_cast<int>(k), K), q[u].load(w, static_cast<int>(k), K);
+            if (k < K) p[u].load_last(x, static_cast<int>(k), K), q[u].load_last(w, static_cast<int>(k), K);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            // (the last few k: those of the last eight that no lane before has)
+            const int64_t k = k0 + u * 2048;
+            const int again = K >= 8 && k < K ? static_cast<int>(k) - (K - 8) : 0;
+            if (again > 0)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < again) p[u].v[i] = q[u].v[i] = static_cast<T>(0.f);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)

@@ -197,6 +197,7 @@ __global__ __launch_bounds__(256) void shrink_narrow_kernel(const T* __restrict_
 template <typename T>
 __global__ __launch_bounds__(256) void shrink_few_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ A, int K, Adapters a, int scaled,
                                                          float* __restrict__ U) {
+    DAB_RESERVE_VGPRS();
     shrink_few(X, ldx, A, K, a, scaled != 0, blockIdx.x, U);
 }
 

@@ -70,15 +70,6 @@ __device__ __forceinline__ float row_sum(float v, float (&part)[2][16], int buff
     return v;
 }
 
-// The lane's own values, those behind the first `again`, moved to the front, zeros behind them.
-__device__ __forceinline__ void own_first(int again, float (&y)[8]) {
-    if (again == 0) return;
-#pragma unroll
-    for (int by = 4; by > 0; by >>= 1)
-        if (again & by)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = i + by < 8 ? y[(i + by) & 7] : 0.f;
-}
 // Eight values of y as bytes with their group's scale, as dab_ckpt8_save() writes them.
 __device__ __forceinline__ void save_eight(const float (&y)[8], int64_t row_groups, int c, int8_t* __restrict__ Q, uint8_t* __restrict__ S) {
     const uint32_t m = group_max(y);

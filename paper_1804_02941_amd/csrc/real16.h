@@ -82,6 +82,16 @@ __device__ __forceinline__ void store8(T* row, int c, int cols, const float (&v)
     }
 }
 
+// Eight values without the first `again`, the others moved to the front, zeros behind them.
+__device__ __forceinline__ void own_first(int again, float (&y)[8]) {
+    if (again == 0) return;
+#pragma unroll
+    for (int by = 4; by > 0; by >>= 1)
+        if (again & by)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = i + by < 8 ? y[(i + by) & 7] : 0.f;
+}
+
 // Largest magnitude, as bits (those of a NaN are larger than those of any number), over the four lanes that hold a group.
 __device__ __forceinline__ uint32_t group_max(const float (&v)[8]) {
     uint32_t m = 0;

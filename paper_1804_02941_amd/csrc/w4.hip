@@ -178,6 +178,7 @@ __global__ __launch_bounds__(256) void w4_tokens_kernel(const T* __restrict__ X,
 template <typename T>
 __global__ __launch_bounds__(256) void w4_tokens_shrink_kernel(const T* __restrict__ X, W4Tokens g, int blocks, bf16* __restrict__ out, const T* __restrict__ A,
                                                                Adapters a, float* __restrict__ U) {
+    DAB_RESERVE_VGPRS();
     const int pass = blockIdx.x / max(blocks, 1), passes = (g.B + g.nb - 1) / g.nb;
     if (blocks > 0 && pass < passes) {
         w4_tokens(X, g, blockIdx.x - pass * blocks, pass, out);
@@ -238,27 +239,31 @@ struct W4Rows {
             const int row = q * LANES + lane;
             b[q].v = {}, u[q] = 0.f;
             if (id >= 0 && row < w.a.r) {
-                b[q].load(static_cast<const T*>(w.B) + (static_cast<int64_t>(id) * w.a.r + row) * F, f, F);
+                b[q].load_last(static_cast<const T*>(w.B) + (static_cast<int64_t>(id) * w.a.r + row) * F, f, F);
                 u[q] = w.U[t * w.a.r + row];
             }
         }
     }
     // y += the lane's part of U_t B_i
     __device__ __forceinline__ void add(const W4Adapters& w, int64_t t, int f, int F, int lane, float (&y)[8]) const {
+        if (id < 0) return;
+        float v[8] = {};
 #pragma unroll
         for (int q = 0; q < ROWS; ++q)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] += u[q] * b[q][i];
-        if (id < 0) return;
+            for (int i = 0; i < 8; ++i) v[i] += u[q] * b[q][i];
         const T* rows = static_cast<const T*>(w.B) + static_cast<int64_t>(id) * w.a.r * F;
 #pragma unroll 4
         for (int row = ROWS * LANES + lane; row < w.a.r; row += LANES) {
             Eight<T> c;
-            c.load(rows + static_cast<int64_t>(row) * F, f, F);
+            c.load_last(rows + static_cast<int64_t>(row) * F, f, F);
             const float by = w.U[t * w.a.r + row];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] += by * c[i];
+            for (int i = 0; i < 8; ++i) v[i] += by * c[i];
         }
+        if (F >= 8) own_first(max(f - (F - 8), 0), v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] += v[i];
     }
 };
 struct NoAdapters {};
