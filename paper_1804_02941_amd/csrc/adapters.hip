@@ -71,6 +71,7 @@ struct Long<T, true> {
 // Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth stretch of 128 k (RT = 1, 16-bit types), whose
 // loads are in flight at once, those of the next one behind them.  This lane's sums over its wavefront's k: rows 4 (lane / 16) .. + 3 of
 // each sixteen from r0 on, of token lane % 16.
+// (sixteen wavefronts a tile where tiles do not fill the chip: 1024 x 4096 bf16 11.5 us, with eight 11.1.)
 constexpr int kShrinkWaves = 8;
 template <typename T, int RT, bool ODD>
 __device__ __forceinline__ void shrink_tile(const T* __restrict__ x, const T* __restrict__ A, int K, const Adapters& a, int id, int r0, v4f (&out)[RT]) {
