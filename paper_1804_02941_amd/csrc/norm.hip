@@ -271,6 +271,88 @@ __global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_k
     }
 }
 
+// Few rows: a workgroup takes rows, for dX, or 32 columns, for dgain, which needs no sum over a row: one launch, nothing to join, and dY and H read twice.
+// first: the number of the launch's first workgroup (dX over dY or H: one launch for the columns, another one behind it for the rows).
+template <typename T, int LOG, int NV>
+__global__ __launch_bounds__(LOG > 8 ? 1 << LOG : kNormThreads) void norm_grad_few_kernel(const T* dY, const T* H, const float* __restrict__ gain,
+                                                                                         const float* __restrict__ rstd, const T* dH, NormGeom g, T* dX,
+                                                                                         float* __restrict__ dgain, int row_blocks, int first) {
+    constexpr int kLanes = 1 << LOG, kRows = LOG > 8 ? 1 : kNormThreads >> LOG, kThreads = kLanes * kRows;
+    __shared__ float part[2][16];
+    __shared__ float sums[kThreads / 4][33];
+    DAB_RESERVE_VGPRS();
+    const int block = blockIdx.x + first;
+    if (block >= row_blocks) {
+        // four lanes for a row's 32 columns
+        const int c0 = (block - row_blocks) * 32, c = c0 + (threadIdx.x & 3) * 8, slice = threadIdx.x >> 2;
+        float v[8] = {};
+        if (c < g.cols) {
+#pragma unroll 4
+            for (int64_t row = slice; row < g.rows; row += kThreads / 4) {
+                float w[8], n[8];
+                const float s = rstd[row];
+                row8(dY + row * g.ldx, c, g.cols, w), row8(H + row * g.ldr, c, g.cols, n);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += w[i] * (n[i] * s);
+            }
+            own_first(again_of(c, g.cols), v);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[slice][(threadIdx.x & 3) * 8 + i] = v[i];
+        __syncthreads();
+        // eight slices by each half wavefront, then those sums
+        const int col = threadIdx.x & 31, share = threadIdx.x >> 5;
+        float w = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w += sums[share * 8 + i][col];
+        __syncthreads();
+        sums[share][col] = w;
+        __syncthreads();
+        if (share != 0 || c0 + col >= g.cols) return;
+        w = 0.f;
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i) w += sums[i][col];
+        dgain[c0 + col] = w;
+        return;
+    }
+    const int lane = threadIdx.x & (kLanes - 1);
+    const int64_t row = static_cast<int64_t>(block) * kRows + (threadIdx.x >> LOG);
+    const bool live = row < g.rows;
+    const float s = live ? rstd[row] : 0.f;
+    float n[NV][8], w[NV][8], d[NV][8];
+    float dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * kLanes + lane) * 8;
+        float gn[8] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[j][i] = 0.f, w[j][i] = 0.f, d[j][i] = 0.f;
+        if (live && c < g.cols) {
+            row8(gain, c, g.cols, gn);
+            row8(dY + row * g.ldx, c, g.cols, w[j]);
+            row8(H + row * g.ldr, c, g.cols, n[j]);
+            if (dH) row8(dH + row * g.ldd, c, g.cols, d[j]);
+            drop(again_of(c, g.cols), w[j]), drop(again_of(c, g.cols), gn);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            n[j][i] *= s;
+            w[j][i] *= gn[i];
+            dot += w[j][i] * n[j][i];
+        }
+    }
+    dot = row_sum<LOG>(dot, part, 0) / static_cast<float>(g.cols);
+    if (!live) return;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * kLanes + lane) * 8;
+        if (c >= g.cols) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[j][i] += (w[j][i] - n[j][i] * dot) * s;
+        put8(dX + row * g.cols, c, g.cols, d[j]);
+    }
+}
+
 // Rows that no workgroup holds: the workgroup's part of dgain lies in its row of `parts` meanwhile.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* dY, const T* H, const float* __restrict__ gain, const float* __restrict__ rstd,
@@ -421,8 +503,39 @@ static int norm_grad_blocks(int rows, NormForm f) {
     if (n >= most) return static_cast<int>(most);
     return static_cast<int>(n <= kNumCU ? n : (n + 1) / 2);
 }
+// Up to this many rows, and elements: the columns' workgroups are few and read every row.  us, one launch and two: 5 x 2000 fp32 6.1 and 9.0, 512 x 2000
+// bf16 8.5 and 9.6, 512 x 4096 8.7 and 12.6, 128 x 16384 8.8 and 14.6; past them, 1024 x 2000 16.3 and 12.5, 512 x 16384 25.9 and 20.4.
+static bool norm_grad_few(int rows, int cols) { return rows <= 512 && cols <= 16384 && rows * cols <= 1 << 21; }
+template <typename T, int LOG, int NV>
+static int norm_grad_few_launch(const NormGradArgs<T>& a, hipStream_t st) {
+    const NormForm f{LOG, NV};
+    const int rows = static_cast<int>(ceil_div64(a.g.rows, norm_rows(f))), columns = ceil_div(a.g.cols, 32);
+    const auto go = [&](int first, int blocks) {
+        return launch(norm_grad_few_kernel<T, LOG, NV>, dim3(blocks), dim3(norm_threads(f)), 0, st, a.dY, a.H, a.gain, a.rstd, a.dH, a.g, a.dX, a.dgain, rows,
+                      first);
+    };
+    if (a.dX != a.dY && a.dX != a.H) return go(0, rows + columns);
+    const int rc = go(rows, columns);
+    return rc ? rc : go(0, rows);
+}
+template <typename T>
+static int norm_grad_few_launch(const NormGradArgs<T>& a, hipStream_t st) {
+    const NormForm f = norm_form(a.g.cols, a.g.cols <= 8192 ? 1 : 2);
+    switch (f.log) {
+        case 2: return norm_grad_few_launch<T, 2, 1>(a, st);
+        case 3: return norm_grad_few_launch<T, 3, 1>(a, st);
+        case 4: return norm_grad_few_launch<T, 4, 1>(a, st);
+        case 5: return norm_grad_few_launch<T, 5, 1>(a, st);
+        case 6: return norm_grad_few_launch<T, 6, 1>(a, st);
+        case 7: return norm_grad_few_launch<T, 7, 1>(a, st);
+        case 8: return norm_grad_few_launch<T, 8, 1>(a, st);
+        case 9: return norm_grad_few_launch<T, 9, 1>(a, st);
+        default: return f.nv == 1 ? norm_grad_few_launch<T, 10, 1>(a, st) : norm_grad_few_launch<T, 10, 2>(a, st);
+    }
+}
 template <typename T>
 static int norm_grad_launch(NormGradArgs<T> a, hipStream_t st) {
+    if (norm_grad_few(a.g.rows, a.g.cols)) return norm_grad_few_launch(a, st);
     const NormForm f = norm_form(a.g.cols, kNormGradNV);
     int rc;
     // (the part of a workgroup that has all rows is the gradient)
@@ -478,7 +591,7 @@ extern "C" int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const voi
 
 extern "C" size_t dab_rms_norm_gradient_workspace_bytes(int32_t rows, int32_t cols) {
     using namespace dab;
-    if (rows < 1 || cols < 1 || cols > kNormMaxCols) return 0;
+    if (rows < 1 || cols < 1 || cols > kNormMaxCols || norm_grad_few(rows, cols)) return 0;
     const NormForm f = norm_form(cols, kNormGradNV);
     const int blocks = norm_grad_blocks(rows, f);
     return blocks == 1 ? 0 : static_cast<size_t>(blocks) * part_ld(cols) * 4;

@@ -41,12 +41,13 @@ def test_norm(lib):
 
 
 def test_norm_gradient(lib):
-    need = lib.dab_rms_norm_gradient_workspace_bytes(100, 40)
+    need = lib.dab_rms_norm_gradient_workspace_bytes(1000, 40)
     assert need >= 160 and lib.dab_rms_norm_gradient_workspace_bytes(0, 40) == 0
-    assert lib.dab_rms_norm_gradient_workspace_bytes(2, 4096) == 0                 # a workgroup's rows
+    assert lib.dab_rms_norm_gradient_workspace_bytes(2, 4096) == 0                 # few rows: nothing to join
+    assert lib.dab_rms_norm_gradient_workspace_bytes(512, 4096) == 0 and lib.dab_rms_norm_gradient_workspace_bytes(513, 4096) > 0
     # parts for what the chip holds at once, not for every row
     assert lib.dab_rms_norm_gradient_workspace_bytes(1 << 24, 4096) < 1 << 27
-    ok = dict(dY=p, lddy=40, H=p, ldh=40, t=F32, g=p, rstd=p, dH=p, lddh=40, rows=100, cols=40, dX=p, dg=p, ws=p, n=need)
+    ok = dict(dY=p, lddy=40, H=p, ldh=40, t=F32, g=p, rstd=p, dH=p, lddh=40, rows=1000, cols=40, dX=p, dg=p, ws=p, n=need)
 
     def call(**k):
         return lib.dab_rms_norm_gradient(*{**ok, **k}.values(), None)

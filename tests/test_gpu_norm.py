@@ -96,6 +96,14 @@ def test_norm_gradient(dtype, rows, cols):
         assert np.all(np.abs(f64(dgain) - wgain) <= (rows + 3) * U * np.abs(f64(dy) * n).sum(axis=0) * 1.01 + 1e-30)
 
 
+# more rows than one launch with whole columns takes: parts of dgain, of every form
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(513, 1), (600, 7), (2100, 33), (1031, 64), (777, 100), (530, 200), (2050, 500), (520, 777), (1999, 1003), (523, 2000), (600, 4096),
+                                       (420, 5000), (257, 8200), (129, 16384)])
+def test_norm_gradient_of_many_rows(dtype, rows, cols):
+    test_norm_gradient(dtype, rows, cols)
+
+
 def test_many_rows():
     """More rows than the chip holds at once, so that workgroups take several, and rows of few values."""
     for rows, cols in ((40000, 40), (9001, 520), (70001, 8)):
@@ -113,8 +121,8 @@ def test_many_rows():
 
 @pytest.mark.parametrize("dtype", TYPES)
 def test_in_place(dtype):
-    for cols in (100, 4096, 40000):
-        x, r, gain, dy, dh = inputs(5, cols, dtype)
+    for rows, cols in ((5, 100), (5, 4096), (5, 40000), (600, 93)):
+        x, r, gain, dy, dh = inputs(rows, cols, dtype)
         Y, H, rstd, _ = dab.dab_rms_norm(x, gain, residual=r)
         a, b = x.clone(), r.clone()
         Y2, H2, _, _ = dab.dab_rms_norm(a, gain, residual=b, out=(a, b, None, None))      # the sum over the residual, the output over the input
@@ -128,6 +136,9 @@ def test_in_place(dtype):
             p, q = dy.clone(), dh.clone()
             got = dab.dab_rms_norm_gradient(p, H, gain, rstd, dH=q, out=((p, q)[i], None))
             assert torch.equal(got[0], dX) and torch.equal(got[1], dgain)
+        p = H.clone()
+        got = dab.dab_rms_norm_gradient(dy, p, gain, rstd, dH=dh, out=(p, None))
+        assert torch.equal(got[0], dX) and torch.equal(got[1], dgain)
 
 
 def test_values_at_the_edges():
@@ -154,10 +165,10 @@ def test_values_at_the_edges():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("cols", [9, 37, 131, 515, 4097, 33003])
-def test_what_the_last_columns_neighbours_hold(dtype, cols):
+@pytest.mark.parametrize("rows,cols", [(5, 9), (5, 37), (5, 131), (5, 515), (5, 4097), (5, 33003), (600, 37), (600, 515), (530, 4097)])
+def test_what_the_last_columns_neighbours_hold(dtype, rows, cols):
     """A row's last few columns are read with those before them, whose infinities and NaN stay where they are."""
-    x, r, gain, dy, dh = inputs(5, cols, dtype, 3)
+    x, r, gain, dy, dh = inputs(rows, cols, dtype, 3)
     at, own = cols - 8, cols % 8                                    # read again; columns of the last lane
     Y, H, rstd, (q, s) = dab.dab_rms_norm(x, gain, r, save=True)
     dX, dgain = dab.dab_rms_norm_gradient(dy, H, gain, rstd, dh)
@@ -175,7 +186,7 @@ def test_what_the_last_columns_neighbours_hold(dtype, cols):
         far = dy.clone()
         far[2, at] = bad                                            # the whole row's dX, but one column's dgain
         dXb, dgb = dab.dab_rms_norm_gradient(far, H, gain, rstd, dh)
-        others = [0, 1, 3, 4]
+        others = [row for row in range(rows) if row != 2]
         assert torch.equal(dXb[others], dX[others]) and torch.isnan(dXb[2].float()).any()
         assert torch.equal(dgb[rest], dgain[rest]) and not torch.isfinite(dgb[at])
     assert own != 0
@@ -208,11 +219,12 @@ def test_offsets_past_32_bits():
     assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
 
 
-def test_captured_and_on_another_stream():
-    x, r, gain, dy, dh = inputs(300, 1000, torch.bfloat16)
-    outs = [torch.empty_like(x), torch.empty_like(x), torch.empty(300, device=DEV), dab.ckpt8_outputs(300, 1000, torch.device(DEV))]
+@pytest.mark.parametrize("rows", [300, 900])
+def test_captured_and_on_another_stream(rows):
+    x, r, gain, dy, dh = inputs(rows, 1000, torch.bfloat16)
+    outs = [torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device=DEV), dab.ckpt8_outputs(rows, 1000, torch.device(DEV))]
     grads = [torch.empty_like(x), torch.empty(1000, device=DEV)]
-    ws = torch.empty(dab.lib().dab_rms_norm_gradient_workspace_bytes(300, 1000), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(dab.lib().dab_rms_norm_gradient_workspace_bytes(rows, 1000), dtype=torch.uint8, device=DEV)
 
     def work():
         dab.dab_rms_norm(x, gain, residual=r, save=True, out=tuple(outs))
