@@ -687,7 +687,8 @@ int dab_state8_save(const float* X, int64_t n, int32_t is_signed, uint8_t* Q, ui
  *   A       [n][r][K], B  [n][r][F] of dtype, contiguous.  r is at most 256, n 65535, T 2^25, K and F 2^21,
  *           the rows' distances (of dY and base too) 2^25
  *   base    [T][F] of dtype or fp32 (base_dtype), rows ldbase apart, or NULL for 0: any projection's output
- *   Y       [T][F] of dtype out.  May be base itself where that is of dtype and its rows are F apart; must not overlap X (DAB_ERR_UNSUPPORTED)
+ *   Y       [T][F] of dtype out.  May be base itself where that is of dtype and its rows are F apart (or T is 1); must not overlap base in
+ *           another way, nor X, nor lie between their rows (DAB_ERR_UNSUPPORTED)
  *   U       fp32 [T][r] out: what the gradient takes
  */
 int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, const void* A, const void* B, const float* scale, int32_t T, int32_t K,
@@ -701,7 +702,7 @@ int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int32_t* ids, 
  *   dY      [T][F] of dtype, rows lddy apart;  X, ids, A, B, scale  as for dab_adapters, U  what it returned
  *   base    [T][K] of dtype or fp32, rows ldbase apart, or NULL for 0: what the shared projection's gradient gives
  *   dX      [T][K] of dtype out, or NULL where it is not needed (base is NULL then).  May be base itself where that is of dtype and its rows are K
- *           apart; must not overlap X or dY (DAB_ERR_UNSUPPORTED)
+ *           apart (or T is 1); must not overlap base in another way, nor X, nor dY, nor lie between their rows (DAB_ERR_UNSUPPORTED)
  *   dA      fp32 [n][r][K] out, dB  fp32 [n][r][F] out, zeros for an adapter without tokens
  *   ws      dab_adapters_gradient_workspace_bytes(T, K, F, n, r) bytes, 256-byte aligned
  */

@@ -868,6 +868,11 @@ static int check_base(const void* base, int32_t dtype, int64_t ld, int32_t cols,
     if ((dtype != DAB_F32 && dtype != own_dtype) || ld > kAdapterLd) return DAB_ERR_UNSUPPORTED;
     return misaligned(base, 16) ? DAB_ERR_ALIGN : DAB_OK;
 }
+// An output over base: only element by element, which the same lane reads before it writes.
+static bool over_base(const void* out, int32_t dtype, const void* base, int32_t base_dtype, int32_t T, int32_t cols, int64_t ld) {
+    if (!out || !base || (out == base && base_dtype == dtype && (ld == cols || T == 1))) return false;
+    return meet({out, T, cols, cols, dtype_bytes(dtype)}, {base, T, cols, ld, dtype_bytes(base_dtype)});
+}
 
 }  // namespace dab
 
@@ -881,6 +886,7 @@ extern "C" int dab_adapters(const void* X, int32_t dtype, int64_t ldx, const int
     if (misaligned(Y, 16) || misaligned(U, 4)) return DAB_ERR_ALIGN;
     // (X is read for other columns of Y)
     if (meet({Y, T, F, F, dtype_bytes(dtype)}, {X, T, K, ldx, dtype_bytes(dtype)})) return DAB_ERR_UNSUPPORTED;
+    if (over_base(Y, dtype, base, base_dtype, T, F, ldbase)) return DAB_ERR_UNSUPPORTED;
     const Adapters a{ids, scale, T, n, r};
     const auto st = static_cast<hipStream_t>(stream);
     const auto go = [&](auto* t) -> int {
@@ -913,6 +919,7 @@ extern "C" int dab_adapters_gradient(const void* dY, int64_t lddy, const void* X
     // (X and dY are read again behind dX)
     const int64_t size = dtype_bytes(dtype);
     if (dX && (meet({dX, T, K, K, size}, {X, T, K, ldx, size}) || meet({dX, T, K, K, size}, {dY, T, F, lddy, size}))) return DAB_ERR_UNSUPPORTED;
+    if (over_base(dX, dtype, base, base_dtype, T, K, ldbase)) return DAB_ERR_UNSUPPORTED;
     const size_t need = dab_adapters_gradient_workspace_bytes(T, K, F, n, r);
     if (!ws || ws_bytes < need || misaligned(ws, 256)) return DAB_ERR_WORKSPACE;
     const Adapters a{ids, scale, T, n, r};
