@@ -586,7 +586,8 @@ int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, c
  *   Y      [rows][cols] of dtype out, or NULL.  May be X or R itself where their rows are cols apart
  *   Q, S   as dab_ckpt8_save writes them for y (in fp32), or both NULL.  One of Y and Q is given
  *   rstd   [rows] fp32 out, what the gradient takes
- * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE; Y or H over X or R in any other way -> DAB_ERR_UNSUPPORTED.
+ * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE; Y or H over X or R in any other way, or over one another -> DAB_ERR_UNSUPPORTED.  Q, S and rstd must
+ * not overlap anything else of the call.
  */
 int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const void* R, int64_t ldr, const float* gain, float eps, int32_t rows, int32_t cols,
                  void* H, void* Y, int8_t* Q, uint8_t* S, float* rstd, void* stream);

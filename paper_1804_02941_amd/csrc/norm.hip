@@ -576,6 +576,8 @@ extern "C" int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const voi
     const int64_t size = dtype_bytes(dtype);
     if (R && (crosses(H, X, rows, cols, ldx, size) || crosses(H, R, rows, cols, ldr, size))) return DAB_ERR_UNSUPPORTED;
     if (crosses(Y, X, rows, cols, ldx, size) || crosses(Y, R, rows, cols, ldr, size)) return DAB_ERR_UNSUPPORTED;
+    // (h is kept for the gradient)
+    if (R && Y && meet({H, rows, cols, cols, size}, {Y, rows, cols, cols, size})) return DAB_ERR_UNSUPPORTED;
     NormGeom g{};
     g.rows = rows, g.cols = cols, g.groups = ceil_div(cols, 32), g.ldx = ldx, g.ldr = ldr, g.eps = eps;
     const auto st = static_cast<hipStream_t>(stream);

@@ -45,3 +45,16 @@ def test_adapters_gradient_over_base(lib, own):
     # element by element, one row, right before and right behind it: the next check's error
     assert call(own, 40, base) == WORKSPACE and call(own, 48, base, T=1) == WORKSPACE and call(F32, 40, base + 5 * 40 * 4) == WORKSPACE
     assert call(F32, 40, base - 5 * 40 * {F32: 4}.get(own, 2)) == WORKSPACE
+
+
+@pytest.mark.parametrize("own", [F32, BF16, F16])
+def test_norm_output_over_its_sum(lib, own):
+    """What the gradient takes as h would be the norm's output."""
+    X, R, H = 1 << 19, 1 << 20, 1 << 21
+    size = 5 * 40 * (4 if own == F32 else 2)
+
+    def call(h, y, r=R):
+        return lib.dab_rms_norm(X, own, 40, r, 40, p, 1e-5, 5, 40, h, y, p, p, p, None)
+    for by in (0, 16, -16, size - 16, 16 - size):
+        assert call(H, H + by) == UNSUPPORTED, by
+    assert call(X, X) == UNSUPPORTED and call(R, R) == UNSUPPORTED          # each alone may be where it is
