@@ -23,7 +23,9 @@ SIZES = [(1, 4096, 4099, (5, 70)),             # eight shares of a row, rows of 
          (20, 300, 40000, (5, 24)),            # four tiles a wavefront, several groups, adapters behind the product
          (32, 700, 16395, (5, 24, 64, 256)), (32, 2000, 16395, (33,)),
          (48, 600, 8200, (8,)), (48, 4100, 8203, (24,)),
-         (70, 4500, 16387, (7, 64))]           # U in a launch of its own
+         (70, 4500, 16387, (7, 64)),           # U in a launch of its own
+         # rows of fewer than eight
+         (1, 40, 1, (1, 12)), (2, 64, 5, (3,)), (3, 5, 20, (4, 33)), (65, 130, 7, (20,)), (66, 7, 3, (2,))]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
