@@ -450,7 +450,8 @@ int dab_weight_gradient(const float* W, int32_t F, int32_t n, const float* thr_v
  * Element types of these calls, and the strides of their inputs: a matrix [rows][cols] is given with
  * the distance ld of its rows in elements (ld >= cols), so that a slice of columns whose first element is 16-byte
  * aligned needs no copy: base pointers are 16-byte aligned (DAB_ERR_ALIGN), the rows behind the first one at any
- * element.  fp32 vectors, scale bytes and targets are aligned as their type wants.  Outputs are contiguous.  Offsets are 64-bit.
+ * element.  fp32 vectors, scale bytes and targets are aligned as their type wants.  Outputs are contiguous, and overlap nothing else of
+ * the call but what its description names.  Offsets are 64-bit.
  * Larger sizes than each call names are DAB_ERR_UNSUPPORTED.
  */
 typedef enum dab_dtype {
@@ -586,8 +587,8 @@ int dab_w4_matvec(const void* X, int32_t dtype, int64_t ldx, const uint8_t* Q, c
  *   Y      [rows][cols] of dtype out, or NULL.  May be X or R itself where their rows are cols apart
  *   Q, S   as dab_ckpt8_save writes them for y (in fp32), or both NULL.  One of Y and Q is given
  *   rstd   [rows] fp32 out, what the gradient takes
- * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE; Y or H over X or R in any other way, or over one another -> DAB_ERR_UNSUPPORTED.  Q, S and rstd must
- * not overlap anything else of the call.
+ * Errors: eps below 0 or a NaN -> DAB_ERR_SHAPE; Y or H over X or R in any other way, or over one another -> DAB_ERR_UNSUPPORTED, and so may a
+ * call of more than 2^34 elements, or of 2^30 rows and more, be.
  */
 int dab_rms_norm(const void* X, int32_t dtype, int64_t ldx, const void* R, int64_t ldr, const float* gain, float eps, int32_t rows, int32_t cols,
                  void* H, void* Y, int8_t* Q, uint8_t* S, float* rstd, void* stream);
@@ -658,7 +659,7 @@ typedef struct dab_adamw_step {
 /*
  * The tensors of a step are laid out once, in a table of the caller's device memory: dab_adamw_plan_of checks the jobs and says how large it is,
  * dab_adamw_table writes it (on `stream`, without reading host memory after it returns), and any number of dab_adamw calls take it as
- * long as the tensors stay where they are.  The plan is the caller's too; what another call than these wrote into plan or table is not supported.
+ * long as the tensors, the gradients among them, stay where they are.  The plan is the caller's too; what another call than these wrote into plan or table is not supported.
  *   table   plan.table_bytes bytes, 256-byte aligned.  More than 2^23 workgroups (2^36 elements) -> DAB_ERR_UNSUPPORTED
  */
 typedef struct dab_adamw_plan {
