@@ -859,6 +859,9 @@ class _AdamwJobs:
 def adamw_jobs(items):
     """The table of a step's tensors from dicts(P, G, M, V, copy=None, weight_decay=0.0, place=None), built once and reused per step.
 
+    It holds addresses: as long as all tensors stay where they are, the gradients among them (write each step's into the same tensors), it serves every step.
+    Building it costs far more than a step does (96 small tensors: 0.5 to 0.6 ms, the step's call 5 us).
+
     P: fp32; G: a gradient of as many elements (fp32, bf16 or f16); M, V: from adamw_states(); copy: a bf16 or f16 tensor that takes the new P
     too; place: of the tensor in the sequence of random numbers (behind the tensor before it unless given).  The tensors are kept alive.  The
     table is written on the current stream and waited for (in a graph that is being captured, it is written at every replay)."""

@@ -6,7 +6,9 @@
 // for all tensors: a table in device memory, written once by kernels that get the addresses with their launch (nothing is copied to the device, so
 // that it may be made in a captured graph too), says which stretch of which tensor a workgroup takes.  Bound by memory: 28 bytes an element with
 // fp32 gradients and states (8.5 M of them 50 us, 4.8 TB/s), 16.1 with bf16 gradients, 8-bit states and a bf16 copy (75.5 M 237 to 263 us, 4.6 to 5.1).
-// 96 tensors of a few thousand elements: 5.8 us, a chain of three reads behind a launch; with the tensors among the arguments, 32 a launch, 21.6.
+// 96 tensors of a few thousand elements: 5.8 us, with the tensors among the arguments, 32 a launch, 21.6.  What is left are reads that wait for one
+// another behind the launch: the tensor's number, the tensor, scale, rate and step where they are in device memory, the gradient, the weights, the states (their
+// addresses come out of the table, so that the compiler takes them for generic ones, and each stands under a branch).
 #include <cmath>
 
 #include "real16.h"

@@ -7,7 +7,7 @@
 // bound by its long rows in memory: 2 r operations an element.  Tokens come in any order; a tile of sixteen takes its adapters one after the other,
 // and what a token is not to take is left out by selection, not by a product with zero, so that no adapter's infinities and NaN
 // reach another's tokens.  8192 tokens of four adapters, 4096 -> 4096, r = 16, bf16: U and Y 46 us (207 MB, 4.5 TB/s), V and dX the same, dA and dB 34
-// (132 MB, 3.6) and 6 for joining shares.
+// (132 MB, 3.9) and 6 for joining shares.
 #include <algorithm>
 
 #include "adapters.h"
@@ -69,8 +69,9 @@ struct Long<T, true> {
 };
 
 // Many tokens: a workgroup takes sixteen of them and 16 RT of the r rows, its wavefronts every eighth stretch of 128 k (RT = 1, 16-bit types), whose
-// loads are in flight at once, those of the next one behind them.  This lane's sums over its wavefront's k: rows 4 (lane / 16) .. + 3 of
-// each sixteen from r0 on, of token lane % 16.
+// loads are in flight at once.  Those of the next stretch are asked for ahead of its products, but each eight's stand under a condition of their own, so that the
+// compiler does not know how many are on their way and waits for all of them: stretches do not overlap.  This lane's sums over its
+// wavefront's k: rows 4 (lane / 16) .. + 3 of each sixteen from r0 on, of token lane % 16.
 // (sixteen wavefronts a tile where tiles do not fill the chip: 1024 x 4096 bf16 11.5 us, with eight 11.1.)
 constexpr int kShrinkWaves = 8;
 template <typename T, int RT, bool ODD>
@@ -482,8 +483,9 @@ __global__ __launch_bounds__(64) void expand_few_kernel(const float* __restrict_
 // slices-th adapter.  Of each adapter that has tokens in its share they are listed, dealt out to the wavefronts and the sums added up in LDS (every
 // wavefront its own stretch of the tokens instead, so that half of them wait where sequences are short: 41 us instead of 35).  With one
 // share that is the gradient; else it goes to parts: [share][adapter][r][columns], and have: [share][adapter] is 1 where the share has
-// tokens of the adapter (other parts are not written).  Sixteen rows a workgroup whatever the rank: r = 64 of four adapters 84 us, with 32 rows 84 and a
-// longer join, with 64 rows 102 (registers).  bf16 products with three pieces of V instead of fp32 ones: 49 -> 37 us.
+// tokens of the adapter (other parts are not written).  Sixteen rows a workgroup whatever the rank, each of which reads X and dY again: these sums of r = 64,
+// four adapters, took 84 us, with 32 rows 84 and a longer join, with 64 rows 102 (registers); they take 80 now, of f16, on the fp32 instruction, 128.
+// bf16 products with three pieces of V instead of fp32 ones: 49 -> 37 us.
 constexpr int kOuterWaves = 8, kOuterIds = 2048;
 template <typename T>
 struct OuterSide {
@@ -694,7 +696,8 @@ struct Join {
     const int32_t* have;
     int shares, n;
 };
-// (a lane four neighbouring elements, the workgroup's four wavefronts every fourth share)
+// (a lane four neighbouring elements, the workgroup's four wavefronts every fourth share: whether it has a part is waited for, then the part, share by share,
+// 5.6 us for 15 MB)
 __global__ __launch_bounds__(256) void outer_join_kernel(const Join j) {
     __shared__ v4f sums[3][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -729,8 +732,10 @@ static bool odd_rows(int64_t ldx, int K) { return ((ldx | K) & 1) != 0; }
 
 template <typename T>
 static int shrink(const T* X, int64_t ldx, const T* A, int K, const Adapters& a, bool scaled, float* U, hipStream_t st) {
-    // A workgroup for every token and row, or for sixteen tokens: the one's time grows with both, the other's with k alone until its workgroups fill the
-    // chip.  bf16, r = 16, rows of 4096: 128 tokens 5.2 us and 10.8, 256 8.7 and 10.8, 512 14.1 and 11.0; of 1024, 256 tokens 6.0 and 4.9.
+    // A workgroup for every token and row, or for sixteen tokens: the one's time grows with tokens, rows and k, the other's with k alone until its workgroups
+    // fill the chip.  bf16, r = 16, rows of 4096: 128 tokens 5.2 us and 10.8, 256 8.7 and 10.8, 512 14.1 and 11.0; of 1024, 256 tokens 6.0 and 4.9.  The
+    // limit is that of rows of up to some 8192 and too high for longer ones (with the 1100 columns of Y behind it, tokens in four runs of one adapter
+    // each: 8192, 288 tokens 19 us and 37, 576 24 and 21; 16384, 544 35 and 66, 1088 56 and 37; 65536, 1040 200 and 232, 4080 820 and 240).
     if (static_cast<int64_t>(a.T) * a.r <= 1024 + K)
         return launch(shrink_few_kernel<T>, dim3(a.T * a.r), dim3(64 * kFewWaves), 0, st, X, ldx, A, K, a, static_cast<int>(scaled), U);
     const unsigned tiles = static_cast<unsigned>(ceil_div64(a.T, 16));
